@@ -68,6 +68,8 @@ typedef enum {
 } dbspmspv_semiring_t;
 
 enum { DBSPMSPV_PATH_AUTO = 0, DBSPMSPV_PATH_PUSH = 1, DBSPMSPV_PATH_PULL = 2 };
+/* Activations of dbspmspv_linear and dbspmspv_gated: z; max(z, 0); z / (1 + exp(-z)); z Phi(z) with the normal distribution Phi */
+enum { DBSPMSPV_ACT_NONE = 0, DBSPMSPV_ACT_RELU = 1, DBSPMSPV_ACT_SILU = 2, DBSPMSPV_ACT_GELU = 3 };
 enum { DBSPMSPV_FORMAT_AUTO = 0, DBSPMSPV_FORMAT_COO = 1, DBSPMSPV_FORMAT_CSR = 2 };
 
 /* Block classes (Section 3.2.1).  INLINE is this library's sub-case of COO: a block whose few
@@ -102,7 +104,12 @@ typedef struct {
                                 the pull levels of db_bfs (4 bytes per stored element) and, fp32,
                                 the pulled steps of db_sssp (8 bytes per stored element; a pull
                                 level then walks whole row-block segments)          (0)    */
-    int32_t reserved[2];
+    int32_t linear;          /* 1: a layer for dbspmspv_linear / dbspmspv_gated and their gradients, whatever its
+                                size and sparsity: the copy by columns is built in any case (2 bytes per matrix
+                                ENTRY, rows rounded up to 64), and an index of the stored weights by row beside it
+                                (a quarter of a byte per entry), which gradients of weights need.  bf16 handles with
+                                finite weights (else ERR_UNSUPPORTED)                (0)    */
+    int32_t reserved[1];
 } dbspmspv_create_opts;
 
 /* Run-time options; may be changed between calls with dbspmspv_set_run_opts.               */
@@ -310,6 +317,52 @@ int db_sssp(dbspmspv_handle_t h, int32_t src, float *dist, int32_t *n_steps, dbs
  *   y        out: m fp32 values; rows without a structural hit are exactly 0
  */
 int dbspmspv_decode(dbspmspv_handle_t h, const void *x, float *y, dbspmspv_stream_t stream);
+
+/*
+ * Linear layers and gated feed-forward blocks over pruned bf16 weights: the layers of dbspmspv_decode (Section 4.3) with what
+ * stands around their product in a network, from one token to a prompt, and their gradients for fine-tuning the surviving weights.
+ *
+ *   dbspmspv_linear            z = W x + bias,  y = act(z) + residual                       for every token
+ *   dbspmspv_gated             g = W_gate x,  u = W_up x,  y = act(g) * u
+ *   dbspmspv_linear_backward   dz = dy * act'(z);  dx = W^T dz,  dW = sum over tokens of dz x^T at the stored places, dbias = sum of dz
+ *   dbspmspv_gated_backward    dg = dy * u * act'(g),  du = dy * act(g);  dx = W_gate^T dg + W_up^T du, dW_gate, dW_up as above
+ *
+ * W is the matrix with zeros in the pruned places (an entry of x that is not finite therefore reaches every row, unlike in
+ * dbspmspv_decode).  The options of dbspmspv_set_run_opts do not apply.
+ *   handles    bf16 handles that hold the copy by columns: those made with the create option `linear`, and those that
+ *              dbspmspv_decode reads by columns anyway; the gradient of weights needs the option.  Else ERR_UNSUPPORTED.  The two
+ *              handles of a gated block have the same m and n (they may be the same handle).
+ *   tokens     rows of x, y, ... (0: forward calls do nothing, gradients of weights and bias are zeroed).  Rows are ldx, ldy, ...
+ *              entries apart, at least their width; what lies between them is neither read nor written.
+ *   x          tokens x n bf16;  bias m bf16 or NULL;  act DBSPMSPV_ACT_*;  residual tokens x m bf16 or NULL
+ *   y          out: tokens x m bf16, or fp32 with y_f32 = 1 (dbspmspv_linear)
+ *   z / g, u   out of the forward call, in for the gradient: tokens x m bf16, what the activation is applied to (and the
+ *              other projection); NULL in a forward call: not kept.  z may be NULL in the gradient of ACT_NONE.
+ *   dy         tokens x m bf16.  The residual's gradient is dy itself.
+ *   dx         out: tokens x n bf16, or NULL: not wanted
+ *   dw         out: one bf16 per stored weight (stats.nnz of them), row by row, columns ascending -- the order of the values of
+ *              a CSR matrix without duplicates whose columns ascend -- or NULL
+ *   dbias      out: m fp32, or NULL
+ *   workspace  device memory of at least the bytes that dbspmspv_linear_workspace names, on 16 bytes.  Forward calls need it only for
+ *              x whose rows do not begin on 16 bytes (x and ldx both count) and more tokens than the kernel over active
+ *              columns takes.  Two calls that may overlap need two workspaces; a captured call keeps its own.
+ *
+ * Sums are fp32.  y, z, g, u, dx and dw are rounded to bf16 once, to nearest even; dz, dg and du are rounded to bf16 before they
+ * enter the products.  Results do not depend on the order in which thread blocks run.  residual may be y itself (same address, same
+ * stride, bf16: an entry is read by the thread that then writes it); no other output may overlap an input or another output.
+ * Alignment: bf16 arrays on 2 bytes, fp32 arrays on 4.  Asynchronous on `stream`; no device memory is allocated.
+ * Errors: INVALID_ARG (also a workspace that is needed and too small), UNSUPPORTED.
+ */
+int dbspmspv_linear_workspace(dbspmspv_handle_t h, dbspmspv_handle_t up /* the other layer of a gated block, or NULL */, int32_t tokens, int backward, int64_t *bytes);
+int dbspmspv_linear(dbspmspv_handle_t h, const void *x, int64_t ldx, int32_t tokens, const void *bias, int act, const void *residual, int64_t ldr,
+                    void *y, int64_t ldy, int y_f32, void *z, int64_t ldz, void *workspace, int64_t workspace_bytes, dbspmspv_stream_t stream);
+int dbspmspv_gated(dbspmspv_handle_t gate, dbspmspv_handle_t up, const void *x, int64_t ldx, int32_t tokens, int act, void *y, int64_t ldy,
+                   void *g, void *u, int64_t ldgu, void *workspace, int64_t workspace_bytes, dbspmspv_stream_t stream);
+int dbspmspv_linear_backward(dbspmspv_handle_t h, const void *x, int64_t ldx, int32_t tokens, int act, const void *z, int64_t ldz, const void *dy, int64_t lddy,
+                             void *dx, int64_t lddx, void *dw, float *dbias, void *workspace, int64_t workspace_bytes, dbspmspv_stream_t stream);
+int dbspmspv_gated_backward(dbspmspv_handle_t gate, dbspmspv_handle_t up, const void *x, int64_t ldx, int32_t tokens, int act, const void *g, const void *u, int64_t ldgu,
+                            const void *dy, int64_t lddy, void *dx, int64_t lddx, void *dw_gate, void *dw_up, void *workspace, int64_t workspace_bytes,
+                            dbspmspv_stream_t stream);
 
 /* Waits for the stream the handle's last run / decode / db_bfs call was enqueued on (not for the
  * whole device) and copies the statistics to the HOST struct `out`.  Returns the deferred

@@ -23,6 +23,7 @@ LIB_PATH = os.environ.get("DBSPMSPV_LIBRARY") or os.path.join(HERE, "libdbspmspv
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALLOC, ERR_CUDA, ERR_CAPACITY, ERR_TIMEOUT, ERR_BOUNDS, ERR_TOO_LARGE, ERR_INTERNAL = range(10)
 F32, BF16, PATTERN = 0, 1, 2
 PLUS_TIMES, OR_AND, MIN_PLUS = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 PATH_AUTO, PATH_PUSH, PATH_PULL = 0, 1, 2
 FORMAT_AUTO, FORMAT_COO, FORMAT_CSR = 0, 1, 2
 BLK_INLINE, BLK_COO, BLK_FCSR, BLK_FCSC, BLK_CSR, BLK_DENSE = range(6)
@@ -35,6 +36,7 @@ EXPORTED_SYMBOLS = (
     "dbspmspv_export_coo", "dbspmspv_export_blocks", "dbspmspv_export_views",
     "dbspmspv_set_run_opts", "dbspmspv_destroy", "dbspmspv_strerror", "dbspmspv_compact_noalloc",
     "dbspmspv_test_bounded_wait", "dbspmspv_test_corrupt_entry", "dbspmspv_decode_batch", "dbspmspv_run_masked", "dbspmspv_count_call_bytes", "dbspmspv_probe_floor",
+    "dbspmspv_linear_workspace", "dbspmspv_linear", "dbspmspv_gated", "dbspmspv_linear_backward", "dbspmspv_gated_backward",
 )
 
 
@@ -45,7 +47,7 @@ class CreateOpts(ctypes.Structure):
                 ("input_on_host", ctypes.c_int32), ("inline_max", ctypes.c_int32),
                 ("w_inline", ctypes.c_int32), ("w_dense_sparse", ctypes.c_int32),
                 ("w_mid_sparse", ctypes.c_int32), ("no_bfs_index", ctypes.c_int32),
-                ("reserved", ctypes.c_int32 * 2)]
+                ("linear", ctypes.c_int32), ("reserved", ctypes.c_int32 * 1)]
 
 
 class RunOpts(ctypes.Structure):
@@ -111,6 +113,11 @@ def lib() -> ctypes.CDLL:
         L.db_sssp.argtypes = [vp, i32, vp, ctypes.POINTER(ctypes.c_int32), vp]
         L.dbspmspv_decode.argtypes = [vp, vp, vp, vp]
         L.dbspmspv_decode_batch.argtypes = [vp, vp, i64, vp, i64, i32, vp]
+        L.dbspmspv_linear_workspace.argtypes = [vp, vp, i32, ctypes.c_int, ctypes.POINTER(i64)]
+        L.dbspmspv_linear.argtypes = [vp, vp, i64, i32, vp, ctypes.c_int, vp, i64, vp, i64, ctypes.c_int, vp, i64, vp, i64, vp]
+        L.dbspmspv_gated.argtypes = [vp, vp, vp, i64, i32, ctypes.c_int, vp, i64, vp, vp, i64, vp, i64, vp]
+        L.dbspmspv_linear_backward.argtypes = [vp, vp, i64, i32, ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp]
+        L.dbspmspv_gated_backward.argtypes = [vp, vp, vp, i64, i32, ctypes.c_int, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp]
         L.dbspmspv_get_stats.argtypes = [vp, ctypes.POINTER(Stats)]
         L.dbspmspv_export_coo.argtypes = [vp, vp, vp, vp]
         L.dbspmspv_export_blocks.argtypes = [vp, vp, vp, vp, vp]
@@ -190,7 +197,15 @@ def _bind_streams() -> None:
 #   dbspmspv_decode_batch(h, x, ldx, y, ldy, batch, stream=None)
 #   db_bfs(h, src, levels, stream=None)
 #   db_sssp(h, src, dist, stream=None) -> number of (min, +) products the search made
-_FAST = ("dbspmspv_run", "dbspmspv_run_masked", "dbspmspv_decode", "dbspmspv_decode_batch", "db_bfs", "db_sssp")
+#   dbspmspv_linear(h, x, ldx, tokens, bias, act, residual, ldr, y, ldy, y_f32, z, ldz, workspace,
+#                   workspace_bytes, stream=None)
+#   dbspmspv_gated(gate, up, x, ldx, tokens, act, y, ldy, g, u, ldgu, workspace, workspace_bytes, stream=None)
+#   dbspmspv_linear_backward(h, x, ldx, tokens, act, z, ldz, dy, lddy, dx, lddx, dw, dbias, workspace,
+#                            workspace_bytes, stream=None)
+#   dbspmspv_gated_backward(gate, up, x, ldx, tokens, act, g, u, ldgu, dy, lddy, dx, lddx, dw_gate, dw_up,
+#                           workspace, workspace_bytes, stream=None)
+_FAST = ("dbspmspv_run", "dbspmspv_run_masked", "dbspmspv_decode", "dbspmspv_decode_batch", "db_bfs", "db_sssp",
+         "dbspmspv_linear", "dbspmspv_gated", "dbspmspv_linear_backward", "dbspmspv_gated_backward")
 
 
 def _not_built(*_args, **_kwargs):
@@ -200,7 +215,8 @@ def _not_built(*_args, **_kwargs):
 
 if _fastcall is not None:
     _fastcall.set_loader(_load_fast, _plain)
-dbspmspv_run, dbspmspv_run_masked, dbspmspv_decode, dbspmspv_decode_batch, db_bfs, db_sssp = (
+(dbspmspv_run, dbspmspv_run_masked, dbspmspv_decode, dbspmspv_decode_batch, db_bfs, db_sssp,
+ dbspmspv_linear, dbspmspv_gated, dbspmspv_linear_backward, dbspmspv_gated_backward) = (
     getattr(_fastcall, name, _not_built) for name in _FAST)
 
 
@@ -235,6 +251,13 @@ def dbspmspv_create_coo(m, n, nnz, row, col, val, dtype, block_size=16,
                                    _stream() if stream is None else stream)
     _check(st, "dbspmspv_create_coo")
     return h.value
+
+
+def dbspmspv_linear_workspace(h, up, tokens: int, backward: bool) -> int:
+    """Bytes of workspace that a call on `tokens` tokens may need (dbspmspv_linear_workspace)."""
+    out = ctypes.c_int64()
+    _check(lib().dbspmspv_linear_workspace(h, up, tokens, int(backward), ctypes.byref(out)), "dbspmspv_linear_workspace")
+    return out.value
 
 
 def dbspmspv_get_stats(h, raise_on_device_status: bool = True) -> Stats:

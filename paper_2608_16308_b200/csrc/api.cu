@@ -206,7 +206,8 @@ int dbspmspv_destroy(dbspmspv_handle_t h) {
     cudaFree(const_cast<int32_t *>(d.csr_inl)); cudaFree(const_cast<int32_t *>(d.payload_pos));
     cudaFree(const_cast<int32_t *>(d.lean_rows)); cudaFree(const_cast<int32_t *>(d.lean_chunk_ord));
     cudaFree(const_cast<int4 *>(d.stage_chunks));
-    cudaFree(const_cast<uint4 *>(d.cols));
+    cudaFree(const_cast<uint16_t *>(h->lin_w));           // (d.cols is the same, or null)
+    cudaFree(h->lin_index);
     if (h->x_nnz_seen_host) cudaFreeHost(h->x_nnz_seen_host);
     cudaFree(const_cast<uint16_t *>(d.hub_slot)); cudaFree(d.hub_acc);
     cudaFree(h->csc2csr); cudaFree(h->block_row);

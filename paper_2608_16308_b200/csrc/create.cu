@@ -1112,25 +1112,38 @@ int build(dbspmspv_handle_s *h, int64_t m, int64_t n, int64_t nnz, const int64_t
 
     // Decode over columns of bf16 layers (decode_columns.cuh): the weights once more, column by column in strips of
     // rows.  Not built when it does not fit, nor for weights that are not finite (a batched call multiplies absent x entries as zeros).
+    // The create option `linear` builds it for any layer, and the index of the stored weights by row beside it (linear.cu).
     d.cols = nullptr;
-    if (h->heavy_stage && d.dtype == DBSPMSPV_BF16 && m >= DC_MIN_ROWS && n <= DC_MAX_COLUMNS) {
-        const int64_t bytes = (m + DC_ROWS - 1) / DC_ROWS * DC_ROWS * n * 2;
+    const int64_t cols_bytes = (m + DC_ROWS - 1) / DC_ROWS * DC_ROWS * n * 2;
+    const bool cols_decode = h->heavy_stage && d.dtype == DBSPMSPV_BF16 && m >= DC_MIN_ROWS && n <= DC_MAX_COLUMNS && cols_bytes <= DC_MAX_RATIO * h->payload_bytes;
+    if (cols_decode || h->copts.linear) {
         void *p = nullptr;
-        if (bytes <= DC_MAX_RATIO * h->payload_bytes) {
-            if (cudaMalloc(&p, (size_t)bytes) != cudaSuccess) { (void)cudaGetLastError(); p = nullptr; }
-        }
+        if (cudaMalloc(&p, (size_t)cols_bytes) != cudaSuccess) { (void)cudaGetLastError(); p = nullptr; }
+        if (!p && h->copts.linear) return DBSPMSPV_ERR_ALLOC;
         if (p) {
-            int32_t *bad, bad_h = 0;
-            DBS_GET(bad, 1);
-            DBS_CUDA(cudaMemsetAsync(bad, 0, 4, st));
-            k_fill_words<<<grid_for(bytes / 4), TPB, 0, st>>>(static_cast<uint32_t *>(p), bytes / 4, DC_ABSENT * 0x10001u);
-            k_columns_copy<<<grid_for(n_entries), TPB, 0, st>>>(d, h->block_row, static_cast<uint16_t *>(p), bad);
-            cudaError_t e = cudaMemcpyAsync(&bad_h, bad, 4, cudaMemcpyDeviceToHost, st);
+            int32_t *bad = nullptr, bad_h = 0;
+            cudaError_t e = tp.get(&bad, 1) ? cudaSuccess : cudaErrorMemoryAllocation;
+            const int status = e == cudaSuccess ? DBSPMSPV_ERR_CUDA : DBSPMSPV_ERR_ALLOC;
+            if (e == cudaSuccess) e = cudaMemsetAsync(bad, 0, 4, st);
+            if (e == cudaSuccess) {
+                k_fill_words<<<grid_for(cols_bytes / 4), TPB, 0, st>>>(static_cast<uint32_t *>(p), cols_bytes / 4, DC_ABSENT * 0x10001u);
+                k_columns_copy<<<grid_for(n_entries), TPB, 0, st>>>(d, h->block_row, static_cast<uint16_t *>(p), bad);
+                e = cudaMemcpyAsync(&bad_h, bad, 4, cudaMemcpyDeviceToHost, st);
+            }
             if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-            tp.release(bad);
+            if (bad) tp.release(bad);
             if (e != cudaSuccess || bad_h) cudaFree(p);
-            if (e != cudaSuccess) return DBSPMSPV_ERR_CUDA;
-            if (!bad_h) { d.cols = static_cast<const uint4 *>(p); h->stage_index_bytes += bytes; }
+            if (e != cudaSuccess) return status;
+            if (bad_h && h->copts.linear) return DBSPMSPV_ERR_UNSUPPORTED;
+            if (!bad_h) {
+                h->lin_w = static_cast<const uint16_t *>(p);
+                if (cols_decode) d.cols = static_cast<const uint4 *>(p);
+                h->stage_index_bytes += cols_bytes;
+                const int s = linear_handle_maps(h);
+                if (s != DBSPMSPV_OK && h->copts.linear) return s;
+                h->lin_ready = s == DBSPMSPV_OK;
+                if (h->copts.linear) { DBS_TRY(build_linear_index(h, st)); h->stage_index_bytes += m * h->lin_words * 8; }
+            }
         }
     }
 
@@ -1236,6 +1249,7 @@ int create_common(dbspmspv_handle_t *out, int64_t m, int64_t n, int64_t nnz, con
     if (dtype != DBSPMSPV_F32 && dtype != DBSPMSPV_BF16 && dtype != DBSPMSPV_PATTERN) return DBSPMSPV_ERR_INVALID_ARG;
     if (dtype != DBSPMSPV_PATTERN && nnz > 0 && !val) return DBSPMSPV_ERR_INVALID_ARG;
     if (block_size != B) return DBSPMSPV_ERR_UNSUPPORTED;
+    if (opts && opts->linear && dtype != DBSPMSPV_BF16) return DBSPMSPV_ERR_UNSUPPORTED;
     dbspmspv_handle_s *h = new (std::nothrow) dbspmspv_handle_s();
     if (!h) return DBSPMSPV_ERR_ALLOC;
     h->graphs = new (std::nothrow) CallGraphs();      // (none: every call launches its kernels one by one)

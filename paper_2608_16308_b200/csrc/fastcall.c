@@ -1,5 +1,5 @@
 /* Argument marshalling of the hot entry points (dbspmspv_run, dbspmspv_run_masked, dbspmspv_decode,
- * dbspmspv_decode_batch, db_bfs, db_sssp) as a CPython extension: the same names, arguments,
+ * dbspmspv_decode_batch, db_bfs, db_sssp, dbspmspv_linear, dbspmspv_gated and their gradients) as a CPython extension: the same names, arguments,
  * defaults and errors as a ctypes wrapper, at a tenth of its cost.
  *
  * What bounds a short call is the host.  Through ctypes the marshalling alone took 6 us of a 10 us
@@ -13,7 +13,7 @@
 #include <Python.h>
 #include <stdint.h>
 
-enum { F_RUN, F_RUN_MASKED, F_DECODE, F_DECODE_BATCH, F_BFS, F_SSSP, N_FUNCS };
+enum { F_RUN, F_RUN_MASKED, F_DECODE, F_DECODE_BATCH, F_BFS, F_SSSP, F_LINEAR, F_GATED, F_LINEAR_BACKWARD, F_GATED_BACKWARD, N_FUNCS };
 
 static void *g_addr[N_FUNCS];
 static PyObject *g_load;          /* called once: loads the library and calls setup() */
@@ -230,6 +230,80 @@ static PyObject *f_sssp(PyObject *self, PyObject *const *args, Py_ssize_t nargs,
     return PyLong_FromLong(steps);
 }
 
+typedef int (*linear_fn)(void *, const void *, int64_t, int32_t, const void *, int, const void *, int64_t, void *, int64_t, int, void *, int64_t, void *, int64_t, void *);
+typedef int (*gated_fn)(void *, void *, const void *, int64_t, int32_t, int, void *, int64_t, void *, void *, int64_t, void *, int64_t, void *);
+typedef int (*linear_backward_fn)(void *, const void *, int64_t, int32_t, int, const void *, int64_t, const void *, int64_t, void *, int64_t, void *, void *, void *, int64_t, void *);
+typedef int (*gated_backward_fn)(void *, void *, const void *, int64_t, int32_t, int, const void *, const void *, int64_t, const void *, int64_t, void *, int64_t, void *, void *,
+                                 void *, int64_t, void *);
+
+static PyObject *f_linear(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kw) {
+    static const char *const names[] = {"h", "x", "ldx", "tokens", "bias", "act", "residual", "ldr", "y", "ldy", "y_f32", "z", "ldz", "workspace", "workspace_bytes", "stream"};
+    PyObject *a[16];
+    void *h, *x, *bias, *res, *y, *z, *ws, *st;
+    int32_t tokens, act, f32;
+    int64_t ldx, ldr, ldy, ldz, bytes;
+    if (!ready() || !unpack("dbspmspv_linear", args, nargs, kw, names, 16, a)) return NULL;
+    if (!as_opaque(a[0], &h) || !as_pointer(a[1], &x) || !as_i64(a[2], &ldx) || !as_i32(a[3], &tokens) || !as_pointer(a[4], &bias) || !as_i32(a[5], &act) ||
+        !as_pointer(a[6], &res) || !as_i64(a[7], &ldr) || !as_pointer(a[8], &y) || !as_i64(a[9], &ldy) || !as_i32(a[10], &f32) || !as_pointer(a[11], &z) ||
+        !as_i64(a[12], &ldz) || !as_pointer(a[13], &ws) || !as_i64(a[14], &bytes) || !as_stream(a[15], &st)) return NULL;
+    int s;
+    Py_BEGIN_ALLOW_THREADS
+    s = ((linear_fn)g_addr[F_LINEAR])(h, x, ldx, tokens, bias, act, res, ldr, y, ldy, f32, z, ldz, ws, bytes, st);
+    Py_END_ALLOW_THREADS
+    return finish(s, "dbspmspv_linear");
+}
+
+static PyObject *f_gated(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kw) {
+    static const char *const names[] = {"gate", "up", "x", "ldx", "tokens", "act", "y", "ldy", "g", "u", "ldgu", "workspace", "workspace_bytes", "stream"};
+    PyObject *a[14];
+    void *h, *up, *x, *y, *g, *u, *ws, *st;
+    int32_t tokens, act;
+    int64_t ldx, ldy, ldgu, bytes;
+    if (!ready() || !unpack("dbspmspv_gated", args, nargs, kw, names, 14, a)) return NULL;
+    if (!as_opaque(a[0], &h) || !as_opaque(a[1], &up) || !as_pointer(a[2], &x) || !as_i64(a[3], &ldx) || !as_i32(a[4], &tokens) || !as_i32(a[5], &act) ||
+        !as_pointer(a[6], &y) || !as_i64(a[7], &ldy) || !as_pointer(a[8], &g) || !as_pointer(a[9], &u) || !as_i64(a[10], &ldgu) || !as_pointer(a[11], &ws) ||
+        !as_i64(a[12], &bytes) || !as_stream(a[13], &st)) return NULL;
+    int s;
+    Py_BEGIN_ALLOW_THREADS
+    s = ((gated_fn)g_addr[F_GATED])(h, up, x, ldx, tokens, act, y, ldy, g, u, ldgu, ws, bytes, st);
+    Py_END_ALLOW_THREADS
+    return finish(s, "dbspmspv_gated");
+}
+
+static PyObject *f_linear_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kw) {
+    static const char *const names[] = {"h", "x", "ldx", "tokens", "act", "z", "ldz", "dy", "lddy", "dx", "lddx", "dw", "dbias", "workspace", "workspace_bytes", "stream"};
+    PyObject *a[16];
+    void *h, *x, *z, *dy, *dx, *dw, *db, *ws, *st;
+    int32_t tokens, act;
+    int64_t ldx, ldz, lddy, lddx, bytes;
+    if (!ready() || !unpack("dbspmspv_linear_backward", args, nargs, kw, names, 16, a)) return NULL;
+    if (!as_opaque(a[0], &h) || !as_pointer(a[1], &x) || !as_i64(a[2], &ldx) || !as_i32(a[3], &tokens) || !as_i32(a[4], &act) || !as_pointer(a[5], &z) ||
+        !as_i64(a[6], &ldz) || !as_pointer(a[7], &dy) || !as_i64(a[8], &lddy) || !as_pointer(a[9], &dx) || !as_i64(a[10], &lddx) || !as_pointer(a[11], &dw) ||
+        !as_pointer(a[12], &db) || !as_pointer(a[13], &ws) || !as_i64(a[14], &bytes) || !as_stream(a[15], &st)) return NULL;
+    int s;
+    Py_BEGIN_ALLOW_THREADS
+    s = ((linear_backward_fn)g_addr[F_LINEAR_BACKWARD])(h, x, ldx, tokens, act, z, ldz, dy, lddy, dx, lddx, dw, db, ws, bytes, st);
+    Py_END_ALLOW_THREADS
+    return finish(s, "dbspmspv_linear_backward");
+}
+
+static PyObject *f_gated_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kw) {
+    static const char *const names[] = {"gate", "up", "x", "ldx", "tokens", "act", "g", "u", "ldgu", "dy", "lddy", "dx", "lddx", "dw_gate", "dw_up", "workspace", "workspace_bytes", "stream"};
+    PyObject *a[18];
+    void *h, *up, *x, *g, *u, *dy, *dx, *dwg, *dwu, *ws, *st;
+    int32_t tokens, act;
+    int64_t ldx, ldgu, lddy, lddx, bytes;
+    if (!ready() || !unpack("dbspmspv_gated_backward", args, nargs, kw, names, 18, a)) return NULL;
+    if (!as_opaque(a[0], &h) || !as_opaque(a[1], &up) || !as_pointer(a[2], &x) || !as_i64(a[3], &ldx) || !as_i32(a[4], &tokens) || !as_i32(a[5], &act) ||
+        !as_pointer(a[6], &g) || !as_pointer(a[7], &u) || !as_i64(a[8], &ldgu) || !as_pointer(a[9], &dy) || !as_i64(a[10], &lddy) || !as_pointer(a[11], &dx) ||
+        !as_i64(a[12], &lddx) || !as_pointer(a[13], &dwg) || !as_pointer(a[14], &dwu) || !as_pointer(a[15], &ws) || !as_i64(a[16], &bytes) || !as_stream(a[17], &st)) return NULL;
+    int s;
+    Py_BEGIN_ALLOW_THREADS
+    s = ((gated_backward_fn)g_addr[F_GATED_BACKWARD])(h, up, x, ldx, tokens, act, g, u, ldgu, dy, lddy, dx, lddx, dwg, dwu, ws, bytes, st);
+    Py_END_ALLOW_THREADS
+    return finish(s, "dbspmspv_gated_backward");
+}
+
 /* set_loader(load, plain) */
 static PyObject *f_set_loader(PyObject *self, PyObject *args) {
     PyObject *load, *pl;
@@ -266,6 +340,7 @@ static PyObject *f_streams(PyObject *self, PyObject *args) {
 static PyMethodDef methods[] = {
     FAST("dbspmspv_run", f_run), FAST("dbspmspv_run_masked", f_run_masked), FAST("dbspmspv_decode", f_decode),
     FAST("dbspmspv_decode_batch", f_decode_batch), FAST("db_bfs", f_bfs), FAST("db_sssp", f_sssp),
+    FAST("dbspmspv_linear", f_linear), FAST("dbspmspv_gated", f_gated), FAST("dbspmspv_linear_backward", f_linear_backward), FAST("dbspmspv_gated_backward", f_gated_backward),
     {"set_loader", f_set_loader, METH_VARARGS, NULL}, {"setup", f_setup, METH_VARARGS, NULL}, {"streams", f_streams, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -2,6 +2,7 @@
 // the handle, and small device helpers.  Nothing here is part of the public ABI.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -338,6 +339,14 @@ struct dbspmspv_handle_s {
     int32_t *x_nnz_seen_host;   // host view of Device::x_nnz_seen (page-locked, mapped)
     bool heavy_stage;           // most stored elements sit in mask-based blocks: MODE 1 kernels
     bool payload_rich;          // not most, but more than an eighth sit in blocks with a payload (see PD_GROUPS_MIN_NNZ_X)
+    // Linear and gated layers (linear.cu): the copy by columns (Device::cols, or built for the create option `linear` alone), its tensor maps for the forward product of
+    // one layer, of two, and for the gradient of x; the stored weights by row (option `linear`): [row][word of 32 columns] stored columns, place of the first.
+    const uint16_t *lin_w;
+    CUtensorMap lin_maps[3];
+    uint2 *lin_index;
+    int lin_words;
+    bool lin_ready;             // copy and maps are there
+    bool lin_configured[4][9], lin_cols_configured[2][9];    // [..][thread blocks of a cluster]
     cudaEvent_t ev[2];          // optional timing of the traversal kernel (run_opts.timing)
     bool timed;
     int64_t kernel_launches;    // kernels this handle has launched (run / decode / bfs)
@@ -367,6 +376,10 @@ __host__ __device__ inline T ceil_div(T a, T b) { return (a + b - 1) / b; }
 // Streaming decode (run.cu): the payload bytes of one stage that shared memory leaves room for
 // on this handle (0: none).
 int decode_stage_bytes(const Device &d);
+
+// linear.cu, at create: the tensor maps over the copy by columns; the index of the stored weights by row.
+int linear_handle_maps(dbspmspv_handle_s *h);
+int build_linear_index(dbspmspv_handle_s *h, cudaStream_t st);
 
 // Programmatic dependent launch: a kernel launched with the stream-serialisation attribute is set up
 // while its predecessor drains; `pdl_wait` blocks until the predecessor has completed and its

@@ -1,0 +1,505 @@
+// Linear and gated feed-forward layers over pruned bf16 weights, from one token to a prompt, with their gradients
+// (Section 4.3's layers with what stands around their product in a network): entry points, the choice of kernel, and the
+// small kernels beside the products.  The products: linear_columns.cuh (single tokens), linear_gemm.cuh (tensor cores).
+#include <cub/cub.cuh>
+
+#include "call_graph.cuh"
+#include "internal.cuh"
+#include "microkernels.cuh"
+#include "linear_columns.cuh"
+#include "linear_gemm.cuh"
+
+namespace dbs {
+
+constexpr int LIN_COLS_MAX_SMEM = 200 * 1024;
+// Tokens that a call over active columns takes one by one, side by side in the grid; more go to the tensor cores.
+constexpr int LIN_COLS_MAX_TOKENS = 2;
+
+// ---- at create ------------------------------------------------------------------------------
+// Stored columns of a row, 32 to a word, from the copy by columns; a warp takes the 32 rows of half a strip.
+__global__ void k_linear_words(const uint16_t *w, int64_t m, int64_t n, int words, uint2 *index, int32_t *count) {
+    const int64_t warp = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5;
+    const int lane = threadIdx.x & 31;
+    const int64_t half = warp / words, row = half * 32 + lane;
+    const int word = (int)(warp % words);
+    if (row >= m) return;
+    const uint16_t *p = w + ((row / DC_ROWS) * n + (int64_t)word * 32) * DC_ROWS + row % DC_ROWS;
+    uint32_t bits = 0;
+    for (int c = 0; c < 32; ++c)
+        if ((int64_t)word * 32 + c < n && p[(int64_t)c * DC_ROWS] != DC_ABSENT) bits |= 1u << c;
+    index[row * words + word].x = bits;
+    count[row * words + word] = __popc(bits);
+}
+__global__ void k_linear_places(int64_t n, const int32_t *first, uint2 *index) {
+    const int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
+    if (i < n) index[i].y = (uint32_t)first[i];
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled encode_tiled() {
+    static EncodeTiled f = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) { (void)cudaGetLastError(); p = nullptr; }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return f;
+}
+// bf16, the first dimension 64 entries of a box (the 128 bytes of a swizzle row); places outside are read as zeros
+static int encode(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box) {
+    const cuuint32_t ones[3] = {1, 1, 1};
+    EncodeTiled f = encode_tiled();
+    if (!f) return DBSPMSPV_ERR_CUDA;
+    return f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? DBSPMSPV_OK : DBSPMSPV_ERR_CUDA;
+}
+// `rows` rows of `width` entries, ld entries apart; a box holds 64 entries of box_rows rows
+static int encode_rows(CUtensorMap *map, const uint16_t *p, int64_t rows, int64_t width, int64_t ld, int box_rows) {
+    const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    return encode(map, p, 2, dims, strides, box);
+}
+// the copy by columns: 64 rows of a strip, `cols` columns, `strips` strips
+static int encode_weights(CUtensorMap *map, const dbspmspv_handle_s *h, int cols, int strips) {
+    const cuuint64_t dims[3] = {(cuuint64_t)DC_ROWS, (cuuint64_t)h->d.n, (cuuint64_t)((h->d.m + DC_ROWS - 1) / DC_ROWS)};
+    const cuuint64_t strides[2] = {DC_ROWS * 2, (cuuint64_t)h->d.n * DC_ROWS * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)cols, (cuuint32_t)strips};
+    return encode(map, h->lin_w, 3, dims, strides, box);
+}
+int linear_handle_maps(dbspmspv_handle_s *h) {
+    int s = encode_weights(&h->lin_maps[0], h, LG_K, LG_N / DC_ROWS);
+    if (s == DBSPMSPV_OK) s = encode_weights(&h->lin_maps[1], h, LG_K, LG_N / DC_ROWS / 2);
+    if (s == DBSPMSPV_OK) s = encode_weights(&h->lin_maps[2], h, LG_N, 1);
+    return s;
+}
+
+// Behind the copy by columns: the index of the stored weights by row.
+int build_linear_index(dbspmspv_handle_s *h, cudaStream_t st) {
+    const int64_t m = h->d.m, n = h->d.n;
+    const int words = (int)((n + 31) / 32);
+    const int64_t items = m * words;
+    uint2 *index = nullptr;
+    int32_t *count = nullptr, *first = nullptr;
+    void *tmp = nullptr;
+    size_t bytes = 0;
+    int s = DBSPMSPV_OK;
+    if (cudaMalloc(&index, (size_t)items * sizeof(uint2)) != cudaSuccess) { (void)cudaGetLastError(); return DBSPMSPV_ERR_ALLOC; }
+    h->lin_index = index;
+    h->lin_words = words;
+    if (cub::DeviceScan::ExclusiveSum(nullptr, bytes, count, first, items, st) != cudaSuccess) return DBSPMSPV_ERR_CUDA;
+    if (cudaMalloc(&count, (size_t)items * 4) != cudaSuccess || cudaMalloc(&first, (size_t)items * 4) != cudaSuccess || cudaMalloc(&tmp, bytes ? bytes : 1) != cudaSuccess) s = DBSPMSPV_ERR_ALLOC;
+    if (s == DBSPMSPV_OK) {
+        const int64_t threads = (m + 31) / 32 * words * 32;
+        k_linear_words<<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(h->lin_w, m, n, words, index, count);
+        if (cub::DeviceScan::ExclusiveSum(tmp, bytes, count, first, items, st) != cudaSuccess) s = DBSPMSPV_ERR_CUDA;
+        k_linear_places<<<(unsigned)((items + 255) / 256), 256, 0, st>>>(items, first, index);
+        if (cudaStreamSynchronize(st) != cudaSuccess) s = DBSPMSPV_ERR_CUDA;
+    }
+    cudaFree(count); cudaFree(first); cudaFree(tmp);
+    if (s != DBSPMSPV_OK) (void)cudaGetLastError();
+    return s;
+}
+
+// ---- beside the products --------------------------------------------------------------------
+// eight neighbouring entries j .. j + 7 of a row of `width`, as fp32; past its end 0
+__device__ __forceinline__ void lin_load8(const uint16_t *row, int64_t j, int64_t width, float (&v)[8]) {
+    if (j + 8 <= width && (reinterpret_cast<uintptr_t>(row + j) & 15u) == 0) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(row + j);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { v[2 * k] = __uint_as_float(w[k] << 16); v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = j + k < width ? lin_f32(row[j + k]) : 0.f;
+    }
+}
+// (rows of a workspace buffer begin on 16 bytes and are padded to a multiple of eight entries)
+__device__ __forceinline__ void lin_store8(uint16_t *row, int64_t j, const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = lin_bf16(v[2 * k]) | lin_bf16(v[2 * k + 1]) << 16;
+    *reinterpret_cast<uint4 *>(row + j) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// x whose rows TMA cannot address, with rows that it can
+__global__ void k_linear_pack(const uint16_t *x, int64_t ldx, int64_t tokens, int64_t n, uint16_t *out, int64_t ldo) {
+    pdl_wait();
+    const int64_t per = ldo / 8, total = tokens * per;
+    for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t t = i / per, j = (i - t * per) * 8;
+        float v[8];
+        lin_load8(x + t * ldx, j, n, v);
+        lin_store8(out + t * ldo, j, v);
+    }
+}
+
+// What the products of a gradient take: dz = dy act'(z), or dg = dy u act'(g) and du = dy act(g), rounded to bf16 (the tensor cores' operands; the
+// roundings are independent, so a sum over rows or tokens is off by about 2^-9 of its own size, as much as its own rounding to bf16), and the bias' gradient
+// from the unrounded ones.  A cluster of eight thread blocks takes 64 columns, each an eighth of the tokens, its 32 row lanes in turn; the sums meet in a
+// fixed order.  Bound by HBM: 2 bytes for each of dy, z, u, dz.
+constexpr int LS_CTA = 256, LS_RANKS = 8;
+struct LsArgs {
+    const uint16_t *dy, *z, *u;
+    int64_t lddy, ldz, tokens, m;
+    int act;
+    uint16_t *d0, *d1;              // null: not wanted
+    int64_t ldd;
+    float *dbias;
+};
+template <bool GATED>
+__global__ void __cluster_dims__(LS_RANKS, 1, 1) __launch_bounds__(LS_CTA)
+k_linear_slopes(const __grid_constant__ LsArgs a) {
+    namespace cg = cooperative_groups;
+    __shared__ float s_sum[LS_CTA / 8][64];
+    __shared__ float s_all[LS_RANKS][64];
+    const int rank = (int)(blockIdx.x % LS_RANKS), tid = threadIdx.x;
+    const int64_t j = (int64_t)(blockIdx.x / LS_RANKS) * 64 + (tid & 7) * 8;
+    pdl_wait();
+    float sum[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] = 0.f;
+    const int64_t t1 = a.tokens * (rank + 1) / LS_RANKS;
+    for (int64_t t = a.tokens * rank / LS_RANKS + (tid >> 3); t < t1 && j < a.m; t += LS_CTA / 8) {
+        float dy[8], z[8];
+        lin_load8(a.dy + t * a.lddy, j, a.m, dy);
+        if (GATED || a.z) lin_load8(a.z + t * a.ldz, j, a.m, z);
+        if (GATED) {
+            float u[8], d[8];
+            lin_load8(a.u + t * a.ldz, j, a.m, u);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { d[k] = dy[k] * u[k] * lin_act_slope(z[k], a.act); dy[k] *= lin_act(z[k], a.act); }
+            lin_store8(a.d0 + t * a.ldd, j, d);
+            lin_store8(a.d1 + t * a.ldd, j, dy);
+        } else {
+            if (a.z) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) dy[k] *= lin_act_slope(z[k], a.act);
+            }
+            if (a.d0) lin_store8(a.d0 + t * a.ldd, j, dy);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += dy[k];
+        }
+    }
+    if (GATED || !a.dbias) return;                                    // (the same for the whole grid)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s_sum[tid >> 3][(tid & 7) * 8 + k] = sum[k];
+    __syncthreads();
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();                                                   // (every block has started before its shared memory is written)
+    if (tid < 64) {
+        float v = 0.f;
+        for (int k = 0; k < LS_CTA / 8; ++k) v += s_sum[k][tid];
+        cluster.map_shared_rank(&s_all[0][0], 0)[rank * 64 + tid] = v;
+    }
+    cluster.sync();
+    const int64_t col = (int64_t)(blockIdx.x / LS_RANKS) * 64 + tid;
+    if (rank == 0 && tid < 64 && col < a.m) {
+        float v = 0.f;
+        for (int k = 0; k < LS_RANKS; ++k) v += s_all[k][tid];
+        a.dbias[col] = v;
+    }
+}
+
+// ---- launches -------------------------------------------------------------------------------
+static int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+static bool tma_rows(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld & 7) == 0; }
+
+template <int FORM, int C>
+static int add_gemm_c(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps, const LgArgs &a, int grid) {
+    bool &done = h->lin_configured[FORM][C];
+    if (!done) {
+        DBS_CUDA(cudaFuncSetAttribute(k_linear_gemm<FORM, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, LG_SMEM));
+        done = true;
+    }
+    calls.add(k_linear_gemm<FORM, C>, grid, LG_CTA, LG_SMEM, calls.n > 0, maps, a);
+    return DBSPMSPV_OK;
+}
+// Thread blocks that share a tile's K: as many as fit on the SMs that the tiles leave free, each with at least four blocks of K.
+template <int FORM>
+static int add_gemm(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps, const LgArgs &a) {
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n * a.products;
+    if (tiles >= (1ll << 30)) return DBSPMSPV_ERR_UNSUPPORTED;
+    if constexpr (FORM != LG_DW) {
+        const int kb = a.k_blocks * a.layers;
+        if (tiles * 8 <= h->sm_count && kb >= 32) return add_gemm_c<FORM, 8>(h, calls, maps, a, (int)tiles * 8);
+        if (tiles * 4 <= h->sm_count && kb >= 16) return add_gemm_c<FORM, 4>(h, calls, maps, a, (int)tiles * 4);
+        if (tiles * 3 <= h->sm_count && kb >= 12) return add_gemm_c<FORM, 3>(h, calls, maps, a, (int)tiles * 3);
+        if (tiles * 2 <= h->sm_count && kb >= 8) return add_gemm_c<FORM, 2>(h, calls, maps, a, (int)tiles * 2);
+    }
+    return add_gemm_c<FORM, 1>(h, calls, maps, a, (int)(tiles < h->sm_count ? tiles : h->sm_count));
+}
+
+template <int LAYERS, int C>
+static int add_columns_c(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a, int strips, int tokens) {
+    bool &done = h->lin_cols_configured[LAYERS - 1][C];
+    if (!done) {
+        DBS_CUDA(cudaFuncSetAttribute(k_linear_cols<LAYERS, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, LIN_COLS_MAX_SMEM));
+        done = true;
+    }
+    calls.add(k_linear_cols<LAYERS, C>, strips * C * tokens, LC_CTA, (size_t)LC_WARPS * lc_warp_entries(a.n, C) * sizeof(float2), false, a, strips);
+    return DBSPMSPV_OK;
+}
+// Thread blocks of a strip: as many as it takes to give every SM one.
+static int columns_cluster(const dbspmspv_handle_s *h, int64_t tokens) {
+    const int64_t units = (h->d.m + DC_ROWS - 1) / DC_ROWS * tokens;
+    int c = 1;
+    while (c < 8 && units * c * 2 <= h->sm_count) c *= 2;
+    return c;
+}
+template <int LAYERS>
+static int add_columns(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a, int tokens) {
+    const int strips = (int)((a.m + DC_ROWS - 1) / DC_ROWS);
+    switch (columns_cluster(h, tokens)) {
+        case 1: return add_columns_c<LAYERS, 1>(h, calls, a, strips, tokens);
+        case 2: return add_columns_c<LAYERS, 2>(h, calls, a, strips, tokens);
+        case 4: return add_columns_c<LAYERS, 4>(h, calls, a, strips, tokens);
+        default: return add_columns_c<LAYERS, 8>(h, calls, a, strips, tokens);
+    }
+}
+static bool over_columns(const dbspmspv_handle_s *h, int64_t tokens) {
+    return tokens <= LIN_COLS_MAX_TOKENS && LC_WARPS * lc_warp_entries(h->d.n, columns_cluster(h, tokens)) * (int64_t)sizeof(float2) <= LIN_COLS_MAX_SMEM;
+}
+
+// ---- workspace: x as TMA can read it, then the products' operands of a gradient ---------------
+struct LinRoom {
+    uint8_t *at;
+    int64_t left;
+    uint16_t *take(int64_t rows, int64_t ld) {
+        const int64_t bytes = round_up(rows * ld * 2, 256);
+        if (!at || left < bytes) return nullptr;
+        uint8_t *p = at;
+        at += bytes;
+        left -= bytes;
+        return reinterpret_cast<uint16_t *>(p);
+    }
+};
+static int64_t workspace_bytes(const dbspmspv_handle_s *h, int layers, int64_t tokens, bool backward) {
+    int64_t b = 0;
+    if (backward || !over_columns(h, tokens)) b += round_up(tokens * round_up(h->d.n, 8) * 2, 256);
+    if (backward) b += layers * round_up(tokens * round_up(h->d.m, 8) * 2, 256);
+    return b;
+}
+
+// x as the tensor maps can address it: as it lies, or packed into the workspace
+static int usable_x(CallList &calls, const dbspmspv_handle_s *h, const uint16_t **x, int64_t *ldx, int tokens, LinRoom &room) {
+    if (tma_rows(*x, *ldx)) return DBSPMSPV_OK;
+    const int64_t n = h->d.n, ld = round_up(n, 8);
+    uint16_t *p = room.take(tokens, ld);
+    if (!p) return DBSPMSPV_ERR_INVALID_ARG;
+    int64_t g = (tokens * (ld / 8) + 255) / 256;
+    if (g > 16 * h->sm_count) g = 16 * h->sm_count;
+    calls.add(k_linear_pack, (int)g, 256, 0, calls.n > 0, *x, *ldx, (int64_t)tokens, n, p, ld);
+    *x = p;
+    *ldx = ld;
+    return DBSPMSPV_OK;
+}
+
+static bool has_linear(const dbspmspv_handle_s *h) { return h->d.dtype == DBSPMSPV_BF16 && h->lin_ready; }
+
+struct LinForward {
+    const uint16_t *x;
+    int64_t ldx;
+    int tokens;
+    const uint16_t *bias;
+    int act;
+    const uint16_t *residual;
+    int64_t ldr;
+    void *y;
+    int64_t ldy;
+    int y_f32;
+    uint16_t *z, *u;
+    int64_t ldz;
+};
+// one layer, or (up != null) the gate and the other layer of a gated block
+static int forward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinForward f, LinRoom room, cudaStream_t st) {
+    const Device &d = h->d;
+    CallList calls;
+    int s = DBSPMSPV_OK;
+    if (over_columns(h, f.tokens)) {
+        LcArgs a = {};
+        a.x = f.x; a.ldx = f.ldx; a.n = d.n; a.m = d.m;
+        a.w[0] = reinterpret_cast<const uint4 *>(h->lin_w);
+        a.w[1] = up ? reinterpret_cast<const uint4 *>(up->lin_w) : nullptr;
+        a.bias = f.bias; a.residual = f.residual; a.ldr = f.ldr; a.y = f.y; a.ldy = f.ldy; a.y_f32 = f.y_f32; a.act = f.act;
+        a.z = f.z; a.u = f.u; a.ldz = f.ldz;
+        s = up ? add_columns<2>(h, calls, a, f.tokens) : add_columns<1>(h, calls, a, f.tokens);
+    } else {
+        s = usable_x(calls, h, &f.x, &f.ldx, f.tokens, room);
+        if (s != DBSPMSPV_OK) return s;
+        LgMaps maps = {};
+        if ((s = encode_rows(&maps.a[0], f.x, f.tokens, d.n, f.ldx, LG_M)) != DBSPMSPV_OK) return s;
+        maps.b[0] = up ? h->lin_maps[1] : h->lin_maps[0];
+        if (up) maps.b[1] = up->lin_maps[1];
+        LgArgs a = {};
+        const int out = up ? LG_N / 2 : LG_N;
+        a.tiles_m = (f.tokens - 1) / LG_M + 1; a.tiles_n = (int)((d.m + out - 1) / out); a.products = 1; a.layers = 1;
+        a.k_blocks = (int)((d.n + LG_K - 1) / LG_K);
+        a.tokens = f.tokens; a.width = d.m;
+        a.y = f.y; a.ldy = f.ldy; a.y_f32 = f.y_f32; a.act = f.act; a.bias = f.bias; a.residual = f.residual; a.ldr = f.ldr;
+        a.z = f.z; a.u = f.u; a.ldz = f.ldz; a.status = &d.ws.ctr->status;
+        s = up ? add_gemm<LG_GATED>(h, calls, maps, a) : add_gemm<LG_FORWARD>(h, calls, maps, a);
+    }
+    return s == DBSPMSPV_OK ? submit_calls(h, calls, st) : s;
+}
+
+struct LinBackward {
+    const uint16_t *x;
+    int64_t ldx;
+    int tokens, act;
+    const uint16_t *z, *u;
+    int64_t ldz;
+    const uint16_t *dy;
+    int64_t lddy;
+    uint16_t *dx;
+    int64_t lddx;
+    uint16_t *dw[2];
+    float *dbias;
+};
+static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, LinRoom room, cudaStream_t st) {
+    const Device &d = h->d;
+    CallList calls;
+    int s = DBSPMSPV_OK;
+    const bool want_w = b.dw[0] || b.dw[1], products = b.dx || want_w;
+    const int layers = up ? 2 : 1;
+    if (want_w && (s = usable_x(calls, h, &b.x, &b.ldx, b.tokens, room)) != DBSPMSPV_OK) return s;
+    const uint16_t *dz[2] = {b.dy, nullptr};
+    int64_t ldd = b.lddy;
+    const bool as_it_is = !up && b.act == DBSPMSPV_ACT_NONE && tma_rows(b.dy, b.lddy);
+    if ((products && !as_it_is) || b.dbias) {
+        LsArgs a = {};
+        a.dy = b.dy; a.lddy = b.lddy; a.z = b.act == DBSPMSPV_ACT_NONE && !up ? nullptr : b.z; a.u = b.u; a.ldz = b.ldz;
+        a.tokens = b.tokens; a.m = d.m; a.act = b.act; a.dbias = b.dbias;
+        if (products && !as_it_is) {
+            ldd = round_up(d.m, 8);
+            a.ldd = ldd;
+            dz[0] = a.d0 = room.take(b.tokens, ldd);
+            if (up) dz[1] = a.d1 = room.take(b.tokens, ldd);
+            if (!a.d0 || (up && !a.d1)) return DBSPMSPV_ERR_INVALID_ARG;
+        }
+        const int64_t g = (d.m + 63) / 64 * LS_RANKS;
+        calls.add(up ? k_linear_slopes<true> : k_linear_slopes<false>, (int)g, LS_CTA, 0, calls.n > 0, a);
+    }
+    LgArgs a = {};
+    a.status = &d.ws.ctr->status;
+    if (b.dx) {
+        LgMaps maps = {};
+        for (int l = 0; l < layers; ++l) {
+            if ((s = encode_rows(&maps.a[l], dz[l], b.tokens, d.m, ldd, LG_M)) != DBSPMSPV_OK) return s;
+            maps.b[l] = l ? up->lin_maps[2] : h->lin_maps[2];
+        }
+        a.tiles_m = (b.tokens - 1) / LG_M + 1; a.tiles_n = (int)((d.n + LG_N - 1) / LG_N); a.products = 1; a.layers = layers;
+        a.k_blocks = (int)((d.m + DC_ROWS - 1) / DC_ROWS);
+        a.tokens = b.tokens; a.width = d.n; a.y = b.dx; a.ldy = b.lddx;
+        if ((s = add_gemm<LG_DX>(h, calls, maps, a)) != DBSPMSPV_OK) return s;
+    }
+    if (want_w) {
+        LgMaps maps = {};
+        if ((s = encode_rows(&maps.a[0], b.x, b.tokens, d.n, b.ldx, LG_K)) != DBSPMSPV_OK) return s;
+        a.products = 0;
+        for (int l = 0; l < layers; ++l) {
+            if (!b.dw[l]) continue;
+            if ((s = encode_rows(&maps.b[a.products], dz[l], b.tokens, d.m, ldd, LG_K)) != DBSPMSPV_OK) return s;
+            a.dw[a.products] = b.dw[l];
+            a.index[a.products++] = (l ? up : h)->lin_index;
+        }
+        a.tiles_m = (int)((d.n + LG_M - 1) / LG_M); a.tiles_n = (int)((d.m + LG_N - 1) / LG_N); a.layers = 1;
+        a.k_blocks = (b.tokens - 1) / LG_K + 1;
+        a.tokens = b.tokens; a.width = d.m; a.index_words = h->lin_index ? h->lin_words : up->lin_words;
+        if ((s = add_gemm<LG_DW>(h, calls, maps, a)) != DBSPMSPV_OK) return s;
+    }
+    return submit_calls(h, calls, st);
+}
+
+static bool act_ok(int act) { return act >= DBSPMSPV_ACT_NONE && act <= DBSPMSPV_ACT_GELU; }
+static bool stride_ok(const void *p, int64_t ld, int64_t width) { return !p || ld >= width; }
+template <typename... P> static bool on_bytes(uintptr_t bytes, P... p) { return (((reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0) && ...); }
+static const uint16_t *in(const void *p) { return static_cast<const uint16_t *>(p); }
+static uint16_t *out(void *p) { return static_cast<uint16_t *>(p); }
+static LinRoom room(void *p, int64_t bytes) { return LinRoom{static_cast<uint8_t *>(p), bytes}; }
+
+}  // namespace dbs
+
+extern "C" {
+
+int dbspmspv_linear_workspace(dbspmspv_handle_t h, dbspmspv_handle_t up, int32_t tokens, int backward, int64_t *bytes) {
+    if (!h || !bytes || tokens < 0) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!dbs::has_linear(h) || (up && !dbs::has_linear(up))) return DBSPMSPV_ERR_UNSUPPORTED;
+    *bytes = dbs::workspace_bytes(h, up ? 2 : 1, tokens, backward != 0);
+    return DBSPMSPV_OK;
+}
+
+int dbspmspv_linear(dbspmspv_handle_t h, const void *x, int64_t ldx, int32_t tokens, const void *bias, int act, const void *residual, int64_t ldr, void *y, int64_t ldy,
+                    int y_f32, void *z, int64_t ldz, void *workspace, int64_t workspace_bytes, dbspmspv_stream_t stream) {
+    using namespace dbs;
+    if (!h || tokens < 0 || workspace_bytes < 0 || !act_ok(act) || (tokens > 0 && (!x || !y))) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!on_handle_device(h)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!has_linear(h)) return DBSPMSPV_ERR_UNSUPPORTED;
+    const int64_t m = h->d.m, n = h->d.n;
+    if (ldx < n || ldy < m || !stride_ok(residual, ldr, m) || !stride_ok(z, ldz, m)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!on_bytes(16, workspace) || !on_bytes(2, x, bias, residual, z) || !on_bytes(y_f32 ? 4 : 2, y)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (tokens == 0) return DBSPMSPV_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    h->last_stream = st;
+    return forward(h, nullptr, {in(x), ldx, tokens, in(bias), act, in(residual), ldr, y, ldy, y_f32 != 0, out(z), nullptr, ldz}, room(workspace, workspace_bytes), st);
+}
+
+int dbspmspv_gated(dbspmspv_handle_t gate, dbspmspv_handle_t up, const void *x, int64_t ldx, int32_t tokens, int act, void *y, int64_t ldy, void *g, void *u, int64_t ldgu,
+                   void *workspace, int64_t workspace_bytes, dbspmspv_stream_t stream) {
+    using namespace dbs;
+    if (!gate || !up || tokens < 0 || workspace_bytes < 0 || !act_ok(act) || (tokens > 0 && (!x || !y))) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!on_handle_device(gate) || !on_handle_device(up)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!has_linear(gate) || !has_linear(up)) return DBSPMSPV_ERR_UNSUPPORTED;
+    const int64_t m = gate->d.m, n = gate->d.n;
+    if (up->d.m != m || up->d.n != n) return DBSPMSPV_ERR_INVALID_ARG;
+    if (ldx < n || ldy < m || !stride_ok(g, ldgu, m) || !stride_ok(u, ldgu, m)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!on_bytes(16, workspace) || !on_bytes(2, x, y, g, u)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (tokens == 0) return DBSPMSPV_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    gate->last_stream = up->last_stream = st;
+    return forward(gate, up, {in(x), ldx, tokens, nullptr, act, nullptr, 0, y, ldy, 0, out(g), out(u), ldgu}, room(workspace, workspace_bytes), st);
+}
+
+int dbspmspv_linear_backward(dbspmspv_handle_t h, const void *x, int64_t ldx, int32_t tokens, int act, const void *z, int64_t ldz, const void *dy, int64_t lddy, void *dx,
+                             int64_t lddx, void *dw, float *dbias, void *workspace, int64_t workspace_bytes, dbspmspv_stream_t stream) {
+    using namespace dbs;
+    if (!h || tokens < 0 || workspace_bytes < 0 || !act_ok(act)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (tokens > 0 && (!dy || (dw && !x) || (act != DBSPMSPV_ACT_NONE && !z))) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!on_handle_device(h)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!has_linear(h) || (dw && !h->lin_index)) return DBSPMSPV_ERR_UNSUPPORTED;
+    const int64_t m = h->d.m, n = h->d.n;
+    if ((dw && ldx < n) || lddy < m || (act != DBSPMSPV_ACT_NONE && ldz < m) || !stride_ok(dx, lddx, n)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!on_bytes(16, workspace) || !on_bytes(2, x, z, dy, dx, dw) || !on_bytes(4, dbias)) return DBSPMSPV_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    h->last_stream = st;
+    if (tokens == 0) {
+        if (dw) DBS_CUDA(cudaMemsetAsync(dw, 0, (size_t)h->nnz * 2, st));
+        if (dbias) DBS_CUDA(cudaMemsetAsync(dbias, 0, (size_t)m * 4, st));
+        return DBSPMSPV_OK;
+    }
+    return backward(h, nullptr, {in(x), ldx, tokens, act, in(z), nullptr, ldz, in(dy), lddy, out(dx), lddx, {out(dw), nullptr}, dbias}, room(workspace, workspace_bytes), st);
+}
+
+int dbspmspv_gated_backward(dbspmspv_handle_t gate, dbspmspv_handle_t up, const void *x, int64_t ldx, int32_t tokens, int act, const void *g, const void *u, int64_t ldgu,
+                            const void *dy, int64_t lddy, void *dx, int64_t lddx, void *dw_gate, void *dw_up, void *workspace, int64_t workspace_bytes, dbspmspv_stream_t stream) {
+    using namespace dbs;
+    if (!gate || !up || tokens < 0 || workspace_bytes < 0 || !act_ok(act)) return DBSPMSPV_ERR_INVALID_ARG;
+    const bool want_w = dw_gate || dw_up;
+    if (tokens > 0 && (!dy || !g || !u || (want_w && !x))) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!on_handle_device(gate) || !on_handle_device(up)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!has_linear(gate) || !has_linear(up) || (dw_gate && !gate->lin_index) || (dw_up && !up->lin_index)) return DBSPMSPV_ERR_UNSUPPORTED;
+    const int64_t m = gate->d.m, n = gate->d.n;
+    if (up->d.m != m || up->d.n != n) return DBSPMSPV_ERR_INVALID_ARG;
+    if ((want_w && ldx < n) || lddy < m || ldgu < m || !stride_ok(dx, lddx, n)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!on_bytes(16, workspace) || !on_bytes(2, x, g, u, dy, dx, dw_gate, dw_up)) return DBSPMSPV_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    gate->last_stream = up->last_stream = st;
+    if (tokens == 0) {
+        if (dw_gate) DBS_CUDA(cudaMemsetAsync(dw_gate, 0, (size_t)gate->nnz * 2, st));
+        if (dw_up) DBS_CUDA(cudaMemsetAsync(dw_up, 0, (size_t)up->nnz * 2, st));
+        return DBSPMSPV_OK;
+    }
+    return backward(gate, up, {in(x), ldx, tokens, act, in(g), in(u), ldgu, in(dy), lddy, out(dx), lddx, {out(dw_gate), out(dw_up)}, nullptr}, room(workspace, workspace_bytes), st);
+}
+
+}  // extern "C"

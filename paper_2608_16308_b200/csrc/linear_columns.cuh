@@ -1,0 +1,169 @@
+// Linear and gated layers for single tokens (and a few): y = act(W x + bias) + residual, y = act(W_gate x) * (W_up x).
+//
+// One pass over the columns that the token reaches, from the copy by columns ([strip of 64 rows][column][row], see
+// decode_columns.cuh): what the call cannot do without is 2 bytes per weight of those columns.  A cluster of C thread blocks owns a
+// strip; a warp blocks its own share of x, keeps the entries that are not zero as a list (column, value) in shared memory and goes on to
+// their columns, 16 bytes a lane, all loads independent.  The sums of warps and ranks meet in shared memory, in a fixed order, and the
+// thread of a row finishes it there, so that neither a second pass over y nor an atomic is needed.
+//   * A gated call reads the same list against both layers' strips: both sums of a row end in one thread.
+//   * Several tokens are several rows of the grid: their columns overlap in L2 (the rule on tokens is in linear.cu).
+// The products are those of the matrix with zeros in the pruned places: a zero entry of x adds nothing (the weights are finite), one
+// that is not finite reaches every row.
+#pragma once
+
+#include <cooperative_groups.h>
+
+#include "linear_gemm.cuh"
+
+namespace dbs {
+
+constexpr int LC_WARPS = 16;
+constexpr int LC_CTA = LC_WARPS * 32;
+constexpr int LC_PIECE = 64;             // entries of x that a warp blocks side by side
+static_assert(DC_ROWS == 64, "eight lanes with eight rows each share a column");
+
+// entries of a warp's list, at most; the ranks and warps take the pieces of x in turn
+__host__ __device__ inline int64_t lc_warp_entries(int64_t n, int c) {
+    const int64_t pieces = (n + LC_PIECE - 1) / LC_PIECE;
+    return (pieces + (int64_t)c * LC_WARPS - 1) / ((int64_t)c * LC_WARPS) * LC_PIECE;
+}
+
+struct LcArgs {
+    const uint16_t *x;
+    int64_t ldx, n, m;
+    const uint4 *w[2];
+    const uint16_t *bias, *residual;
+    int64_t ldr;
+    void *y;
+    int64_t ldy;
+    int y_f32, act;
+    uint16_t *z, *u;
+    int64_t ldz;
+};
+
+template <int LAYERS, int C>
+__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(LC_CTA, 2)
+k_linear_cols(const __grid_constant__ LcArgs a, int strips) {
+    namespace cg = cooperative_groups;
+    constexpr int ILP = 8 / LAYERS;                                   // columns in flight per lane: 4 KB per warp
+    extern __shared__ __align__(16) uint8_t s_dyn[];
+    __shared__ __align__(8) float s_part[LAYERS][LC_WARPS][DC_ROWS];
+    __shared__ float s_sum[C][LAYERS][DC_ROWS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = C > 1 ? (int)(blockIdx.x % C) : 0, unit = (int)(blockIdx.x / C), strip = unit % strips;
+    const int64_t token = unit / strips;
+    // (a cluster: every block has started before its shared memory is written; met again behind the weights)
+    if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    pdl_wait();
+    const uint16_t *x = a.x + token * a.ldx;
+    float2 *list = reinterpret_cast<float2 *>(s_dyn) + (size_t)warp * lc_warp_entries(a.n, C);
+    int n = 0;
+    {
+        const bool aligned = (reinterpret_cast<uintptr_t>(x) & 3u) == 0;
+        for (int64_t j0 = ((int64_t)warp * C + rank) * LC_PIECE; j0 < a.n; j0 += (int64_t)LC_WARPS * C * LC_PIECE) {
+            const int64_t j = j0 + 2 * lane;
+            uint32_t v = 0;
+            if (aligned && j + 1 < a.n) v = *reinterpret_cast<const uint32_t *>(x + j);
+            else {
+                if (j < a.n) v = x[j];
+                if (j + 1 < a.n) v |= (uint32_t)x[j + 1] << 16;
+            }
+            const bool lo = v & 0x7FFFu, hi = v & 0x7FFF0000u;
+            const uint32_t ml = __ballot_sync(FULL, lo), mh = __ballot_sync(FULL, hi), below = (1u << lane) - 1u;
+            int at = n + __popc(ml & below) + __popc(mh & below);
+            if (lo) list[at++] = make_float2(__int_as_float((int)j), __uint_as_float(v << 16));
+            if (hi) list[at] = make_float2(__int_as_float((int)j + 1), __uint_as_float(v & 0xFFFF0000u));
+            n += __popc(ml) + __popc(mh);
+        }
+        __syncwarp();
+    }
+    {
+        const uint4 *w[LAYERS];
+#pragma unroll
+        for (int l = 0; l < LAYERS; ++l) w[l] = a.w[l] + (size_t)strip * a.n * (DC_ROWS / 8) + (lane & 7);
+        float acc[LAYERS][8];
+#pragma unroll
+        for (int l = 0; l < LAYERS; ++l)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) acc[l][r] = 0.f;
+        for (int k0 = 0; k0 < n; k0 += 4 * ILP) {
+            uint4 v[LAYERS][ILP];
+            float xv[ILP];
+#pragma unroll
+            for (int q = 0; q < ILP; ++q) {
+                const int k = k0 + q * 4 + (lane >> 3);
+                xv[q] = 0.f;
+#pragma unroll
+                for (int l = 0; l < LAYERS; ++l) v[l][q] = make_uint4(0u, 0u, 0u, 0u);
+                if (k < n) {
+                    const float2 e = list[k];
+                    xv[q] = e.y;
+#pragma unroll
+                    for (int l = 0; l < LAYERS; ++l) v[l][q] = __ldcs(w[l] + (size_t)__float_as_int(e.x) * (DC_ROWS / 8));
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < ILP; ++q)
+#pragma unroll
+                for (int l = 0; l < LAYERS; ++l) {
+                    const uint32_t p[4] = {v[l][q].x, v[l][q].y, v[l][q].z, v[l][q].w};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        acc[l][2 * r] += __uint_as_float(p[r] << 16) * xv[q];
+                        acc[l][2 * r + 1] += __uint_as_float(p[r] & 0xFFFF0000u) * xv[q];
+                    }
+                }
+        }
+        // sums over the four column slots of the warp: two halving exchanges leave two rows per lane
+        const bool h16 = lane & 16, h8 = lane & 8;
+#pragma unroll
+        for (int l = 0; l < LAYERS; ++l) {
+            float a4[4], a2[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a4[i] = (h16 ? acc[l][i + 4] : acc[l][i]) + __shfl_xor_sync(FULL, h16 ? acc[l][i] : acc[l][i + 4], 16);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) a2[i] = (h8 ? a4[i + 2] : a4[i]) + __shfl_xor_sync(FULL, h8 ? a4[i] : a4[i + 2], 8);
+            *reinterpret_cast<float2 *>(&s_part[l][warp][(lane & 7) * 8 + (h16 ? 4 : 0) + (h8 ? 2 : 0)]) = make_float2(a2[0], a2[1]);
+        }
+    }
+    __syncthreads();
+    float sum = 0.f;                                                  // thread (layer, row)
+    const int layer = tid / DC_ROWS, r = tid % DC_ROWS;
+    if (layer < LAYERS) {
+#pragma unroll
+        for (int k = 0; k < LC_WARPS; ++k) sum += s_part[layer][k][r];
+    }
+    if (C > 1) {
+        cg::cluster_group cluster = cg::this_cluster();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (layer < LAYERS) cluster.map_shared_rank(&s_sum[0][0][0], 0)[(rank * LAYERS + layer) * DC_ROWS + r] = sum;
+        cluster.sync();
+        if (rank != 0) return;
+    } else if (LAYERS > 1) {
+        if (layer < LAYERS) s_sum[0][layer][r] = sum;
+        __syncthreads();
+    }
+    const int64_t row = (int64_t)strip * DC_ROWS + tid;
+    if (tid >= DC_ROWS || row >= a.m) return;
+    float z = sum, up = 0.f;
+    if (C > 1 || LAYERS > 1) {
+        z = 0.f;
+#pragma unroll
+        for (int q = 0; q < C; ++q) {
+            z += s_sum[q][0][tid];
+            if (LAYERS > 1) up += s_sum[q][LAYERS - 1][tid];
+        }
+    }
+    if (a.bias) z += lin_f32(a.bias[row]);
+    if (a.z) a.z[token * a.ldz + row] = (uint16_t)lin_bf16(z);
+    float y = lin_act(z, a.act);
+    if (LAYERS > 1) {
+        if (a.u) a.u[token * a.ldz + row] = (uint16_t)lin_bf16(up);
+        y *= up;
+    }
+    if (a.residual) y += lin_f32(a.residual[token * a.ldr + row]);
+    if (a.y_f32) static_cast<float *>(a.y)[token * a.ldy + row] = y;
+    else static_cast<uint16_t *>(a.y)[token * a.ldy + row] = (uint16_t)lin_bf16(y);
+}
+
+}  // namespace dbs
