@@ -340,13 +340,13 @@ struct dbspmspv_handle_s {
     bool heavy_stage;           // most stored elements sit in mask-based blocks: MODE 1 kernels
     bool payload_rich;          // not most, but more than an eighth sit in blocks with a payload (see PD_GROUPS_MIN_NNZ_X)
     // Linear and gated layers (linear.cu): the copy by columns (Device::cols, or built for the create option `linear` alone), its tensor maps for the forward product of
-    // one layer, of two, and for the gradient of x; the stored weights by row (option `linear`): [row][word of 32 columns] stored columns, place of the first.
+    // one layer, of two, and for the gradient of x; the stored weights by row (option `linear`): [word of 32 columns][row] stored columns, place of the first.
     const uint16_t *lin_w;
     CUtensorMap lin_maps[3];
     uint2 *lin_index;
     int lin_words;
     bool lin_ready;             // copy and maps are there
-    bool lin_configured[4][9], lin_cols_configured[2][9];    // [..][thread blocks of a cluster]
+    bool lin_configured[4][2][5][9], lin_cols_configured[2][9];    // [..][thread blocks of a cluster]
     cudaEvent_t ev[2];          // optional timing of the traversal kernel (run_opts.timing)
     bool timed;
     int64_t kernel_launches;    // kernels this handle has launched (run / decode / bfs)

@@ -27,12 +27,13 @@ __global__ void k_linear_words(const uint16_t *w, int64_t m, int64_t n, int word
     uint32_t bits = 0;
     for (int c = 0; c < 32; ++c)
         if ((int64_t)word * 32 + c < n && p[(int64_t)c * DC_ROWS] != DC_ABSENT) bits |= 1u << c;
-    index[row * words + word].x = bits;
+    index[word * m + row].x = bits;
     count[row * words + word] = __popc(bits);
 }
-__global__ void k_linear_places(int64_t n, const int32_t *first, uint2 *index) {
+// (counted row by row, kept word by word: a tile of the gradient takes the rows of one word side by side)
+__global__ void k_linear_places(int64_t m, int words, const int32_t *first, uint2 *index) {
     const int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
-    if (i < n) index[i].y = (uint32_t)first[i];
+    if (i < m * words) index[i].y = (uint32_t)first[i % m * words + i / m];
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
@@ -68,9 +69,9 @@ static int encode_weights(CUtensorMap *map, const dbspmspv_handle_s *h, int cols
     return encode(map, h->lin_w, 3, dims, strides, box);
 }
 int linear_handle_maps(dbspmspv_handle_s *h) {
-    int s = encode_weights(&h->lin_maps[0], h, LG_K, LG_N / DC_ROWS);
-    if (s == DBSPMSPV_OK) s = encode_weights(&h->lin_maps[1], h, LG_K, LG_N / DC_ROWS / 2);
-    if (s == DBSPMSPV_OK) s = encode_weights(&h->lin_maps[2], h, LG_N, 1);
+    int s = encode_weights(&h->lin_maps[0], h, LG_K, LG_M / DC_ROWS);
+    if (s == DBSPMSPV_OK) s = encode_weights(&h->lin_maps[1], h, LG_K, LG_M / DC_ROWS / 2);
+    if (s == DBSPMSPV_OK) s = encode_weights(&h->lin_maps[2], h, LG_M, 1);
     return s;
 }
 
@@ -93,7 +94,7 @@ int build_linear_index(dbspmspv_handle_s *h, cudaStream_t st) {
         const int64_t threads = (m + 31) / 32 * words * 32;
         k_linear_words<<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(h->lin_w, m, n, words, index, count);
         if (cub::DeviceScan::ExclusiveSum(tmp, bytes, count, first, items, st) != cudaSuccess) s = DBSPMSPV_ERR_CUDA;
-        k_linear_places<<<(unsigned)((items + 255) / 256), 256, 0, st>>>(items, first, index);
+        k_linear_places<<<(unsigned)((items + 255) / 256), 256, 0, st>>>(m, words, first, index);
         if (cudaStreamSynchronize(st) != cudaSuccess) s = DBSPMSPV_ERR_CUDA;
     }
     cudaFree(count); cudaFree(first); cudaFree(tmp);
@@ -205,29 +206,43 @@ k_linear_slopes(const __grid_constant__ LsArgs a) {
 static int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 static bool tma_rows(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld & 7) == 0; }
 
-template <int FORM, int C>
-static int add_gemm_c(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps, const LgArgs &a, int grid) {
-    bool &done = h->lin_configured[FORM][C];
+// How a product is cut: CG thread blocks per tile of CG * 128 x nt, or C that share a tile's K.
+struct LgPlan { int cg, nt, c; };
+
+template <int FORM, int CG, int NT, int C>
+static int add_gemm_as(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps, const LgArgs &a, int grid) {
+    bool &done = h->lin_configured[FORM][CG - 1][NT / 64][C];
     if (!done) {
-        DBS_CUDA(cudaFuncSetAttribute(k_linear_gemm<FORM, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, LG_SMEM));
+        DBS_CUDA(cudaFuncSetAttribute(k_linear_gemm<FORM, CG, NT, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, lg_smem(CG, NT)));
         done = true;
     }
-    calls.add(k_linear_gemm<FORM, C>, grid, LG_CTA, LG_SMEM, calls.n > 0, maps, a);
+    calls.add(k_linear_gemm<FORM, CG, NT, C>, grid, LG_CTA, lg_smem(CG, NT), calls.n > 0, maps, a);
     return DBSPMSPV_OK;
 }
-// Thread blocks that share a tile's K: as many as fit on the SMs that the tiles leave free, each with at least four blocks of K.
 template <int FORM>
-static int add_gemm(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps, const LgArgs &a) {
+static int add_gemm(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps, const LgArgs &a, LgPlan p) {
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n * a.products;
-    if (tiles >= (1ll << 30)) return DBSPMSPV_ERR_UNSUPPORTED;
-    if constexpr (FORM != LG_DW) {
-        const int kb = a.k_blocks * a.layers;
-        if (tiles * 8 <= h->sm_count && kb >= 32) return add_gemm_c<FORM, 8>(h, calls, maps, a, (int)tiles * 8);
-        if (tiles * 4 <= h->sm_count && kb >= 16) return add_gemm_c<FORM, 4>(h, calls, maps, a, (int)tiles * 4);
-        if (tiles * 3 <= h->sm_count && kb >= 12) return add_gemm_c<FORM, 3>(h, calls, maps, a, (int)tiles * 3);
-        if (tiles * 2 <= h->sm_count && kb >= 8) return add_gemm_c<FORM, 2>(h, calls, maps, a, (int)tiles * 2);
+    if (tiles >= (1ll << 27)) return DBSPMSPV_ERR_UNSUPPORTED;
+    const int slots = h->sm_count * (p.nt <= 64 ? 2 : 1) / p.cg, grid = (int)(tiles < slots ? tiles : slots) * p.cg;
+    if (p.cg == 2) return add_gemm_as<FORM, 2, 256, 1>(h, calls, maps, a, grid);
+    if constexpr (FORM == LG_DW) return add_gemm_as<FORM, 1, 256, 1>(h, calls, maps, a, grid);
+    else {
+#define LG_CASE(NT, C) if (p.nt == NT && p.c == C) return add_gemm_as<FORM, 1, NT, C>(h, calls, maps, a, C > 1 ? (int)tiles * C : grid);
+        LG_CASE(16, 1) LG_CASE(16, 2) LG_CASE(16, 4) LG_CASE(16, 8) LG_CASE(64, 1) LG_CASE(64, 2) LG_CASE(64, 4) LG_CASE(64, 8)
+        LG_CASE(128, 1) LG_CASE(128, 2) LG_CASE(128, 4) LG_CASE(128, 8) LG_CASE(256, 1) LG_CASE(256, 2) LG_CASE(256, 4) LG_CASE(256, 8)
+#undef LG_CASE
+        return DBSPMSPV_ERR_CUDA;
     }
-    return add_gemm_c<FORM, 1>(h, calls, maps, a, (int)(tiles < h->sm_count ? tiles : h->sm_count));
+}
+static int64_t ceil64(int64_t v, int64_t by) { return (v + by - 1) / by; }
+// `out`: output columns of a tile of one thread block
+static LgPlan plan_gemm(const dbspmspv_handle_s *h, int64_t tokens, int64_t width, int out, int64_t kb) {
+    if (tokens > 128 && ceil64(width, 2 * out) * ceil64(tokens, 256) * 4 >= h->sm_count / 2 * 3) return {2, 256, 1};
+    LgPlan p = {1, tokens <= 16 ? 16 : tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256, 1};
+    if (p.nt == 256 && ceil64(tokens, 128) * 128 < ceil64(tokens, 256) * 256) p.nt = 128;
+    const int64_t tiles = ceil64(width, out) * ceil64(tokens, p.nt), slots = h->sm_count * (p.nt <= 64 ? 2 : 1);
+    while (p.c < 8 && tiles * p.c * 2 <= slots && kb >= 8 * p.c) p.c *= 2;
+    return p;
 }
 
 template <int LAYERS, int C>
@@ -327,18 +342,19 @@ static int forward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinForward f, Li
     } else {
         s = usable_x(calls, h, &f.x, &f.ldx, f.tokens, room);
         if (s != DBSPMSPV_OK) return s;
+        const int out = up ? LG_M / 2 : LG_M;
+        const int64_t kb = ceil64(d.n, LG_K);
+        const LgPlan p = plan_gemm(h, f.tokens, d.m, out, kb);
         LgMaps maps = {};
-        if ((s = encode_rows(&maps.a[0], f.x, f.tokens, d.n, f.ldx, LG_M)) != DBSPMSPV_OK) return s;
-        maps.b[0] = up ? h->lin_maps[1] : h->lin_maps[0];
-        if (up) maps.b[1] = up->lin_maps[1];
+        maps.a[0] = up ? h->lin_maps[1] : h->lin_maps[0];
+        if (up) maps.a[1] = up->lin_maps[1];
+        if ((s = encode_rows(&maps.b[0], f.x, f.tokens, d.n, f.ldx, p.nt / p.cg)) != DBSPMSPV_OK) return s;
         LgArgs a = {};
-        const int out = up ? LG_N / 2 : LG_N;
-        a.tiles_m = (f.tokens - 1) / LG_M + 1; a.tiles_n = (int)((d.m + out - 1) / out); a.products = 1; a.layers = 1;
-        a.k_blocks = (int)((d.n + LG_K - 1) / LG_K);
+        a.tiles_m = (int)ceil64(d.m, p.cg * out); a.tiles_n = (int)ceil64(f.tokens, p.nt); a.products = 1; a.layers = 1; a.k_blocks = (int)kb;
         a.tokens = f.tokens; a.width = d.m;
         a.y = f.y; a.ldy = f.ldy; a.y_f32 = f.y_f32; a.act = f.act; a.bias = f.bias; a.residual = f.residual; a.ldr = f.ldr;
         a.z = f.z; a.u = f.u; a.ldz = f.ldz; a.status = &d.ws.ctr->status;
-        s = up ? add_gemm<LG_GATED>(h, calls, maps, a) : add_gemm<LG_FORWARD>(h, calls, maps, a);
+        s = up ? add_gemm<LG_GATED>(h, calls, maps, a, p) : add_gemm<LG_FORWARD>(h, calls, maps, a, p);
     }
     return s == DBSPMSPV_OK ? submit_calls(h, calls, st) : s;
 }
@@ -383,15 +399,16 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
     LgArgs a = {};
     a.status = &d.ws.ctr->status;
     if (b.dx) {
+        const int64_t kb = ceil64(d.m, DC_ROWS);
+        const LgPlan p = plan_gemm(h, b.tokens, d.n, LG_M, kb * layers);
         LgMaps maps = {};
         for (int l = 0; l < layers; ++l) {
-            if ((s = encode_rows(&maps.a[l], dz[l], b.tokens, d.m, ldd, LG_M)) != DBSPMSPV_OK) return s;
-            maps.b[l] = l ? up->lin_maps[2] : h->lin_maps[2];
+            maps.a[l] = l ? up->lin_maps[2] : h->lin_maps[2];
+            if ((s = encode_rows(&maps.b[l], dz[l], b.tokens, d.m, ldd, p.nt / p.cg)) != DBSPMSPV_OK) return s;
         }
-        a.tiles_m = (b.tokens - 1) / LG_M + 1; a.tiles_n = (int)((d.n + LG_N - 1) / LG_N); a.products = 1; a.layers = layers;
-        a.k_blocks = (int)((d.m + DC_ROWS - 1) / DC_ROWS);
+        a.tiles_m = (int)ceil64(d.n, p.cg * LG_M); a.tiles_n = (int)ceil64(b.tokens, p.nt); a.products = 1; a.layers = layers; a.k_blocks = (int)kb;
         a.tokens = b.tokens; a.width = d.n; a.y = b.dx; a.ldy = b.lddx;
-        if ((s = add_gemm<LG_DX>(h, calls, maps, a)) != DBSPMSPV_OK) return s;
+        if ((s = add_gemm<LG_DX>(h, calls, maps, a, p)) != DBSPMSPV_OK) return s;
     }
     if (want_w) {
         LgMaps maps = {};
@@ -403,10 +420,11 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
             a.dw[a.products] = b.dw[l];
             a.index[a.products++] = (l ? up : h)->lin_index;
         }
-        a.tiles_m = (int)((d.n + LG_M - 1) / LG_M); a.tiles_n = (int)((d.m + LG_N - 1) / LG_N); a.layers = 1;
-        a.k_blocks = (b.tokens - 1) / LG_K + 1;
+        LgPlan p = {2, 256, 1};
+        if (ceil64(d.n, 2 * LG_M) * ceil64(d.m, p.nt) * a.products * 4 < h->sm_count / 2 * 3) p.cg = 1;
+        a.tiles_m = (int)ceil64(d.n, p.cg * LG_M); a.tiles_n = (int)ceil64(d.m, p.nt); a.layers = 1; a.k_blocks = (int)ceil64(b.tokens, LG_K);
         a.tokens = b.tokens; a.width = d.m; a.index_words = h->lin_index ? h->lin_words : up->lin_words;
-        if ((s = add_gemm<LG_DW>(h, calls, maps, a)) != DBSPMSPV_OK) return s;
+        if ((s = add_gemm<LG_DW>(h, calls, maps, a, p)) != DBSPMSPV_OK) return s;
     }
     return submit_calls(h, calls, st);
 }

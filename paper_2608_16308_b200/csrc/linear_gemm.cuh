@@ -4,22 +4,25 @@
 // From a handful of tokens on every weight is reached, and a layer pruned without a pattern to half has no form that the
 // tensor cores could skip anything of: the product of the matrix with zeros in the pruned places is the fast one.  All three products
 //
-//   forward          Y [token][row]     = X [token][column]  times  W [row][column] over the columns
-//   gradient of x    dX [token][column] = dZ [token][row]    times  W [row][column] over the rows
-//   gradient of W    dW [column][row]   = X [token][column]  times  dZ [token][row] over the tokens (stored places only)
+//   forward          Y^T [row][token]    = W [row][column]     times  X [token][column] over the columns
+//   gradient of x    dX^T [column][token] = W [row][column]    times  dZ [token][row] over the rows
+//   gradient of W    dW^T [column][row]  = X [token][column]   times  dZ [token][row] over the tokens (stored places only)
 //
 // read the operands as they lie -- tokens row by row, W in the strips of the copy by columns ([strip of 64 rows][column][row], 128
 // bytes per column and strip).  64 rows of bf16 are the 128 bytes of one swizzle row, so a strip is an operand tile with the rows
-// along M/N for the forward product and along K for the gradient of x; nothing is transposed or laid out again.
+// along M for the forward product and along K for the gradient of x; nothing is transposed or laid out again.
 //
-//   * Tile 128 x 256, K in blocks of 64, four stages of 48 KB filled by TMA (edges are zero-filled by the tensor maps), one thread
-//     issues the loads, one the products, four warps empty the accumulators.  Two accumulators of 256 TMEM columns take turns, so
-//     the epilogue of one tile runs under the products of the next.
-//   * Gated: the tile's 256 columns are 128 rows of the gate and the same 128 of the other layer; both sums of an output
-//     meet in one thread.
-//   * Gradient of W: M are the columns and N the rows, so that the lanes of a warp hold 32 neighbouring columns of one row and the
-//     stored ones among them are neighbours in the values' array: one popc gives each its place.
-//   * Few tiles: the C thread blocks of a cluster share K and add their sums up through distributed shared memory, in rank order.
+//   * M (the lanes of an accumulator) is the dimension that lies side by side in the output: a warp's 32 lanes write neighbours,
+//     whatever the strides are, and tokens are N, so that few tokens are a narrow tile.  Tiles are 128 x NT.
+//   * One thread issues the loads (TMA; edges are zero-filled by the tensor maps), one the products, four warps empty the accumulators.
+//     Two accumulators take turns, so the epilogue of one tile runs under the products of the next.
+//   * CG = 2: the two thread blocks of a cluster work on one 256 x 256 tile, each with half of either operand in its shared memory:
+//     32 KB per block of K and SM where one block alone would need 48.
+//   * Gated: M are 64 rows of the gate and the same 64 of the other layer; the warps of the two halves exchange what the other
+//     needs through shared memory, each finishes half of the tokens.
+//   * Gradient of W: the lanes of a warp hold 32 neighbouring columns of one row, and the stored ones among them are neighbours in the
+//     values' array: one popc gives each its place.
+//   * C > 1, few tiles: the C thread blocks of a cluster share K and add their sums up through distributed shared memory, in rank order.
 //
 // Sums are fp32 in TMEM; what is handed on in bf16 is rounded once.  Every wait is bounded.
 #pragma once
@@ -32,25 +35,28 @@
 
 namespace dbs {
 
-constexpr int LG_M = 128, LG_N = 256, LG_K = 64;
-constexpr int LG_A_BYTES = LG_M * LG_K * 2, LG_B_BYTES = LG_N * LG_K * 2, LG_STAGE_BYTES = LG_A_BYTES + LG_B_BYTES;
-constexpr int LG_STAGES = 4;
-constexpr int LG_SMEM = LG_STAGES * LG_STAGE_BYTES + 1024;     // (the swizzle's pattern repeats every 1024 bytes: the stages begin on a multiple)
+constexpr int LG_M = 128, LG_K = 64;
+constexpr int LG_A_BYTES = LG_M * LG_K * 2;
 constexpr int LG_WARPS = 6;                                    // loads, products, four for the accumulators
 constexpr int LG_CTA = LG_WARPS * 32;
-constexpr int LG_CHUNK = 16;                                   // accumulator columns that a thread takes at a time
-static_assert(LG_N * LG_M * 4 <= LG_STAGES * LG_STAGE_BYTES, "a tile's sums, for the other thread blocks of a cluster, lie in the stages");
+constexpr int LG_EXCHANGE = 4 * 16 * 32 * 4;                   // gated: 16 tokens of 32 lanes for each of the four warps
+
+// Stages of a form: a block of K of both operands.  Narrow tiles (few tokens, bound by HBM) leave room for two thread blocks per SM.
+__host__ __device__ constexpr int lg_stage_bytes(int cg, int nt) { return LG_A_BYTES + nt / cg * LG_K * 2; }
+__host__ __device__ constexpr int lg_stages(int cg, int nt) { return nt <= 16 ? 5 : nt <= 64 ? 4 : nt <= 128 || cg == 2 ? 6 : 4; }
+// (the swizzle's pattern repeats every 1024 bytes: the stages begin on a multiple)
+__host__ __device__ constexpr int lg_smem(int cg, int nt) { return lg_stages(cg, nt) * lg_stage_bytes(cg, nt) + LG_EXCHANGE + 1024; }
 
 enum LgForm { LG_FORWARD = 0, LG_GATED = 1, LG_DX = 2, LG_DW = 3 };
 
 struct LgMaps { CUtensorMap a[2], b[2]; };                     // (the second ones: the second layer of a gated block)
 
 struct LgArgs {
-    int tiles_m, tiles_n;           // tiles of one product
+    int tiles_m, tiles_n;           // tiles of one product: of the output's width (LG_DW: of its columns), of the tokens (LG_DW: of its rows)
     int products;                   // LG_DW: 2 for the two layers of a gated block, as one list of tiles
     int k_blocks;                   // of one layer
     int layers;                     // LG_DX: the layers whose products are added up, one behind the other along K
-    int64_t tokens, width;          // rows and columns of y (LG_DW: rows of W = columns of dZ)
+    int64_t tokens, width;          // rows and columns of y (LG_DW: width = rows of W)
     void *y;
     int64_t ldy;
     int y_f32, act;
@@ -59,7 +65,7 @@ struct LgArgs {
     uint16_t *z, *u;                // in front of the activation; the other projection (may be null)
     int64_t ldz;
     uint16_t *dw[2];
-    const uint2 *index[2];          // [row][word of 32 columns]: stored columns, place of the first of them
+    const uint2 *index[2];          // [word of 32 columns][row]: stored columns, place of the first of them
     int index_words;
     int32_t *status;
 };
@@ -85,39 +91,80 @@ __device__ __forceinline__ uint32_t lin_bf16(float v) { return (uint32_t)__bfloa
 __device__ __forceinline__ float lin_f32(uint32_t half) { return __uint_as_float(half << 16); }
 
 // ---- instructions ------------------------------------------------------------------------
+template <int CG>
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int c0, int c1, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+    if (CG == 1)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
 }
+template <int CG>
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+    if (CG == 1)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
 }
+template <int CG>
 __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+    if (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
+// arrives on the barrier (CG = 2: on the one at the same place in both thread blocks) when every product issued so far has been made
+template <int CG>
 __device__ __forceinline__ void tc_commit(uint64_t *bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+    if (CG == 1) asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+    else asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)), "h"((uint16_t)3) : "memory");
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_load16(uint32_t addr, float (&v)[LG_CHUNK]) {
-    uint32_t r[LG_CHUNK];
+__device__ __forceinline__ void tc_load16(uint32_t addr, float (&v)[16]) {
+    uint32_t r[16];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
                    "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
 #pragma unroll
-    for (int i = 0; i < LG_CHUNK; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 // (the loaded registers are named, so that nothing that uses them moves in front of the wait)
-__device__ __forceinline__ void tc_load_wait(float (&v)[LG_CHUNK]) {
+__device__ __forceinline__ void tc_load_wait(float (&v)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
                    "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]) :: "memory");
 }
-__device__ __forceinline__ void mbar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
+    uint32_t far;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(addr), "r"(rank));
+    return far;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t far) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(far) : "memory"); }
+__device__ __forceinline__ float ld_cluster(uint32_t far) {
+    float f;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(far) : "memory");
+    return f;
+}
+__device__ __forceinline__ void st_shared(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+__device__ __forceinline__ float ld_shared(uint32_t addr) {
+    float f;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(addr) : "memory");
+    return f;
+}
+
+// whether `ok` holds in both warps of a pair
+__device__ __forceinline__ bool pair_all(int barrier, bool ok) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"((uint32_t)ok), "r"(barrier) : "memory");
+    return all != 0;
+}
 
 // Descriptor of an operand tile in shared memory under the 128-byte swizzle.  K along the swizzle rows: 64 of K per row, eight rows of M/N 1024
 // bytes on (the other stride is not used).  M/N along them: eight of K 1024 bytes on, the next 64 of M/N behind the block's 64 of K.
@@ -125,8 +172,8 @@ __device__ __forceinline__ uint64_t lg_desc(uint32_t addr, bool mn_major) {
     const uint64_t leading = mn_major ? LG_K * 128 : 16;
     return (uint64_t)((addr >> 4) & 0x3FFFu) | (leading >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
-__host__ __device__ constexpr uint32_t lg_idesc(bool a_mn, bool b_mn) {        // fp32 sums, bf16 operands
-    return 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)a_mn << 15 | (uint32_t)b_mn << 16 | (uint32_t)(LG_N >> 3) << 17 | (uint32_t)(LG_M >> 4) << 24;
+__host__ __device__ constexpr uint32_t lg_idesc(int m, int n, bool a_mn, bool b_mn) {        // fp32 sums, bf16 operands
+    return 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)a_mn << 15 | (uint32_t)b_mn << 16 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
 
 // Bounded wait that also gives up when another thread of the block has (s_fail).
@@ -140,107 +187,114 @@ __device__ __forceinline__ bool lg_wait(uint64_t *bar, uint32_t parity, volatile
     return false;
 }
 
-// ---- what becomes of 16 neighbouring sums of one token -----------------------------------
-__device__ __forceinline__ void lg_store16(uint16_t *p, const float (&v)[LG_CHUNK], int count) {
-    if (count == LG_CHUNK && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
-        uint32_t w[LG_CHUNK / 2];
-#pragma unroll
-        for (int i = 0; i < LG_CHUNK / 2; ++i) w[i] = lin_bf16(v[2 * i]) | lin_bf16(v[2 * i + 1]) << 16;
-        reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < LG_CHUNK; ++i)
-            if (i < count) p[i] = (uint16_t)lin_bf16(v[i]);
-    }
-}
-__device__ __forceinline__ void lg_add16(const uint16_t *p, float (&v)[LG_CHUNK], int count) {
-    if (count == LG_CHUNK && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
-        const uint4 a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1];
-        const uint32_t w[LG_CHUNK / 2] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int i = 0; i < LG_CHUNK / 2; ++i) { v[2 * i] += __uint_as_float(w[i] << 16); v[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < LG_CHUNK; ++i)
-            if (i < count) v[i] += lin_f32(p[i]);
-    }
-}
-__device__ __forceinline__ void lg_act16(float (&v)[LG_CHUNK], int act) {
+// ---- what becomes of CH neighbouring tokens' sums of one output column (the lane's) --------
+template <int CH>
+__device__ __forceinline__ void lg_act(float (&v)[CH], int act) {
     if (act == DBSPMSPV_ACT_NONE) return;
     if (act == DBSPMSPV_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < LG_CHUNK; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_RELU);
+        for (int i = 0; i < CH; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_RELU);
     } else if (act == DBSPMSPV_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < LG_CHUNK; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_SILU);
+        for (int i = 0; i < CH; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_SILU);
     } else {
 #pragma unroll
-        for (int i = 0; i < LG_CHUNK; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_GELU);
+        for (int i = 0; i < CH; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_GELU);
     }
 }
-// outputs [col, col + 16) of token `t`; v: the sums, u: the other layer's (gated)
-template <int FORM>
-__device__ __forceinline__ void lg_finish(const LgArgs &a, int64_t t, int64_t col, float (&v)[LG_CHUNK], const float (&u)[LG_CHUNK]) {
-    if (t >= a.tokens || col >= a.width) return;
-    const int count = a.width - col < LG_CHUNK ? (int)(a.width - col) : LG_CHUNK;
-    if (FORM == LG_FORWARD && a.bias) lg_add16(a.bias + col, v, count);
-    if (FORM != LG_DX && a.z) lg_store16(a.z + t * a.ldz + col, v, count);
-    if (FORM != LG_DX) lg_act16(v, a.act);
-    if (FORM == LG_GATED) {
-        if (a.u) lg_store16(a.u + t * a.ldz + col, u, count);
+template <int CH>
+__device__ __forceinline__ void lg_store(uint16_t *p, int64_t ld, const float (&v)[CH], int count) {
 #pragma unroll
-        for (int i = 0; i < LG_CHUNK; ++i) v[i] *= u[i];
+    for (int i = 0; i < CH; ++i)
+        if (i < count) p[i * ld] = (uint16_t)lin_bf16(v[i]);
+}
+// tokens [t, t + CH) of output column `col`; v: the sums, u: the other layer's (gated)
+template <int FORM, int CH>
+__device__ __forceinline__ void lg_finish(const LgArgs &a, int64_t t, int64_t col, float (&v)[CH], const float (&u)[CH]) {
+    if (t >= a.tokens || col >= a.width) return;
+    const int count = a.tokens - t < CH ? (int)(a.tokens - t) : CH;
+    float r[CH];
+    if (FORM == LG_FORWARD && a.residual) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) r[i] = i < count ? lin_f32(a.residual[(t + i) * a.ldr + col]) : 0.f;
     }
-    if (FORM == LG_FORWARD && a.residual) lg_add16(a.residual + t * a.ldr + col, v, count);
+    if (FORM == LG_FORWARD && a.bias) {
+        const float b = lin_f32(a.bias[col]);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) v[i] += b;
+    }
+    if (FORM != LG_DX && a.z) lg_store<CH>(a.z + t * a.ldz + col, a.ldz, v, count);
+    if (FORM != LG_DX) lg_act<CH>(v, a.act);
+    if (FORM == LG_GATED) {
+        if (a.u) lg_store<CH>(a.u + t * a.ldz + col, a.ldz, u, count);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) v[i] *= u[i];
+    }
+    if (FORM == LG_FORWARD && a.residual) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) v[i] += r[i];
+    }
     if (FORM == LG_FORWARD && a.y_f32) {
         float *p = static_cast<float *>(a.y) + t * a.ldy + col;
 #pragma unroll
-        for (int i = 0; i < LG_CHUNK; ++i)
-            if (i < count) p[i] = v[i];
+        for (int i = 0; i < CH; ++i)
+            if (i < count) p[i * a.ldy] = v[i];
     } else {
-        lg_store16(static_cast<uint16_t *>(a.y) + t * a.ldy + col, v, count);
+        lg_store<CH>(static_cast<uint16_t *>(a.y) + t * a.ldy + col, a.ldy, v, count);
     }
 }
 
-// Tiles in the order they are taken: those of one weight tile side by side, so that its weights come from L2 after the first.
+// Tiles in the order they are taken: the token tiles of one weight tile side by side, so that its weights come from L2 after the first.
 struct LgTile { int m, n, product; };
 __device__ __forceinline__ LgTile lg_tile(const LgArgs &a, int i) {
     const int per = a.tiles_m * a.tiles_n;
     LgTile t;
     t.product = i / per;
     i -= t.product * per;
-    t.n = i / a.tiles_m;
-    t.m = i - t.n * a.tiles_m;
+    t.m = i / a.tiles_n;
+    t.n = i - t.m * a.tiles_n;
     return t;
 }
 
-template <int FORM, int C>
-__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(LG_CTA, 1)
+// CG thread blocks of a cluster per tile of CG * 128 x NT; C of them (CG = 1) share its K.
+template <int FORM, int CG, int NT, int C>
+__global__ void __cluster_dims__(CG * C, 1, 1) __launch_bounds__(LG_CTA, NT <= 64 ? 2 : 1)
 k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArgs a) {
     namespace cg = cooperative_groups;
-    constexpr bool A_MN = FORM == LG_DW, B_MN = FORM != LG_DX;
+    static_assert(CG == 1 || (CG == 2 && C == 1 && NT == 256), "");
+    static_assert(FORM != LG_DW || (C == 1 && NT == 256), "");
+    constexpr bool A_MN = FORM != LG_DX, B_MN = FORM == LG_DW;
+    constexpr int STAGES = lg_stages(CG, NT), STAGE_BYTES = lg_stage_bytes(CG, NT), NB = NT / CG;     // NB: rows of operand B in this block's shared memory
+    constexpr int TMEM_COLS = 2 * NT < 32 ? 32 : 2 * NT;
+    constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M;                                           // output columns of this block's tile
+    static_assert(C == 1 || NT * LG_M * 4 <= STAGES * STAGE_BYTES, "a tile's sums, for the other thread blocks of the cluster, lie in the stages");
     extern __shared__ uint8_t s_raw[];
-    __shared__ __align__(8) uint64_t s_full[LG_STAGES], s_empty[LG_STAGES], s_done[2], s_free[2];
+    __shared__ __align__(8) uint64_t s_full[STAGES], s_empty[STAGES], s_done[2], s_free[2];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_fail;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t stages = (smem_addr(s_raw) + 1023u) & ~1023u;
-    const int rank = C > 1 ? (int)(blockIdx.x % C) : 0;
-    const int first = (int)(blockIdx.x / C), step = (int)(gridDim.x / C), n_tiles = a.tiles_m * a.tiles_n * a.products;
+    const uint32_t stages = (smem_addr(s_raw) + 1023u) & ~1023u, exchange = stages + STAGES * STAGE_BYTES;
+    const int rank = C > 1 ? (int)(blockIdx.x % C) : 0, half = CG > 1 ? (int)(blockIdx.x & 1) : 0;
+    const int first = (int)(blockIdx.x / (CG * C)), step = (int)(gridDim.x / (CG * C)), n_tiles = a.tiles_m * a.tiles_n * a.products;
     const int kb_all = a.k_blocks * a.layers, kb0 = (int)((int64_t)kb_all * rank / C), kb1 = (int)((int64_t)kb_all * (rank + 1) / C);
     if (tid == 0) {
-        for (int s = 0; s < LG_STAGES; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&s_done[s], 1); mbar_init(&s_free[s], 4); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&s_done[s], 1); mbar_init(&s_free[s], 4 * CG); }
         s_fail = 0;
         fence_barrier_init();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        if (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "n"(TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "n"(TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        }
     }
     tc_fence_before();
-    __syncthreads();
+    if (CG > 1) cg::this_cluster().sync();                             // (the other block's barriers are there)
+    else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     pdl_wait();
@@ -250,52 +304,60 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
             bool ok = true;
             for (int i = first; i < n_tiles && ok; i += step) {
                 const LgTile t = lg_tile(a, i);
+                const int m0 = (t.m * CG + half) * OUT, n0 = t.n * NT + half * NB;    // (gated: 64 rows of both layers)
                 for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = it % LG_STAGES, layer = kb >= a.k_blocks, k = kb - layer * a.k_blocks;
-                    if (it >= LG_STAGES && !lg_wait(&s_empty[s], (uint32_t)((it / LG_STAGES - 1) & 1), &s_fail, a.status)) { ok = false; break; }
-                    const uint32_t pa = stages + s * LG_STAGE_BYTES, pb = pa + LG_A_BYTES, bar = smem_addr(&s_full[s]);
-                    mbar_arrive_expect_tx(&s_full[s], LG_STAGE_BYTES);
+                    const int s = it % STAGES, layer = kb >= a.k_blocks, k = kb - layer * a.k_blocks;
+                    if (it >= STAGES && !lg_wait(&s_empty[s], (uint32_t)((it / STAGES - 1) & 1), &s_fail, a.status)) { ok = false; break; }
+                    const uint32_t pa = stages + s * STAGE_BYTES, pb = pa + LG_A_BYTES;
+                    // (both blocks' copies are counted by the first one's barrier)
+                    const uint32_t bar = CG > 1 ? cluster_addr(smem_addr(&s_full[s]), 0) : smem_addr(&s_full[s]);
+                    if (half == 0) mbar_arrive_expect_tx(&s_full[s], CG * STAGE_BYTES);
                     if (FORM == LG_DW) {
 #pragma unroll
-                        for (int q = 0; q < LG_M / 64; ++q) tma_load_2d(pa + q * 8192, &maps.a[0], t.m * LG_M + q * 64, k * LG_K, bar);
+                        for (int q = 0; q < LG_M / 64; ++q) tma_load_2d<CG>(pa + q * 8192, &maps.a[0], m0 + q * 64, k * LG_K, bar);
 #pragma unroll
-                        for (int q = 0; q < LG_N / 64; ++q) tma_load_2d(pb + q * 8192, &maps.b[t.product], t.n * LG_N + q * 64, k * LG_K, bar);
+                        for (int q = 0; q < NB / 64; ++q) tma_load_2d<CG>(pb + q * 8192, &maps.b[t.product], n0 + q * 64, k * LG_K, bar);
                     } else {
-                        tma_load_2d(pa, &maps.a[layer], k * LG_K, t.m * LG_M, bar);
-                        if (FORM == LG_DX) tma_load_3d(pb, &maps.b[layer], 0, t.n * LG_N, k, bar);
-                        else if (FORM == LG_FORWARD) tma_load_3d(pb, &maps.b[0], 0, k * LG_K, t.n * (LG_N / DC_ROWS), bar);
+                        if (FORM == LG_DX) tma_load_3d<CG>(pa, &maps.a[layer], 0, m0, k, bar);
+                        else if (FORM == LG_FORWARD) tma_load_3d<CG>(pa, &maps.a[0], 0, k * LG_K, m0 / DC_ROWS, bar);
                         else {
-                            tma_load_3d(pb, &maps.b[0], 0, k * LG_K, t.n * (LG_N / DC_ROWS / 2), bar);
-                            tma_load_3d(pb + LG_B_BYTES / 2, &maps.b[1], 0, k * LG_K, t.n * (LG_N / DC_ROWS / 2), bar);
+                            tma_load_3d<CG>(pa, &maps.a[0], 0, k * LG_K, m0 / DC_ROWS, bar);
+                            tma_load_3d<CG>(pa + LG_A_BYTES / 2, &maps.a[1], 0, k * LG_K, m0 / DC_ROWS, bar);
                         }
+                        tma_load_2d<CG>(pb, &maps.b[layer], k * LG_K, n0, bar);
                     }
                 }
             }
-            if (!ok)                                                   // gave up: the copies in flight land before the block ends
-                for (int q = it < LG_STAGES ? 0 : it - LG_STAGES; q < it; ++q) (void)mbar_wait_bounded(&s_full[q % LG_STAGES], (uint32_t)((q / LG_STAGES) & 1), 1 << 16);
+            if (!ok) {                                                 // gave up: the copies in flight land before the block ends
+                if (CG == 1)
+                    for (int q = it < STAGES ? 0 : it - STAGES; q < it; ++q) (void)mbar_wait_bounded(&s_full[q % STAGES], (uint32_t)((q / STAGES) & 1), 1 << 16);
+                else                                                   // (the barrier that counts them may be the other block's: far longer than a copy takes)
+                    for (int q = 0; q < 2000; ++q) __nanosleep(1000);
+            }
         }
     } else if (warp == 1) {
-        if (lane == 0) {                                               // ---- products
+        if (lane == 0 && half == 0) {                                  // ---- products
+            constexpr uint32_t idesc = lg_idesc(CG * LG_M, NT, A_MN, B_MN);
             int it = 0, n = 0;
             bool ok = true;
             for (int i = first; i < n_tiles && ok; i += step, ++n) {
-                const uint32_t d = tmem + (uint32_t)(n & 1) * LG_N;
+                const uint32_t d = tmem + (uint32_t)(n & 1) * NT;
                 if (n >= 2 && !lg_wait(&s_free[n & 1], (uint32_t)((n / 2 - 1) & 1), &s_fail, a.status)) { ok = false; break; }
                 tc_fence_after();
                 for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = it % LG_STAGES;
-                    if (!lg_wait(&s_full[s], (uint32_t)((it / LG_STAGES) & 1), &s_fail, a.status)) { ok = false; break; }
+                    const int s = it % STAGES;
+                    if (!lg_wait(&s_full[s], (uint32_t)((it / STAGES) & 1), &s_fail, a.status)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t pa = stages + s * LG_STAGE_BYTES, pb = pa + LG_A_BYTES;
+                    const uint32_t pa = stages + s * STAGE_BYTES, pb = pa + LG_A_BYTES;
 #pragma unroll
                     for (int k = 0; k < LG_K / 16; ++k)
-                        tc_mma(d, lg_desc(pa + k * (A_MN ? 2048 : 32), A_MN), lg_desc(pb + k * (B_MN ? 2048 : 32), B_MN), lg_idesc(A_MN, B_MN), kb > kb0 || k > 0);
-                    tc_commit(&s_empty[s]);
+                        tc_mma<CG>(d, lg_desc(pa + k * (A_MN ? 2048 : 32), A_MN), lg_desc(pb + k * (B_MN ? 2048 : 32), B_MN), idesc, kb > kb0 || k > 0);
+                    tc_commit<CG>(&s_empty[s]);
                 }
-                if (ok) tc_commit(&s_done[n & 1]);
+                if (ok) tc_commit<CG>(&s_done[n & 1]);
             }
             if (!ok && it > 0)                                         // gave up: the products in flight end before the accumulators are given back
-                (void)mbar_wait_bounded(&s_empty[(it - 1) % LG_STAGES], (uint32_t)(((it - 1) / LG_STAGES) & 1), 1 << 16);
+                (void)mbar_wait_bounded(&s_empty[(it - 1) % STAGES], (uint32_t)(((it - 1) / STAGES) & 1), 1 << 16);
         }
     } else {                                                           // ---- accumulators: warp w reads the lanes 32 (w % 4) ...
         const int quad = warp & 3;
@@ -303,106 +365,122 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
         int n = 0;
         for (int i = first; i < n_tiles; i += step, ++n) {
             const LgTile t = lg_tile(a, i);
-            if (!lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status)) break;
-            __syncwarp();
-            tc_fence_after();
-            const uint32_t d = mine + (uint32_t)(n & 1) * LG_N;
+            const uint32_t d = mine + (uint32_t)(n & 1) * NT;
             if constexpr (FORM == LG_DW) {
-                const int word = t.m * (LG_M / 32) + quad;
-                const uint2 *index = a.index[t.product] + word;
+                // (the index of the tile's 256 rows, eight of them a lane, is fetched while the products run)
+                const int word = (t.m * CG + half) * (LG_M / 32) + quad;
+                const int64_t row0 = (int64_t)t.n * NT;
+                const uint2 *index = a.index[t.product] + (int64_t)word * a.width;
                 uint16_t *dw = a.dw[t.product];
-                const int64_t row0 = (int64_t)t.n * LG_N;
                 const uint32_t below = (1u << lane) - 1u;
-                for (int c = 0; c < LG_N; c += LG_CHUNK) {
-                    uint2 e[LG_CHUNK];
+                uint2 e[NT / 32];
 #pragma unroll
-                    for (int k = 0; k < LG_CHUNK; ++k) {
-                        e[k] = make_uint2(0u, 0u);
-                        if (word < a.index_words && row0 + c + k < a.width) e[k] = __ldg(index + (row0 + c + k) * a.index_words);
-                    }
-                    float v[LG_CHUNK];
-                    tc_load16(d + c, v);
+                for (int q = 0; q < NT / 32; ++q) {
+                    e[q] = make_uint2(0u, 0u);
+                    if (word < a.index_words && row0 + q * 32 + lane < a.width) e[q] = __ldg(index + row0 + q * 32 + lane);
+                }
+                if (!__all_sync(0xFFFFFFFFu, lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status))) break;
+                tc_fence_after();
+#pragma unroll
+                for (int q = 0; q < NT / 16; ++q) {
+                    float v[16];
+                    tc_load16(d + q * 16, v);
                     tc_load_wait(v);
 #pragma unroll
-                    for (int k = 0; k < LG_CHUNK; ++k)
-                        if ((e[k].x >> lane) & 1u) dw[(size_t)e[k].y + __popc(e[k].x & below)] = (uint16_t)lin_bf16(v[k]);
+                    for (int k = 0; k < 16; ++k) {
+                        const uint32_t bits = __shfl_sync(0xFFFFFFFFu, e[q / 2].x, (q & 1) * 16 + k), at = __shfl_sync(0xFFFFFFFFu, e[q / 2].y, (q & 1) * 16 + k);
+                        if ((bits >> lane) & 1u) dw[(size_t)at + __popc(bits & below)] = (uint16_t)lin_bf16(v[k]);
+                    }
                     __syncwarp();
                 }
-            } else if constexpr (C == 1) {
-                const int64_t token = (int64_t)t.m * LG_M + quad * 32 + lane;
-                constexpr int OUT = FORM == LG_GATED ? LG_N / 2 : LG_N;
-                if ((int64_t)t.m * LG_M + quad * 32 < a.tokens) {
-                    for (int c = 0; c < OUT; c += LG_CHUNK) {
-                        float v[LG_CHUNK], u[LG_CHUNK];
-                        tc_load16(d + c, v);
-                        if (FORM == LG_GATED) { tc_load16(d + OUT + c, u); tc_load_wait(u); }
-                        tc_load_wait(v);
-                        lg_finish<FORM>(a, token, (int64_t)t.n * OUT + c, v, u);
-                        __syncwarp();
-                    }
-                }
             } else {
-                // this block's sums into its own shared memory, [column][token]: every copy has landed and every product has been made
-                const uint32_t at = stages + (uint32_t)(quad * 32 + lane) * 4;
-                if ((int64_t)t.m * LG_M + quad * 32 < a.tokens) {
-                    for (int c = 0; c < LG_N; c += LG_CHUNK) {
-                        float v[LG_CHUNK];
+                bool ok = __all_sync(0xFFFFFFFFu, lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status));
+                if (FORM == LG_GATED && C == 1) ok = pair_all(1 + (quad & 1), ok);      // (both warps of an exchange go on, or none)
+                if (!ok) break;
+                tc_fence_after();
+                const int64_t col = (int64_t)(t.m * CG + half) * OUT + (FORM == LG_GATED ? quad & 1 : quad) * 32 + lane, t0 = (int64_t)t.n * NT;
+                if constexpr (C > 1) {
+                    // this block's sums into its own shared memory, [token][lane]: every copy has landed and every product has been made
+                    const uint32_t at = stages + (uint32_t)(quad * 32 + lane) * 4;
+                    for (int c = 0; c < NT && t0 + c < a.tokens; c += 16) {
+                        float v[16];
                         tc_load16(d + c, v);
                         tc_load_wait(v);
 #pragma unroll
-                        for (int k = 0; k < LG_CHUNK; ++k)
-                            asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + (uint32_t)(c + k) * (LG_M * 4)), "f"(v[k]) : "memory");
+                        for (int k = 0; k < 16; ++k) st_shared(at + (uint32_t)(c + k) * (LG_M * 4), v[k]);
+                    }
+                } else if constexpr (FORM == LG_GATED) {
+                    // two chunks of tokens: the gate's warps finish the first one, the other layer's the second
+                    const bool is_up = quad >= 2;
+                    const uint32_t give = exchange + (uint32_t)quad * (16 * 32 * 4) + lane * 4, get = exchange + (uint32_t)(quad ^ 2) * (16 * 32 * 4) + lane * 4;
+                    for (int c = 0; c < NT && t0 + c < a.tokens; c += 32) {
+                        float keep[16], other[16];
+                        tc_load16(d + c + (is_up && NT > 16 ? 16 : 0), keep);
+                        tc_load16(d + c + (is_up || NT == 16 ? 0 : 16), other);
+                        tc_load_wait(keep);
+                        tc_load_wait(other);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) st_shared(give + k * 128, other[k]);
+                        asm volatile("bar.sync %0, 64;" ::"r"(1 + (quad & 1)) : "memory");
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) other[k] = ld_shared(get + k * 128);
+                        if (is_up) { if (NT > 16) lg_finish<FORM, 16>(a, t0 + c + 16, col, other, keep); }
+                        else lg_finish<FORM, 16>(a, t0 + c, col, keep, other);
+                        asm volatile("bar.sync %0, 64;" ::"r"(1 + (quad & 1)) : "memory");
+                    }
+                } else {
+                    for (int c = 0; c < NT && t0 + c < a.tokens; c += 16) {
+                        float v[16];
+                        tc_load16(d + c, v);
+                        tc_load_wait(v);
+                        lg_finish<FORM, 16>(a, t0 + c, col, v, v);
+                        __syncwarp();
                     }
                 }
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&s_free[n & 1]);
+            if (lane == 0) mbar_arrive_cluster(cluster_addr(smem_addr(&s_free[n & 1]), CG > 1 ? 0 : rank));
         }
     }
     __syncwarp();
-    if constexpr (C > 1 && FORM != LG_DW) {
-        // (one tile per cluster)  Rank r adds up the C sums of its share of the columns and finishes them.
+    if constexpr (C > 1) {
+        // (one tile per cluster)  Rank r adds up the C sums of its share of the tokens and finishes them.
+        constexpr int CH = NT / C < 8 ? NT / C : 8;
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
         if (warp >= 2 && !s_fail && first < n_tiles) {
             const LgTile t = lg_tile(a, first);
-            const int quad = warp & 3;
-            constexpr int OUT = FORM == LG_GATED ? LG_N / 2 : LG_N;
-            const uint32_t at = stages + (uint32_t)(quad * 32 + lane) * 4;
-            const int64_t token = (int64_t)t.m * LG_M + quad * 32 + lane;
-            if ((int64_t)t.m * LG_M + quad * 32 < a.tokens) {
-                for (int c = rank * LG_CHUNK; c < OUT; c += C * LG_CHUNK) {
-                    float v[LG_CHUNK], u[LG_CHUNK];
+            constexpr int PER = OUT / 32;                              // warps that an output column takes part in: with 64 of them, two share the tokens
+            const int quad = warp & 3, lanes = quad % PER * 32 + lane;
+            const int64_t col = (int64_t)t.m * OUT + lanes, t0 = (int64_t)t.n * NT;
+            const uint32_t at = stages + (uint32_t)lanes * 4;
+            for (int c = (rank * (4 / PER) + quad / PER) * CH; c < NT && t0 + c < a.tokens; c += C * (4 / PER) * CH) {
+                float v[CH], u[CH];
 #pragma unroll
-                    for (int k = 0; k < LG_CHUNK; ++k) v[k] = u[k] = 0.f;
+                for (int k = 0; k < CH; ++k) v[k] = u[k] = 0.f;
 #pragma unroll
-                    for (int r = 0; r < C; ++r) {
-                        uint32_t far;
-                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(at), "r"(r));
+                for (int r = 0; r < C; ++r) {
+                    const uint32_t far = cluster_addr(at, r);
 #pragma unroll
-                        for (int k = 0; k < LG_CHUNK; ++k) {
-                            float f;
-                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(far + (uint32_t)(c + k) * (LG_M * 4)) : "memory");
-                            v[k] += f;
-                            if (FORM == LG_GATED) {
-                                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(far + (uint32_t)(OUT + c + k) * (LG_M * 4)) : "memory");
-                                u[k] += f;
-                            }
-                        }
+                    for (int k = 0; k < CH; ++k) {
+                        v[k] += ld_cluster(far + (uint32_t)(c + k) * (LG_M * 4));
+                        if (FORM == LG_GATED) u[k] += ld_cluster(far + (uint32_t)(c + k) * (LG_M * 4) + OUT * 4);
                     }
-                    lg_finish<FORM>(a, token, (int64_t)t.n * OUT + c, v, u);
                 }
+                lg_finish<FORM, CH>(a, t0 + c, col, v, u);
             }
         }
         __syncwarp();
-        cluster.sync();
     }
-    __syncwarp();
     tc_fence_before();
-    __syncthreads();
+    if (CG * C > 1) cg::this_cluster().sync();                         // (nobody reads this block's shared memory or works on its accumulators any more)
+    else __syncthreads();
     tc_fence_after();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    if (warp == 1) {
+        if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(TMEM_COLS));
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(TMEM_COLS));
+    }
 }
 
 }  // namespace dbs

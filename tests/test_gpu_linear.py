@@ -9,7 +9,10 @@ from linear_util import ACT, DEV, HALF, SUM, Layer, Rows, gated_want, grads_want
 pytestmark = pytest.mark.gpu
 
 SHAPES = [(1, 1), (64, 64), (65, 17), (200, 333), (1030, 130), (129, 2050), (520, 1032)]
-TOKENS = [1, 2, 3, 9, 128, 301]
+TOKENS = [1, 2, 3, 17, 65, 250, 301]
+# enough tiles that two thread blocks work on each
+PAIRS = [((2050, 1930), 1900)]
+CASES = [(s, t) for s in SHAPES for t in TOKENS] + PAIRS
 
 
 def run_linear(layer, t, name, pad, lead, bias, residual, keep, f32, zeros, seed):
@@ -31,8 +34,7 @@ def run_linear(layer, t, name, pad, lead, bias, residual, keep, f32, zeros, seed
         assert z.untouched()
 
 
-@pytest.mark.parametrize("shape", SHAPES)
-@pytest.mark.parametrize("t", TOKENS)
+@pytest.mark.parametrize("shape,t", CASES, ids=str)
 def test_linear(shape, t):
     layer = Layer(*shape, seed=t)
     for k, (name, pad, lead, bias, residual, keep, f32, zeros) in enumerate([
@@ -42,8 +44,7 @@ def test_linear(shape, t):
     layer.close()
 
 
-@pytest.mark.parametrize("shape", SHAPES)
-@pytest.mark.parametrize("t", TOKENS)
+@pytest.mark.parametrize("shape,t", CASES, ids=str)
 def test_gated(shape, t):
     m, n = shape
     gate, up = Layer(m, n, 0.5, seed=1), Layer(m, n, 0.3, seed=2)
@@ -62,8 +63,7 @@ def test_gated(shape, t):
     gate.close(), up.close()
 
 
-@pytest.mark.parametrize("shape", SHAPES)
-@pytest.mark.parametrize("t", TOKENS)
+@pytest.mark.parametrize("shape,t", CASES, ids=str)
 def test_linear_backward(shape, t):
     layer = Layer(*shape, seed=3)
     m, n = shape
@@ -86,8 +86,7 @@ def test_linear_backward(shape, t):
     layer.close()
 
 
-@pytest.mark.parametrize("shape", SHAPES)
-@pytest.mark.parametrize("t", TOKENS)
+@pytest.mark.parametrize("shape,t", CASES, ids=str)
 def test_gated_backward(shape, t):
     m, n = shape
     gate, up = Layer(m, n, 0.5, seed=4), Layer(m, n, 0.3, seed=5)
