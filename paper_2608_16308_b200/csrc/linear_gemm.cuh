@@ -12,14 +12,16 @@
 // bytes per column and strip).  64 rows of bf16 are the 128 bytes of one swizzle row, so a strip is an operand tile with the rows
 // along M for the forward product and along K for the gradient of x; nothing is transposed or laid out again.
 //
-//   * M (the lanes of an accumulator) is the dimension that lies side by side in the output: a warp's 32 lanes write neighbours,
-//     whatever the strides are, and tokens are N, so that few tokens are a narrow tile.  Tiles are 128 x NT.
-//   * One thread issues the loads (TMA; edges are zero-filled by the tensor maps), one the products, four warps empty the accumulators.
+//   * M (the lanes of an accumulator) is the dimension that lies side by side in the output, and tokens are N, so that few tokens
+//     are a narrow tile.  Tiles are 128 x NT.
+//   * One thread issues the loads (TMA; edges are zero-filled by the tensor maps), one the products, eight warps empty the accumulators.
 //     Two accumulators take turns, so the epilogue of one tile runs under the products of the next.
+//   * Epilogue: the sums of a few tokens at a time go through shared memory, [token][lane], and are finished from there, eight neighbours of a
+//     token per thread: 16 bytes a load or store, 256 bytes side by side, the residual fetched in front of the exchange.
+//     (A lane's own values, 2 bytes at a time, by four warps: the epilogue was the longer half: PLACEHOLDER)
 //   * CG = 2: the two thread blocks of a cluster work on one 256 x 256 tile, each with half of either operand in its shared memory:
 //     32 KB per block of K and SM where one block alone would need 48.
-//   * Gated: M are 64 rows of the gate and the same 64 of the other layer; the warps of the two halves exchange what the other
-//     needs through shared memory, each finishes half of the tokens.
+//   * Gated: M are 64 rows of the gate and the same 64 of the other layer; both sums of an output meet in that exchange.
 //   * Gradient of W: the lanes of a warp hold 32 neighbouring columns of one row, and the stored ones among them are neighbours in the
 //     values' array: one popc gives each its place.
 //   * C > 1, few tiles: the C thread blocks of a cluster share K and add their sums up through distributed shared memory, in rank order.
@@ -37,15 +39,18 @@ namespace dbs {
 
 constexpr int LG_M = 128, LG_K = 64;
 constexpr int LG_A_BYTES = LG_M * LG_K * 2;
-constexpr int LG_WARPS = 6;                                    // loads, products, four for the accumulators
-constexpr int LG_CTA = LG_WARPS * 32;
-constexpr int LG_EXCHANGE = 4 * 16 * 32 * 4;                   // gated: 16 tokens of 32 lanes for each of the four warps
+constexpr int LG_FINISH = 8;                                   // warps that empty the accumulators, two for each quarter of the lanes
+constexpr int LG_CTA = (2 + LG_FINISH) * 32;                   // (and one warp each for the loads and the products)
 
 // Stages of a form: a block of K of both operands.  Narrow tiles (few tokens, bound by HBM) leave room for two thread blocks per SM.
 __host__ __device__ constexpr int lg_stage_bytes(int cg, int nt) { return LG_A_BYTES + nt / cg * LG_K * 2; }
 __host__ __device__ constexpr int lg_stages(int cg, int nt) { return nt <= 16 ? 5 : nt <= 64 ? 4 : nt <= 128 || cg == 2 ? 6 : 4; }
+// Tokens whose sums are exchanged at a time, and how many such buffers there are
+__host__ __device__ constexpr int lg_tokens(int nt) { return nt <= 64 ? 16 : 32; }
+__host__ __device__ constexpr int lg_buffers(int nt) { return nt == 64 ? 1 : 2; }
+__host__ __device__ constexpr int lg_exchange(int nt) { return lg_tokens(nt) * lg_buffers(nt) * LG_M * 4; }
 // (the swizzle's pattern repeats every 1024 bytes: the stages begin on a multiple)
-__host__ __device__ constexpr int lg_smem(int cg, int nt) { return lg_stages(cg, nt) * lg_stage_bytes(cg, nt) + LG_EXCHANGE + 1024; }
+__host__ __device__ constexpr int lg_smem(int cg, int nt) { return lg_stages(cg, nt) * lg_stage_bytes(cg, nt) + lg_exchange(nt) + 1024; }
 
 enum LgForm { LG_FORWARD = 0, LG_GATED = 1, LG_DX = 2, LG_DW = 3 };
 
@@ -64,6 +69,7 @@ struct LgArgs {
     int64_t ldr;
     uint16_t *z, *u;                // in front of the activation; the other projection (may be null)
     int64_t ldz;
+    int vec;                        // neighbours that a thread finishes: 8 (every row of y, z, u, residual begins on 16 bytes), 2 (on 4) or 1
     uint16_t *dw[2];
     const uint2 *index[2];          // [word of 32 columns][row]: stored columns, place of the first of them
     int index_words;
@@ -146,24 +152,35 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
     return far;
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t far) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(far) : "memory"); }
-__device__ __forceinline__ float ld_cluster(uint32_t far) {
-    float f;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(far) : "memory");
-    return f;
+template <int V>
+__device__ __forceinline__ void ld_cluster(uint32_t far, float (&v)[V]) {
+    if constexpr (V >= 4) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4)
+            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i]), "=f"(v[i + 1]), "=f"(v[i + 2]), "=f"(v[i + 3]) : "r"(far + i * 4) : "memory");
+    } else if constexpr (V == 2) asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(far) : "memory");
+    else asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[0]) : "r"(far) : "memory");
+}
+template <int V>
+__device__ __forceinline__ void ld_shared(uint32_t addr, float (&v)[V]) {
+    if constexpr (V >= 4) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4)
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i]), "=f"(v[i + 1]), "=f"(v[i + 2]), "=f"(v[i + 3]) : "r"(addr + i * 4) : "memory");
+    } else if constexpr (V == 2) asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(addr) : "memory");
+    else asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[0]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void st_shared(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
-__device__ __forceinline__ float ld_shared(uint32_t addr) {
-    float f;
-    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(addr) : "memory");
-    return f;
-}
-
-// whether `ok` holds in both warps of a pair
-__device__ __forceinline__ bool pair_all(int barrier, bool ok) {
+// the warps that empty the accumulators meet; with a vote: whether `ok` holds in all of them
+__device__ __forceinline__ void finish_sync() { asm volatile("bar.sync 1, %0;" ::"n"(LG_FINISH * 32) : "memory"); }
+__device__ __forceinline__ bool finish_all(bool ok) {
     uint32_t all;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(all) : "r"((uint32_t)ok), "r"(barrier) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"((uint32_t)ok), "n"(LG_FINISH * 32) : "memory");
     return all != 0;
+}
+__device__ __forceinline__ void store_if(bool p, uint16_t *at, uint32_t v) {       // (predicated: no branch per element)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %0, 0;\n\t@p st.global.b16 [%1], %2;\n\t}" ::"r"((uint32_t)p), "l"(at), "h"((uint16_t)v) : "memory");
 }
 
 // Descriptor of an operand tile in shared memory under the 128-byte swizzle.  K along the swizzle rows: 64 of K per row, eight rows of M/N 1024
@@ -187,61 +204,117 @@ __device__ __forceinline__ bool lg_wait(uint64_t *bar, uint32_t parity, volatile
     return false;
 }
 
-// ---- what becomes of CH neighbouring tokens' sums of one output column (the lane's) --------
-template <int CH>
-__device__ __forceinline__ void lg_act(float (&v)[CH], int act) {
+// ---- what becomes of V neighbouring sums of one token ------------------------------------
+template <int V>
+__device__ __forceinline__ void lg_act(float (&v)[V], int act) {
     if (act == DBSPMSPV_ACT_NONE) return;
     if (act == DBSPMSPV_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_RELU);
+        for (int i = 0; i < V; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_RELU);
     } else if (act == DBSPMSPV_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_SILU);
+        for (int i = 0; i < V; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_SILU);
     } else {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_GELU);
+        for (int i = 0; i < V; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_GELU);
     }
 }
-template <int CH>
-__device__ __forceinline__ void lg_store(uint16_t *p, int64_t ld, const float (&v)[CH], int count) {
+template <int V>
+__device__ __forceinline__ void lg_get(const uint16_t *p, int count, float (&v)[V]) {
+    if (V == 8 && count == V) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(p);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
-        if (i < count) p[i * ld] = (uint16_t)lin_bf16(v[i]);
-}
-// tokens [t, t + CH) of output column `col`; v: the sums, u: the other layer's (gated)
-template <int FORM, int CH>
-__device__ __forceinline__ void lg_finish(const LgArgs &a, int64_t t, int64_t col, float (&v)[CH], const float (&u)[CH]) {
-    if (t >= a.tokens || col >= a.width) return;
-    const int count = a.tokens - t < CH ? (int)(a.tokens - t) : CH;
-    float r[CH];
-    if (FORM == LG_FORWARD && a.residual) {
+        for (int i = 0; i < V / 2; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+    } else if (V == 2 && count == V) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(p);
+        v[0] = __uint_as_float(w << 16);
+        v[V - 1] = __uint_as_float(w & 0xFFFF0000u);
+    } else {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) r[i] = i < count ? lin_f32(a.residual[(t + i) * a.ldr + col]) : 0.f;
+        for (int i = 0; i < V; ++i) v[i] = i < count ? lin_f32(p[i]) : 0.f;
     }
+}
+template <int V>
+__device__ __forceinline__ void lg_put(uint16_t *p, int count, const float (&v)[V]) {
+    if (V == 8 && count == V) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = lin_bf16(v[2 * i % V]) | lin_bf16(v[(2 * i + 1) % V]) << 16;
+        *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else if (V == 2 && count == V) {
+        *reinterpret_cast<uint32_t *>(p) = lin_bf16(v[0]) | lin_bf16(v[V - 1]) << 16;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < count) p[i] = (uint16_t)lin_bf16(v[i]);
+    }
+}
+// output columns [col, col + V) of token t; v: the sums, u: the other layer's (gated), r: the residual
+template <int FORM, int V>
+__device__ __forceinline__ void lg_finish(const LgArgs &a, int64_t t, int64_t col, float (&v)[V], const float (&u)[V], const float (&r)[V]) {
+    const int count = a.width - col < V ? (int)(a.width - col) : V;
     if (FORM == LG_FORWARD && a.bias) {
-        const float b = lin_f32(a.bias[col]);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) v[i] += b;
+        for (int i = 0; i < V; ++i) v[i] += i < count ? lin_f32(__ldg(a.bias + col + i)) : 0.f;
     }
-    if (FORM != LG_DX && a.z) lg_store<CH>(a.z + t * a.ldz + col, a.ldz, v, count);
-    if (FORM != LG_DX) lg_act<CH>(v, a.act);
+    if (FORM != LG_DX && a.z) lg_put<V>(a.z + t * a.ldz + col, count, v);
+    if (FORM != LG_DX) lg_act<V>(v, a.act);
     if (FORM == LG_GATED) {
-        if (a.u) lg_store<CH>(a.u + t * a.ldz + col, a.ldz, u, count);
+        if (a.u) lg_put<V>(a.u + t * a.ldz + col, count, u);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) v[i] *= u[i];
+        for (int i = 0; i < V; ++i) v[i] *= u[i];
     }
     if (FORM == LG_FORWARD && a.residual) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i) v[i] += r[i];
+        for (int i = 0; i < V; ++i) v[i] += r[i];
     }
     if (FORM == LG_FORWARD && a.y_f32) {
         float *p = static_cast<float *>(a.y) + t * a.ldy + col;
+        if (V == 8 && count == V) {
+            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1 % V], v[2 % V], v[3 % V]);
+            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4 % V], v[5 % V], v[6 % V], v[7 % V]);
+        } else {
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
-            if (i < count) p[i * a.ldy] = v[i];
+            for (int i = 0; i < V; ++i)
+                if (i < count) p[i] = v[i];
+        }
     } else {
-        lg_store<CH>(static_cast<uint16_t *>(a.y) + t * a.ldy + col, a.ldy, v, count);
+        lg_put<V>(static_cast<uint16_t *>(a.y) + t * a.ldy + col, count, v);
     }
+}
+// The tokens t0 + q * every, q < CT, of the tile's output columns from col0 on, by thread e of LG_FINISH * 32.  exchange() brings their sums to where read(q, lane, v)
+// finds them; the residual is fetched in front of it.
+template <int FORM, int V, int CT, class Exchange, class Read>
+__device__ __forceinline__ void lg_tokens_of(const LgArgs &a, int64_t t0, int every, int64_t col0, int e, Exchange exchange, Read read) {
+    constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M, G = OUT / V, THREADS = LG_FINISH * 32, ITEMS = (CT * G + THREADS - 1) / THREADS;
+    float r[ITEMS][V];
+    if (FORM == LG_FORWARD && a.residual) {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const int i = k * THREADS + e, q = i / G;
+            const int64_t t = t0 + (int64_t)q * every, col = col0 + i % G * V;
+            if (q < CT && t < a.tokens && col < a.width) lg_get<V>(a.residual + t * a.ldr + col, a.width - col < V ? (int)(a.width - col) : V, r[k]);
+        }
+    }
+    exchange();
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+        const int i = k * THREADS + e, q = i / G;
+        const int64_t t = t0 + (int64_t)q * every, col = col0 + i % G * V;
+        if (q < CT && t < a.tokens && col < a.width) {
+            float v[V], u[V];
+            read(q, i % G * V, v);
+            if (FORM == LG_GATED) read(q, OUT + i % G * V, u);
+            lg_finish<FORM, V>(a, t, col, v, u, r[k]);
+        }
+    }
+}
+template <int FORM, int CT, class Exchange, class Read>
+__device__ __forceinline__ void lg_tokens_at(const LgArgs &a, int64_t t0, int every, int64_t col0, int e, Exchange exchange, Read read) {
+    if (a.vec == 8) lg_tokens_of<FORM, 8, CT>(a, t0, every, col0, e, exchange, read);
+    else if (a.vec == 2) lg_tokens_of<FORM, 2, CT>(a, t0, every, col0, e, exchange, read);
+    else lg_tokens_of<FORM, 1, CT>(a, t0, every, col0, e, exchange, read);
 }
 
 // Tiles in the order they are taken: the token tiles of one weight tile side by side, so that its weights come from L2 after the first.
@@ -279,7 +352,7 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
     const int kb_all = a.k_blocks * a.layers, kb0 = (int)((int64_t)kb_all * rank / C), kb1 = (int)((int64_t)kb_all * (rank + 1) / C);
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&s_done[s], 1); mbar_init(&s_free[s], 4 * CG); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&s_done[s], 1); mbar_init(&s_free[s], LG_FINISH * CG); }
         s_fail = 0;
         fence_barrier_init();
     }
@@ -360,81 +433,69 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                 (void)mbar_wait_bounded(&s_empty[(it - 1) % STAGES], (uint32_t)(((it - 1) / STAGES) & 1), 1 << 16);
         }
     } else {                                                           // ---- accumulators: warp w reads the lanes 32 (w % 4) ...
-        const int quad = warp & 3;
+        const int quad = warp & 3, group = (warp - 2) >> 2, e = tid - 64;
         const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
-        int n = 0;
+        int n = 0, turn = 0;
         for (int i = first; i < n_tiles; i += step, ++n) {
             const LgTile t = lg_tile(a, i);
             const uint32_t d = mine + (uint32_t)(n & 1) * NT;
             if constexpr (FORM == LG_DW) {
-                // (the index of the tile's 256 rows, eight of them a lane, is fetched while the products run)
+                // (the index of the tile's 256 rows, half of them a group's, four a lane's, is fetched while the products run)
+                constexpr int ROWS = NT / 2;
                 const int word = (t.m * CG + half) * (LG_M / 32) + quad;
-                const int64_t row0 = (int64_t)t.n * NT;
+                const int64_t row0 = (int64_t)t.n * NT + group * ROWS;
                 const uint2 *index = a.index[t.product] + (int64_t)word * a.width;
                 uint16_t *dw = a.dw[t.product];
                 const uint32_t below = (1u << lane) - 1u;
-                uint2 e[NT / 32];
+                uint2 x[ROWS / 32];
 #pragma unroll
-                for (int q = 0; q < NT / 32; ++q) {
-                    e[q] = make_uint2(0u, 0u);
-                    if (word < a.index_words && row0 + q * 32 + lane < a.width) e[q] = __ldg(index + row0 + q * 32 + lane);
+                for (int q = 0; q < ROWS / 32; ++q) {
+                    x[q] = make_uint2(0u, 0u);
+                    if (word < a.index_words && row0 + q * 32 + lane < a.width) x[q] = __ldg(index + row0 + q * 32 + lane);
                 }
                 if (!__all_sync(0xFFFFFFFFu, lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status))) break;
                 tc_fence_after();
 #pragma unroll
-                for (int q = 0; q < NT / 16; ++q) {
+                for (int q = 0; q < ROWS / 16; ++q) {
                     float v[16];
-                    tc_load16(d + q * 16, v);
+                    tc_load16(d + group * ROWS + q * 16, v);
                     tc_load_wait(v);
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
-                        const uint32_t bits = __shfl_sync(0xFFFFFFFFu, e[q / 2].x, (q & 1) * 16 + k), at = __shfl_sync(0xFFFFFFFFu, e[q / 2].y, (q & 1) * 16 + k);
-                        if ((bits >> lane) & 1u) dw[(size_t)at + __popc(bits & below)] = (uint16_t)lin_bf16(v[k]);
+                        const uint32_t bits = __shfl_sync(0xFFFFFFFFu, x[q / 2].x, (q & 1) * 16 + k), at = __shfl_sync(0xFFFFFFFFu, x[q / 2].y, (q & 1) * 16 + k);
+                        store_if((bits >> lane) & 1u, dw + at + __popc(bits & below), lin_bf16(v[k]));
                     }
-                    __syncwarp();
                 }
             } else {
                 bool ok = __all_sync(0xFFFFFFFFu, lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status));
-                if (FORM == LG_GATED && C == 1) ok = pair_all(1 + (quad & 1), ok);      // (both warps of an exchange go on, or none)
+                if (C == 1) ok = finish_all(ok);                       // (all of them go on to the exchange, or none)
                 if (!ok) break;
                 tc_fence_after();
-                const int64_t col = (int64_t)(t.m * CG + half) * OUT + (FORM == LG_GATED ? quad & 1 : quad) * 32 + lane, t0 = (int64_t)t.n * NT;
+                const int64_t t0 = (int64_t)t.n * NT;
                 if constexpr (C > 1) {
                     // this block's sums into its own shared memory, [token][lane]: every copy has landed and every product has been made
-                    const uint32_t at = stages + (uint32_t)(quad * 32 + lane) * 4;
-                    for (int c = 0; c < NT && t0 + c < a.tokens; c += 16) {
+                    for (int c = group * 16; c < NT && t0 + c < a.tokens; c += 32) {
                         float v[16];
                         tc_load16(d + c, v);
                         tc_load_wait(v);
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) st_shared(at + (uint32_t)(c + k) * (LG_M * 4), v[k]);
-                    }
-                } else if constexpr (FORM == LG_GATED) {
-                    // two chunks of tokens: the gate's warps finish the first one, the other layer's the second
-                    const bool is_up = quad >= 2;
-                    const uint32_t give = exchange + (uint32_t)quad * (16 * 32 * 4) + lane * 4, get = exchange + (uint32_t)(quad ^ 2) * (16 * 32 * 4) + lane * 4;
-                    for (int c = 0; c < NT && t0 + c < a.tokens; c += 32) {
-                        float keep[16], other[16];
-                        tc_load16(d + c + (is_up && NT > 16 ? 16 : 0), keep);
-                        tc_load16(d + c + (is_up || NT == 16 ? 0 : 16), other);
-                        tc_load_wait(keep);
-                        tc_load_wait(other);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) st_shared(give + k * 128, other[k]);
-                        asm volatile("bar.sync %0, 64;" ::"r"(1 + (quad & 1)) : "memory");
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) other[k] = ld_shared(get + k * 128);
-                        if (is_up) { if (NT > 16) lg_finish<FORM, 16>(a, t0 + c + 16, col, other, keep); }
-                        else lg_finish<FORM, 16>(a, t0 + c, col, keep, other);
-                        asm volatile("bar.sync %0, 64;" ::"r"(1 + (quad & 1)) : "memory");
+                        for (int k = 0; k < 16; ++k) st_shared(stages + (uint32_t)((c + k) * LG_M + quad * 32 + lane) * 4, v[k]);
                     }
                 } else {
-                    for (int c = 0; c < NT && t0 + c < a.tokens; c += 16) {
-                        float v[16];
-                        tc_load16(d + c, v);
-                        tc_load_wait(v);
-                        lg_finish<FORM, 16>(a, t0 + c, col, v, v);
-                        __syncwarp();
+                    constexpr int CT = lg_tokens(NT), BUFFERS = lg_buffers(NT);
+                    for (int c = 0; c < NT && t0 + c < a.tokens; c += CT, ++turn) {
+                        const uint32_t buffer = exchange + (BUFFERS > 1 ? (uint32_t)(turn & 1) * (CT * LG_M * 4) : 0u);
+                        lg_tokens_at<FORM, CT>(a, t0 + c, 1, (int64_t)(t.m * CG + half) * OUT, e, [&] {
+                            if (BUFFERS == 1) finish_sync();           // (everybody has read the tokens before)
+                            if (group * 16 < CT) {
+                                float v[16];
+                                tc_load16(d + c + group * 16, v);
+                                tc_load_wait(v);
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) st_shared(buffer + (uint32_t)((group * 16 + k) * LG_M + quad * 32 + lane) * 4, v[k]);
+                            }
+                            finish_sync();
+                        }, [&](int q, int l, auto &v) { ld_shared(buffer + (uint32_t)(q * LG_M + l) * 4, v); });
                     }
                 }
             }
@@ -445,31 +506,24 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
     }
     __syncwarp();
     if constexpr (C > 1) {
-        // (one tile per cluster)  Rank r adds up the C sums of its share of the tokens and finishes them.
-        constexpr int CH = NT / C < 8 ? NT / C : 8;
-        cg::cluster_group cluster = cg::this_cluster();
-        cluster.sync();
+        // (one tile per cluster)  Rank r adds up the C sums of every C-th token and finishes them.
+        cg::this_cluster().sync();
         if (warp >= 2 && !s_fail && first < n_tiles) {
             const LgTile t = lg_tile(a, first);
-            constexpr int PER = OUT / 32;                              // warps that an output column takes part in: with 64 of them, two share the tokens
-            const int quad = warp & 3, lanes = quad % PER * 32 + lane;
-            const int64_t col = (int64_t)t.m * OUT + lanes, t0 = (int64_t)t.n * NT;
-            const uint32_t at = stages + (uint32_t)lanes * 4;
-            for (int c = (rank * (4 / PER) + quad / PER) * CH; c < NT && t0 + c < a.tokens; c += C * (4 / PER) * CH) {
-                float v[CH], u[CH];
+            constexpr int CT = NT / C < 32 ? NT / C : 32;
+            for (int c = rank; c < NT; c += CT * C)
+                lg_tokens_at<FORM, CT>(a, (int64_t)t.n * NT + c, C, (int64_t)t.m * OUT, tid - 64, [] {}, [&](int q, int l, auto &v) {
+                    constexpr int V = sizeof(v) / sizeof(float);
+                    float part[C][V];
 #pragma unroll
-                for (int k = 0; k < CH; ++k) v[k] = u[k] = 0.f;
+                    for (int r = 0; r < C; ++r) ld_cluster(cluster_addr(stages, r) + (uint32_t)((c + q * C) * LG_M + l) * 4, part[r]);
 #pragma unroll
-                for (int r = 0; r < C; ++r) {
-                    const uint32_t far = cluster_addr(at, r);
+                    for (int j = 0; j < V; ++j) {
+                        v[j] = part[0][j];
 #pragma unroll
-                    for (int k = 0; k < CH; ++k) {
-                        v[k] += ld_cluster(far + (uint32_t)(c + k) * (LG_M * 4));
-                        if (FORM == LG_GATED) u[k] += ld_cluster(far + (uint32_t)(c + k) * (LG_M * 4) + OUT * 4);
+                        for (int r = 1; r < C; ++r) v[j] += part[r][j];
                     }
-                }
-                lg_finish<FORM, CH>(a, t0 + c, col, v, u);
-            }
+                });
         }
         __syncwarp();
     }
