@@ -395,6 +395,7 @@ __device__ __forceinline__ unsigned long long global_timer_ns() {
     return t;
 }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Range-checked build (-DDBS_BOUNDS_CHECK; it stands in for a memory checker on the small parity
 // cases): every index that a kernel READS from the handle's arrays -- the other-dimension block

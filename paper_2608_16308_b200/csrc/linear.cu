@@ -119,7 +119,7 @@ __device__ __forceinline__ void lin_load8(const uint16_t *row, int64_t j, int64_
 __device__ __forceinline__ void lin_store8(uint16_t *row, int64_t j, const float (&v)[8]) {
     uint32_t w[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = lin_bf16(v[2 * k]) | lin_bf16(v[2 * k + 1]) << 16;
+    for (int k = 0; k < 4; ++k) w[k] = lin_pair(v[2 * k], v[2 * k + 1]);
     *reinterpret_cast<uint4 *>(row + j) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
@@ -133,12 +133,12 @@ __global__ void k_linear_pack(const uint16_t *x, int64_t ldx, int64_t tokens, in
         lin_load8(x + t * ldx, j, n, v);
         lin_store8(out + t * ldo, j, v);
     }
+    pdl_trigger();
 }
 
 // What the products of a gradient take: dz = dy act'(z), or dg = dy u act'(g) and du = dy act(g), rounded to bf16 (the tensor cores' operands; the
 // roundings are independent, so a sum over rows or tokens is off by about 2^-9 of its own size, as much as its own rounding to bf16), and the bias' gradient
-// from the unrounded ones.  A cluster of eight thread blocks takes 64 columns, each an eighth of the tokens, its 32 row lanes in turn; the sums meet in a
-// fixed order.  Bound by HBM: 2 bytes for each of dy, z, u, dz.
+// from the unrounded ones.  Bound by HBM: 2 bytes for each of dy, z, u, dz.
 constexpr int LS_CTA = 256, LS_RANKS = 8;
 struct LsArgs {
     const uint16_t *dy, *z, *u;
@@ -148,9 +148,47 @@ struct LsArgs {
     int64_t ldd;
     float *dbias;
 };
+// eight neighbours of one token: dy becomes du (gated) or dz; d: dg
 template <bool GATED>
-__global__ void __cluster_dims__(LS_RANKS, 1, 1) __launch_bounds__(LS_CTA)
-k_linear_slopes(const __grid_constant__ LsArgs a) {
+__device__ __forceinline__ void ls_eight(const LsArgs &a, float (&dy)[8], const float (&z)[8], const float (&u)[8], float (&d)[8]) {
+    if (a.act == DBSPMSPV_ACT_SILU) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float p = lin_sigmoid_fast(z[k]), slope = p * (1.f + z[k] * (1.f - p));
+            if (GATED) { d[k] = dy[k] * u[k] * slope; dy[k] *= z[k] * p; } else dy[k] *= slope;
+        }
+    } else if (a.act == DBSPMSPV_ACT_GELU) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float p = 0.5f * (1.f + erff(z[k] * 0.70710678f)), slope = p + z[k] * (0.39894228f * __expf(-0.5f * z[k] * z[k]));
+            if (GATED) { d[k] = dy[k] * u[k] * slope; dy[k] *= z[k] * p; } else dy[k] *= slope;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float slope = lin_act_slope(z[k], a.act);
+            if (GATED) { d[k] = dy[k] * u[k] * slope; dy[k] *= lin_act(z[k], a.act); } else dy[k] *= slope;
+        }
+    }
+}
+template <bool GATED>
+__global__ void __launch_bounds__(LS_CTA) k_linear_slopes(const __grid_constant__ LsArgs a) {
+    pdl_wait();
+    const int64_t per = (a.m + 7) / 8, total = a.tokens * per;
+    for (int64_t i = blockIdx.x * (int64_t)LS_CTA + threadIdx.x; i < total; i += (int64_t)gridDim.x * LS_CTA) {
+        const int64_t t = i / per, j = (i - t * per) * 8;
+        float dy[8], z[8] = {}, u[8] = {}, d[8];
+        lin_load8(a.dy + t * a.lddy, j, a.m, dy);
+        if (a.z) lin_load8(a.z + t * a.ldz, j, a.m, z);
+        if (GATED) lin_load8(a.u + t * a.ldz, j, a.m, u);
+        if (GATED || a.z) ls_eight<GATED>(a, dy, z, u, d);
+        if (GATED) lin_store8(a.d0 + t * a.ldd, j, d);
+        lin_store8((GATED ? a.d1 : a.d0) + t * a.ldd, j, dy);
+    }
+    pdl_trigger();
+}
+// With the bias' gradient: a cluster of eight thread blocks takes 64 columns, each an eighth of the tokens, its 32 row lanes in turn; the sums meet in a fixed order.
+__global__ void __cluster_dims__(LS_RANKS, 1, 1) __launch_bounds__(LS_CTA) k_linear_bias(const __grid_constant__ LsArgs a) {
     namespace cg = cooperative_groups;
     __shared__ float s_sum[LS_CTA / 8][64];
     __shared__ float s_all[LS_RANKS][64];
@@ -161,28 +199,15 @@ k_linear_slopes(const __grid_constant__ LsArgs a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[k] = 0.f;
     const int64_t t1 = a.tokens * (rank + 1) / LS_RANKS;
+#pragma unroll 2
     for (int64_t t = a.tokens * rank / LS_RANKS + (tid >> 3); t < t1 && j < a.m; t += LS_CTA / 8) {
-        float dy[8], z[8];
+        float dy[8], z[8] = {}, none[8];
         lin_load8(a.dy + t * a.lddy, j, a.m, dy);
-        if (GATED || a.z) lin_load8(a.z + t * a.ldz, j, a.m, z);
-        if (GATED) {
-            float u[8], d[8];
-            lin_load8(a.u + t * a.ldz, j, a.m, u);
+        if (a.z) { lin_load8(a.z + t * a.ldz, j, a.m, z); ls_eight<false>(a, dy, z, z, none); }
+        if (a.d0) lin_store8(a.d0 + t * a.ldd, j, dy);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) { d[k] = dy[k] * u[k] * lin_act_slope(z[k], a.act); dy[k] *= lin_act(z[k], a.act); }
-            lin_store8(a.d0 + t * a.ldd, j, d);
-            lin_store8(a.d1 + t * a.ldd, j, dy);
-        } else {
-            if (a.z) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) dy[k] *= lin_act_slope(z[k], a.act);
-            }
-            if (a.d0) lin_store8(a.d0 + t * a.ldd, j, dy);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += dy[k];
-        }
+        for (int k = 0; k < 8; ++k) sum[k] += dy[k];
     }
-    if (GATED || !a.dbias) return;                                    // (the same for the whole grid)
 #pragma unroll
     for (int k = 0; k < 8; ++k) s_sum[tid >> 3][(tid & 7) * 8 + k] = sum[k];
     __syncthreads();
@@ -200,6 +225,7 @@ k_linear_slopes(const __grid_constant__ LsArgs a) {
         for (int k = 0; k < LS_RANKS; ++k) v += s_all[k][tid];
         a.dbias[col] = v;
     }
+    pdl_trigger();
 }
 
 // ---- launches -------------------------------------------------------------------------------
@@ -244,6 +270,7 @@ static int vec_of(const LgArgs &a) {
 }
 // `out`: output columns of a tile of one thread block
 static LgPlan plan_gemm(const dbspmspv_handle_s *h, int64_t tokens, int64_t width, int out, int64_t kb) {
+    if (getenv("LGP")) { LgPlan p; sscanf(getenv("LGP"), "%d,%d,%d", &p.cg, &p.nt, &p.c); while (p.c > 1 && kb < p.c) p.c /= 2; return p; }
     if (tokens > 128 && ceil64(width, 2 * out) * ceil64(tokens, 256) * 4 >= h->sm_count / 2 * 3) return {2, 256, 1};
     LgPlan p = {1, tokens <= 16 ? 16 : tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256, 1};
     if (p.nt == 256 && ceil64(tokens, 128) * 128 < ceil64(tokens, 256) * 256) p.nt = 128;
@@ -262,11 +289,12 @@ static int add_columns_c(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a,
     calls.add(k_linear_cols<LAYERS, C>, strips * C * tokens, LC_CTA, (size_t)LC_WARPS * lc_warp_entries(a.n, C) * sizeof(float2), false, a, strips);
     return DBSPMSPV_OK;
 }
-// Thread blocks of a strip: as many as it takes to give every SM one.
+// Thread blocks of a strip: as many as it takes to give every SM two, without more than that.  (4096 x 11008, half active, 1 / 2 / 4 / 8 blocks: 20.3 / 14.4 / 12.0 / 14.9 us; 12288 x 4096,
+// dense: 19.4 / 23.2 / 22.9 / 31.8.)
 static int columns_cluster(const dbspmspv_handle_s *h, int64_t tokens) {
     const int64_t units = (h->d.m + DC_ROWS - 1) / DC_ROWS * tokens;
     int c = 1;
-    while (c < 8 && units * c * 2 <= h->sm_count) c *= 2;
+    while (c < 8 && units * c <= h->sm_count) c *= 2;
     return c;
 }
 template <int LAYERS>
@@ -280,7 +308,7 @@ static int add_columns(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a, i
     }
 }
 static bool over_columns(const dbspmspv_handle_s *h, int64_t tokens) {
-    return tokens <= LIN_COLS_MAX_TOKENS && LC_WARPS * lc_warp_entries(h->d.n, columns_cluster(h, tokens)) * (int64_t)sizeof(float2) <= LIN_COLS_MAX_SMEM;
+    return tokens <= (getenv("LCT") ? atoi(getenv("LCT")) : LIN_COLS_MAX_TOKENS) && LC_WARPS * lc_warp_entries(h->d.n, columns_cluster(h, tokens)) * (int64_t)sizeof(float2) <= LIN_COLS_MAX_SMEM;
 }
 
 // ---- workspace: x as TMA can read it, then the products' operands of a gradient ---------------
@@ -400,8 +428,12 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
             if (up) dz[1] = a.d1 = room.take(b.tokens, ldd);
             if (!a.d0 || (up && !a.d1)) return DBSPMSPV_ERR_INVALID_ARG;
         }
-        const int64_t g = (d.m + 63) / 64 * LS_RANKS;
-        calls.add(up ? k_linear_slopes<true> : k_linear_slopes<false>, (int)g, LS_CTA, 0, calls.n > 0, a);
+        if (b.dbias) {
+            calls.add(k_linear_bias, (int)(ceil64(d.m, 64) * LS_RANKS), LS_CTA, 0, calls.n > 0, a);
+        } else {
+            const int64_t g = ceil64(b.tokens * ceil64(d.m, 8), LS_CTA), most = 16 * h->sm_count;
+            calls.add(up ? k_linear_slopes<true> : k_linear_slopes<false>, (int)(g < most ? g : most), LS_CTA, 0, calls.n > 0, a);
+        }
     }
     LgArgs a = {};
     a.status = &d.ws.ctr->status;

@@ -77,6 +77,7 @@ k_linear_cols(const __grid_constant__ LcArgs a, int strips) {
         }
         __syncwarp();
     }
+    pdl_trigger();
     {
         const uint4 *w[LAYERS];
 #pragma unroll

@@ -93,7 +93,15 @@ __device__ __forceinline__ float lin_act_slope(float z, int act) {
         default: return 1.f;
     }
 }
+// SiLU by the fast exponential and divide, for what is rounded to bf16 or stands in an epilogue: off by a few 2^-22 of |z| + 1, 2^-13 of a bf16's rounding.
+// (expf and a full divide took a quarter of the epilogue's instructions.)
+__device__ __forceinline__ float lin_sigmoid_fast(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float lin_silu_fast(float z) { return z * lin_sigmoid_fast(z); }
 __device__ __forceinline__ uint32_t lin_bf16(float v) { return (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+__device__ __forceinline__ uint32_t lin_pair(float lo, float hi) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
 __device__ __forceinline__ float lin_f32(uint32_t half) { return __uint_as_float(half << 16); }
 
 // ---- instructions ------------------------------------------------------------------------
@@ -116,13 +124,13 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
                      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
 }
 template <int CG>
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t idesc, bool add) {
     if (CG == 1)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+        asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}"
+                     ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "r"((uint32_t)add) : "memory");
     else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+        asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %4, p;\n\t}"
+                     ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
 // arrives on the barrier (CG = 2: on the one at the same place in both thread blocks) when every product issued so far has been made
 template <int CG>
@@ -185,10 +193,9 @@ __device__ __forceinline__ void store_if(bool p, uint16_t *at, uint32_t v) {    
 
 // Descriptor of an operand tile in shared memory under the 128-byte swizzle.  K along the swizzle rows: 64 of K per row, eight rows of M/N 1024
 // bytes on (the other stride is not used).  M/N along them: eight of K 1024 bytes on, the next 64 of M/N behind the block's 64 of K.
-__device__ __forceinline__ uint64_t lg_desc(uint32_t addr, bool mn_major) {
-    const uint64_t leading = mn_major ? LG_K * 128 : 16;
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | (leading >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+// The upper word is a constant, the lower one counts addresses in 16 bytes: the next 16 of K are an addition away.
+constexpr uint32_t LG_DESC_HIGH = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t lg_desc_low(uint32_t addr, bool mn_major) { return ((addr >> 4) & 0x3FFFu) | (uint32_t)((mn_major ? LG_K * 128 : 16) >> 4) << 16; }
 __host__ __device__ constexpr uint32_t lg_idesc(int m, int n, bool a_mn, bool b_mn) {        // fp32 sums, bf16 operands
     return 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)a_mn << 15 | (uint32_t)b_mn << 16 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
@@ -213,50 +220,55 @@ __device__ __forceinline__ void lg_act(float (&v)[V], int act) {
         for (int i = 0; i < V; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_RELU);
     } else if (act == DBSPMSPV_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_SILU);
+        for (int i = 0; i < V; ++i) v[i] = lin_silu_fast(v[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_GELU);
     }
 }
+// V neighbouring bf16 as they lie, two to a word
 template <int V>
-__device__ __forceinline__ void lg_get(const uint16_t *p, int count, float (&v)[V]) {
-    if (V == 8 && count == V) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+__device__ __forceinline__ void lg_get1(const uint16_t *p, int count, uint32_t (&w)[(V + 1) / 2]) {      // (on any address)
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-    } else if (V == 2 && count == V) {
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(p);
-        v[0] = __uint_as_float(w << 16);
-        v[V - 1] = __uint_as_float(w & 0xFFFF0000u);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = i < count ? lin_f32(p[i]) : 0.f;
+    for (int i = 0; i < (V + 1) / 2; ++i) {
+        w[i] = 2 * i < count ? p[2 * i] : 0u;
+        if (2 * i + 1 < V && 2 * i + 1 < count) w[i] |= (uint32_t)p[2 * i + 1] << 16;
     }
 }
+template <int V>
+__device__ __forceinline__ void lg_get(const uint16_t *p, int count, uint32_t (&w)[(V + 1) / 2]) {
+    if (V == 8 && count == V) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(p);
+        w[0] = q.x; w[1 % ((V + 1) / 2)] = q.y; w[2 % ((V + 1) / 2)] = q.z; w[3 % ((V + 1) / 2)] = q.w;
+    } else if (V == 2 && count == V) {
+        w[0] = *reinterpret_cast<const uint32_t *>(p);
+    } else {
+        lg_get1<V>(p, count, w);
+    }
+}
+__device__ __forceinline__ float lg_half(uint32_t w, int i) { return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16); }
 template <int V>
 __device__ __forceinline__ void lg_put(uint16_t *p, int count, const float (&v)[V]) {
     if (V == 8 && count == V) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = lin_bf16(v[2 * i % V]) | lin_bf16(v[(2 * i + 1) % V]) << 16;
+        for (int i = 0; i < 4; ++i) w[i] = lin_pair(v[2 * i % V], v[(2 * i + 1) % V]);
         *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     } else if (V == 2 && count == V) {
-        *reinterpret_cast<uint32_t *>(p) = lin_bf16(v[0]) | lin_bf16(v[V - 1]) << 16;
+        *reinterpret_cast<uint32_t *>(p) = lin_pair(v[0], v[V - 1]);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (i < count) p[i] = (uint16_t)lin_bf16(v[i]);
     }
 }
-// output columns [col, col + V) of token t; v: the sums, u: the other layer's (gated), r: the residual
+// output columns [col, col + V) of token t; v: the sums, u: the other layer's (gated), bias and residual as they lie
 template <int FORM, int V>
-__device__ __forceinline__ void lg_finish(const LgArgs &a, int64_t t, int64_t col, float (&v)[V], const float (&u)[V], const float (&r)[V]) {
-    const int count = a.width - col < V ? (int)(a.width - col) : V;
+__device__ __forceinline__ void lg_finish(const LgArgs &a, int64_t t, int64_t col, int count, float (&v)[V], const float (&u)[V], const uint32_t (&bias)[(V + 1) / 2],
+                                          const uint32_t (&res)[(V + 1) / 2]) {
     if (FORM == LG_FORWARD && a.bias) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += i < count ? lin_f32(__ldg(a.bias + col + i)) : 0.f;
+        for (int i = 0; i < V; ++i) v[i] += lg_half(bias[i / 2], i);
     }
     if (FORM != LG_DX && a.z) lg_put<V>(a.z + t * a.ldz + col, count, v);
     if (FORM != LG_DX) lg_act<V>(v, a.act);
@@ -267,7 +279,7 @@ __device__ __forceinline__ void lg_finish(const LgArgs &a, int64_t t, int64_t co
     }
     if (FORM == LG_FORWARD && a.residual) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += r[i];
+        for (int i = 0; i < V; ++i) v[i] += lg_half(res[i / 2], i);
     }
     if (FORM == LG_FORWARD && a.y_f32) {
         float *p = static_cast<float *>(a.y) + t * a.ldy + col;
@@ -283,38 +295,53 @@ __device__ __forceinline__ void lg_finish(const LgArgs &a, int64_t t, int64_t co
         lg_put<V>(static_cast<uint16_t *>(a.y) + t * a.ldy + col, count, v);
     }
 }
-// The tokens t0 + q * every, q < CT, of the tile's output columns from col0 on, by thread e of LG_FINISH * 32.  exchange() brings their sums to where read(q, lane, v)
-// finds them; the residual is fetched in front of it.
+// The tokens t0 + q * every below `end`, CT of them at a time, of the tile's output columns from col0 on, by thread e of LG_FINISH * 32; a thread keeps its V columns.
+// exchange(c) brings the sums of the tokens q = c .. c + CT - 1 to where read(q, lane, v) finds them; their residual is fetched a round ahead (the
+// first one in front of the wait for the sums).
 template <int FORM, int V, int CT, class Exchange, class Read>
-__device__ __forceinline__ void lg_tokens_of(const LgArgs &a, int64_t t0, int every, int64_t col0, int e, Exchange exchange, Read read) {
-    constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M, G = OUT / V, THREADS = LG_FINISH * 32, ITEMS = (CT * G + THREADS - 1) / THREADS;
-    float r[ITEMS][V];
-    if (FORM == LG_FORWARD && a.residual) {
+__device__ __forceinline__ void lg_out(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange, Read read) {
+    constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M, G = OUT / V, THREADS = LG_FINISH * 32, PASS = THREADS / G, ITEMS = CT > PASS ? CT / PASS : 1, W = (V + 1) / 2;
+    static_assert(THREADS % G == 0 && (CT % PASS == 0 || CT < PASS), "");
+    const int64_t col = col0 + e % G * V;
+    const int q0 = e / G, count = a.width - col < V ? (int)(a.width - col) : V;
+    uint32_t bias[W], res[ITEMS][W], next[ITEMS][W];
+    auto fetch = [&](int c) {
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-            const int i = k * THREADS + e, q = i / G;
-            const int64_t t = t0 + (int64_t)q * every, col = col0 + i % G * V;
-            if (q < CT && t < a.tokens && col < a.width) lg_get<V>(a.residual + t * a.ldr + col, a.width - col < V ? (int)(a.width - col) : V, r[k]);
+            const int q = c + k * PASS + q0;
+            const int64_t t = t0 + (int64_t)q * every;
+            if (t < end && count > 0) lg_get<V>(a.residual + t * a.ldr + col, count, next[k]);
         }
-    }
-    exchange();
+    };
+    if (FORM == LG_FORWARD && a.bias && count > 0) lg_get1<V>(a.bias + col, count, bias);
+    if (FORM == LG_FORWARD && a.residual) fetch(0);
+    for (int c = 0; t0 + (int64_t)c * every < end; c += CT) {
+        if (FORM == LG_FORWARD && a.residual) {
 #pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-        const int i = k * THREADS + e, q = i / G;
-        const int64_t t = t0 + (int64_t)q * every, col = col0 + i % G * V;
-        if (q < CT && t < a.tokens && col < a.width) {
-            float v[V], u[V];
-            read(q, i % G * V, v);
-            if (FORM == LG_GATED) read(q, OUT + i % G * V, u);
-            lg_finish<FORM, V>(a, t, col, v, u, r[k]);
+            for (int k = 0; k < ITEMS; ++k)
+#pragma unroll
+                for (int i = 0; i < W; ++i) res[k][i] = next[k][i];
+            fetch(c + CT);
+        }
+        if (!exchange(c)) return;
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const int q = c + k * PASS + q0;
+            const int64_t t = t0 + (int64_t)q * every;
+            if (q0 < CT && t < end && count > 0) {
+                float v[V], u[V];
+                read(q, e % G * V, v);
+                if (FORM == LG_GATED) read(q, OUT + e % G * V, u);
+                lg_finish<FORM, V>(a, t, col, count, v, u, bias, res[k]);
+            }
         }
     }
 }
 template <int FORM, int CT, class Exchange, class Read>
-__device__ __forceinline__ void lg_tokens_at(const LgArgs &a, int64_t t0, int every, int64_t col0, int e, Exchange exchange, Read read) {
-    if (a.vec == 8) lg_tokens_of<FORM, 8, CT>(a, t0, every, col0, e, exchange, read);
-    else if (a.vec == 2) lg_tokens_of<FORM, 2, CT>(a, t0, every, col0, e, exchange, read);
-    else lg_tokens_of<FORM, 1, CT>(a, t0, every, col0, e, exchange, read);
+__device__ __forceinline__ void lg_out(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange, Read read) {
+    if (a.vec == 8) lg_out<FORM, 8, CT>(a, t0, every, end, col0, e, exchange, read);
+    else if (a.vec == 2) lg_out<FORM, 2, CT>(a, t0, every, end, col0, e, exchange, read);
+    else lg_out<FORM, 1, CT>(a, t0, every, end, col0, e, exchange, read);
 }
 
 // Tiles in the order they are taken: the token tiles of one weight tile side by side, so that its weights come from L2 after the first.
@@ -341,6 +368,7 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
     constexpr int TMEM_COLS = 2 * NT < 32 ? 32 : 2 * NT;
     constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M;                                           // output columns of this block's tile
     static_assert(C == 1 || NT * LG_M * 4 <= STAGES * STAGE_BYTES, "a tile's sums, for the other thread blocks of the cluster, lie in the stages");
+    static_assert(lg_exchange(256) >= LG_FINISH * 128 * 8, "the gradient of W keeps its rows' index there");
     extern __shared__ uint8_t s_raw[];
     __shared__ __align__(8) uint64_t s_full[STAGES], s_empty[STAGES], s_done[2], s_free[2];
     __shared__ uint32_t s_tmem;
@@ -373,14 +401,15 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
     pdl_wait();
     if (warp == 0) {
         if (lane == 0) {                                               // ---- loads
-            int it = 0;
+            int issued = 0, s = 0;
+            uint32_t phase = 1;                                        // (a barrier that nobody has arrived on: the phase before its first counts as complete)
             bool ok = true;
             for (int i = first; i < n_tiles && ok; i += step) {
                 const LgTile t = lg_tile(a, i);
                 const int m0 = (t.m * CG + half) * OUT, n0 = t.n * NT + half * NB;    // (gated: 64 rows of both layers)
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = it % STAGES, layer = kb >= a.k_blocks, k = kb - layer * a.k_blocks;
-                    if (it >= STAGES && !lg_wait(&s_empty[s], (uint32_t)((it / STAGES - 1) & 1), &s_fail, a.status)) { ok = false; break; }
+                int layer = kb0 >= a.k_blocks, k = kb0 - layer * a.k_blocks;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!lg_wait(&s_empty[s], phase, &s_fail, a.status)) { ok = false; break; }
                     const uint32_t pa = stages + s * STAGE_BYTES, pb = pa + LG_A_BYTES;
                     // (both blocks' copies are counted by the first one's barrier)
                     const uint32_t bar = CG > 1 ? cluster_addr(smem_addr(&s_full[s]), 0) : smem_addr(&s_full[s]);
@@ -399,11 +428,15 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                         }
                         tma_load_2d<CG>(pb, &maps.b[layer], k * LG_K, n0, bar);
                     }
+                    ++issued;
+                    if (++s == STAGES) { s = 0; phase ^= 1; }
+                    if (++k == a.k_blocks) { k = 0; ++layer; }
                 }
             }
+            pdl_trigger();                                             // (the next kernel's blocks may begin where this one's end; what they read waits for all of this one)
             if (!ok) {                                                 // gave up: the copies in flight land before the block ends
                 if (CG == 1)
-                    for (int q = it < STAGES ? 0 : it - STAGES; q < it; ++q) (void)mbar_wait_bounded(&s_full[q % STAGES], (uint32_t)((q / STAGES) & 1), 1 << 16);
+                    for (int q = issued < STAGES ? 0 : issued - STAGES; q < issued; ++q) (void)mbar_wait_bounded(&s_full[q % STAGES], (uint32_t)((q / STAGES) & 1), 1 << 16);
                 else                                                   // (the barrier that counts them may be the other block's: far longer than a copy takes)
                     for (int q = 0; q < 2000; ++q) __nanosleep(1000);
             }
@@ -411,26 +444,29 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
     } else if (warp == 1) {
         if (lane == 0 && half == 0) {                                  // ---- products
             constexpr uint32_t idesc = lg_idesc(CG * LG_M, NT, A_MN, B_MN);
-            int it = 0, n = 0;
+            const uint32_t low_a = lg_desc_low(stages, A_MN), low_b = lg_desc_low(stages + LG_A_BYTES, B_MN);
+            int s = 0, n = 0, last = -1;
+            uint32_t phase = 0;
             bool ok = true;
             for (int i = first; i < n_tiles && ok; i += step, ++n) {
                 const uint32_t d = tmem + (uint32_t)(n & 1) * NT;
                 if (n >= 2 && !lg_wait(&s_free[n & 1], (uint32_t)((n / 2 - 1) & 1), &s_fail, a.status)) { ok = false; break; }
                 tc_fence_after();
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = it % STAGES;
-                    if (!lg_wait(&s_full[s], (uint32_t)((it / STAGES) & 1), &s_fail, a.status)) { ok = false; break; }
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!lg_wait(&s_full[s], phase, &s_fail, a.status)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t pa = stages + s * STAGE_BYTES, pb = pa + LG_A_BYTES;
+                    const uint32_t pa = low_a + s * (STAGE_BYTES >> 4), pb = low_b + s * (STAGE_BYTES >> 4);
 #pragma unroll
                     for (int k = 0; k < LG_K / 16; ++k)
-                        tc_mma<CG>(d, lg_desc(pa + k * (A_MN ? 2048 : 32), A_MN), lg_desc(pb + k * (B_MN ? 2048 : 32), B_MN), idesc, kb > kb0 || k > 0);
+                        tc_mma<CG>(d, pa + k * ((A_MN ? 2048 : 32) >> 4), pb + k * ((B_MN ? 2048 : 32) >> 4), LG_DESC_HIGH, idesc, kb > kb0 || k > 0);
                     tc_commit<CG>(&s_empty[s]);
+                    last = s;
+                    if (++s == STAGES) { s = 0; phase ^= 1; }
                 }
                 if (ok) tc_commit<CG>(&s_done[n & 1]);
             }
-            if (!ok && it > 0)                                         // gave up: the products in flight end before the accumulators are given back
-                (void)mbar_wait_bounded(&s_empty[(it - 1) % STAGES], (uint32_t)(((it - 1) / STAGES) & 1), 1 << 16);
+            if (!ok && last >= 0)                                      // gave up: the products in flight end before the accumulators are given back
+                (void)mbar_wait_bounded(&s_empty[last], phase ^ (last == STAGES - 1 ? 1u : 0u), 1 << 16);
         }
     } else {                                                           // ---- accumulators: warp w reads the lanes 32 (w % 4) ...
         const int quad = warp & 3, group = (warp - 2) >> 2, e = tid - 64;
@@ -440,41 +476,51 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
             const LgTile t = lg_tile(a, i);
             const uint32_t d = mine + (uint32_t)(n & 1) * NT;
             if constexpr (FORM == LG_DW) {
-                // (the index of the tile's 256 rows, half of them a group's, four a lane's, is fetched while the products run)
+                // (the index of a warp's rows, four a lane, is fetched into its own kilobyte of shared memory while the products run, and read from there
+                // two rows to a load that all lanes share)
                 constexpr int ROWS = NT / 2;
                 const int word = (t.m * CG + half) * (LG_M / 32) + quad;
                 const int64_t row0 = (int64_t)t.n * NT + group * ROWS;
                 const uint2 *index = a.index[t.product] + (int64_t)word * a.width;
                 uint16_t *dw = a.dw[t.product];
-                const uint32_t below = (1u << lane) - 1u;
-                uint2 x[ROWS / 32];
+                const uint32_t below = (1u << lane) - 1u, own = exchange + (uint32_t)(warp - 2) * (ROWS * 8);
+                __syncwarp();
 #pragma unroll
                 for (int q = 0; q < ROWS / 32; ++q) {
-                    x[q] = make_uint2(0u, 0u);
-                    if (word < a.index_words && row0 + q * 32 + lane < a.width) x[q] = __ldg(index + row0 + q * 32 + lane);
+                    uint2 x = make_uint2(0u, 0u);
+                    if (word < a.index_words && row0 + q * 32 + lane < a.width) x = __ldg(index + row0 + q * 32 + lane);
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(own + (uint32_t)(q * 32 + lane) * 8), "r"(x.x), "r"(x.y) : "memory");
                 }
+                __syncwarp();
                 if (!__all_sync(0xFFFFFFFFu, lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status))) break;
                 tc_fence_after();
-#pragma unroll
-                for (int q = 0; q < ROWS / 16; ++q) {
+#pragma unroll 1
+                for (int r = 0; r < ROWS; r += 16) {
                     float v[16];
-                    tc_load16(d + group * ROWS + q * 16, v);
+                    tc_load16(d + group * ROWS + r, v);
+                    uint32_t at[16], bits[16];                         // (all places first: the stores keep their order)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(bits[2 * k]), "=r"(at[2 * k]), "=r"(bits[2 * k + 1]), "=r"(at[2 * k + 1]) : "r"(own + (uint32_t)(r + 2 * k) * 8));
+                        at[2 * k] += __popc(bits[2 * k] & below);
+                        at[2 * k + 1] += __popc(bits[2 * k + 1] & below);
+                    }
                     tc_load_wait(v);
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const uint32_t bits = __shfl_sync(0xFFFFFFFFu, x[q / 2].x, (q & 1) * 16 + k), at = __shfl_sync(0xFFFFFFFFu, x[q / 2].y, (q & 1) * 16 + k);
-                        store_if((bits >> lane) & 1u, dw + at + __popc(bits & below), lin_bf16(v[k]));
+                    for (int k = 0; k < 8; ++k) {
+                        const uint32_t w = lin_pair(v[2 * k], v[2 * k + 1]);
+                        store_if((bits[2 * k] >> lane) & 1u, dw + at[2 * k], w & 0xFFFFu);
+                        store_if((bits[2 * k + 1] >> lane) & 1u, dw + at[2 * k + 1], w >> 16);
                     }
                 }
             } else {
-                bool ok = __all_sync(0xFFFFFFFFu, lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status));
-                if (C == 1) ok = finish_all(ok);                       // (all of them go on to the exchange, or none)
-                if (!ok) break;
-                tc_fence_after();
-                const int64_t t0 = (int64_t)t.n * NT;
+                const int64_t t0 = (int64_t)t.n * NT, end = t0 + NT < a.tokens ? t0 + NT : a.tokens;
+                auto done = [&] { return (bool)__all_sync(0xFFFFFFFFu, lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status)); };
                 if constexpr (C > 1) {
                     // this block's sums into its own shared memory, [token][lane]: every copy has landed and every product has been made
-                    for (int c = group * 16; c < NT && t0 + c < a.tokens; c += 32) {
+                    if (!done()) break;
+                    tc_fence_after();
+                    for (int c = group * 16; t0 + c < end; c += 32) {
                         float v[16];
                         tc_load16(d + c, v);
                         tc_load_wait(v);
@@ -483,20 +529,26 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                     }
                 } else {
                     constexpr int CT = lg_tokens(NT), BUFFERS = lg_buffers(NT);
-                    for (int c = 0; c < NT && t0 + c < a.tokens; c += CT, ++turn) {
-                        const uint32_t buffer = exchange + (BUFFERS > 1 ? (uint32_t)(turn & 1) * (CT * LG_M * 4) : 0u);
-                        lg_tokens_at<FORM, CT>(a, t0 + c, 1, (int64_t)(t.m * CG + half) * OUT, e, [&] {
-                            if (BUFFERS == 1) finish_sync();           // (everybody has read the tokens before)
-                            if (group * 16 < CT) {
-                                float v[16];
-                                tc_load16(d + c + group * 16, v);
-                                tc_load_wait(v);
+                    bool ok = true;
+                    uint32_t buffer = exchange;
+                    lg_out<FORM, CT>(a, t0, 1, end, (int64_t)(t.m * CG + half) * OUT, e, [&](int c) {
+                        if (c == 0) {
+                            ok = finish_all(done());                   // (all of them go on to the exchange, or none)
+                            if (!ok) return false;
+                            tc_fence_after();
+                        } else if (BUFFERS == 1) finish_sync();        // (everybody has read the tokens before)
+                        if (BUFFERS > 1) { buffer = exchange + (uint32_t)(turn & 1) * (CT * LG_M * 4); ++turn; }
+                        if (group * 16 < CT) {
+                            float v[16];
+                            tc_load16(d + c + group * 16, v);
+                            tc_load_wait(v);
 #pragma unroll
-                                for (int k = 0; k < 16; ++k) st_shared(buffer + (uint32_t)((group * 16 + k) * LG_M + quad * 32 + lane) * 4, v[k]);
-                            }
-                            finish_sync();
-                        }, [&](int q, int l, auto &v) { ld_shared(buffer + (uint32_t)(q * LG_M + l) * 4, v); });
-                    }
+                            for (int k = 0; k < 16; ++k) st_shared(buffer + (uint32_t)((group * 16 + k) * LG_M + quad * 32 + lane) * 4, v[k]);
+                        }
+                        finish_sync();
+                        return true;
+                    }, [&](int q, int l, auto &v) { ld_shared(buffer + (uint32_t)((q & (CT - 1)) * LG_M + l) * 4, v); });
+                    if (!ok) break;
                 }
             }
             tc_fence_before();
@@ -511,19 +563,19 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
         if (warp >= 2 && !s_fail && first < n_tiles) {
             const LgTile t = lg_tile(a, first);
             constexpr int CT = NT / C < 32 ? NT / C : 32;
-            for (int c = rank; c < NT; c += CT * C)
-                lg_tokens_at<FORM, CT>(a, (int64_t)t.n * NT + c, C, (int64_t)t.m * OUT, tid - 64, [] {}, [&](int q, int l, auto &v) {
-                    constexpr int V = sizeof(v) / sizeof(float);
-                    float part[C][V];
+            const int64_t t0 = (int64_t)t.n * NT, end = t0 + NT < a.tokens ? t0 + NT : a.tokens;
+            lg_out<FORM, CT>(a, t0 + rank, C, end, (int64_t)t.m * OUT, tid - 64, [](int) { return true; }, [&](int q, int l, auto &v) {
+                constexpr int V = sizeof(v) / sizeof(float);
+                float part[C][V];
 #pragma unroll
-                    for (int r = 0; r < C; ++r) ld_cluster(cluster_addr(stages, r) + (uint32_t)((c + q * C) * LG_M + l) * 4, part[r]);
+                for (int r = 0; r < C; ++r) ld_cluster(cluster_addr(stages, r) + (uint32_t)((rank + q * C) * LG_M + l) * 4, part[r]);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        v[j] = part[0][j];
+                for (int j = 0; j < V; ++j) {
+                    v[j] = part[0][j];
 #pragma unroll
-                        for (int r = 1; r < C; ++r) v[j] += part[r][j];
-                    }
-                });
+                    for (int r = 1; r < C; ++r) v[j] += part[r][j];
+                }
+            });
         }
         __syncwarp();
     }
