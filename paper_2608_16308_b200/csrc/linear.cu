@@ -242,7 +242,7 @@ static int add_gemm_as(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps
         DBS_CUDA(cudaFuncSetAttribute(k_linear_gemm<FORM, CG, NT, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, lg_smem(CG, NT)));
         done = true;
     }
-    calls.add(k_linear_gemm<FORM, CG, NT, C>, grid, LG_CTA, lg_smem(CG, NT), calls.n > 0, maps, a);
+    calls.add(k_linear_gemm<FORM, CG, NT, C>, grid, lg_threads(FORM == LG_DW), lg_smem(CG, NT), calls.n > 0, maps, a);
     return DBSPMSPV_OK;
 }
 template <int FORM>
@@ -261,12 +261,10 @@ static int add_gemm(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps, c
     }
 }
 static int64_t ceil64(int64_t v, int64_t by) { return (v + by - 1) / by; }
-// neighbours of a token that a thread finishes at once (LgArgs::vec)
-static int vec_of(const LgArgs &a) {
-    auto fits = [](const void *p, int64_t ld, int64_t item, int64_t v) { return !p || ((reinterpret_cast<uintptr_t>(p) % (uintptr_t)(v < 8 ? v * item : 16)) == 0 && ld % (v < 8 ? v : 16 / item) == 0); };
-    for (int v : {8, 2})
-        if (fits(a.y, a.ldy, a.y_f32 ? 4 : 2, v) && fits(a.z, a.ldz, 2, v) && fits(a.u, a.ldz, 2, v) && fits(a.residual, a.ldr, 2, v)) return v;
-    return 1;
+// whether every row of the outputs and of the residual begins on 16 bytes (LgArgs::aligned)
+static int aligned_rows(const LgArgs &a) {
+    auto fits = [](const void *p, int64_t ld, int64_t item) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * item % 16 == 0); };
+    return fits(a.y, a.ldy, a.y_f32 ? 4 : 2) && fits(a.z, a.ldz, 2) && fits(a.u, a.ldz, 2) && fits(a.residual, a.ldr, 2);
 }
 // `out`: output columns of a tile of one thread block
 static LgPlan plan_gemm(const dbspmspv_handle_s *h, int64_t tokens, int64_t width, int out, int64_t kb) {
@@ -388,7 +386,7 @@ static int forward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinForward f, Li
         a.tiles_m = (int)ceil64(d.m, p.cg * out); a.tiles_n = (int)ceil64(f.tokens, p.nt); a.products = 1; a.layers = 1; a.k_blocks = (int)kb;
         a.tokens = f.tokens; a.width = d.m;
         a.y = f.y; a.ldy = f.ldy; a.y_f32 = f.y_f32; a.act = f.act; a.bias = f.bias; a.residual = f.residual; a.ldr = f.ldr;
-        a.z = f.z; a.u = f.u; a.ldz = f.ldz; a.vec = vec_of(a); a.status = &d.ws.ctr->status;
+        a.z = f.z; a.u = f.u; a.ldz = f.ldz; a.aligned = aligned_rows(a); a.status = &d.ws.ctr->status;
         s = up ? add_gemm<LG_GATED>(h, calls, maps, a, p) : add_gemm<LG_FORWARD>(h, calls, maps, a, p);
     }
     return s == DBSPMSPV_OK ? submit_calls(h, calls, st) : s;
@@ -446,7 +444,7 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
             if ((s = encode_rows(&maps.b[l], dz[l], b.tokens, d.m, ldd, p.nt / p.cg)) != DBSPMSPV_OK) return s;
         }
         a.tiles_m = (int)ceil64(d.n, p.cg * LG_M); a.tiles_n = (int)ceil64(b.tokens, p.nt); a.products = 1; a.layers = layers; a.k_blocks = (int)kb;
-        a.tokens = b.tokens; a.width = d.n; a.y = b.dx; a.ldy = b.lddx; a.vec = vec_of(a);
+        a.tokens = b.tokens; a.width = d.n; a.y = b.dx; a.ldy = b.lddx; a.aligned = aligned_rows(a);
         if ((s = add_gemm<LG_DX>(h, calls, maps, a, p)) != DBSPMSPV_OK) return s;
     }
     if (want_w) {

@@ -40,7 +40,8 @@ namespace dbs {
 constexpr int LG_M = 128, LG_K = 64;
 constexpr int LG_A_BYTES = LG_M * LG_K * 2;
 constexpr int LG_FINISH = 8;                                   // warps that empty the accumulators, two for each quarter of the lanes
-constexpr int LG_CTA = (2 + LG_FINISH) * 32;                   // (and one warp each for the loads and the products)
+constexpr int LG_FINISH_DW = 16;                               // ... for the gradient of W, whose values go one by one: twice as many
+__host__ __device__ constexpr int lg_threads(bool dw) { return (2 + (dw ? LG_FINISH_DW : LG_FINISH)) * 32; }       // (and one warp each for the loads and the products)
 
 // Stages of a form: a block of K of both operands.  Narrow tiles (few tokens, bound by HBM) leave room for two thread blocks per SM.
 __host__ __device__ constexpr int lg_stage_bytes(int cg, int nt) { return LG_A_BYTES + nt / cg * LG_K * 2; }
@@ -69,7 +70,7 @@ struct LgArgs {
     int64_t ldr;
     uint16_t *z, *u;                // in front of the activation; the other projection (may be null)
     int64_t ldz;
-    int vec;                        // neighbours that a thread finishes: 8 (every row of y, z, u, residual begins on 16 bytes), 2 (on 4) or 1
+    int aligned;                    // every row of y, z, u and the residual begins on 16 bytes
     uint16_t *dw[2];
     const uint2 *index[2];          // [word of 32 columns][row]: stored columns, place of the first of them
     int index_words;
@@ -160,23 +161,15 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
     return far;
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t far) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(far) : "memory"); }
-template <int V>
-__device__ __forceinline__ void ld_cluster(uint32_t far, float (&v)[V]) {
-    if constexpr (V >= 4) {
-#pragma unroll
-        for (int i = 0; i < V; i += 4)
-            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i]), "=f"(v[i + 1]), "=f"(v[i + 2]), "=f"(v[i + 3]) : "r"(far + i * 4) : "memory");
-    } else if constexpr (V == 2) asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(far) : "memory");
-    else asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[0]) : "r"(far) : "memory");
+__device__ __forceinline__ float4 ld_cluster(uint32_t far) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(far) : "memory");
+    return v;
 }
-template <int V>
-__device__ __forceinline__ void ld_shared(uint32_t addr, float (&v)[V]) {
-    if constexpr (V >= 4) {
+__device__ __forceinline__ void ld_shared(uint32_t addr, float (&v)[8]) {
 #pragma unroll
-        for (int i = 0; i < V; i += 4)
-            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i]), "=f"(v[i + 1]), "=f"(v[i + 2]), "=f"(v[i + 3]) : "r"(addr + i * 4) : "memory");
-    } else if constexpr (V == 2) asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v[0]), "=f"(v[1]) : "r"(addr) : "memory");
-    else asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[0]) : "r"(addr) : "memory");
+    for (int i = 0; i < 8; i += 4)
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i]), "=f"(v[i + 1]), "=f"(v[i + 2]), "=f"(v[i + 3]) : "r"(addr + i * 4) : "memory");
 }
 __device__ __forceinline__ void st_shared(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
 // the warps that empty the accumulators meet; with a vote: whether `ok` holds in all of them
@@ -211,137 +204,145 @@ __device__ __forceinline__ bool lg_wait(uint64_t *bar, uint32_t parity, volatile
     return false;
 }
 
-// ---- what becomes of V neighbouring sums of one token ------------------------------------
-template <int V>
-__device__ __forceinline__ void lg_act(float (&v)[V], int act) {
+// ---- what becomes of neighbouring sums of one token --------------------------------------
+__device__ __forceinline__ void lg_act(float (&v)[8], int act) {
     if (act == DBSPMSPV_ACT_NONE) return;
     if (act == DBSPMSPV_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_RELU);
+        for (int i = 0; i < 8; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_RELU);
     } else if (act == DBSPMSPV_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = lin_silu_fast(v[i]);
+        for (int i = 0; i < 8; ++i) v[i] = lin_silu_fast(v[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_GELU);
+        for (int i = 0; i < 8; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_GELU);
     }
 }
-// V neighbouring bf16 as they lie, two to a word
-template <int V>
-__device__ __forceinline__ void lg_get1(const uint16_t *p, int count, uint32_t (&w)[(V + 1) / 2]) {      // (on any address)
-#pragma unroll
-    for (int i = 0; i < (V + 1) / 2; ++i) {
-        w[i] = 2 * i < count ? p[2 * i] : 0u;
-        if (2 * i + 1 < V && 2 * i + 1 < count) w[i] |= (uint32_t)p[2 * i + 1] << 16;
-    }
-}
-template <int V>
-__device__ __forceinline__ void lg_get(const uint16_t *p, int count, uint32_t (&w)[(V + 1) / 2]) {
-    if (V == 8 && count == V) {
+// the first `count` of eight neighbouring bf16, two to a word; `aligned`: p lies on 16 bytes
+__device__ __forceinline__ void lg_get(const uint16_t *p, bool aligned, int count, uint32_t (&w)[4]) {
+    if (aligned && count == 8) {
         const uint4 q = *reinterpret_cast<const uint4 *>(p);
-        w[0] = q.x; w[1 % ((V + 1) / 2)] = q.y; w[2 % ((V + 1) / 2)] = q.z; w[3 % ((V + 1) / 2)] = q.w;
-    } else if (V == 2 && count == V) {
-        w[0] = *reinterpret_cast<const uint32_t *>(p);
-    } else {
-        lg_get1<V>(p, count, w);
-    }
-}
-__device__ __forceinline__ float lg_half(uint32_t w, int i) { return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16); }
-template <int V>
-__device__ __forceinline__ void lg_put(uint16_t *p, int count, const float (&v)[V]) {
-    if (V == 8 && count == V) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = lin_pair(v[2 * i % V], v[(2 * i + 1) % V]);
-        *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else if (V == 2 && count == V) {
-        *reinterpret_cast<uint32_t *>(p) = lin_pair(v[0], v[V - 1]);
+        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < count) p[i] = (uint16_t)lin_bf16(v[i]);
+        for (int i = 0; i < 4; ++i) w[i] = (2 * i < count ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < count ? (uint32_t)p[2 * i + 1] << 16 : 0u);
     }
 }
-// output columns [col, col + V) of token t; v: the sums, u: the other layer's (gated), bias and residual as they lie
-template <int FORM, int V>
-__device__ __forceinline__ void lg_finish(const LgArgs &a, int64_t t, int64_t col, int count, float (&v)[V], const float (&u)[V], const uint32_t (&bias)[(V + 1) / 2],
-                                          const uint32_t (&res)[(V + 1) / 2]) {
-    if (FORM == LG_FORWARD && a.bias) {
+__device__ __forceinline__ float lg_half(const uint32_t (&w)[4], int i) { return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); }
+
+// Columns 8 j .. 8 j + 7 of a tile's part of a row (`row` points to its first column, `width` of its columns exist; 0: nothing is stored), a thread each, the G threads of a
+// row side by side in the warp.  A row that does not begin on 16 bytes is stored in the eights that do: a thread takes the end of its neighbour's
+// values and the beginning of its own.  (All threads of the warp call it together.)
+template <int G, bool ALIGNED>
+__device__ __forceinline__ void lg_put(uint16_t *row, int j, int width, const float (&v)[8]) {
+    uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += lg_half(bias[i / 2], i);
-    }
-    if (FORM != LG_DX && a.z) lg_put<V>(a.z + t * a.ldz + col, count, v);
-    if (FORM != LG_DX) lg_act<V>(v, a.act);
-    if (FORM == LG_GATED) {
-        if (a.u) lg_put<V>(a.u + t * a.ldz + col, count, u);
+    for (int i = 0; i < 4; ++i) w[i] = lin_pair(v[2 * i], v[2 * i + 1]);
+    int lo = 0, at = 8 * j;
+    if (!ALIGNED) {
+        const int s = (int)((reinterpret_cast<uintptr_t>(row) >> 1) & 7u), from = 8 - s;       // first half word, of the neighbour's eight and then this thread's
+        uint32_t c[9];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] *= u[i];
-    }
-    if (FORM == LG_FORWARD && a.residual) {
+        for (int i = 0; i < 4; ++i) { c[i] = __shfl_up_sync(0xFFFFFFFFu, w[i], 1, G); c[i + 4] = w[i]; }
+        c[8] = 0u;
+        const uint32_t keep[4] = {w[0], w[1], w[2], w[3]};
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += lg_half(res[i / 2], i);
-    }
-    if (FORM == LG_FORWARD && a.y_f32) {
-        float *p = static_cast<float *>(a.y) + t * a.ldy + col;
-        if (V == 8 && count == V) {
-            reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1 % V], v[2 % V], v[3 % V]);
-            reinterpret_cast<float4 *>(p)[1] = make_float4(v[4 % V], v[5 % V], v[6 % V], v[7 % V]);
-        } else {
+        for (int i = 0; i < 5; ++i) c[i] = from & 8 ? c[i + 4] : c[i];
+        if (from & 8) c[5] = c[6] = c[7] = 0u;                          // (not read)
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (i < count) p[i] = v[i];
+        for (int i = 0; i < 6; ++i) c[i] = from & 4 ? c[i + 2] : c[i];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) c[i] = from & 2 ? c[i + 1] : c[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = from & 1 ? __funnelshift_r(c[i], c[i + 1], 16) : c[i];
+        at -= s;
+        lo = j == 0 ? s : 0;
+        if (j == G - 1) {                                              // what lies behind the last eight
+#pragma unroll
+            for (int k = 1; k < 8; ++k)
+                if (k >= from && 8 * j + k < width) row[8 * j + k] = (uint16_t)(keep[k / 2] >> (16 * (k & 1)));
         }
-    } else {
-        lg_put<V>(static_cast<uint16_t *>(a.y) + t * a.ldy + col, count, v);
+    }
+    const int hi = width - at < 8 ? width - at : 8;
+    if (lo == 0 && hi == 8) *reinterpret_cast<uint4 *>(row + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k >= lo && k < hi) row[at + k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
     }
 }
-// The tokens t0 + q * every below `end`, CT of them at a time, of the tile's output columns from col0 on, by thread e of LG_FINISH * 32; a thread keeps its V columns.
-// exchange(c) brings the sums of the tokens q = c .. c + CT - 1 to where read(q, lane, v) finds them; their residual is fetched a round ahead (the
-// first one in front of the wait for the sums).
-template <int FORM, int V, int CT, class Exchange, class Read>
-__device__ __forceinline__ void lg_out(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange, Read read) {
-    constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M, G = OUT / V, THREADS = LG_FINISH * 32, PASS = THREADS / G, ITEMS = CT > PASS ? CT / PASS : 1, W = (V + 1) / 2;
-    static_assert(THREADS % G == 0 && (CT % PASS == 0 || CT < PASS), "");
-    const int64_t col = col0 + e % G * V;
-    const int q0 = e / G, count = a.width - col < V ? (int)(a.width - col) : V;
-    uint32_t bias[W], res[ITEMS][W], next[ITEMS][W];
+
+// The tokens t0 + q * every below `end`, CT of them at a time, of the tile's output columns from col0 on, by thread e of LG_FINISH * 32, which keeps its eight columns.
+// exchange(c) brings the sums of the tokens q = c .. c + CT - 1 to shared memory, [token][lane], and says where (0: gave up).  The residual is fetched a
+// round ahead, the first one in front of the wait for the sums (4096 x 11008, 2048 tokens, 155 -> 149 us).
+template <int FORM, int CT, bool ALIGNED, class Exchange>
+__device__ __forceinline__ void lg_out_as(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange) {
+    constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M, G = OUT / 8, PASS = LG_FINISH * 32 / G, ITEMS = CT > PASS ? CT / PASS : 1;
+    static_assert(CT % PASS == 0 || CT < PASS, "");
+    const int q0 = e / G, j = e % G, part = a.width - col0 < OUT ? (int)(a.width - col0) : OUT, count = part - 8 * j < 8 ? part - 8 * j : 8;
+    uint32_t bias[4], res[ITEMS][4], next[ITEMS][4];
     auto fetch = [&](int c) {
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-            const int q = c + k * PASS + q0;
-            const int64_t t = t0 + (int64_t)q * every;
-            if (t < end && count > 0) lg_get<V>(a.residual + t * a.ldr + col, count, next[k]);
+            const int64_t t = t0 + (int64_t)(c + k * PASS + q0) * every;
+            if (q0 < CT && t < end && count > 0) lg_get(a.residual + t * a.ldr + col0 + 8 * j, ALIGNED, count, next[k]);
         }
     };
-    if (FORM == LG_FORWARD && a.bias && count > 0) lg_get1<V>(a.bias + col, count, bias);
+    if (FORM == LG_FORWARD && a.bias) lg_get(a.bias + col0 + 8 * j, false, count, bias);
     if (FORM == LG_FORWARD && a.residual) fetch(0);
     for (int c = 0; t0 + (int64_t)c * every < end; c += CT) {
         if (FORM == LG_FORWARD && a.residual) {
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k)
 #pragma unroll
-                for (int i = 0; i < W; ++i) res[k][i] = next[k][i];
+                for (int i = 0; i < 4; ++i) res[k][i] = next[k][i];
             fetch(c + CT);
         }
-        if (!exchange(c)) return;
+        const uint32_t sums = exchange(c);
+        if (!sums) return;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
-            const int q = c + k * PASS + q0;
-            const int64_t t = t0 + (int64_t)q * every;
-            if (q0 < CT && t < end && count > 0) {
-                float v[V], u[V];
-                read(q, e % G * V, v);
-                if (FORM == LG_GATED) read(q, OUT + e % G * V, u);
-                lg_finish<FORM, V>(a, t, col, count, v, u, bias, res[k]);
+            const int q = q0 < CT ? k * PASS + q0 : 0;
+            const int64_t t = t0 + (int64_t)(c + q) * every;
+            const int width = q0 < CT && t < end ? part : 0;           // (a thread without a token stores nothing, but the other rows' threads may need it)
+            if (ALIGNED && width <= 8 * j) continue;
+            float v[8], u[8];
+            ld_shared(sums + (uint32_t)(q * LG_M + 8 * j) * 4, v);
+            if (FORM == LG_GATED) ld_shared(sums + (uint32_t)(q * LG_M + OUT + 8 * j) * 4, u);
+            if (FORM == LG_FORWARD && a.bias) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += lg_half(bias, i);
             }
+            if (FORM != LG_DX && a.z) lg_put<G, ALIGNED>(a.z + t * a.ldz + col0, j, width, v);
+            if (FORM != LG_DX) lg_act(v, a.act);
+            if (FORM == LG_GATED) {
+                if (a.u) lg_put<G, ALIGNED>(a.u + t * a.ldz + col0, j, width, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= u[i];
+            }
+            if (FORM == LG_FORWARD && a.residual) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] += lg_half(res[k], i);
+            }
+            if (FORM == LG_FORWARD && a.y_f32) {
+                float *p = static_cast<float *>(a.y) + t * a.ldy + col0 + 8 * j;
+                if (ALIGNED && width - 8 * j >= 8) {
+                    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (8 * j + i < width) p[i] = v[i];
+                }
+            } else lg_put<G, ALIGNED>(static_cast<uint16_t *>(a.y) + t * a.ldy + col0, j, width, v);
         }
     }
 }
-template <int FORM, int CT, class Exchange, class Read>
-__device__ __forceinline__ void lg_out(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange, Read read) {
-    if (a.vec == 8) lg_out<FORM, 8, CT>(a, t0, every, end, col0, e, exchange, read);
-    else if (a.vec == 2) lg_out<FORM, 2, CT>(a, t0, every, end, col0, e, exchange, read);
-    else lg_out<FORM, 1, CT>(a, t0, every, end, col0, e, exchange, read);
+
+template <int FORM, int CT, class Exchange>
+__device__ __forceinline__ void lg_out(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange) {
+    if (a.aligned) lg_out_as<FORM, CT, true>(a, t0, every, end, col0, e, exchange);
+    else lg_out_as<FORM, CT, false>(a, t0, every, end, col0, e, exchange);
 }
 
 // Tiles in the order they are taken: the token tiles of one weight tile side by side, so that its weights come from L2 after the first.
@@ -358,17 +359,18 @@ __device__ __forceinline__ LgTile lg_tile(const LgArgs &a, int i) {
 
 // CG thread blocks of a cluster per tile of CG * 128 x NT; C of them (CG = 1) share its K.
 template <int FORM, int CG, int NT, int C>
-__global__ void __cluster_dims__(CG * C, 1, 1) __launch_bounds__(LG_CTA, NT <= 64 ? 2 : 1)
+__global__ void __cluster_dims__(CG * C, 1, 1) __launch_bounds__(lg_threads(FORM == LG_DW), NT <= 64 ? 2 : 1)
 k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArgs a) {
     namespace cg = cooperative_groups;
     static_assert(CG == 1 || (CG == 2 && C == 1 && NT == 256), "");
     static_assert(FORM != LG_DW || (C == 1 && NT == 256), "");
     constexpr bool A_MN = FORM != LG_DX, B_MN = FORM == LG_DW;
     constexpr int STAGES = lg_stages(CG, NT), STAGE_BYTES = lg_stage_bytes(CG, NT), NB = NT / CG;     // NB: rows of operand B in this block's shared memory
+    constexpr int FINISH = FORM == LG_DW ? LG_FINISH_DW : LG_FINISH;
     constexpr int TMEM_COLS = 2 * NT < 32 ? 32 : 2 * NT;
     constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M;                                           // output columns of this block's tile
     static_assert(C == 1 || NT * LG_M * 4 <= STAGES * STAGE_BYTES, "a tile's sums, for the other thread blocks of the cluster, lie in the stages");
-    static_assert(lg_exchange(256) >= LG_FINISH * 128 * 8, "the gradient of W keeps its rows' index there");
+
     extern __shared__ uint8_t s_raw[];
     __shared__ __align__(8) uint64_t s_full[STAGES], s_empty[STAGES], s_done[2], s_free[2];
     __shared__ uint32_t s_tmem;
@@ -380,7 +382,7 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
     const int kb_all = a.k_blocks * a.layers, kb0 = (int)((int64_t)kb_all * rank / C), kb1 = (int)((int64_t)kb_all * (rank + 1) / C);
     if (tid == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&s_done[s], 1); mbar_init(&s_free[s], LG_FINISH * CG); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&s_done[s], 1); mbar_init(&s_free[s], FINISH * CG); }
         s_fail = 0;
         fence_barrier_init();
     }
@@ -476,9 +478,8 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
             const LgTile t = lg_tile(a, i);
             const uint32_t d = mine + (uint32_t)(n & 1) * NT;
             if constexpr (FORM == LG_DW) {
-                // (the index of a warp's rows, four a lane, is fetched into its own kilobyte of shared memory while the products run, and read from there
-                // two rows to a load that all lanes share)
-                constexpr int ROWS = NT / 2;
+                // (the index of a warp's rows is fetched into its own part of shared memory while the products run, and read from there two rows to a load that all lanes share)
+                constexpr int ROWS = NT / (FINISH / 4);
                 const int word = (t.m * CG + half) * (LG_M / 32) + quad;
                 const int64_t row0 = (int64_t)t.n * NT + group * ROWS;
                 const uint2 *index = a.index[t.product] + (int64_t)word * a.width;
@@ -530,14 +531,13 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                 } else {
                     constexpr int CT = lg_tokens(NT), BUFFERS = lg_buffers(NT);
                     bool ok = true;
-                    uint32_t buffer = exchange;
-                    lg_out<FORM, CT>(a, t0, 1, end, (int64_t)(t.m * CG + half) * OUT, e, [&](int c) {
+                    lg_out<FORM, CT>(a, t0, 1, end, (int64_t)(t.m * CG + half) * OUT, e, [&](int c) -> uint32_t {
                         if (c == 0) {
                             ok = finish_all(done());                   // (all of them go on to the exchange, or none)
-                            if (!ok) return false;
+                            if (!ok) return 0u;
                             tc_fence_after();
                         } else if (BUFFERS == 1) finish_sync();        // (everybody has read the tokens before)
-                        if (BUFFERS > 1) { buffer = exchange + (uint32_t)(turn & 1) * (CT * LG_M * 4); ++turn; }
+                        const uint32_t buffer = exchange + (BUFFERS > 1 ? (uint32_t)(turn++ & 1) * (CT * LG_M * 4) : 0u);
                         if (group * 16 < CT) {
                             float v[16];
                             tc_load16(d + c + group * 16, v);
@@ -546,8 +546,8 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                             for (int k = 0; k < 16; ++k) st_shared(buffer + (uint32_t)((group * 16 + k) * LG_M + quad * 32 + lane) * 4, v[k]);
                         }
                         finish_sync();
-                        return true;
-                    }, [&](int q, int l, auto &v) { ld_shared(buffer + (uint32_t)((q & (CT - 1)) * LG_M + l) * 4, v); });
+                        return buffer;
+                    });
                     if (!ok) break;
                 }
             }
@@ -562,19 +562,23 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
         cg::this_cluster().sync();
         if (warp >= 2 && !s_fail && first < n_tiles) {
             const LgTile t = lg_tile(a, first);
-            constexpr int CT = NT / C < 32 ? NT / C : 32;
-            const int64_t t0 = (int64_t)t.n * NT, end = t0 + NT < a.tokens ? t0 + NT : a.tokens;
-            lg_out<FORM, CT>(a, t0 + rank, C, end, (int64_t)t.m * OUT, tid - 64, [](int) { return true; }, [&](int q, int l, auto &v) {
-                constexpr int V = sizeof(v) / sizeof(float);
-                float part[C][V];
+            constexpr int CT = NT / C < lg_tokens(NT) ? NT / C : lg_tokens(NT);
+            const int64_t t0 = (int64_t)t.n * NT, end = t0 + NT < a.tokens ? t0 + NT : a.tokens, col0 = (int64_t)t.m * OUT;
+            const int e = tid - 64;
+            lg_out<FORM, CT>(a, t0 + rank, C, end, col0, e, [&](int c) -> uint32_t {
+                finish_sync();                                         // (everybody has read the tokens before)
+                for (int i = e; i < CT * LG_M / 4; i += LG_FINISH * 32) {
+                    const int q = i / (LG_M / 4), l = i % (LG_M / 4) * 4;
+                    float4 part[C];
 #pragma unroll
-                for (int r = 0; r < C; ++r) ld_cluster(cluster_addr(stages, r) + (uint32_t)((rank + q * C) * LG_M + l) * 4, part[r]);
+                    for (int r = 0; r < C; ++r) part[r] = ld_cluster(cluster_addr(stages, r) + (uint32_t)((rank + (c + q) * C) * LG_M + l) * 4);
+                    float4 v = part[0];
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    v[j] = part[0][j];
-#pragma unroll
-                    for (int r = 1; r < C; ++r) v[j] += part[r][j];
+                    for (int r = 1; r < C; ++r) { v.x += part[r].x; v.y += part[r].y; v.z += part[r].z; v.w += part[r].w; }
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(exchange + (uint32_t)(q * LG_M + l) * 4), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
                 }
+                finish_sync();
+                return exchange;
             });
         }
         __syncwarp();
