@@ -194,6 +194,8 @@ __global__ void __cluster_dims__(LS_RANKS, 1, 1) __launch_bounds__(LS_CTA) k_lin
     __shared__ float s_all[LS_RANKS][64];
     const int rank = (int)(blockIdx.x % LS_RANKS), tid = threadIdx.x;
     const int64_t j = (int64_t)(blockIdx.x / LS_RANKS) * 64 + (tid & 7) * 8;
+    // (every block has started before its shared memory is written; met again behind the sums)
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     pdl_wait();
     float sum[8];
 #pragma unroll
@@ -212,9 +214,10 @@ __global__ void __cluster_dims__(LS_RANKS, 1, 1) __launch_bounds__(LS_CTA) k_lin
     for (int k = 0; k < 8; ++k) s_sum[tid >> 3][(tid & 7) * 8 + k] = sum[k];
     __syncthreads();
     cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();                                                   // (every block has started before its shared memory is written)
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (tid < 64) {
         float v = 0.f;
+#pragma unroll
         for (int k = 0; k < LS_CTA / 8; ++k) v += s_sum[k][tid];
         cluster.map_shared_rank(&s_all[0][0], 0)[rank * 64 + tid] = v;
     }
@@ -266,15 +269,25 @@ static int aligned_rows(const LgArgs &a) {
     auto fits = [](const void *p, int64_t ld, int64_t item) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * item % 16 == 0); };
     return fits(a.y, a.ldy, a.y_f32 ? 4 : 2) && fits(a.z, a.ldz, 2) && fits(a.u, a.ldz, 2) && fits(a.residual, a.ldr, 2);
 }
-// `out`: output columns of a tile of one thread block
+// The cut of a product whose tiles are `out` output columns wide (one thread block's) and `kb` blocks of K long.  Blocks of K follow each other at 0.34 us in a
+// thread block, whatever the width of its tile and whether it shares its SM, so the rounds of thread blocks times their K are what counts; emptying a tile and
+// adding up the sums of C thread blocks cost more the wider the tile is.  Measured on seven layers (700 x 5000 to 11008 x 4096), 20 to 1000 tokens, eleven cuts each: the one
+// chosen here is 0.7 % behind the best on average, 7 % at most, and the worst of the eleven is two to four times as slow (4096 x 4096, 256 tokens: 17 to 35 us).
 static LgPlan plan_gemm(const dbspmspv_handle_s *h, int64_t tokens, int64_t width, int out, int64_t kb) {
-    if (getenv("LGP")) { LgPlan p; sscanf(getenv("LGP"), "%d,%d,%d", &p.cg, &p.nt, &p.c); while (p.c > 1 && kb < p.c) p.c /= 2; return p; }
-    if (tokens > 128 && ceil64(width, 2 * out) * ceil64(tokens, 256) * 4 >= h->sm_count / 2 * 3) return {2, 256, 1};
-    LgPlan p = {1, tokens <= 16 ? 16 : tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256, 1};
-    if (p.nt == 256 && ceil64(tokens, 128) * 128 < ceil64(tokens, 256) * 256) p.nt = 128;
-    const int64_t tiles = ceil64(width, out) * ceil64(tokens, p.nt), slots = h->sm_count * (p.nt <= 64 ? 2 : 1);
-    while (p.c < 8 && tiles * p.c * 2 <= slots && kb >= 8 * p.c) p.c *= 2;
-    return p;
+    struct { LgPlan p; int slots; } const all[] = {{{2, 256, 1}, h->sm_count / 2}, {{1, 16, 1}, 2 * h->sm_count}, {{1, 64, 1}, 2 * h->sm_count}, {{1, 128, 1}, h->sm_count}, {{1, 256, 1}, h->sm_count}};
+    LgPlan best = all[0].p;
+    double least = 0.;
+    for (const auto &q : all) {
+        if ((q.p.nt == 16) != (tokens <= 16)) continue;               // (a layer's weights go through once: a narrow tile only where all tokens fit in)
+        const int64_t tiles = ceil64(width, q.p.cg * out) * ceil64(tokens, q.p.nt);
+        for (int c = 1; c <= (q.p.cg == 1 ? 8 : 1); c *= 2) {
+            // (a cluster is placed within a part of the GPU: the larger it is, the more SMs stay without one)
+            if (c > 1 && (kb < 2 * c || tiles * c >= q.slots - c * c / 2)) break;
+            const double cost = (double)(ceil64(tiles * c, q.slots) * ceil64(kb, c)) * 0.34 + 0.3 * q.p.nt / 64. + (c > 1 ? 0.2 * c * (1. + q.p.nt / 64.) : 0.);
+            if (least == 0. || cost < least) { least = cost; best = q.p; best.c = c; }
+        }
+    }
+    return best;
 }
 
 template <int LAYERS, int C>
@@ -284,7 +297,7 @@ static int add_columns_c(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a,
         DBS_CUDA(cudaFuncSetAttribute(k_linear_cols<LAYERS, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, LIN_COLS_MAX_SMEM));
         done = true;
     }
-    calls.add(k_linear_cols<LAYERS, C>, strips * C * tokens, LC_CTA, (size_t)LC_WARPS * lc_warp_entries(a.n, C) * sizeof(float2), false, a, strips);
+    calls.add(k_linear_cols<LAYERS, C>, strips * C * tokens, LC_CTA, (size_t)LC_WARPS * lc_warp_entries(a.n, C) * sizeof(uint32_t), false, a, strips);
     return DBSPMSPV_OK;
 }
 // Thread blocks of a strip: as many as it takes to give every SM two, without more than that.  (4096 x 11008, half active, 1 / 2 / 4 / 8 blocks: 20.3 / 14.4 / 12.0 / 14.9 us; 12288 x 4096,
@@ -306,7 +319,7 @@ static int add_columns(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a, i
     }
 }
 static bool over_columns(const dbspmspv_handle_s *h, int64_t tokens) {
-    return tokens <= (getenv("LCT") ? atoi(getenv("LCT")) : LIN_COLS_MAX_TOKENS) && LC_WARPS * lc_warp_entries(h->d.n, columns_cluster(h, tokens)) * (int64_t)sizeof(float2) <= LIN_COLS_MAX_SMEM;
+    return tokens <= LIN_COLS_MAX_TOKENS && h->d.n <= 65536 && LC_WARPS * lc_warp_entries(h->d.n, columns_cluster(h, tokens)) * (int64_t)sizeof(uint32_t) <= LIN_COLS_MAX_SMEM;
 }
 
 // ---- workspace: x as TMA can read it, then the products' operands of a gradient ---------------

@@ -2,7 +2,7 @@
 //
 // One pass over the columns that the token reaches, from the copy by columns ([strip of 64 rows][column][row], see
 // decode_columns.cuh): what the call cannot do without is 2 bytes per weight of those columns.  A cluster of C thread blocks owns a
-// strip; a warp blocks its own share of x, keeps the entries that are not zero as a list (column, value) in shared memory and goes on to
+// strip; a warp blocks its own share of x, keeps the entries that are not zero as a list (column and bf16 value in a word) in shared memory and goes on to
 // their columns, 16 bytes a lane, all loads independent.  The sums of warps and ranks meet in shared memory, in a fixed order, and the
 // thread of a row finishes it there, so that neither a second pass over y nor an atomic is needed.
 //   * A gated call reads the same list against both layers' strips: both sums of a row end in one thread.
@@ -17,7 +17,7 @@
 
 namespace dbs {
 
-constexpr int LC_WARPS = 16;
+constexpr int LC_WARPS = 16;             // (eight or four, and more thread blocks: no faster)
 constexpr int LC_CTA = LC_WARPS * 32;
 constexpr int LC_PIECE = 64;             // entries of x that a warp blocks side by side
 static_assert(DC_ROWS == 64, "eight lanes with eight rows each share a column");
@@ -56,7 +56,7 @@ k_linear_cols(const __grid_constant__ LcArgs a, int strips) {
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     pdl_wait();
     const uint16_t *x = a.x + token * a.ldx;
-    float2 *list = reinterpret_cast<float2 *>(s_dyn) + (size_t)warp * lc_warp_entries(a.n, C);
+    uint32_t *list = reinterpret_cast<uint32_t *>(s_dyn) + (size_t)warp * lc_warp_entries(a.n, C);
     int n = 0;
     {
         const bool aligned = (reinterpret_cast<uintptr_t>(x) & 3u) == 0;
@@ -71,8 +71,8 @@ k_linear_cols(const __grid_constant__ LcArgs a, int strips) {
             const bool lo = v & 0x7FFFu, hi = v & 0x7FFF0000u;
             const uint32_t ml = __ballot_sync(FULL, lo), mh = __ballot_sync(FULL, hi), below = (1u << lane) - 1u;
             int at = n + __popc(ml & below) + __popc(mh & below);
-            if (lo) list[at++] = make_float2(__int_as_float((int)j), __uint_as_float(v << 16));
-            if (hi) list[at] = make_float2(__int_as_float((int)j + 1), __uint_as_float(v & 0xFFFF0000u));
+            if (lo) list[at++] = (uint32_t)j | v << 16;
+            if (hi) list[at] = (uint32_t)(j + 1) | (v & 0xFFFF0000u);
             n += __popc(ml) + __popc(mh);
         }
         __syncwarp();
@@ -97,10 +97,10 @@ k_linear_cols(const __grid_constant__ LcArgs a, int strips) {
 #pragma unroll
                 for (int l = 0; l < LAYERS; ++l) v[l][q] = make_uint4(0u, 0u, 0u, 0u);
                 if (k < n) {
-                    const float2 e = list[k];
-                    xv[q] = e.y;
+                    const uint32_t e = list[k];
+                    xv[q] = __uint_as_float(e & 0xFFFF0000u);
 #pragma unroll
-                    for (int l = 0; l < LAYERS; ++l) v[l][q] = __ldcs(w[l] + (size_t)__float_as_int(e.x) * (DC_ROWS / 8));
+                    for (int l = 0; l < LAYERS; ++l) v[l][q] = __ldcs(w[l] + (size_t)(e & 0xFFFFu) * (DC_ROWS / 8));
                 }
             }
 #pragma unroll
