@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(LS_CTA) k_linear_slopes(const __grid_constant_
 // With the bias' gradient: a cluster of eight thread blocks takes 64 columns, each an eighth of the tokens, its 32 row lanes in turn; the sums meet in a fixed order.
 __global__ void __cluster_dims__(LS_RANKS, 1, 1) __launch_bounds__(LS_CTA) k_linear_bias(const __grid_constant__ LsArgs a) {
     namespace cg = cooperative_groups;
-    __shared__ float s_sum[LS_CTA / 8][64];
+    __shared__ float s_sum[LS_CTA / 32][64];
     __shared__ float s_all[LS_RANKS][64];
     const int rank = (int)(blockIdx.x % LS_RANKS), tid = threadIdx.x;
     const int64_t j = (int64_t)(blockIdx.x / LS_RANKS) * 64 + (tid & 7) * 8;
@@ -211,14 +211,18 @@ __global__ void __cluster_dims__(LS_RANKS, 1, 1) __launch_bounds__(LS_CTA) k_lin
         for (int k = 0; k < 8; ++k) sum[k] += dy[k];
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s_sum[tid >> 3][(tid & 7) * 8 + k] = sum[k];
+    for (int k = 0; k < 8; ++k) {
+        sum[k] += __shfl_xor_sync(FULL, sum[k], 8);
+        sum[k] += __shfl_xor_sync(FULL, sum[k], 16);
+        if ((tid & 31) < 8) s_sum[tid >> 5][(tid & 7) * 8 + k] = sum[k];
+    }
     __syncthreads();
     cg::cluster_group cluster = cg::this_cluster();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (tid < 64) {
         float v = 0.f;
 #pragma unroll
-        for (int k = 0; k < LS_CTA / 8; ++k) v += s_sum[k][tid];
+        for (int k = 0; k < LS_CTA / 32; ++k) v += s_sum[k][tid];
         cluster.map_shared_rank(&s_all[0][0], 0)[rank * 64 + tid] = v;
     }
     cluster.sync();

@@ -204,6 +204,19 @@ __device__ __forceinline__ bool lg_wait(uint64_t *bar, uint32_t parity, volatile
     return false;
 }
 
+// The same for the two threads that everything waits for: they look again at once.
+__device__ __forceinline__ bool lg_spin(uint64_t *bar, uint32_t parity, volatile int *fail, int32_t *status) {
+    for (int i = 0; i < (1 << 26); ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+        if (ok) return true;
+        if ((i & 255) == 255 && *fail) return false;
+    }
+    *fail = 1;
+    *status = DBSPMSPV_ERR_TIMEOUT;
+    return false;
+}
+
 // ---- what becomes of neighbouring sums of one token --------------------------------------
 __device__ __forceinline__ void lg_act(float (&v)[8], int act) {
     if (act == DBSPMSPV_ACT_NONE) return;
@@ -411,7 +424,7 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                 const int m0 = (t.m * CG + half) * OUT, n0 = t.n * NT + half * NB;    // (gated: 64 rows of both layers)
                 int layer = kb0 >= a.k_blocks, k = kb0 - layer * a.k_blocks;
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!lg_wait(&s_empty[s], phase, &s_fail, a.status)) { ok = false; break; }
+                    if (!lg_spin(&s_empty[s], phase, &s_fail, a.status)) { ok = false; break; }
                     const uint32_t pa = stages + s * STAGE_BYTES, pb = pa + LG_A_BYTES;
                     // (both blocks' copies are counted by the first one's barrier)
                     const uint32_t bar = CG > 1 ? cluster_addr(smem_addr(&s_full[s]), 0) : smem_addr(&s_full[s]);
@@ -452,10 +465,10 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
             bool ok = true;
             for (int i = first; i < n_tiles && ok; i += step, ++n) {
                 const uint32_t d = tmem + (uint32_t)(n & 1) * NT;
-                if (n >= 2 && !lg_wait(&s_free[n & 1], (uint32_t)((n / 2 - 1) & 1), &s_fail, a.status)) { ok = false; break; }
+                if (n >= 2 && !lg_spin(&s_free[n & 1], (uint32_t)((n / 2 - 1) & 1), &s_fail, a.status)) { ok = false; break; }
                 tc_fence_after();
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!lg_wait(&s_full[s], phase, &s_fail, a.status)) { ok = false; break; }
+                    if (!lg_spin(&s_full[s], phase, &s_fail, a.status)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t pa = low_a + s * (STAGE_BYTES >> 4), pb = low_b + s * (STAGE_BYTES >> 4);
 #pragma unroll
