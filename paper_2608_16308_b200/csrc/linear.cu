@@ -472,6 +472,7 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
             if (!b.dw[l]) continue;
             if ((s = encode_rows(&maps.b[a.products], dz[l], b.tokens, d.m, ldd, LG_K)) != DBSPMSPV_OK) return s;
             a.dw[a.products] = b.dw[l];
+            a.stored[a.products] = (uint32_t)(l ? up : h)->nnz;
             a.index[a.products++] = (l ? up : h)->lin_index;
         }
         LgPlan p = {2, 256, 1};

@@ -72,6 +72,7 @@ struct LgArgs {
     int64_t ldz;
     int aligned;                    // every row of y, z, u and the residual begins on 16 bytes
     uint16_t *dw[2];
+    uint32_t stored[2];             // their weights (for the range-checked build)
     const uint2 *index[2];          // [word of 32 columns][row]: stored columns, place of the first of them
     int index_words;
     int32_t *status;
@@ -370,6 +371,14 @@ __device__ __forceinline__ LgTile lg_tile(const LgArgs &a, int i) {
     return t;
 }
 
+// Range-checked build: a place of the index that lies behind the last weight is recorded and skipped.
+__device__ __forceinline__ bool lg_in_range(const LgArgs &a, int product, uint32_t at) {
+#ifdef DBS_BOUNDS_CHECK
+    if (at >= a.stored[product]) { *a.status = DBSPMSPV_ERR_INTERNAL; return false; }
+#endif
+    return true;
+}
+
 // CG thread blocks of a cluster per tile of CG * 128 x NT; C of them (CG = 1) share its K.
 template <int FORM, int CG, int NT, int C>
 __global__ void __cluster_dims__(CG * C, 1, 1) __launch_bounds__(lg_threads(FORM == LG_DW), NT <= 64 ? 2 : 1)
@@ -523,8 +532,8 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const uint32_t w = lin_pair(v[2 * k], v[2 * k + 1]);
-                        store_if((bits[2 * k] >> lane) & 1u, dw + at[2 * k], w & 0xFFFFu);
-                        store_if((bits[2 * k + 1] >> lane) & 1u, dw + at[2 * k + 1], w >> 16);
+                        store_if(((bits[2 * k] >> lane) & 1u) && lg_in_range(a, t.product, at[2 * k]), dw + at[2 * k], w & 0xFFFFu);
+                        store_if(((bits[2 * k + 1] >> lane) & 1u) && lg_in_range(a, t.product, at[2 * k + 1]), dw + at[2 * k + 1], w >> 16);
                     }
                 }
             } else {
