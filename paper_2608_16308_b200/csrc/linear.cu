@@ -123,23 +123,33 @@ __device__ __forceinline__ void lin_store8(uint16_t *row, int64_t j, const float
     *reinterpret_cast<uint4 *>(row + j) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// x whose rows TMA cannot address, with rows that it can
-__global__ void k_linear_pack(const uint16_t *x, int64_t ldx, int64_t tokens, int64_t n, uint16_t *out, int64_t ldo) {
-    pdl_wait();
-    const int64_t per = ldo / 8, total = tokens * per;
-    for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+// x whose rows TMA cannot address, with rows that it can, by thread blocks `block` of `blocks`
+struct LinPack {
+    const uint16_t *x;
+    int64_t ldx, tokens, n;
+    uint16_t *out;
+    int64_t ldo;
+};
+__device__ __forceinline__ void lin_pack(const LinPack &a, int64_t block, int64_t blocks) {
+    const int64_t per = a.ldo / 8, total = a.tokens * per;
+    for (int64_t i = block * blockDim.x + threadIdx.x; i < total; i += blocks * blockDim.x) {
         const int64_t t = i / per, j = (i - t * per) * 8;
         float v[8];
-        lin_load8(x + t * ldx, j, n, v);
-        lin_store8(out + t * ldo, j, v);
+        lin_load8(a.x + t * a.ldx, j, a.n, v);
+        lin_store8(a.out + t * a.ldo, j, v);
     }
+}
+__global__ void k_linear_pack(const __grid_constant__ LinPack a) {
+    pdl_wait();
+    lin_pack(a, blockIdx.x, gridDim.x);
     pdl_trigger();
 }
 
 // What the products of a gradient take: dz = dy act'(z), or dg = dy u act'(g) and du = dy act(g), rounded to bf16 (the tensor cores' operands; the
 // roundings are independent, so a sum over rows or tokens is off by about 2^-9 of its own size, as much as its own rounding to bf16), and the bias' gradient
-// from the unrounded ones.  Bound by HBM: 2 bytes for each of dy, z, u, dz.
-constexpr int LS_CTA = 256, LS_RANKS = 8;
+// from the unrounded ones.  Bound by HBM: 2 bytes for each of dy, z, u, dz.  The thread blocks from pack_from on pack x meanwhile.
+constexpr int LS_CTA = 256;
+constexpr int LS_COLS = 32;              // columns of a thread block that adds up the bias' gradient: four threads, 64 tokens side by side
 struct LsArgs {
     const uint16_t *dy, *z, *u;
     int64_t lddy, ldz, tokens, m;
@@ -147,7 +157,14 @@ struct LsArgs {
     uint16_t *d0, *d1;              // null: not wanted
     int64_t ldd;
     float *dbias;
+    int aligned;                    // every row of dy, z and u begins on 16 bytes
+    int pack_from;
+    LinPack pack;
 };
+__device__ __forceinline__ void ls_unpack(const uint32_t (&w)[4], float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = lg_half(w, k);
+}
 // eight neighbours of one token: dy becomes du (gated) or dz; d: dg
 template <bool GATED>
 __device__ __forceinline__ void ls_eight(const LsArgs &a, float (&dy)[8], const float (&z)[8], const float (&u)[8], float (&d)[8]) {
@@ -174,62 +191,93 @@ __device__ __forceinline__ void ls_eight(const LsArgs &a, float (&dy)[8], const 
 template <bool GATED>
 __global__ void __launch_bounds__(LS_CTA) k_linear_slopes(const __grid_constant__ LsArgs a) {
     pdl_wait();
-    const int64_t per = (a.m + 7) / 8, total = a.tokens * per;
-    for (int64_t i = blockIdx.x * (int64_t)LS_CTA + threadIdx.x; i < total; i += (int64_t)gridDim.x * LS_CTA) {
-        const int64_t t = i / per, j = (i - t * per) * 8;
-        float dy[8], z[8] = {}, u[8] = {}, d[8];
-        lin_load8(a.dy + t * a.lddy, j, a.m, dy);
-        if (a.z) lin_load8(a.z + t * a.ldz, j, a.m, z);
-        if (GATED) lin_load8(a.u + t * a.ldz, j, a.m, u);
-        if (GATED || a.z) ls_eight<GATED>(a, dy, z, u, d);
-        if (GATED) lin_store8(a.d0 + t * a.ldd, j, d);
-        lin_store8((GATED ? a.d1 : a.d0) + t * a.ldd, j, dy);
+    if ((int)blockIdx.x >= a.pack_from) {
+        lin_pack(a.pack, (int)blockIdx.x - a.pack_from, (int)gridDim.x - a.pack_from);
+    } else {
+        // (two at a time: what is loaded for both is under way before either is worked on)
+        const int64_t per = (a.m + 7) / 8, total = a.tokens * per, step = (int64_t)a.pack_from * LS_CTA;
+        for (int64_t i0 = blockIdx.x * (int64_t)LS_CTA + threadIdx.x; i0 < total; i0 += 2 * step) {
+            uint32_t wy[2][4], wz[2][4] = {}, wu[2][4] = {};
+            int64_t t[2], j[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int64_t i = i0 + q * step;
+                t[q] = i / per;
+                j[q] = (i - t[q] * per) * 8;
+                if (i < total) {
+                    const int count = a.m - j[q] < 8 ? (int)(a.m - j[q]) : 8;
+                    lg_get(a.dy + t[q] * a.lddy + j[q], a.aligned, count, wy[q]);
+                    if (GATED || a.z) lg_get(a.z + t[q] * a.ldz + j[q], a.aligned, count, wz[q]);
+                    if (GATED) lg_get(a.u + t[q] * a.ldz + j[q], a.aligned, count, wu[q]);
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                if (i0 + q * step >= total) break;
+                float dy[8], z[8], u[8], d[8];
+                ls_unpack(wy[q], dy);
+                ls_unpack(wz[q], z);
+                ls_unpack(wu[q], u);
+                if (GATED || a.z) ls_eight<GATED>(a, dy, z, u, d);
+                if (GATED) lin_store8(a.d0 + t[q] * a.ldd, j[q], d);
+                lin_store8((GATED ? a.d1 : a.d0) + t[q] * a.ldd, j[q], dy);
+            }
+        }
     }
     pdl_trigger();
 }
-// With the bias' gradient: a cluster of eight thread blocks takes 64 columns, each an eighth of the tokens, its 32 row lanes in turn; the sums meet in a fixed order.
-__global__ void __cluster_dims__(LS_RANKS, 1, 1) __launch_bounds__(LS_CTA) k_linear_bias(const __grid_constant__ LsArgs a) {
-    namespace cg = cooperative_groups;
-    __shared__ float s_sum[LS_CTA / 32][64];
-    __shared__ float s_all[LS_RANKS][64];
-    const int rank = (int)(blockIdx.x % LS_RANKS), tid = threadIdx.x;
-    const int64_t j = (int64_t)(blockIdx.x / LS_RANKS) * 64 + (tid & 7) * 8;
-    // (every block has started before its shared memory is written; met again behind the sums)
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+// With the bias' gradient: a thread block takes LS_COLS columns of all tokens; its sums meet in a fixed order.
+__global__ void __launch_bounds__(LS_CTA) k_linear_bias(const __grid_constant__ LsArgs a) {
+    constexpr int G = LS_COLS / 8, LANES = LS_CTA / G;
+    __shared__ float s_sum[LS_CTA / 32][LS_COLS];
+    const int tid = threadIdx.x;
     pdl_wait();
+    if ((int)blockIdx.x >= a.pack_from) {
+        lin_pack(a.pack, (int)blockIdx.x - a.pack_from, (int)gridDim.x - a.pack_from);
+        pdl_trigger();
+        return;
+    }
+    const int64_t j = (int64_t)blockIdx.x * LS_COLS + (tid % G) * 8;
     float sum[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[k] = 0.f;
-    const int64_t t1 = a.tokens * (rank + 1) / LS_RANKS;
-#pragma unroll 2
-    for (int64_t t = a.tokens * rank / LS_RANKS + (tid >> 3); t < t1 && j < a.m; t += LS_CTA / 8) {
-        float dy[8], z[8] = {}, none[8];
-        lin_load8(a.dy + t * a.lddy, j, a.m, dy);
-        if (a.z) { lin_load8(a.z + t * a.ldz, j, a.m, z); ls_eight<false>(a, dy, z, z, none); }
-        if (a.d0) lin_store8(a.d0 + t * a.ldd, j, dy);
+    const int count = a.m - j < 8 ? (int)(a.m - j) : 8;
+    for (int64_t t0 = tid / G; t0 < a.tokens && count > 0; t0 += 4 * LANES) {
+        uint32_t wy[4][4] = {}, wz[4][4] = {};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum[k] += dy[k];
+        for (int q = 0; q < 4; ++q) {
+            const int64_t t = t0 + q * LANES;
+            if (t < a.tokens) {
+                lg_get(a.dy + t * a.lddy + j, a.aligned, count, wy[q]);
+                if (a.z) lg_get(a.z + t * a.ldz + j, a.aligned, count, wz[q]);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t t = t0 + q * LANES;
+            if (t >= a.tokens) break;
+            float dy[8], z[8], none[8];
+            ls_unpack(wy[q], dy);
+            ls_unpack(wz[q], z);
+            if (a.z) ls_eight<false>(a, dy, z, z, none);
+            if (a.d0) lin_store8(a.d0 + t * a.ldd, j, dy);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += dy[k];
+        }
     }
+    __syncwarp();
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        sum[k] += __shfl_xor_sync(FULL, sum[k], 8);
-        sum[k] += __shfl_xor_sync(FULL, sum[k], 16);
-        if ((tid & 31) < 8) s_sum[tid >> 5][(tid & 7) * 8 + k] = sum[k];
+#pragma unroll
+        for (int o = G; o < 32; o <<= 1) sum[k] += __shfl_xor_sync(FULL, sum[k], o);
+        if ((tid & 31) < G) s_sum[tid >> 5][(tid % G) * 8 + k] = sum[k];
     }
     __syncthreads();
-    cg::cluster_group cluster = cg::this_cluster();
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (tid < 64) {
+    const int64_t col = (int64_t)blockIdx.x * LS_COLS + tid;
+    if (tid < LS_COLS && col < a.m) {
         float v = 0.f;
 #pragma unroll
         for (int k = 0; k < LS_CTA / 32; ++k) v += s_sum[k][tid];
-        cluster.map_shared_rank(&s_all[0][0], 0)[rank * 64 + tid] = v;
-    }
-    cluster.sync();
-    const int64_t col = (int64_t)(blockIdx.x / LS_RANKS) * 64 + tid;
-    if (rank == 0 && tid < 64 && col < a.m) {
-        float v = 0.f;
-        for (int k = 0; k < LS_RANKS; ++k) v += s_all[k][tid];
         a.dbias[col] = v;
     }
     pdl_trigger();
@@ -346,18 +394,22 @@ static int64_t workspace_bytes(const dbspmspv_handle_s *h, int layers, int64_t t
     return b;
 }
 
-// x as the tensor maps can address it: as it lies, or packed into the workspace
-static int usable_x(CallList &calls, const dbspmspv_handle_s *h, const uint16_t **x, int64_t *ldx, int tokens, LinRoom &room) {
+// x as the tensor maps can address it: as it lies (p.out null), or packed into the workspace by a kernel to come
+static int usable_x(const dbspmspv_handle_s *h, const uint16_t **x, int64_t *ldx, int tokens, LinRoom &room, LinPack *p) {
+    *p = LinPack{};
     if (tma_rows(*x, *ldx)) return DBSPMSPV_OK;
     const int64_t n = h->d.n, ld = round_up(n, 8);
-    uint16_t *p = room.take(tokens, ld);
-    if (!p) return DBSPMSPV_ERR_INVALID_ARG;
-    int64_t g = (tokens * (ld / 8) + 255) / 256;
-    if (g > 16 * h->sm_count) g = 16 * h->sm_count;
-    calls.add(k_linear_pack, (int)g, 256, 0, calls.n > 0, *x, *ldx, (int64_t)tokens, n, p, ld);
-    *x = p;
+    uint16_t *out = room.take(tokens, ld);
+    if (!out) return DBSPMSPV_ERR_INVALID_ARG;
+    *p = LinPack{*x, *ldx, tokens, n, out, ld};
+    *x = out;
     *ldx = ld;
     return DBSPMSPV_OK;
+}
+static int pack_blocks(const dbspmspv_handle_s *h, const LinPack &p) {
+    if (!p.out) return 0;
+    const int64_t g = (p.tokens * (p.ldo / 8) + LS_CTA - 1) / LS_CTA, most = 16 * h->sm_count;
+    return (int)(g < most ? g : most);
 }
 
 static bool has_linear(const dbspmspv_handle_s *h) { return h->d.dtype == DBSPMSPV_BF16 && h->lin_ready; }
@@ -390,8 +442,9 @@ static int forward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinForward f, Li
         a.z = f.z; a.u = f.u; a.ldz = f.ldz;
         s = up ? add_columns<2>(h, calls, a, f.tokens) : add_columns<1>(h, calls, a, f.tokens);
     } else {
-        s = usable_x(calls, h, &f.x, &f.ldx, f.tokens, room);
-        if (s != DBSPMSPV_OK) return s;
+        LinPack pack;
+        if ((s = usable_x(h, &f.x, &f.ldx, f.tokens, room, &pack)) != DBSPMSPV_OK) return s;
+        if (pack.out) calls.add(k_linear_pack, pack_blocks(h, pack), LS_CTA, 0, false, pack);
         const int out = up ? LG_M / 2 : LG_M;
         const int64_t kb = ceil64(d.n, LG_K);
         const LgPlan p = plan_gemm(h, f.tokens, d.m, out, kb);
@@ -428,7 +481,8 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
     int s = DBSPMSPV_OK;
     const bool want_w = b.dw[0] || b.dw[1], products = b.dx || want_w;
     const int layers = up ? 2 : 1;
-    if (want_w && (s = usable_x(calls, h, &b.x, &b.ldx, b.tokens, room)) != DBSPMSPV_OK) return s;
+    LinPack pack = {};
+    if (want_w && (s = usable_x(h, &b.x, &b.ldx, b.tokens, room, &pack)) != DBSPMSPV_OK) return s;
     const uint16_t *dz[2] = {b.dy, nullptr};
     int64_t ldd = b.lddy;
     const bool as_it_is = !up && b.act == DBSPMSPV_ACT_NONE && tma_rows(b.dy, b.lddy);
@@ -443,12 +497,13 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
             if (up) dz[1] = a.d1 = room.take(b.tokens, ldd);
             if (!a.d0 || (up && !a.d1)) return DBSPMSPV_ERR_INVALID_ARG;
         }
-        if (b.dbias) {
-            calls.add(k_linear_bias, (int)(ceil64(d.m, 64) * LS_RANKS), LS_CTA, 0, calls.n > 0, a);
-        } else {
-            const int64_t g = ceil64(b.tokens * ceil64(d.m, 8), LS_CTA), most = 16 * h->sm_count;
-            calls.add(up ? k_linear_slopes<true> : k_linear_slopes<false>, (int)(g < most ? g : most), LS_CTA, 0, calls.n > 0, a);
-        }
+        const int64_t g = b.dbias ? ceil64(d.m, LS_COLS) : ceil64(b.tokens * ceil64(d.m, 8), LS_CTA), most = b.dbias ? g : 8 * h->sm_count;
+        a.pack_from = (int)(g < most ? g : most);
+        a.pack = pack;
+        a.aligned = tma_rows(b.dy, b.lddy) && (!a.z || tma_rows(a.z, b.ldz)) && (!up || tma_rows(b.u, b.ldz));
+        calls.add(b.dbias ? k_linear_bias : up ? k_linear_slopes<true> : k_linear_slopes<false>, a.pack_from + pack_blocks(h, pack), LS_CTA, 0, false, a);
+    } else if (pack.out) {
+        calls.add(k_linear_pack, pack_blocks(h, pack), LS_CTA, 0, false, pack);
     }
     LgArgs a = {};
     a.status = &d.ws.ctr->status;
