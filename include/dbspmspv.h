@@ -344,8 +344,7 @@ int dbspmspv_decode(dbspmspv_handle_t h, const void *x, float *y, dbspmspv_strea
  *              a CSR matrix without duplicates whose columns ascend -- or NULL
  *   dbias      out: m fp32, or NULL
  *   workspace  device memory of at least the bytes that dbspmspv_linear_workspace names, on 16 bytes.  Forward calls need it only for
- *              x whose rows do not begin on 16 bytes (x and ldx both count) and more tokens than the kernel over active
- *              columns takes.  Two calls that may overlap need two workspaces; a captured call keeps its own.
+ *              x whose rows do not begin on 16 bytes (x and ldx both count) and more than two tokens (small layers: 16).  Two calls that may overlap need two workspaces; a captured call keeps its own.
  *
  * Sums are fp32.  y, z, g, u, dx and dw are rounded to bf16 once, to nearest even; dz, dg and du are rounded to bf16 before they
  * enter the products.  Results do not depend on the order in which thread blocks run.  residual may be y itself (same address, same

@@ -14,6 +14,7 @@ namespace dbs {
 constexpr int LIN_COLS_MAX_SMEM = 200 * 1024;
 // Tokens that a call over active columns takes one by one, side by side in the grid; more go to the tensor cores.
 constexpr int LIN_COLS_MAX_TOKENS = 2;
+constexpr int64_t LIN_COLS_MAX_WEIGHTS = 16ll << 20;
 
 // ---- at create ------------------------------------------------------------------------------
 // Stored columns of a row, 32 to a word, from the copy by columns; a warp takes the 32 rows of half a strip.
@@ -370,8 +371,12 @@ static int add_columns(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a, i
         default: return add_columns_c<LAYERS, 8>(h, calls, a, strips, tokens);
     }
 }
-static bool over_columns(const dbspmspv_handle_s *h, int64_t tokens) {
-    return tokens <= LIN_COLS_MAX_TOKENS && h->d.n <= 65536 && LC_WARPS * lc_warp_entries(h->d.n, columns_cluster(h, tokens)) * (int64_t)sizeof(uint32_t) <= LIN_COLS_MAX_SMEM;
+// Whether a forward call goes over the columns: up to LIN_COLS_MAX_TOKENS tokens; and small layers whose x would have to be packed for the tensor cores (a kernel more), as long as the tokens'
+// passes over the weights are few bytes (1037 x 515, eight tokens: 5.8 against 8.5 us; 2751 x 1025, five: 6.0 / 8.9, six are past it; gated 1037 x 515, eight: 6.1 / 8.7,
+// but 1500 x 1500, three: 11.2 / 8.8).
+static bool over_columns(const dbspmspv_handle_s *h, int layers, int64_t tokens, bool packed) {
+    if (h->d.n > 65536 || LC_WARPS * lc_warp_entries(h->d.n, columns_cluster(h, tokens)) * (int64_t)sizeof(uint32_t) > LIN_COLS_MAX_SMEM) return false;
+    return tokens <= LIN_COLS_MAX_TOKENS || (packed && tokens <= 16 && tokens * layers * layers * h->d.m * h->d.n <= LIN_COLS_MAX_WEIGHTS);
 }
 
 // ---- workspace: x as TMA can read it, then the products' operands of a gradient ---------------
@@ -389,7 +394,7 @@ struct LinRoom {
 };
 static int64_t workspace_bytes(const dbspmspv_handle_s *h, int layers, int64_t tokens, bool backward) {
     int64_t b = 0;
-    if (backward || !over_columns(h, tokens)) b += round_up(tokens * round_up(h->d.n, 8) * 2, 256);
+    if (backward || !over_columns(h, layers, tokens, false)) b += round_up(tokens * round_up(h->d.n, 8) * 2, 256);
     if (backward) b += layers * round_up(tokens * round_up(h->d.m, 8) * 2, 256);
     return b;
 }
@@ -433,7 +438,7 @@ static int forward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinForward f, Li
     const Device &d = h->d;
     CallList calls;
     int s = DBSPMSPV_OK;
-    if (over_columns(h, f.tokens)) {
+    if (over_columns(h, up ? 2 : 1, f.tokens, !tma_rows(f.x, f.ldx))) {
         LcArgs a = {};
         a.x = f.x; a.ldx = f.ldx; a.n = d.n; a.m = d.m;
         a.w[0] = reinterpret_cast<const uint4 *>(h->lin_w);

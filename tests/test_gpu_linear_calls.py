@@ -119,14 +119,14 @@ def test_handles_that_do_not_serve():
 
 def test_refused_arguments():
     a, b, c = Layer(96, 72), Layer(96, 72), Layer(96, 80)
-    t = 5
+    t = 20
     x, y, z = Rows(t, 72, 8, values=normal((t, 72), 1)), Rows(t, 96), Rows(t, 96)
     ok = dict(h=a.h, x=x.start, ldx=x.ld, tokens=t, bias=None, act=0, residual=None, ldr=0, y=y.start, ldy=y.ld, y_f32=0, z=None, ldz=0, workspace=None, workspace_bytes=0)
     B.dbspmspv_linear(**ok)
     odd = torch.zeros(4096, dtype=torch.uint8, device=DEV)[1:]
     for change in (dict(x=None), dict(y=None), dict(tokens=-1), dict(act=4), dict(act=-1), dict(ldx=71), dict(ldy=95), dict(residual=z.start, ldr=95), dict(z=z.start, ldz=95),
                    dict(workspace_bytes=-1), dict(workspace=odd, workspace_bytes=1000), dict(y=odd), dict(y_f32=1, y=y.buf[1:]), dict(x=odd), dict(ldx=73),
-                   dict(ldx=73, workspace=odd[15:], workspace_bytes=5 * 72 * 2 - 1), dict(h=None)):
+                   dict(ldx=73, workspace=odd[15:], workspace_bytes=20 * 72 * 2 - 1), dict(h=None)):
         assert status(B.dbspmspv_linear, **{**ok, **change}) == B.ERR_INVALID_ARG, change
     g = dict(gate=a.h, up=b.h, x=x.start, ldx=x.ld, tokens=t, act=2, y=y.start, ldy=y.ld, g=None, u=None, ldgu=0, workspace=None, workspace_bytes=0)
     B.dbspmspv_gated(**g)
