@@ -161,7 +161,8 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(addr), "r"(rank));
     return far;
 }
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t far) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(far) : "memory"); }
+// (relaxed: what is handed on is the accumulator, whose loads have ended; a release would wait for the warp's stores to global memory)
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t far) { asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(far) : "memory"); }
 __device__ __forceinline__ float4 ld_cluster(uint32_t far) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(far) : "memory");
@@ -496,24 +497,31 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
         const int quad = warp & 3, group = (warp - 2) >> 2, e = tid - 64;
         const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
         int n = 0, turn = 0;
+        uint2 ahead[NT / FINISH / 8 + 1];                              // (gradient of W)
         for (int i = first; i < n_tiles; i += step, ++n) {
             const LgTile t = lg_tile(a, i);
             const uint32_t d = mine + (uint32_t)(n & 1) * NT;
             if constexpr (FORM == LG_DW) {
-                // (the index of a warp's rows is fetched into its own part of shared memory while the products run, and read from there two rows to a load that all lanes share)
+                // (the index of a warp's rows is fetched a tile ahead, the first one while the products run; it is read from the warp's own part of shared memory, two rows to a load
+                // that all lanes share)
                 constexpr int ROWS = NT / (FINISH / 4);
-                const int word = (t.m * CG + half) * (LG_M / 32) + quad;
-                const int64_t row0 = (int64_t)t.n * NT + group * ROWS;
-                const uint2 *index = a.index[t.product] + (int64_t)word * a.width;
                 uint16_t *dw = a.dw[t.product];
                 const uint32_t below = (1u << lane) - 1u, own = exchange + (uint32_t)(warp - 2) * (ROWS * 8);
+                uint2 x[ROWS / 32];
+                auto fetch = [&](const LgTile &t) {
+                    const int word = (t.m * CG + half) * (LG_M / 32) + quad;
+                    const int64_t row0 = (int64_t)t.n * NT + group * ROWS;
+                    const uint2 *index = a.index[t.product] + (int64_t)word * a.width;
+#pragma unroll
+                    for (int q = 0; q < ROWS / 32; ++q) ahead[q] = word < a.index_words && row0 + q * 32 + lane < a.width ? __ldg(index + row0 + q * 32 + lane) : make_uint2(0u, 0u);
+                };
+                if (n == 0) fetch(t);
+#pragma unroll
+                for (int q = 0; q < ROWS / 32; ++q) x[q] = ahead[q];
+                if (i + step < n_tiles) fetch(lg_tile(a, i + step));
                 __syncwarp();
 #pragma unroll
-                for (int q = 0; q < ROWS / 32; ++q) {
-                    uint2 x = make_uint2(0u, 0u);
-                    if (word < a.index_words && row0 + q * 32 + lane < a.width) x = __ldg(index + row0 + q * 32 + lane);
-                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(own + (uint32_t)(q * 32 + lane) * 8), "r"(x.x), "r"(x.y) : "memory");
-                }
+                for (int q = 0; q < ROWS / 32; ++q) asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(own + (uint32_t)(q * 32 + lane) * 8), "r"(x[q].x), "r"(x[q].y) : "memory");
                 __syncwarp();
                 if (!__all_sync(0xFFFFFFFFu, lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status))) break;
                 tc_fence_after();
