@@ -290,10 +290,10 @@ __device__ __forceinline__ void lg_put(uint16_t *row, int j, int width, const fl
 }
 
 // The tokens t0 + q * every below `end`, CT of them at a time, of the tile's output columns from col0 on, by thread e of LG_FINISH * 32, which keeps its eight columns.
-// exchange(c) brings the sums of the tokens q = c .. c + CT - 1 to shared memory, [token][lane], and says where (0: gave up).  The residual is fetched a
+// exchange(c) brings the sums of the tokens q = c .. c + CT - 1 to where read(q, lane, v) finds eight of them (false: gave up).  The residual is fetched a
 // round ahead, the first one in front of the wait for the sums (4096 x 11008, 2048 tokens, 155 -> 149 us).
-template <int FORM, int CT, bool ALIGNED, class Exchange>
-__device__ __forceinline__ void lg_out_as(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange) {
+template <int FORM, int CT, bool ALIGNED, class Exchange, class Read>
+__device__ __forceinline__ void lg_out_as(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange, Read read) {
     constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M, G = OUT / 8, PASS = LG_FINISH * 32 / G, ITEMS = CT > PASS ? CT / PASS : 1;
     static_assert(CT % PASS == 0 || CT < PASS, "");
     const int q0 = e / G, j = e % G, part = a.width - col0 < OUT ? (int)(a.width - col0) : OUT, count = part - 8 * j < 8 ? part - 8 * j : 8;
@@ -315,8 +315,7 @@ __device__ __forceinline__ void lg_out_as(const LgArgs &a, int64_t t0, int every
                 for (int i = 0; i < 4; ++i) res[k][i] = next[k][i];
             fetch(c + CT);
         }
-        const uint32_t sums = exchange(c);
-        if (!sums) return;
+        if (!exchange(c)) return;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int q = q0 < CT ? k * PASS + q0 : 0;
@@ -324,8 +323,8 @@ __device__ __forceinline__ void lg_out_as(const LgArgs &a, int64_t t0, int every
             const int width = q0 < CT && t < end ? part : 0;           // (a thread without a token stores nothing, but the other rows' threads may need it)
             if (ALIGNED && width <= 8 * j) continue;
             float v[8], u[8];
-            ld_shared(sums + (uint32_t)(q * LG_M + 8 * j) * 4, v);
-            if (FORM == LG_GATED) ld_shared(sums + (uint32_t)(q * LG_M + OUT + 8 * j) * 4, u);
+            read(c + q, 8 * j, v);
+            if (FORM == LG_GATED) read(c + q, OUT + 8 * j, u);
             if (FORM == LG_FORWARD && a.bias) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] += lg_half(bias, i);
@@ -356,10 +355,10 @@ __device__ __forceinline__ void lg_out_as(const LgArgs &a, int64_t t0, int every
     }
 }
 
-template <int FORM, int CT, class Exchange>
-__device__ __forceinline__ void lg_out(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange) {
-    if (a.aligned) lg_out_as<FORM, CT, true>(a, t0, every, end, col0, e, exchange);
-    else lg_out_as<FORM, CT, false>(a, t0, every, end, col0, e, exchange);
+template <int FORM, int CT, class Exchange, class Read>
+__device__ __forceinline__ void lg_out(const LgArgs &a, int64_t t0, int every, int64_t end, int64_t col0, int e, Exchange exchange, Read read) {
+    if (a.aligned) lg_out_as<FORM, CT, true>(a, t0, every, end, col0, e, exchange, read);
+    else lg_out_as<FORM, CT, false>(a, t0, every, end, col0, e, exchange, read);
 }
 
 // Tiles in the order they are taken: the token tiles of one weight tile side by side, so that its weights come from L2 after the first.
@@ -411,6 +410,7 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
         s_fail = 0;
         fence_barrier_init();
     }
+    if (warp == 0 && lane < 4) asm volatile("prefetch.tensormap [%0];" ::"l"(lane & 2 ? &maps.b[lane & 1] : &maps.a[lane & 1]) : "memory");
     if (warp == 1) {
         if (CG == 1) {
             asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "n"(TMEM_COLS) : "memory");
@@ -563,13 +563,14 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                 } else {
                     constexpr int CT = lg_tokens(NT), BUFFERS = lg_buffers(NT);
                     bool ok = true;
-                    lg_out<FORM, CT>(a, t0, 1, end, (int64_t)(t.m * CG + half) * OUT, e, [&](int c) -> uint32_t {
+                    uint32_t buffer = exchange;
+                    lg_out<FORM, CT>(a, t0, 1, end, (int64_t)(t.m * CG + half) * OUT, e, [&](int c) {
                         if (c == 0) {
                             ok = finish_all(done());                   // (all of them go on to the exchange, or none)
-                            if (!ok) return 0u;
+                            if (!ok) return false;
                             tc_fence_after();
                         } else if (BUFFERS == 1) finish_sync();        // (everybody has read the tokens before)
-                        const uint32_t buffer = exchange + (BUFFERS > 1 ? (uint32_t)(turn++ & 1) * (CT * LG_M * 4) : 0u);
+                        if (BUFFERS > 1) buffer = exchange + (uint32_t)(turn++ & 1) * (CT * LG_M * 4);
                         if (group * 16 < CT) {
                             float v[16];
                             tc_load16(d + c + group * 16, v);
@@ -578,8 +579,8 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                             for (int k = 0; k < 16; ++k) st_shared(buffer + (uint32_t)((group * 16 + k) * LG_M + quad * 32 + lane) * 4, v[k]);
                         }
                         finish_sync();
-                        return buffer;
-                    });
+                        return true;
+                    }, [&](int q, int l, float (&v)[8]) { ld_shared(buffer + (uint32_t)((q & (CT - 1)) * LG_M + l) * 4, v); });
                     if (!ok) break;
                 }
             }
@@ -597,7 +598,8 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
             constexpr int CT = NT / C < lg_tokens(NT) ? NT / C : lg_tokens(NT);
             const int64_t t0 = (int64_t)t.n * NT, end = t0 + NT < a.tokens ? t0 + NT : a.tokens, col0 = (int64_t)t.m * OUT;
             const int e = tid - 64;
-            lg_out<FORM, CT>(a, t0 + rank, C, end, col0, e, [&](int c) -> uint32_t {
+            // (through shared memory once more: a thread's eight sums from every rank directly are 32 bytes a lane of remote memory, 29.3 -> 33.4 us for the gradient of x and W at 64 tokens)
+            lg_out<FORM, CT>(a, t0 + rank, C, end, col0, e, [&](int c) {
                 finish_sync();                                         // (everybody has read the tokens before)
                 for (int i = e; i < CT * LG_M / 4; i += LG_FINISH * 32) {
                     const int q = i / (LG_M / 4), l = i % (LG_M / 4) * 4;
@@ -610,8 +612,8 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                     asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(exchange + (uint32_t)(q * LG_M + l) * 4), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
                 }
                 finish_sync();
-                return exchange;
-            });
+                return true;
+            }, [&](int q, int l, float (&v)[8]) { ld_shared(exchange + (uint32_t)((q & (CT - 1)) * LG_M + l) * 4, v); });
         }
         __syncwarp();
     }
