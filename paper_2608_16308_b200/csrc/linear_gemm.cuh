@@ -144,19 +144,11 @@ __device__ __forceinline__ void tc_commit(uint64_t *bar) {
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// (load and wait in one statement: nothing may touch the registers in between)
 __device__ __forceinline__ void tc_load16(uint32_t addr, float (&v)[16]) {
-    uint32_t r[16];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-// (the loaded registers are named, so that nothing that uses them moves in front of the wait)
-__device__ __forceinline__ void tc_load_wait(float (&v)[16]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
-                   "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]) :: "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+                   "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
     uint32_t far;
@@ -394,7 +386,6 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
     constexpr int TMEM_COLS = 2 * NT < 32 ? 32 : 2 * NT;
     constexpr int OUT = FORM == LG_GATED ? LG_M / 2 : LG_M;                                           // output columns of this block's tile
     static_assert(C == 1 || NT * LG_M * 4 <= STAGES * STAGE_BYTES, "a tile's sums, for the other thread blocks of the cluster, lie in the stages");
-
     extern __shared__ uint8_t s_raw[];
     __shared__ __align__(8) uint64_t s_full[STAGES], s_empty[STAGES], s_done[2], s_free[2];
     __shared__ uint32_t s_tmem;
@@ -530,7 +521,6 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
 #pragma unroll 1
                 for (int r = 0; r < ROWS; r += 16) {
                     float v[16];
-                    tc_load16(d + group * ROWS + r, v);
                     uint32_t at[16], bits[16];                         // (all places first: the stores keep their order)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
@@ -538,7 +528,7 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                         at[2 * k] += __popc(bits[2 * k] & below);
                         at[2 * k + 1] += __popc(bits[2 * k + 1] & below);
                     }
-                    tc_load_wait(v);
+                    tc_load16(d + group * ROWS + r, v);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const uint32_t w = lin_pair(v[2 * k], v[2 * k + 1]);
@@ -556,7 +546,6 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                     for (int c = group * 16; t0 + c < end; c += 32) {
                         float v[16];
                         tc_load16(d + c, v);
-                        tc_load_wait(v);
 #pragma unroll
                         for (int k = 0; k < 16; ++k) st_shared(stages + (uint32_t)((c + k) * LG_M + quad * 32 + lane) * 4, v[k]);
                     }
@@ -574,7 +563,6 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                         if (group * 16 < CT) {
                             float v[16];
                             tc_load16(d + c + group * 16, v);
-                            tc_load_wait(v);
 #pragma unroll
                             for (int k = 0; k < 16; ++k) st_shared(buffer + (uint32_t)((group * 16 + k) * LG_M + quad * 32 + lane) * 4, v[k]);
                         }
