@@ -104,18 +104,6 @@ int build_linear_index(dbspmspv_handle_s *h, cudaStream_t st) {
 }
 
 // ---- beside the products --------------------------------------------------------------------
-// eight neighbouring entries j .. j + 7 of a row of `width`, as fp32; past its end 0
-__device__ __forceinline__ void lin_load8(const uint16_t *row, int64_t j, int64_t width, float (&v)[8]) {
-    if (j + 8 <= width && (reinterpret_cast<uintptr_t>(row + j) & 15u) == 0) {
-        const uint4 u = *reinterpret_cast<const uint4 *>(row + j);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { v[2 * k] = __uint_as_float(w[k] << 16); v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = j + k < width ? lin_f32(row[j + k]) : 0.f;
-    }
-}
 // (rows of a workspace buffer begin on 16 bytes and are padded to a multiple of eight entries)
 __device__ __forceinline__ void lin_store8(uint16_t *row, int64_t j, const float (&v)[8]) {
     uint32_t w[4];
@@ -135,9 +123,9 @@ __device__ __forceinline__ void lin_pack(const LinPack &a, int64_t block, int64_
     const int64_t per = a.ldo / 8, total = a.tokens * per;
     for (int64_t i = block * blockDim.x + threadIdx.x; i < total; i += blocks * blockDim.x) {
         const int64_t t = i / per, j = (i - t * per) * 8;
-        float v[8];
-        lin_load8(a.x + t * a.ldx, j, a.n, v);
-        lin_store8(a.out + t * a.ldo, j, v);
+        uint32_t w[4];
+        lg_get(a.x + t * a.ldx, j, a.n, false, w);
+        *reinterpret_cast<uint4 *>(a.out + t * a.ldo + j) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 __global__ void k_linear_pack(const __grid_constant__ LinPack a) {
@@ -206,10 +194,9 @@ __global__ void __launch_bounds__(LS_CTA) k_linear_slopes(const __grid_constant_
                 t[q] = i / per;
                 j[q] = (i - t[q] * per) * 8;
                 if (i < total) {
-                    const int count = a.m - j[q] < 8 ? (int)(a.m - j[q]) : 8;
-                    lg_get(a.dy + t[q] * a.lddy + j[q], a.aligned, count, wy[q]);
-                    if (GATED || a.z) lg_get(a.z + t[q] * a.ldz + j[q], a.aligned, count, wz[q]);
-                    if (GATED) lg_get(a.u + t[q] * a.ldz + j[q], a.aligned, count, wu[q]);
+                    lg_get(a.dy + t[q] * a.lddy, j[q], a.m, a.aligned, wy[q]);
+                    if (GATED || a.z) lg_get(a.z + t[q] * a.ldz, j[q], a.m, a.aligned, wz[q]);
+                    if (GATED) lg_get(a.u + t[q] * a.ldz, j[q], a.m, a.aligned, wu[q]);
                 }
             }
 #pragma unroll
@@ -242,15 +229,14 @@ __global__ void __launch_bounds__(LS_CTA) k_linear_bias(const __grid_constant__ 
     float sum[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum[k] = 0.f;
-    const int count = a.m - j < 8 ? (int)(a.m - j) : 8;
-    for (int64_t t0 = tid / G; t0 < a.tokens && count > 0; t0 += 4 * LANES) {
+    for (int64_t t0 = tid / G; t0 < a.tokens && j < a.m; t0 += 4 * LANES) {
         uint32_t wy[4][4] = {}, wz[4][4] = {};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int64_t t = t0 + q * LANES;
             if (t < a.tokens) {
-                lg_get(a.dy + t * a.lddy + j, a.aligned, count, wy[q]);
-                if (a.z) lg_get(a.z + t * a.ldz + j, a.aligned, count, wz[q]);
+                lg_get(a.dy + t * a.lddy, j, a.m, a.aligned, wy[q]);
+                if (a.z) lg_get(a.z + t * a.ldz, j, a.m, a.aligned, wz[q]);
             }
         }
 #pragma unroll
@@ -322,12 +308,14 @@ static int aligned_rows(const LgArgs &a) {
     auto fits = [](const void *p, int64_t ld, int64_t item) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * item % 16 == 0); };
     return fits(a.y, a.ldy, a.y_f32 ? 4 : 2) && fits(a.z, a.ldz, 2) && fits(a.u, a.ldz, 2) && fits(a.residual, a.ldr, 2);
 }
-// The cut of a product whose tiles are `out` output columns wide (one thread block's) and `kb` blocks of K long.  Blocks of K follow each other at 0.34 us in a
-// thread block, whatever the width of its tile and whether it shares its SM, so the rounds of thread blocks times their K are what counts; emptying a tile and
-// adding up the sums of C thread blocks cost more the wider the tile is.  Measured on seven layers (700 x 5000 to 11008 x 4096), 20 to 1000 tokens, eleven cuts each: the one
-// chosen here is 0.7 % behind the best on average, 7 % at most, and the worst of the eleven is two to four times as slow (4096 x 4096, 256 tokens: 17 to 35 us).
-static LgPlan plan_gemm(const dbspmspv_handle_s *h, int64_t tokens, int64_t width, int out, int64_t kb) {
+// The cut of a product whose tiles are `out` output columns wide (one thread block's) and `kb` blocks of K long; `arrays` beside y are read or written with the outputs.  Blocks of K follow each other at 0.34 us
+// in a thread block, whatever the width of its tile and whether it shares its SM; a tile is emptied under the products of the next, the last one is not; emptying it, and adding up the sums of C thread
+// blocks, cost more the wider it is.  Measured on seven layers (700 x 5000 to 11008 x 4096), 20 to 1000 tokens, eleven cuts each: the one
+// chosen here is 0.7 % behind the best on average, 7 % at most, and the worst of the eleven is two to four times as slow (4096 x 4096, 256 tokens: 17 to 35 us).  With three arrays whose rows begin anywhere (5803 x 558,
+// 587 tokens) tiles of 64 tokens take 30 us, of 256 39.
+static LgPlan plan_gemm(const dbspmspv_handle_s *h, int64_t tokens, int64_t width, int out, int64_t kb, int arrays, bool aligned) {
     struct { LgPlan p; int slots; } const all[] = {{{2, 256, 1}, h->sm_count / 2}, {{1, 16, 1}, 2 * h->sm_count}, {{1, 64, 1}, 2 * h->sm_count}, {{1, 128, 1}, h->sm_count}, {{1, 256, 1}, h->sm_count}};
+    const double each = (aligned ? 0.3 + 0.5 * arrays : 1.3 + 1.2 * arrays) * out / LG_M;      // us to empty 64 tokens of a tile
     LgPlan best = all[0].p;
     double least = 0.;
     for (const auto &q : all) {
@@ -336,7 +324,8 @@ static LgPlan plan_gemm(const dbspmspv_handle_s *h, int64_t tokens, int64_t widt
         for (int c = 1; c <= (q.p.cg == 1 ? 8 : 1); c *= 2) {
             // (a cluster is placed within a part of the GPU: the larger it is, the more SMs stay without one)
             if (c > 1 && (kb < 2 * c || tiles * c >= q.slots - c * c / 2)) break;
-            const double cost = (double)(ceil64(tiles * c, q.slots) * ceil64(kb, c)) * 0.34 + 0.3 * q.p.nt / 64. + (c > 1 ? 0.2 * c * (1. + q.p.nt / 64.) : 0.);
+            const double products = (double)ceil64(kb, c) * 0.34, rounds = (double)ceil64(tiles * c, q.slots), empty = each * q.p.nt / 64. / (c == 1 ? 1. : c == 2 ? 1.4 : c == 4 ? 2. : 2.8);
+            const double cost = products + empty + (rounds - 1.) * (products > empty ? products : empty) + (c > 1 ? 0.2 * c * (1. + q.p.nt / 64.) : 0.);
             if (least == 0. || cost < least) { least = cost; best = q.p; best.c = c; }
         }
     }
@@ -452,16 +441,16 @@ static int forward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinForward f, Li
         if (pack.out) calls.add(k_linear_pack, pack_blocks(h, pack), LS_CTA, 0, false, pack);
         const int out = up ? LG_M / 2 : LG_M;
         const int64_t kb = ceil64(d.n, LG_K);
-        const LgPlan p = plan_gemm(h, f.tokens, d.m, out, kb);
+        LgArgs a = {};
+        a.tokens = f.tokens; a.width = d.m;
+        a.y = f.y; a.ldy = f.ldy; a.y_f32 = f.y_f32; a.act = f.act; a.bias = f.bias; a.residual = f.residual; a.ldr = f.ldr;
+        a.z = f.z; a.u = f.u; a.ldz = f.ldz; a.aligned = aligned_rows(a); a.status = &d.ws.ctr->status;
+        const LgPlan p = plan_gemm(h, f.tokens, d.m, out, kb, !!a.z + !!a.u + !!a.residual, a.aligned);
         LgMaps maps = {};
         maps.a[0] = up ? h->lin_maps[1] : h->lin_maps[0];
         if (up) maps.a[1] = up->lin_maps[1];
         if ((s = encode_rows(&maps.b[0], f.x, f.tokens, d.n, f.ldx, p.nt / p.cg)) != DBSPMSPV_OK) return s;
-        LgArgs a = {};
         a.tiles_m = (int)ceil64(d.m, p.cg * out); a.tiles_n = (int)ceil64(f.tokens, p.nt); a.products = 1; a.layers = 1; a.k_blocks = (int)kb;
-        a.tokens = f.tokens; a.width = d.m;
-        a.y = f.y; a.ldy = f.ldy; a.y_f32 = f.y_f32; a.act = f.act; a.bias = f.bias; a.residual = f.residual; a.ldr = f.ldr;
-        a.z = f.z; a.u = f.u; a.ldz = f.ldz; a.aligned = aligned_rows(a); a.status = &d.ws.ctr->status;
         s = up ? add_gemm<LG_GATED>(h, calls, maps, a, p) : add_gemm<LG_FORWARD>(h, calls, maps, a, p);
     }
     return s == DBSPMSPV_OK ? submit_calls(h, calls, st) : s;
@@ -514,14 +503,14 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
     a.status = &d.ws.ctr->status;
     if (b.dx) {
         const int64_t kb = ceil64(d.m, DC_ROWS);
-        const LgPlan p = plan_gemm(h, b.tokens, d.n, LG_M, kb * layers);
+        a.tokens = b.tokens; a.width = d.n; a.y = b.dx; a.ldy = b.lddx; a.aligned = aligned_rows(a);
+        const LgPlan p = plan_gemm(h, b.tokens, d.n, LG_M, kb * layers, 0, a.aligned);
         LgMaps maps = {};
         for (int l = 0; l < layers; ++l) {
             maps.a[l] = l ? up->lin_maps[2] : h->lin_maps[2];
             if ((s = encode_rows(&maps.b[l], dz[l], b.tokens, d.m, ldd, p.nt / p.cg)) != DBSPMSPV_OK) return s;
         }
         a.tiles_m = (int)ceil64(d.n, p.cg * LG_M); a.tiles_n = (int)ceil64(b.tokens, p.nt); a.products = 1; a.layers = layers; a.k_blocks = (int)kb;
-        a.tokens = b.tokens; a.width = d.n; a.y = b.dx; a.ldy = b.lddx; a.aligned = aligned_rows(a);
         if ((s = add_gemm<LG_DX>(h, calls, maps, a, p)) != DBSPMSPV_OK) return s;
     }
     if (want_w) {

@@ -227,57 +227,77 @@ __device__ __forceinline__ void lg_act(float (&v)[8], int act) {
         for (int i = 0; i < 8; ++i) v[i] = lin_act(v[i], DBSPMSPV_ACT_GELU);
     }
 }
-// the first `count` of eight neighbouring bf16, two to a word; `aligned`: p lies on 16 bytes
-__device__ __forceinline__ void lg_get(const uint16_t *p, bool aligned, int count, uint32_t (&w)[4]) {
-    if (aligned && count == 8) {
+// Half words [from, from + 8) of the sixteen in c[0 .. 7], two to a word; from = 0 .. 8
+__device__ __forceinline__ void lg_shift(uint32_t (&c)[9], int from, uint32_t (&w)[4]) {
+    c[8] = 0u;                                                         // (not read)
+#pragma unroll
+    for (int i = 0; i < 5; ++i) c[i] = from & 8 ? c[i + 4] : c[i];
+#pragma unroll
+    for (int i = 0; i < 6; ++i) c[i] = from & 4 ? c[i + 2] : c[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) c[i] = from & 2 ? c[i + 1] : c[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = from & 1 ? __funnelshift_r(c[i], c[i + 1], 16) : c[i];
+}
+// Columns col .. col + 7 of a row of `width` bf16, two to a word; past the row's end 0.  `aligned`: rows begin on 16 bytes, and col is a multiple of eight.  Elsewhere the sixteen that lie
+// on 16 bytes around them are loaded, where all of them belong to the row.
+__device__ __forceinline__ void lg_get(const uint16_t *row, int64_t col, int64_t width, bool aligned, uint32_t (&w)[4]) {
+    const uint16_t *p = row + col;
+    if (aligned && col + 8 <= width) {
         const uint4 q = *reinterpret_cast<const uint4 *>(p);
         w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+    } else if (!aligned && col >= 8 && col + 16 <= width) {
+        const int s = (int)((reinterpret_cast<uintptr_t>(p) >> 1) & 7u);
+        const uint4 q = *reinterpret_cast<const uint4 *>(p - s), r = *reinterpret_cast<const uint4 *>(p - s + 8);
+        uint32_t c[9] = {q.x, q.y, q.z, q.w, r.x, r.y, r.z, r.w, 0u};
+        lg_shift(c, s, w);
     } else {
+        const int64_t count = width - col;
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = (2 * i < count ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < count ? (uint32_t)p[2 * i + 1] << 16 : 0u);
     }
 }
 __device__ __forceinline__ float lg_half(const uint32_t (&w)[4], int i) { return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16); }
 
-// Columns 8 j .. 8 j + 7 of a tile's part of a row (`row` points to its first column, `width` of its columns exist; 0: nothing is stored), a thread each, the G threads of a
+// Columns 8 j .. 8 j + 7 of a tile's part of a row (`row` points to its first column, `width` of its columns exist; none: nothing is stored), a thread each, the G threads of a
 // row side by side in the warp.  A row that does not begin on 16 bytes is stored in the eights that do: a thread takes the end of its neighbour's
-// values and the beginning of its own.  (All threads of the warp call it together.)
+// values and the beginning of its own; the first one has the end of the last one's, and stores both edges in pieces of 8, 4 and 2 bytes.  (All threads of the warp call it together.)
 template <int G, bool ALIGNED>
 __device__ __forceinline__ void lg_put(uint16_t *row, int j, int width, const float (&v)[8]) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = lin_pair(v[2 * i], v[2 * i + 1]);
-    int lo = 0, at = 8 * j;
+    const int s = ALIGNED ? 0 : (int)((reinterpret_cast<uintptr_t>(row) >> 1) & 7u);
     if (!ALIGNED) {
-        const int s = (int)((reinterpret_cast<uintptr_t>(row) >> 1) & 7u), from = 8 - s;       // first half word, of the neighbour's eight and then this thread's
         uint32_t c[9];
+        const int before = ((threadIdx.x & 31) & ~(G - 1)) | ((j - 1) & (G - 1));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { c[i] = __shfl_up_sync(0xFFFFFFFFu, w[i], 1, G); c[i + 4] = w[i]; }
-        c[8] = 0u;
-        const uint32_t keep[4] = {w[0], w[1], w[2], w[3]};
-#pragma unroll
-        for (int i = 0; i < 5; ++i) c[i] = from & 8 ? c[i + 4] : c[i];
-        if (from & 8) c[5] = c[6] = c[7] = 0u;                          // (not read)
-#pragma unroll
-        for (int i = 0; i < 6; ++i) c[i] = from & 4 ? c[i + 2] : c[i];
-#pragma unroll
-        for (int i = 0; i < 5; ++i) c[i] = from & 2 ? c[i + 1] : c[i];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = from & 1 ? __funnelshift_r(c[i], c[i + 1], 16) : c[i];
-        at -= s;
-        lo = j == 0 ? s : 0;
-        if (j == G - 1) {                                              // what lies behind the last eight
-#pragma unroll
-            for (int k = 1; k < 8; ++k)
-                if (k >= from && 8 * j + k < width) row[8 * j + k] = (uint16_t)(keep[k / 2] >> (16 * (k & 1)));
-        }
+        for (int i = 0; i < 4; ++i) { c[i] = __shfl_sync(0xFFFFFFFFu, w[i], before); c[i + 4] = w[i]; }
+        lg_shift(c, 8 - s, w);
     }
-    const int hi = width - at < 8 ? width - at : 8;
-    if (lo == 0 && hi == 8) *reinterpret_cast<uint4 *>(row + at) = make_uint4(w[0], w[1], w[2], w[3]);
-    else {
+    auto one_by_one = [&](uint16_t *p, int lo, int hi) {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (k >= lo && k < hi) row[at + k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
+            if (k >= lo && k < hi) p[k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
+    };
+    uint16_t *p = row + 8 * j - s;
+    const int hi = width - (8 * j - s) < 8 ? width - (8 * j - s) : 8;
+    if (ALIGNED || s == 0 || j > 0) {
+        if (hi == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else one_by_one(p, 0, hi);
+    } else {
+        if (hi == 8 && width > 0) {                                    // places s .. 7 of the first eight
+            if (s & 1) p[s] = (uint16_t)((s & 4 ? (s & 2 ? w[3] : w[2]) : (s & 2 ? w[1] : w[0])) >> 16);
+            const int e = s + (s & 1);
+            if (e & 2) *reinterpret_cast<uint32_t *>(p + e) = e & 4 ? w[3] : w[1];
+            if (e <= 4) *reinterpret_cast<uint2 *>(p + 4) = make_uint2(w[2], w[3]);
+        } else one_by_one(p, s, hi);
+        p = row + 8 * G - s;                                           // places 0 .. s - 1 of the eight behind the last one
+        if (width >= 8 * G) {
+            if (s & 4) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+            if (s & 2) *reinterpret_cast<uint32_t *>(p + (s & 4)) = s & 4 ? w[2] : w[0];
+            if (s & 1) p[s - 1] = (uint16_t)(s & 4 ? (s & 2 ? w[3] : w[2]) : (s & 2 ? w[1] : w[0]));
+        } else one_by_one(p, 0, width - (8 * G - s) < s ? width - (8 * G - s) : s);
     }
 }
 
@@ -294,10 +314,10 @@ __device__ __forceinline__ void lg_out_as(const LgArgs &a, int64_t t0, int every
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int64_t t = t0 + (int64_t)(c + k * PASS + q0) * every;
-            if (q0 < CT && t < end && count > 0) lg_get(a.residual + t * a.ldr + col0 + 8 * j, ALIGNED, count, next[k]);
+            if (q0 < CT && t < end && count > 0) lg_get(a.residual + t * a.ldr, col0 + 8 * j, a.width, ALIGNED, next[k]);
         }
     };
-    if (FORM == LG_FORWARD && a.bias) lg_get(a.bias + col0 + 8 * j, false, count, bias);
+    if (FORM == LG_FORWARD && a.bias && count > 0) lg_get(a.bias, col0 + 8 * j, a.width, false, bias);
     if (FORM == LG_FORWARD && a.residual) fetch(0);
     for (int c = 0; t0 + (int64_t)c * every < end; c += CT) {
         if (FORM == LG_FORWARD && a.residual) {
