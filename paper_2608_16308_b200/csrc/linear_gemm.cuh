@@ -162,6 +162,11 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t far) {
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(far) : "memory");
     return v;
 }
+__device__ __forceinline__ float ld_cluster1(uint32_t far) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(far) : "memory");
+    return v;
+}
 __device__ __forceinline__ void ld_shared(uint32_t addr, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; i += 4)
@@ -399,7 +404,7 @@ __global__ void __cluster_dims__(CG * C, 1, 1) __launch_bounds__(lg_threads(FORM
 k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArgs a) {
     namespace cg = cooperative_groups;
     static_assert(CG == 1 || (CG == 2 && C == 1 && NT == 256), "");
-    static_assert(FORM != LG_DW || (C == 1 && NT == 256), "");
+    static_assert(FORM != LG_DW || NT == 256, "");
     constexpr bool A_MN = FORM != LG_DX, B_MN = FORM == LG_DW;
     constexpr int STAGES = lg_stages(CG, NT), STAGE_BYTES = lg_stage_bytes(CG, NT), NB = NT / CG;     // NB: rows of operand B in this block's shared memory
     constexpr int FINISH = FORM == LG_DW ? LG_FINISH_DW : LG_FINISH;
@@ -514,7 +519,17 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
         for (int i = first; i < n_tiles; i += step, ++n) {
             const LgTile t = lg_tile(a, i);
             const uint32_t d = mine + (uint32_t)(n & 1) * NT;
-            if constexpr (FORM == LG_DW) {
+            if constexpr (FORM == LG_DW && C > 1) {
+                // this block's sums into its own shared memory, [row][lane]
+                if (!__all_sync(0xFFFFFFFFu, lg_wait(&s_done[n & 1], (uint32_t)((n / 2) & 1), &s_fail, a.status))) break;
+                tc_fence_after();
+                for (int c = group * 16; c < NT; c += FINISH / 4 * 16) {
+                    float v[16];
+                    tc_load16(d + c, v);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) st_shared(stages + (uint32_t)((c + k) * LG_M + quad * 32 + lane) * 4, v[k]);
+                }
+            } else if constexpr (FORM == LG_DW) {
                 // (the index of a warp's rows is fetched a tile ahead, the first one while the products run; it is read from the warp's own part of shared memory, two rows to a load
                 // that all lanes share)
                 constexpr int ROWS = NT / (FINISH / 4);
@@ -598,7 +613,7 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
         }
     }
     __syncwarp();
-    if constexpr (C > 1) {
+    if constexpr (C > 1 && FORM != LG_DW) {
         // (one tile per cluster)  Rank r adds up the C sums of every C-th token and finishes them.
         cg::this_cluster().sync();
         if (warp >= 2 && !s_fail && first < n_tiles) {
@@ -622,6 +637,39 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                 finish_sync();
                 return true;
             }, [&](int q, int l, float (&v)[8]) { ld_shared(exchange + (uint32_t)((q & (CT - 1)) * LG_M + l) * 4, v); });
+        }
+        __syncwarp();
+    }
+    if constexpr (C > 1 && FORM == LG_DW) {
+        // Rank r adds up the C sums of every C-th row and stores them; a warp has its 32 columns, eight rows at a time.
+        cg::this_cluster().sync();
+        if (warp >= 2 && !s_fail && first < n_tiles) {
+            const LgTile t = lg_tile(a, first);
+            const int quad = warp & 3, group = (warp - 2) >> 2, word = t.m * (LG_M / 32) + quad;
+            const int64_t row0 = (int64_t)t.n * NT;
+            const uint2 *index = a.index[t.product] + (int64_t)word * a.width;
+            const uint32_t below = (1u << lane) - 1u, from = stages + (uint32_t)(quad * 32 + lane) * 4;
+            uint16_t *dw = a.dw[t.product];
+            for (int r0 = rank + C * group; r0 < NT && row0 + r0 < a.width && word < a.index_words; r0 += C * (FINISH / 4) * 8) {
+                uint2 x[8];
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int r = r0 + k * C * (FINISH / 4);
+                    x[k] = r < NT && row0 + r < a.width ? __ldg(index + row0 + r) : make_uint2(0u, 0u);
+                    float part[C];
+#pragma unroll
+                    for (int q = 0; q < C; ++q) part[q] = ld_cluster1(cluster_addr(from, q) + (uint32_t)(r < NT ? r : 0) * (LG_M * 4));
+                    v[k] = part[0];
+#pragma unroll
+                    for (int q = 1; q < C; ++q) v[k] += part[q];
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t at = x[k].y + __popc(x[k].x & below);
+                    store_if(((x[k].x >> lane) & 1u) && lg_in_range(a, t.product, at), dw + at, lin_bf16(v[k]));
+                }
+            }
         }
         __syncwarp();
     }

@@ -10,9 +10,11 @@ pytestmark = pytest.mark.gpu
 
 SHAPES = [(1, 1), (64, 64), (65, 17), (200, 333), (1030, 130), (129, 2050), (520, 1032)]
 TOKENS = [1, 2, 3, 17, 65, 250, 301]
+# few tiles and many tokens, which clusters of two, four and eight share
+LONG = [((1000, 1100), 1040), ((520, 640), 2100), ((300, 250), 2600)]
 # enough tiles that two thread blocks work on each
 PAIRS = [((2050, 1930), 1900)]
-CASES = [(s, t) for s in SHAPES for t in TOKENS] + PAIRS
+CASES = [(s, t) for s in SHAPES for t in TOKENS] + LONG + PAIRS
 
 
 def run_linear(layer, t, name, pad, lead, bias, residual, keep, f32, zeros, seed):
