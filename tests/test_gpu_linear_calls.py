@@ -185,6 +185,90 @@ def test_some_of_the_gradients(wanted):
     gate.close(), up.close()
 
 
+@pytest.mark.parametrize("t", [1, 3, 130])
+def test_nothing_left_of_a_layer(t):
+    """Every weight is pruned: sums are zeros, bias and residual remain, no gradient of weights is written."""
+    layer, up = Layer(200, 140, 0.0, seed=1), Layer(200, 140, 0.5, seed=2)
+    assert layer.nnz == 0
+    x, r, y, z, dx = Rows(t, 140, values=normal((t, 140), 1)), Rows(t, 200, values=normal((t, 200), 2)), Rows(t, 200), Rows(t, 200), Rows(t, 140)
+    bias = normal((200,), 3)
+    ws, nb = room(layer, up, t, True)
+    linear(layer, x, y, bias=bias, name="relu", residual=r, z=z, ws=ws, nb=nb)
+    torch.cuda.synchronize()
+    assert torch.equal(z.v, bias.expand(t, -1))
+    near(y.v, torch.relu(bias.double()) + r.f64(), (HALF + 2.0 ** -23) * (torch.relu(bias.double()) + r.f64()).abs())      # (both terms exact, their sum rounded to fp32 and to bf16)
+    dw = torch.full((8,), 9.0, dtype=torch.bfloat16, device=DEV)
+    db = torch.full((200,), 9.0, device=DEV)
+    B.dbspmspv_linear_backward(layer.h, x.start, x.ld, t, B.ACT_NONE, None, 0, r.start, r.ld, dx.start, dx.ld, dw, db, ws, nb)
+    torch.cuda.synchronize()
+    assert not dx.v.any() and bool((dw == 9.0).all())
+    near(db, r.f64().sum(0), SUM * r.f64().abs().sum(0))
+    B.dbspmspv_gated(layer.h, up.h, x.start, x.ld, t, B.ACT_SILU, y.start, y.ld, None, None, 0, ws, nb)
+    torch.cuda.synchronize()
+    assert not y.v.any()
+    layer.close(), up.close()
+
+
+@pytest.mark.parametrize("t", [1, 40, 300])
+def test_one_handle_as_both_layers(t):
+    """y = act(W x) * (W x), and its gradients: those of the two uses, which a program adds up."""
+    w = Layer(264, 200, 0.5, seed=5)
+    x, y, g, u = Rows(t, 200, values=normal((t, 200), 1)), Rows(t, 264), Rows(t, 264), Rows(t, 264)
+    dy, dx = Rows(t, 264, values=normal((t, 264), 2)), Rows(t, 200)
+    dw = [torch.zeros(w.nnz, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    ws, nb = room(w, w, t, True)
+    B.dbspmspv_gated(w.h, w.h, x.start, x.ld, t, B.ACT_GELU, y.start, y.ld, g.start, u.start, g.ld, ws, nb)
+    B.dbspmspv_gated_backward(w.h, w.h, x.start, x.ld, t, B.ACT_GELU, g.start, u.start, g.ld, dy.start, dy.ld, dx.start, dx.ld, dw[0], dw[1], ws, nb)
+    torch.cuda.synchronize()
+    wy, ey, wg, eg, wu, eu = gated_want(w, w, x.f64(), "gelu")
+    near(y.v, wy, ey + HALF * (wy.abs() + ey))
+    near(g.v, wg, eg + HALF * (wg.abs() + eg))
+    assert torch.equal(g.v, u.v)
+    d, e = slopes(dy.f64(), g.f64(), u.f64(), "gelu")
+    wx, bx, ww, bw = grads_want([w, w], x.f64(), d, e)
+    near(dx.v, wx, bx + HALF * (wx.abs() + bx))
+    for a, b, c in zip(dw, ww, bw):
+        near(a, b, c + HALF * (b.abs() + c))
+    w.close()
+
+
+def test_two_streams_at_once():
+    """One handle, two streams, two workspaces: calls that overlap give what they give alone."""
+    gate, up = Layer(1030, 777, 0.5, seed=1), Layer(1030, 777, 0.4, seed=2)
+    t = 150
+    x = [Rows(t, 777, values=normal((t, 777), k)) for k in range(2)]
+    dy = [Rows(t, 1030, values=normal((t, 1030), 5 + k)) for k in range(2)]
+    rooms = [room(gate, up, t, True) for _ in range(2)]
+
+    def call(k, stream):
+        y, g, u, dx = Rows(t, 1030), Rows(t, 1030), Rows(t, 1030), Rows(t, 777)
+        dw = [torch.zeros(w.nnz, dtype=torch.bfloat16, device=DEV) for w in (gate, up)]
+        torch.cuda.synchronize()
+        ws, nb = rooms[k]
+
+        def go():
+            B.dbspmspv_gated(gate.h, up.h, x[k].start, x[k].ld, t, B.ACT_SILU, y.start, y.ld, g.start, u.start, g.ld, ws, nb, stream)
+            B.dbspmspv_gated_backward(gate.h, up.h, x[k].start, x[k].ld, t, B.ACT_SILU, g.start, u.start, g.ld, dy[k].start, dy[k].ld, dx.start, dx.ld, dw[0], dw[1], ws, nb, stream)
+        return go, (y.v, g.v, u.v, dx.v, dw[0], dw[1])
+
+    alone = []
+    for k in range(2):
+        go, out = call(k, None)
+        go()
+        torch.cuda.synchronize()
+        alone.append([v.clone() for v in out])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(10):
+        pair = [call(k, streams[k].cuda_stream) for k in range(2)]
+        for _ in range(3):
+            for go, _ in pair:
+                go()
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(alone[k], pair[k][1]))
+    gate.close(), up.close()
+
+
 @pytest.mark.parametrize("t", [1, 7, 300])
 def test_block_forwards_and_backwards(t):
     """norm's output -> gated block -> projection back onto the residual stream, then the gradients of all of it; the layers in
