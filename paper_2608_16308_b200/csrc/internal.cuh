@@ -346,7 +346,7 @@ struct dbspmspv_handle_s {
     uint2 *lin_index;
     int lin_words;
     bool lin_ready;             // copy and maps are there
-    bool lin_configured[4][2][5][9], lin_cols_configured[2][9];    // [..][thread blocks of a cluster]
+    bool lin_configured[4][2][5][9], lin_cols_configured[3][9];    // [..][thread blocks of a cluster]
     cudaEvent_t ev[2];          // optional timing of the traversal kernel (run_opts.timing)
     bool timed;
     int64_t kernel_launches;    // kernels this handle has launched (run / decode / bfs)

@@ -338,14 +338,16 @@ static LgPlan plan_gemm(const dbspmspv_handle_s *h, int64_t tokens, int64_t widt
     return best;
 }
 
-template <int LAYERS, int C>
+template <int LAYERS, int C, int ROUNDS = 1>
 static int add_columns_c(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a, int strips, int tokens) {
-    bool &done = h->lin_cols_configured[LAYERS - 1][C];
+    if constexpr (LAYERS == 2 && ROUNDS == 1)
+        if (lc_warp_entries(a.n, C) >= LC_LONG_LIST) return add_columns_c<LAYERS, C, 2>(h, calls, a, strips, tokens);
+    bool &done = h->lin_cols_configured[LAYERS + ROUNDS - 2][C];
     if (!done) {
-        DBS_CUDA(cudaFuncSetAttribute(k_linear_cols<LAYERS, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, LIN_COLS_MAX_SMEM));
+        DBS_CUDA(cudaFuncSetAttribute(k_linear_cols<LAYERS, C, ROUNDS>, cudaFuncAttributeMaxDynamicSharedMemorySize, LIN_COLS_MAX_SMEM));
         done = true;
     }
-    calls.add(k_linear_cols<LAYERS, C>, strips * C * tokens, LC_CTA, (size_t)LC_WARPS * lc_warp_entries(a.n, C) * sizeof(uint32_t), false, a, strips);
+    calls.add(k_linear_cols<LAYERS, C, ROUNDS>, strips * C * tokens, LC_CTA, (size_t)lc_smem(a.n, LAYERS, C), false, a, strips);
     return DBSPMSPV_OK;
 }
 // Thread blocks of a strip: as many as it takes to give every SM two, without more than that.  (4096 x 11008, half active, 1 / 2 / 4 / 8 blocks: 20.3 / 14.4 / 12.0 / 14.9 us; 12288 x 4096,
@@ -370,7 +372,7 @@ static int add_columns(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a, i
 // passes over the weights are few bytes (1037 x 515, eight tokens: 5.8 against 8.5 us; 2751 x 1025, five: 6.0 / 8.9, six are past it; gated 1037 x 515, eight: 6.1 / 8.7,
 // but 1500 x 1500, three: 11.2 / 8.8).
 static bool over_columns(const dbspmspv_handle_s *h, int layers, int64_t tokens, bool packed) {
-    if (h->d.n > 65536 || LC_WARPS * lc_warp_entries(h->d.n, columns_cluster(h, tokens)) * (int64_t)sizeof(uint32_t) > LIN_COLS_MAX_SMEM) return false;
+    if (h->d.n > 65536 || lc_smem(h->d.n, layers, columns_cluster(h, tokens)) > LIN_COLS_MAX_SMEM) return false;
     return tokens <= LIN_COLS_MAX_TOKENS || (packed && tokens <= 16 && tokens * layers * layers * h->d.m * h->d.n <= LIN_COLS_MAX_WEIGHTS);
 }
 

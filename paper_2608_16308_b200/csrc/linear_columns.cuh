@@ -13,6 +13,8 @@
 
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "linear_gemm.cuh"
 
 namespace dbs {
@@ -41,21 +43,28 @@ struct LcArgs {
     int64_t ldz;
 };
 
-template <int LAYERS, int C>
+// Shared memory: the warps' lists, their sums [layer][warp][row], the sums of every rank [rank][layer][row]
+__host__ __device__ inline int64_t lc_smem(int64_t n, int layers, int c) { return LC_WARPS * lc_warp_entries(n, c) * 4 + (LC_WARPS + c) * layers * DC_ROWS * 4; }
+
+// Long lists of two layers are walked two rounds at a time: the loads of the second do not wait for the sums of the first (gated, 11008 x 4096: 36.6 -> 31.5 us, 4.8 -> 5.7 TB/s;
+// 4096 x 11008: 32.2 -> 30.0; but 1037 x 515, eight tokens: 8.2 -> 9.5, and one layer gains nothing).
+constexpr int LC_LONG_LIST = 128;        // entries of a warp, where none of x is zero
+template <int LAYERS, int C, int ROUNDS>
 __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(LC_CTA, 2)
 k_linear_cols(const __grid_constant__ LcArgs a, int strips) {
     namespace cg = cooperative_groups;
     constexpr int ILP = 8 / LAYERS;                                   // columns in flight per lane: 4 KB per warp
     extern __shared__ __align__(16) uint8_t s_dyn[];
-    __shared__ __align__(8) float s_part[LAYERS][LC_WARPS][DC_ROWS];
-    __shared__ float s_sum[C][LAYERS][DC_ROWS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rank = C > 1 ? (int)(blockIdx.x % C) : 0, unit = (int)(blockIdx.x / C), strip = unit % strips;
+    const int rank = C > 1 ? (int)(blockIdx.x % C) : 0, unit = (int)(blockIdx.x / C);
     const int64_t token = unit / strips;
+    const std::conditional_t<ROUNDS == 1, int, int64_t> strip = unit - (int)token * strips;
     // (a cluster: every block has started before its shared memory is written; met again behind the weights)
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     pdl_wait();
     const uint16_t *x = a.x + token * a.ldx;
+    float (*s_part)[LC_WARPS][DC_ROWS] = reinterpret_cast<float (*)[LC_WARPS][DC_ROWS]>(s_dyn + (size_t)LC_WARPS * lc_warp_entries(a.n, C) * 4);
+    float (*s_sum)[LAYERS][DC_ROWS] = reinterpret_cast<float (*)[LAYERS][DC_ROWS]>(s_part + LAYERS);
     uint32_t *list = reinterpret_cast<uint32_t *>(s_dyn) + (size_t)warp * lc_warp_entries(a.n, C);
     int n = 0;
     {
@@ -87,6 +96,7 @@ k_linear_cols(const __grid_constant__ LcArgs a, int strips) {
         for (int l = 0; l < LAYERS; ++l)
 #pragma unroll
             for (int r = 0; r < 8; ++r) acc[l][r] = 0.f;
+#pragma unroll ROUNDS
         for (int k0 = 0; k0 < n; k0 += 4 * ILP) {
             uint4 v[LAYERS][ILP];
             float xv[ILP];
