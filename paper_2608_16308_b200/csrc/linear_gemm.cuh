@@ -477,6 +477,12 @@ k_linear_gemm(const __grid_constant__ LgMaps maps, const __grid_constant__ LgArg
                 }
             }
             pdl_trigger();                                             // (the next kernel's blocks may begin where this one's end; what they read waits for all of this one)
+            // Every stage is given back before the block may leave: the products' thread of a pair arrives in both blocks, and nothing may arrive in shared memory of a block that is gone.
+            // (The accumulators' barriers do not tell: which of two commits arrives first in the other block is not said.  Stages that were never filled count as given back.)
+            for (int q = 0; q < STAGES && ok; ++q) {
+                ok = lg_spin(&s_empty[s], phase, &s_fail, a.status);
+                if (++s == STAGES) { s = 0; phase ^= 1; }
+            }
             if (!ok) {                                                 // gave up: the copies in flight land before the block ends
                 if (CG == 1)
                     for (int q = issued < STAGES ? 0 : issued - STAGES; q < issued; ++q) (void)mbar_wait_bounded(&s_full[q % STAGES], (uint32_t)((q / STAGES) & 1), 1 << 16);
