@@ -166,7 +166,7 @@ __device__ __forceinline__ void ls_eight(const LsArgs &a, float (&dy)[8], const 
     } else if (a.act == DBSPMSPV_ACT_GELU) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float p = 0.5f * (1.f + erff(z[k] * 0.70710678f)), slope = p + z[k] * (0.39894228f * __expf(-0.5f * z[k] * z[k]));
+            const float p = lin_phi(z[k]), slope = p + z[k] * (0.39894228f * __expf(-0.5f * z[k] * z[k]));
             if (GATED) { d[k] = dy[k] * u[k] * slope; dy[k] *= z[k] * p; } else dy[k] *= slope;
         }
     } else {
