@@ -81,12 +81,17 @@ struct LgArgs {
 };
 
 // ---- activations -------------------------------------------------------------------------
+// 1 / (1 + exp(-z)) by the exponential of -|z|: the other one is infinite from -88.7 on, where z times the result is still a normal number.
+__device__ __forceinline__ float lin_sigmoid(float z) {
+    const float e = expf(-fabsf(z));
+    return (z < 0.f ? e : 1.f) / (1.f + e);
+}
 // Phi(z).  (By erfc: 1 + erf cancels on the left, off by 10 % at -5 and nothing left from -5.5 on.)
 __device__ __forceinline__ float lin_phi(float z) { return 0.5f * erfcf(z * -0.70710678f); }
 __device__ __forceinline__ float lin_act(float z, int act) {
     switch (act) {
         case DBSPMSPV_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-        case DBSPMSPV_ACT_SILU: return z / (1.f + expf(-z));
+        case DBSPMSPV_ACT_SILU: return z * lin_sigmoid(z);
         case DBSPMSPV_ACT_GELU: return z * lin_phi(z);
         default: return z;
     }
@@ -94,14 +99,17 @@ __device__ __forceinline__ float lin_act(float z, int act) {
 __device__ __forceinline__ float lin_act_slope(float z, int act) {
     switch (act) {
         case DBSPMSPV_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-        case DBSPMSPV_ACT_SILU: { const float p = 1.f / (1.f + expf(-z)); return p * (1.f + z * (1.f - p)); }
+        case DBSPMSPV_ACT_SILU: { const float p = lin_sigmoid(z); return p * (1.f + z * (1.f - p)); }
         case DBSPMSPV_ACT_GELU: return lin_phi(z) + z * (0.39894228f * expf(-0.5f * z * z));
         default: return 1.f;
     }
 }
-// SiLU by the fast exponential and divide, for what is rounded to bf16 or stands in an epilogue: off by a few 2^-22 of |z| + 1, 2^-13 of a bf16's rounding.
+// The same by the fast exponential and divide, for what is rounded to bf16 or stands in an epilogue: off by (1.2 |z| + 8) 2^-23 of the result at most.
 // (expf and a full divide took a quarter of the epilogue's instructions.)
-__device__ __forceinline__ float lin_sigmoid_fast(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float lin_sigmoid_fast(float z) {
+    const float e = __expf(-fabsf(z));
+    return __fdividef(z < 0.f ? e : 1.f, 1.f + e);
+}
 __device__ __forceinline__ float lin_silu_fast(float z) { return z * lin_sigmoid_fast(z); }
 __device__ __forceinline__ uint32_t lin_bf16(float v) { return (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 __device__ __forceinline__ uint32_t lin_pair(float lo, float hi) {

@@ -69,7 +69,7 @@ def rounded(want, err):
 
 
 @pytest.mark.parametrize("t", [1, 17])
-@pytest.mark.parametrize("name", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("name", ["none", "relu", "silu", "gelu"])
 def test_values(column, name, t):
     """over the column and on the tensor cores, in bf16 and in fp32, as a layer and as a gate"""
     h, m, zb, z = column
@@ -94,7 +94,7 @@ def test_values(column, name, t):
         assert torch.isinf(y[k][want > 2.0 ** 128]).all()
 
 
-@pytest.mark.parametrize("name", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("name", ["none", "relu", "silu", "gelu"])
 def test_slopes(column, name):
     h, m, zb, z = column
     one = torch.ones(8, dtype=torch.bfloat16, device=DEV)
