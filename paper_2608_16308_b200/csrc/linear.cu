@@ -172,8 +172,9 @@ __device__ __forceinline__ void ls_eight(const LsArgs &a, float (&dy)[8], const 
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float slope = lin_act_slope(z[k], a.act);
-            if (GATED) { d[k] = dy[k] * u[k] * slope; dy[k] *= lin_act(z[k], a.act); } else dy[k] *= slope;
+            const bool relu = a.act == DBSPMSPV_ACT_RELU;
+            const float slope = relu && !(z[k] > 0.f) ? 0.f : 1.f;
+            if (GATED) { d[k] = dy[k] * u[k] * slope; dy[k] *= relu ? lin_act(z[k], DBSPMSPV_ACT_RELU) : z[k]; } else dy[k] *= slope;
         }
     }
 }

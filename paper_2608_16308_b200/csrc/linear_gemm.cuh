@@ -96,14 +96,6 @@ __device__ __forceinline__ float lin_act(float z, int act) {
         default: return z;
     }
 }
-__device__ __forceinline__ float lin_act_slope(float z, int act) {
-    switch (act) {
-        case DBSPMSPV_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-        case DBSPMSPV_ACT_SILU: { const float p = lin_sigmoid(z); return p * (1.f + z * (1.f - p)); }
-        case DBSPMSPV_ACT_GELU: return lin_phi(z) + z * (0.39894228f * expf(-0.5f * z * z));
-        default: return 1.f;
-    }
-}
 // The same by the fast exponential and divide, for what is rounded to bf16 or stands in an epilogue: off by (1.2 |z| + 8) 2^-23 of the result at most.
 // (expf and a full divide took a quarter of the epilogue's instructions.)
 __device__ __forceinline__ float lin_sigmoid_fast(float z) {
