@@ -8,6 +8,7 @@
 #include "microkernels.cuh"
 #include "linear_columns.cuh"
 #include "linear_gemm.cuh"
+#include "linear_plan.h"
 
 namespace dbs {
 
@@ -275,9 +276,6 @@ __global__ void __launch_bounds__(LS_CTA) k_linear_bias(const __grid_constant__ 
 static int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 static bool tma_rows(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld & 7) == 0; }
 
-// How a product is cut: CG thread blocks per tile of CG * 128 x nt, or C that share a tile's K.
-struct LgPlan { int cg, nt, c; };
-
 template <int FORM, int CG, int NT, int C>
 static int add_gemm_as(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps, const LgArgs &a, int grid) {
     bool &done = h->lin_configured[FORM][CG - 1][NT / 64][C];
@@ -303,42 +301,16 @@ static int add_gemm(dbspmspv_handle_s *h, CallList &calls, const LgMaps &maps, c
         }
     } else {
 #define LG_CASE(NT, C) if (p.nt == NT && p.c == C) return add_gemm_as<FORM, 1, NT, C>(h, calls, maps, a, C > 1 ? (int)tiles * C : grid);
-        LG_CASE(16, 1) LG_CASE(16, 2) LG_CASE(16, 4) LG_CASE(16, 8) LG_CASE(64, 1) LG_CASE(64, 2) LG_CASE(64, 4) LG_CASE(64, 8)
-        LG_CASE(128, 1) LG_CASE(128, 2) LG_CASE(128, 4) LG_CASE(128, 8) LG_CASE(256, 1) LG_CASE(256, 2) LG_CASE(256, 4) LG_CASE(256, 8)
+        LG_TILES(LG_CASE)
 #undef LG_CASE
         return DBSPMSPV_ERR_CUDA;
     }
 }
-static int64_t ceil64(int64_t v, int64_t by) { return (v + by - 1) / by; }
 // whether every row of the outputs and of the residual begins on 16 bytes (LgArgs::aligned)
 static int aligned_rows(const LgArgs &a) {
     auto fits = [](const void *p, int64_t ld, int64_t item) { return !p || ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * item % 16 == 0); };
     return fits(a.y, a.ldy, a.y_f32 ? 4 : 2) && fits(a.z, a.ldz, 2) && fits(a.u, a.ldz, 2) && fits(a.residual, a.ldr, 2);
 }
-// The cut of a product whose tiles are `out` output columns wide (one thread block's) and `kb` blocks of K long; `arrays` beside y are read or written with the outputs.  Blocks of K follow each other at 0.34 us
-// in a thread block, whatever the width of its tile and whether it shares its SM; a tile is emptied under the products of the next, the last one is not; emptying it, and adding up the sums of C thread
-// blocks, cost more the wider it is.  Measured on seven layers (700 x 5000 to 11008 x 4096), 20 to 1000 tokens, eleven cuts each: the one
-// chosen here is 0.7 % behind the best on average, 7 % at most, and the worst of the eleven is two to four times as slow (4096 x 4096, 256 tokens: 17 to 35 us).  With three arrays whose rows begin anywhere (5803 x 558,
-// 587 tokens) tiles of 64 tokens take 30 us, of 256 39.
-static LgPlan plan_gemm(const dbspmspv_handle_s *h, int64_t tokens, int64_t width, int out, int64_t kb, int arrays, bool aligned) {
-    struct { LgPlan p; int slots; } const all[] = {{{2, 256, 1}, h->sm_count / 2}, {{1, 16, 1}, 2 * h->sm_count}, {{1, 64, 1}, 2 * h->sm_count}, {{1, 128, 1}, h->sm_count}, {{1, 256, 1}, h->sm_count}};
-    const double each = (aligned ? 0.3 + 0.5 * arrays : 1.3 + 1.2 * arrays) * out / LG_M;      // us to empty 64 tokens of a tile
-    LgPlan best = all[0].p;
-    double least = 0.;
-    for (const auto &q : all) {
-        if ((q.p.nt == 16) != (tokens <= 16)) continue;               // (a layer's weights go through once: a narrow tile only where all tokens fit in)
-        const int64_t tiles = ceil64(width, q.p.cg * out) * ceil64(tokens, q.p.nt);
-        for (int c = 1; c <= (q.p.cg == 1 ? 8 : 1); c *= 2) {
-            // (a cluster is placed within a part of the GPU: the larger it is, the more SMs stay without one)
-            if (c > 1 && (kb < 2 * c || tiles * c >= q.slots - c * c / 2)) break;
-            const double products = (double)ceil64(kb, c) * 0.34, rounds = (double)ceil64(tiles * c, q.slots), empty = each * q.p.nt / 64. / (c == 1 ? 1. : c == 2 ? 1.4 : c == 4 ? 2. : 2.8);
-            const double cost = products + empty + (rounds - 1.) * (products > empty ? products : empty) + (c > 1 ? 0.2 * c * (1. + q.p.nt / 64.) : 0.);
-            if (least == 0. || cost < least) { least = cost; best = q.p; best.c = c; }
-        }
-    }
-    return best;
-}
-
 template <int LAYERS, int C, int ROUNDS = 1>
 static int add_columns_c(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a, int strips, int tokens) {
     if constexpr (LAYERS == 2 && ROUNDS == 1)
@@ -454,7 +426,7 @@ static int forward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinForward f, Li
         a.tokens = f.tokens; a.width = d.m;
         a.y = f.y; a.ldy = f.ldy; a.y_f32 = f.y_f32; a.act = f.act; a.bias = f.bias; a.residual = f.residual; a.ldr = f.ldr;
         a.z = f.z; a.u = f.u; a.ldz = f.ldz; a.aligned = aligned_rows(a); a.status = &d.ws.ctr->status;
-        const LgPlan p = plan_gemm(h, f.tokens, d.m, out, kb, !!a.z + !!a.u + !!a.residual, a.aligned);
+        const LgPlan p = plan_gemm(h->sm_count, f.tokens, d.m, out, kb, !!a.z + !!a.u + !!a.residual, a.aligned);
         LgMaps maps = {};
         maps.a[0] = up ? h->lin_maps[1] : h->lin_maps[0];
         if (up) maps.a[1] = up->lin_maps[1];
@@ -513,7 +485,7 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
     if (b.dx) {
         const int64_t kb = ceil64(d.m, DC_ROWS);
         a.tokens = b.tokens; a.width = d.n; a.y = b.dx; a.ldy = b.lddx; a.aligned = aligned_rows(a);
-        const LgPlan p = plan_gemm(h, b.tokens, d.n, LG_M, kb * layers, 0, a.aligned);
+        const LgPlan p = plan_gemm(h->sm_count, b.tokens, d.n, LG_M, kb * layers, 0, a.aligned);
         LgMaps maps = {};
         for (int l = 0; l < layers; ++l) {
             maps.a[l] = l ? up->lin_maps[2] : h->lin_maps[2];
@@ -533,15 +505,8 @@ static int backward(dbspmspv_handle_s *h, dbspmspv_handle_s *up, LinBackward b, 
             a.stored[a.products] = (uint32_t)(l ? up : h)->nnz;
             a.index[a.products++] = (l ? up : h)->lin_index;
         }
-        // Pairs where they fill the GPU; else thread blocks of one tile share the tokens while SMs would stay idle and each has four blocks of tokens or more (whole
-        // gradient, shared out / not: 1024 x 1024, 2048 tokens 24 / 30 us, 1000 tokens 19.6 / 20.1; 250 x 300, 2000 tokens 21 / 27; 944 x 1835, 1378 tokens 39 / 39).
-        LgPlan p = {2, 256, 1};
+        const LgPlan p = plan_weights(h->sm_count, b.tokens, d.m, d.n, a.products);
         const int64_t kb = ceil64(b.tokens, LG_K);
-        if (ceil64(d.n, 2 * LG_M) * ceil64(d.m, p.nt) * a.products * 4 < h->sm_count / 2 * 3) {
-            p.cg = 1;
-            const int64_t tiles = ceil64(d.n, LG_M) * ceil64(d.m, p.nt) * a.products;
-            while (p.c < 8 && tiles * p.c * 2 < h->sm_count - 2 * p.c * p.c && kb >= 8 * p.c) p.c *= 2;
-        }
         a.tiles_m = (int)ceil64(d.n, p.cg * LG_M); a.tiles_n = (int)ceil64(d.m, p.nt); a.layers = 1; a.k_blocks = (int)kb;
         a.tokens = b.tokens; a.width = d.m; a.index_words = h->lin_index ? h->lin_words : up->lin_words;
         if ((s = add_gemm<LG_DW>(h, calls, maps, a, p)) != DBSPMSPV_OK) return s;

@@ -35,11 +35,11 @@
 #include <cuda.h>
 
 #include "internal.cuh"
+#include "linear_plan.h"
 #include "staging.cuh"
 
 namespace dbs {
 
-constexpr int LG_M = 128, LG_K = 64;
 constexpr int LG_A_BYTES = LG_M * LG_K * 2;
 constexpr int LG_FINISH = 8;                                   // warps that empty the accumulators, two for each quarter of the lanes
 constexpr int LG_FINISH_DW = 16;                               // ... for the gradient of W, whose values go one by one: twice as many
@@ -47,7 +47,7 @@ __host__ __device__ constexpr int lg_threads(bool dw) { return (2 + (dw ? LG_FIN
 
 // Stages of a form: a block of K of both operands.  Narrow tiles (few tokens, bound by HBM) leave room for two thread blocks per SM.
 __host__ __device__ constexpr int lg_stage_bytes(int cg, int nt) { return LG_A_BYTES + nt / cg * LG_K * 2; }
-__host__ __device__ constexpr int lg_stages(int cg, int nt) { return nt <= 16 ? 5 : nt <= 64 ? 4 : nt <= 128 || cg == 2 ? 6 : 4; }
+__host__ __device__ constexpr int lg_stages(int cg, int nt) { return nt <= 16 ? 5 : cg == 2 ? 6 : 4; }
 // Tokens whose sums are exchanged at a time, and how many such buffers there are
 __host__ __device__ constexpr int lg_tokens(int nt) { return nt <= 64 ? 16 : 32; }
 __host__ __device__ constexpr int lg_buffers(int nt) { return nt == 64 ? 1 : 2; }
