@@ -346,7 +346,8 @@ int dbspmspv_decode(dbspmspv_handle_t h, const void *x, float *y, dbspmspv_strea
  *   workspace  device memory of at least the bytes that dbspmspv_linear_workspace names, on 16 bytes.  Forward calls need it only for
  *              x whose rows do not begin on 16 bytes (x and ldx both count) and more than two tokens (small layers: 16).  Two calls that may overlap need two workspaces; a captured call keeps its own.
  *
- * Sums are fp32 (those of the tensor cores: off by 3e-6 of a result's 2-norm at 11,000 columns).  y, z, g, u, dx and dw are rounded to bf16 once, to nearest even; dz, dg and du are rounded to bf16 before they
+ * Sums are fp32.  Those of the tensor cores are cut off, not rounded: off by 3e-6 of a result's 2-norm at 11,000 terms of both signs, by 5.5e-9 of a sum per term where all have one sign
+ * (11,000 terms 4.5e-5).  An accumulator takes 131,072 terms at most in sums of up to a million.  y, z, g, u, dx and dw are rounded to bf16 once, to nearest even; dz, dg and du are rounded to bf16 before they
  * enter the products.  Results do not depend on the order in which thread blocks run.  residual may be y itself (same address, same
  * stride, bf16: every entry is read before it is written); no other output may overlap an input or another output.
  * Alignment: bf16 arrays on 2 bytes, fp32 arrays on 4.  Asynchronous on `stream`; no device memory is allocated.

@@ -103,3 +103,22 @@ def test_gradient_of_weights(t):
     check_backward([gate], t, want_dx=False)
     check_backward([gate, up], t, "silu", want_dx=False)
     gate.close(), up.close()
+
+
+def test_a_million_tokens_of_one_sign():
+    """The gradient of weights over a million tokens whose terms are all positive: an accumulator cuts off up to 2^-23 of itself per step of 16 terms,
+    which 131,072 terms make 8192 * 2^-23 at most, and one rounding to bf16."""
+    m, n, t = 1800, 1160, 1 << 20
+    layer = Layer(m, n, 0.05, seed=1)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    x, dy = (torch.empty((t, w), dtype=torch.bfloat16, device=DEV).uniform_(0.5, 1.5, generator=gen) for w in (n, m))
+    dw = torch.full((layer.nnz + 1,), 77.0, dtype=torch.bfloat16, device=DEV)
+    B.dbspmspv_linear_backward(layer.h, x, n, t, B.ACT_NONE, None, 0, dy, m, None, 0, dw, None, None, 0)
+    rows = 8
+    want = sum(dy[k:k + 16384, -rows:].double().T @ x[k:k + 16384].double() for k in range(0, t, 16384))
+    torch.cuda.synchronize()
+    last = layer.at >= (m - rows) * n
+    want = want.reshape(-1)[layer.at[last] - (m - rows) * n]
+    near(dw[:-1][last], want, (HALF + 8192 * 2.0 ** -23) * want)
+    assert int(last.sum()) > 100 and float(dw[-1]) == 77.0
+    layer.close()
