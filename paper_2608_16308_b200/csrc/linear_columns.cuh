@@ -13,8 +13,6 @@
 
 #include <cooperative_groups.h>
 
-#include <type_traits>
-
 #include "linear_gemm.cuh"
 
 namespace dbs {
@@ -46,8 +44,8 @@ struct LcArgs {
 // Shared memory: the warps' lists, their sums [layer][warp][row], the sums of every rank [rank][layer][row]
 __host__ __device__ inline int64_t lc_smem(int64_t n, int layers, int c) { return LC_WARPS * lc_warp_entries(n, c) * 4 + (LC_WARPS + c) * layers * DC_ROWS * 4; }
 
-// Long lists of two layers are walked two rounds at a time: the loads of the second do not wait for the sums of the first (gated, 11008 x 4096: 36.6 -> 31.5 us, 4.8 -> 5.7 TB/s;
-// 4096 x 11008: 32.2 -> 30.0; but 1037 x 515, eight tokens: 8.2 -> 9.5, and one layer gains nothing).
+// Long lists of two layers are walked two rounds at a time: the loads of the second do not wait for the sums of the first (gated, calls of one size one behind the other, 11008 x 4096: 36.6 -> 31.7 us;
+// 4096 x 11008: 32.2 -> 30.3; but 1037 x 515, eight tokens: 8.2 -> 9.5, and one layer gains nothing.  Among other calls the first takes 33.3 us, 5.4 TB/s).
 constexpr int LC_LONG_LIST = 128;        // entries of a warp, where none of x is zero
 template <int LAYERS, int C, int ROUNDS>
 __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(LC_CTA, 2)
@@ -58,7 +56,10 @@ k_linear_cols(const __grid_constant__ LcArgs a, int strips) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = C > 1 ? (int)(blockIdx.x % C) : 0, unit = (int)(blockIdx.x / C);
     const int64_t token = unit / strips;
-    const std::conditional_t<ROUNDS == 1, int, int64_t> strip = ROUNDS == 1 ? unit % strips : unit - (int)token * strips;     // (as measured: 1000 x 2000 6.7 and 8.2 us, 4096 x 11008 32.2 and 30.0)
+    // (What differs is what the compiler makes of the loop under 64 registers.  Behind the remainder, the gated kernels of short lists spill 24 to 64 bytes and keep all loads of a round in flight; behind the
+    // product they fit, and wait for memory twice as long: stalls for it 4.6 in place of 2.5 per instruction, 1000 x 2000 8.4 in place of 7.0 us.  Those of long lists spill up to
+    // 112 bytes behind the remainder and none behind the product: 4096 x 11008 32.7 and 30.3 us.)
+    const int strip = ROUNDS == 1 ? unit % strips : unit - (int)token * strips;
     // (a cluster: every block has started before its shared memory is written; met again behind the weights)
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     pdl_wait();
