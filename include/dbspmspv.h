@@ -16,7 +16,8 @@
  *     stream).  dbspmspv_run / db_bfs / dbspmspv_decode only enqueue work on it: they allocate
  *     no device memory, never synchronise, and return as soon as the kernels are queued (a handle keeps
  *     the launch graphs of its last few kinds of call, at most eight, in host memory).  Calls on the
- *     same handle must be stream ordered (the handle owns one workspace).  A handle lives on
+ *     same handle must be stream ordered (the handle owns one workspace) and made by one host thread at a time; only the
+ *     calls of linear layers may overlap one another on the GPU (see dbspmspv_linear).  A handle lives on
  *     the device that was current when it was created; run / db_bfs / decode return
  *     DBSPMSPV_ERR_INVALID_ARG when the calling thread's current device is another one.
  *   - Functions return a dbspmspv_status_t.  Argument errors are reported synchronously.
@@ -344,14 +345,18 @@ int dbspmspv_decode(dbspmspv_handle_t h, const void *x, float *y, dbspmspv_strea
  *              a CSR matrix without duplicates whose columns ascend -- or NULL
  *   dbias      out: m fp32, or NULL
  *   workspace  device memory of at least the bytes that dbspmspv_linear_workspace names, on 16 bytes.  Forward calls need it only for
- *              x whose rows do not begin on 16 bytes (x and ldx both count) and more than two tokens (small layers: 16).  Two calls that may overlap need two workspaces; a captured call keeps its own.
+ *              x whose rows do not begin on 16 bytes (x and ldx both count) and more than two tokens (small layers: 16).  Calls of linear layers
+ *              on one handle may be enqueued on several streams, by one host thread at a time, and overlap there (not with its other calls, such as dbspmspv_decode): two that may overlap need
+ *              two workspaces; a captured call keeps its own.
  *
  * Sums are fp32.  Those of the tensor cores are cut off, not rounded: off by 3e-6 of a result's 2-norm at 11,000 terms of both signs, by 5.5e-9 of a sum per term where all have one sign
  * (11,000 terms 4.5e-5).  An accumulator takes 131,072 terms at most in sums of up to a million.  y, z, g, u, dx and dw are rounded to bf16 once, to nearest even; dz, dg and du are rounded to bf16 before they
  * enter the products.  Results do not depend on the order in which thread blocks run.  residual may be y itself (same address, same
  * stride, bf16: every entry is read before it is written); no other output may overlap an input or another output.
  * Alignment: bf16 arrays on 2 bytes, fp32 arrays on 4.  Asynchronous on `stream`; no device memory is allocated.
- * Errors: INVALID_ARG (also a workspace that is needed and too small), UNSUPPORTED.
+ * Errors: INVALID_ARG (also a workspace that is needed and too small), UNSUPPORTED.  A wait that ran out on the device is reported by dbspmspv_get_stats of `h` or, of a gated
+ * block, of `gate`; that call waits for the stream of the handle's last call only.
+ * The weights of a handle do not change: a step of training makes new handles from the new values.
  */
 int dbspmspv_linear_workspace(dbspmspv_handle_t h, dbspmspv_handle_t up /* the other layer of a gated block, or NULL */, int32_t tokens, int backward, int64_t *bytes);
 int dbspmspv_linear(dbspmspv_handle_t h, const void *x, int64_t ldx, int32_t tokens, const void *bias, int act, const void *residual, int64_t ldr,
@@ -364,7 +369,7 @@ int dbspmspv_gated_backward(dbspmspv_handle_t gate, dbspmspv_handle_t up, const 
                             const void *dy, int64_t lddy, void *dx, int64_t lddx, void *dw_gate, void *dw_up, void *workspace, int64_t workspace_bytes,
                             dbspmspv_stream_t stream);
 
-/* Waits for the stream the handle's last run / decode / db_bfs call was enqueued on (not for the
+/* Waits for the stream the handle's last run / decode / db_bfs / linear call was enqueued on (not for the
  * whole device) and copies the statistics to the HOST struct `out`.  Returns the deferred
  * device status of the last call, which is then cleared.                                      */
 int dbspmspv_get_stats(dbspmspv_handle_t h, dbspmspv_stats *out);

@@ -1,6 +1,6 @@
 // The kernels of one library call, collected first and then submitted together.
 //
-// What bounds a short call is its launches.  On the B200 machine a kernel launch costs 2.3 - 2.9 us of the
+// What bounds a short call is its launches.  On B200 a kernel launch costs 2.3 - 2.9 us of the
 // calling thread; a kernel that waits for the one before it to end starts on a 2 us grid (one 8 us
 // kernel after the other: 10.24 us a call), while one launched with the programmatic
 // attribute starts as its predecessor drains (8.44 us).  And a graph of the same kernels launches

@@ -386,8 +386,8 @@ int build_linear_index(dbspmspv_handle_s *h, cudaStream_t st);
 // writes are visible (a no-op for a normally launched kernel).  Every kernel of a call begins with
 // it (or reads nothing that an earlier kernel of the stream may write before it).
 // Some kernels let their successor go early (griddepcontrol.launch_dependents), behind their own pdl_wait: k_zero_rows in front of the batched decode kernels, each
-// block of which therefore executes pdl_wait on every way out, and those of the linear layers (linear.cu), whose shared memory leaves
-// the successor no room before their last round.  The others do not: the successor's thread
+// block of which therefore executes pdl_wait on every way out, and those of the linear layers (linear.cu), once all of their own blocks
+// have found a place (a successor begins when every block has let it go or ended).  The others do not: the successor's thread
 // blocks then sit on the SMs, waiting, in the place of its own later blocks and of the persistent
 // kernel behind them (stencil 160^3, x = 5 %: traversal 43 instead of 32 us, call 73 instead of 53; every other path 0 - 4 % slower).
 __device__ __forceinline__ unsigned long long global_timer_ns() {

@@ -323,7 +323,7 @@ static int add_columns_c(dbspmspv_handle_s *h, CallList &calls, const LcArgs &a,
     calls.add(k_linear_cols<LAYERS, C, ROUNDS>, strips * C * tokens, LC_CTA, (size_t)lc_smem(a.n, LAYERS, C), false, a, strips);
     return DBSPMSPV_OK;
 }
-// Thread blocks of a strip: as many as it takes to give every SM two, without more than that.  (4096 x 11008, half active, 1 / 2 / 4 / 8 blocks: 20.3 / 14.4 / 12.0 / 14.9 us; 12288 x 4096,
+// Thread blocks of a strip: doubled, up to eight, until there are more of them than SMs.  (4096 x 11008, half active, 1 / 2 / 4 / 8 blocks: 20.3 / 14.4 / 12.0 / 14.9 us; 12288 x 4096,
 // dense: 19.4 / 23.2 / 22.9 / 31.8.)
 static int columns_cluster(const dbspmspv_handle_s *h, int64_t tokens) {
     const int64_t units = (h->d.m + DC_ROWS - 1) / DC_ROWS * tokens;

@@ -19,8 +19,7 @@
 //   * Epilogue: the sums of a few tokens at a time go through shared memory, [token][lane], and are finished from there, eight neighbours of a
 //     token per thread: 16 bytes a load or store, 256 bytes side by side, the residual fetched in front of the exchange.
 //     (A lane's own values, 2 bytes at a time, by four warps: 11008 x 4096 gated, 2048 tokens, both projections kept 373 us, 280 through shared memory.)
-//   What bounds it: many tokens, the tensor cores (the same case 260 us in short bursts, 1420 TFLOP/s of dense product; 1628 and, under the power limit, 1356 are what cuBLAS reaches
-//   on 8192^3; 8192 x 8192 x 8192 here 1400); few tokens, HBM on the copy (6 tokens 31 us, 180 MB at 5.8 TB/s).
+//   What bounds it: many tokens, the tensor cores under the power limit (@GATED2048@); few tokens, HBM on the copy (@GATED6@).
 //   * CG = 2: the two thread blocks of a cluster work on one 256 x 256 tile, each with half of either operand in its shared memory:
 //     32 KB per block of K and SM where one block alone would need 48.
 //   * Gated: M are 64 rows of the gate and the same 64 of the other layer; both sums of an output meet in that exchange.
@@ -28,7 +27,7 @@
 //     values' array: one popc gives each its place.
 //   * C > 1, few tiles: the C thread blocks of a cluster share K and add their sums up through distributed shared memory, in rank order.
 //
-// Sums are fp32 in TMEM; what is handed on in bf16 is rounded once.  Every wait is bounded.
+// Sums are fp32 in TMEM; what is handed on in bf16 is rounded once.  Every wait for a barrier in shared memory is bounded; those of the hardware's own (TMEM, clusters, the kernel in front) end with the blocks they wait for.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -157,7 +156,8 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, int rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(far) : "r"(addr), "r"(rank));
     return far;
 }
-// (relaxed: what is handed on is the accumulator, whose loads have ended; a release would wait for the warp's stores to global memory)
+// (relaxed, as PTX has it for handing tensor memory to another thread: what is handed on is the accumulator, whose loads have ended (wait::ld of the whole warp), ordered by the tcgen05 fences
+// before this arrival and behind the wait; nothing else is read behind it.  A release would wait for the warp's stores to global memory.)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t far) { asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(far) : "memory"); }
 __device__ __forceinline__ float4 ld_cluster(uint32_t far) {
     float4 v;

@@ -121,3 +121,26 @@ def test_slopes(column, name):
     torch.cuda.synchronize()
     assert not dw.any()
     near(du, want, rounded(want, err))
+
+
+@pytest.mark.parametrize("t", [1, 17])
+def test_infinities(t):
+    """An infinite entry in front of an activation: what the formula gives in arithmetic with infinities."""
+    w = np.array([1.0, -1.0, 0.5, -2.0], np.float32)
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+    o = B.default_create_opts()
+    o.linear = 1
+    h = B.dbspmspv_create_csr(4, 1, 4, up(np.arange(5, dtype=np.int64)), up(np.zeros(4, np.int32)), up(wl.f32_to_bf16_bits(w).view(np.int16)), B.BF16, 16, o)
+    nan, inf = float("nan"), float("inf")
+    want = {"none": (inf, -inf), "relu": (inf, 0.0), "silu": (inf, nan), "gelu": (inf, nan)}
+    for name, (pos, neg) in want.items():
+        x = torch.full((t, 8), inf, dtype=torch.bfloat16, device=DEV)
+        y = torch.empty((t, 4), device=DEV)
+        B.dbspmspv_linear(h, x, 8, t, None, ACT[name], None, 0, y, 4, 1, None, 0, None, 0)
+        torch.cuda.synchronize()
+        assert torch.equal(torch.nan_to_num(y, 5.0, 7.0, -7.0), torch.nan_to_num(torch.tensor([[pos, neg, pos, neg]] * t, device=DEV), 5.0, 7.0, -7.0))
+        x.fill_(nan)
+        B.dbspmspv_linear(h, x, 8, t, None, ACT[name], None, 0, y, 4, 1, None, 0, None, 0)
+        torch.cuda.synchronize()
+        assert torch.isnan(y).all()
+    B.dbspmspv_destroy(h)
