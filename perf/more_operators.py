@@ -179,14 +179,17 @@ class _State:
         self.targets = torch.where(padding, -1, at.gather(1, best)[:, 0]).to(torch.int32)
         k = c["top"]
         if c["kind"] == "logprobs":
-            self.logprob, self.lse = torch.empty(t, device=DEV), torch.empty(t, device=DEV)
+            self.logprob, self.stats = torch.empty(t, device=DEV), torch.empty((t, 2), device=DEV)
             self.entropy = torch.empty(t, device=DEV) if c["entropy"] else None
             self.top_ids = torch.empty((t, k), dtype=torch.int32, device=DEV) if k else None
             self.top_logprobs = torch.empty((t, k), device=DEV) if k else None
             return
-        z = self.logits.float() / c["temperature"]
+        # what a forward call kept: the largest logit, and the logarithm of the sum relative to it
+        z = self.logits.float()
+        most = z.amax(dim=1, keepdim=True)
+        z = (z - most) / c["temperature"]
+        self.stats = torch.cat([most, torch.logsumexp(z, dim=1, keepdim=True)], dim=1)
         logp = torch.log_softmax(z, dim=1)
-        self.lse = torch.logsumexp(z, dim=1)
         self.entropy = -(logp.exp() * logp.clamp(min=-1e30)).sum(dim=1) if c["entropy"] else None
         self.top_ids = logp.topk(k, dim=1).indices.to(torch.int32) if k else None
         self.dlogprob = -torch.rand(t, generator=self.gen, device=DEV) / t
@@ -288,10 +291,10 @@ def _plain_dropout(s):
 def _plain_logprobs(s):
     c, k = s.case, s.case["top"]
     logits = s.logits.float()
-    z = logits / c["temperature"]
-    top = z.amax(dim=1, keepdim=True)
-    lse = (top + (z - top).exp().sum(dim=1, keepdim=True).log())
-    logp = z - lse
+    most = logits.amax(dim=1, keepdim=True)
+    z = (logits - most) / c["temperature"]
+    total = z.exp().sum(dim=1, keepdim=True).log()
+    logp = z - total
     target = s.targets.long()
     logprob = torch.where(target < 0, 0.0, logp.gather(1, target.clamp(min=0)[:, None])[:, 0])
     entropy = -(logp.exp() * torch.where(logp == -math.inf, 0.0, logp)).sum(dim=1) if c["entropy"] else None
@@ -301,12 +304,12 @@ def _plain_logprobs(s):
         bits = (logits + 0.0).view(torch.int32).long()
         order = torch.where(bits < 0, bits ^ 0x7FFFFFFF, bits) * (1 << 32) - torch.arange(c["vocab"], device=DEV)
         ids = order.topk(k, dim=1).indices
-    return {"logprob": logprob, "lse": lse[:, 0], "entropy": entropy, "top_ids": None if ids is None else ids.to(torch.int32), "top_logprobs": None if ids is None else logp.gather(1, ids)}
+    return {"logprob": logprob, "stats": torch.cat([most, total], dim=1), "entropy": entropy, "top_ids": None if ids is None else ids.to(torch.int32), "top_logprobs": None if ids is None else logp.gather(1, ids)}
 
 
 def _plain_logprobs_backward(s):
     c = s.case
-    logp = s.logits.float() / c["temperature"] - s.lse[:, None]
+    logp = (s.logits.float() - s.stats[:, :1]) / c["temperature"] - s.stats[:, 1:]
     p = logp.exp()
     target = s.targets.long()
     d = torch.where(target < 0, 0.0, s.dlogprob)
@@ -332,10 +335,10 @@ def _calls(s):
         B.dbspmspv_dropout(s.x, _ld(s.x), int(c["f32"]), t, c["n"], c["drop"], s.random, s.y, _ld(s.y))
         return {"y": s.y}
     if c["kind"] == "logprobs":
-        B.dbspmspv_logprobs(s.logits, _ld(s.logits), int(c["f32"]), t, c["vocab"], c["temperature"], s.targets, s.logprob, s.entropy, s.lse, c["top"], s.top_ids, s.top_logprobs)
-        return {"logprob": s.logprob, "lse": s.lse, "entropy": s.entropy, "top_ids": s.top_ids, "top_logprobs": s.top_logprobs}
+        B.dbspmspv_logprobs(s.logits, _ld(s.logits), int(c["f32"]), t, c["vocab"], c["temperature"], s.targets, s.logprob, s.entropy, s.stats, c["top"], s.top_ids, s.top_logprobs)
+        return {"logprob": s.logprob, "stats": s.stats, "entropy": s.entropy, "top_ids": s.top_ids, "top_logprobs": s.top_logprobs}
     if c["kind"] == "logprobs_backward":
-        B.dbspmspv_logprobs_backward(s.logits, _ld(s.logits), int(c["f32"]), t, c["vocab"], c["temperature"], s.targets, s.lse, s.entropy, c["top"], s.top_ids, s.dlogprob, s.dentropy,
+        B.dbspmspv_logprobs_backward(s.logits, _ld(s.logits), int(c["f32"]), t, c["vocab"], c["temperature"], s.targets, s.stats, s.entropy, c["top"], s.top_ids, s.dlogprob, s.dentropy,
                                      s.dtop, s.dlogits, _ld(s.dlogits), int(c["f32"]))
         return {"dlogits": s.dlogits}
     if c["kind"] == "join":
@@ -358,8 +361,8 @@ def work(case):
     if case["kind"].startswith("logprobs"):
         size = (4 if case["f32"] else 2) * case["vocab"]
         if case["kind"] == "logprobs":
-            return {"bytes": t * (size + 16 + 8.0 * case["top"]), "flops": 6.0 * t * case["vocab"]}
-        return {"bytes": t * (2 * size + 20 + 8.0 * case["top"]), "flops": 8.0 * t * case["vocab"]}
+            return {"bytes": t * (size + 20 + 8.0 * case["top"]), "flops": 6.0 * t * case["vocab"]}
+        return {"bytes": t * (2 * size + 24 + 8.0 * case["top"]), "flops": 8.0 * t * case["vocab"]}
     n = case["n"]
     if case["kind"] == "dropout":
         return {"bytes": 2.0 * t * n * (4 if case["f32"] else 2) + 16, "flops": 2.0 * t * n}
@@ -455,8 +458,8 @@ def exact(case, seed):
         p = torch.softmax(z, dim=1)
         top = z.sort(dim=1, descending=True).values[:, :c["top"]] - lse[:, None] if c["top"] else None
         return {"logprob": (torch.take_along_dim(z, target, 1)[:, 0] - lse) * have if not c["masked"] else torch.where(have, torch.take_along_dim(z, target, 1)[:, 0] - lse, 0.0),
-                "lse": lse, "entropy": torch.special.entr(p).sum(dim=1) if c["entropy"] else None, "top_ids": None, "top_logprobs": top}
-    p = torch.exp(z - s.lse.double()[:, None])
+                "stats": torch.stack([s.logits.double().amax(dim=1), lse - z.amax(dim=1)], dim=1), "entropy": torch.special.entr(p).sum(dim=1) if c["entropy"] else None, "top_ids": None, "top_logprobs": top}
+    p = torch.exp((s.logits.double() - s.stats[:, :1].double()) / c["temperature"] - s.stats[:, 1:].double())
     weight = torch.zeros_like(z)
     weight.scatter_add_(1, target, (s.dlogprob * have).double()[:, None])
     if c["top"]:
