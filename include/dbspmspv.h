@@ -369,6 +369,90 @@ int dbspmspv_gated_backward(dbspmspv_handle_t gate, dbspmspv_handle_t up, const 
                             const void *dy, int64_t lddy, void *dx, int64_t lddx, void *dw_gate, void *dw_up, void *workspace, int64_t workspace_bytes,
                             dbspmspv_stream_t stream);
 
+/*
+ * What stands between the layers of a network and behind the last one.  (Outside the paper's scope, like the layers above.)  These calls need no handle: they
+ * run on the calling thread's current device, whose memory every array has to be (an array of the host or of another device: INVALID_ARG where it is the first input or output of the call).  Rows are
+ * tokens, ld... entries apart (at least their width; what lies between them is neither read nor written); bf16 arrays begin on 2 bytes, fp32 and int32 arrays on 4, `random` on 8.
+ * Arithmetic, sums and statistics are fp32; every output is rounded to its type once.  Results do not depend on the order in which thread blocks run.  A token with an infinity or a NaN spoils its own
+ * rows and the sums over tokens, no other row.  No output may overlap an input or another output, except where it says "in place": the same address, stride and type.
+ * Asynchronous on `stream`, no memory is allocated, nothing is kept between calls: calls on several streams and captured calls overlap freely, each with its own workspace.
+ *
+ * Random numbers.  `random` is the address of two 64-bit numbers in DEVICE memory, seed and offset; a program writes a new offset for every call that is to draw new numbers (before the call on its
+ * stream, or between two replays of a graph).  Entry (token t, column c) takes 16 bits of Philox 4x32-10 (Salmon, Moraes, Dror, Shaw: Parallel random numbers: as easy as 1, 2, 3, 2011) with the
+ * key (seed's low word, high word) and the counter (c / 8, t, offset's low word, high word): bits 16 (c % 2) and up of output word c % 8 / 2.  It is dropped when they are below
+ * P = floor(65536 drop + 0.5), else multiplied with 65536 / (65536 - P).  No mask is stored: the gradient draws the same numbers again from the same `random`.  Strides and types do not matter.
+ */
+enum { DBSPMSPV_NORM_NONE = 0, DBSPMSPV_NORM_RMS = 1, DBSPMSPV_NORM_LAYER = 2 };
+
+/* A block's place in the residual stream.  Call dbspmspv_default_join_opts first.            */
+typedef struct {
+    int32_t norm_block;      /* DBSPMSPV_NORM_* of what the block gave                (NONE)  */
+    int32_t norm_next;       /* ... in front of the next block                        (RMS)   */
+    float eps_block;         /*                                                       (1e-5)  */
+    float eps_next;          /*                                                       (1e-5)  */
+    float scale;             /* residual scale                                        (1)     */
+    float drop;              /* probability of dropout, 0 to 1                        (0)     */
+    int32_t stream_f32;      /* r, out, dout, dr are fp32, else bf16                  (0)     */
+    int32_t block_f32;       /* b is fp32, else bf16                                  (0)     */
+    int32_t params_f32;      /* weights, biases and gates are fp32, else bf16         (0)     */
+    int32_t dblock_f32;      /* db is fp32, else bf16 (as the layers' gradients take it) (0)  */
+    int32_t reserved[2];
+} dbspmspv_join_opts;
+void dbspmspv_default_join_opts(dbspmspv_join_opts *opts);
+
+/*
+ * One pass:   out = r + scale drop(gate * norm_block(b)),   h = norm_next(out)
+ *   norm(x)    NONE x;  RMS x / sqrt(mean(x^2) + eps) * w + c;  LAYER (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * w + c;  over the n columns of a token.  The norm of `out` is that of
+ *              the sum before it is rounded to the stream's type.
+ *   tokens     0: nothing is done.   n  columns, 1 to 32768 (more: UNSUPPORTED)
+ *   r          tokens x n, or NULL: zeros.   b  tokens x n, or NULL: nothing joins (out = r).  One of them is there.
+ *   w_, c_     weights and biases of the two norms, n entries, or NULL: ones and zeros.  NORM_NONE takes none.
+ *   gate       n entries (ldg = 0, the same for every token), or tokens x n (ldg >= n), or NULL: ones
+ *   random     two numbers, see above; NULL where drop is 0 or b is NULL
+ *   out        tokens x n, may be r in place; NULL: not wanted.   h  tokens x n bf16, or NULL: not wanted.  One of them is there.
+ *   stats      out, for the gradient: four fp32 a token (on 16 bytes): mean and 1 / sqrt(...) of norm_block, then of norm_next (0 where a norm takes no mean, 0 and 1 for NONE); NULL: not kept
+ */
+int dbspmspv_join(const dbspmspv_join_opts *opts, int32_t tokens, int64_t n, const void *r, int64_t ldr, const void *b, int64_t ldb, const void *w_block, const void *c_block,
+                  const void *gate, int64_t ldg, const void *w_next, const void *c_next, const uint64_t *random, void *out, int64_t ldo, void *h, int64_t ldh, float *stats,
+                  dbspmspv_stream_t stream);
+/*
+ * Its gradient, from what the forward call took, `out` as it left it, and `stats`:
+ *   G = dout + (slope of norm_next)(dh);   dr = G;   q = scale drop(G);   dgate = q * norm_block(b);   db = (slope of norm_block)(q * gate)
+ *   out        needed with a norm_next (and dh);   b  needed for db through a norm_block, dw_block and dgate;   stats  needed with a norm
+ *   dh, dout   tokens x n (bf16; the stream's type): what reaches h and out; one of them may be NULL (zeros)
+ *   dr         tokens x n, the stream's type, may be dout in place;   db  tokens x n;   NULL: not wanted
+ *   dw_, dc_   sums over the tokens, n fp32 each, or NULL: not wanted (tokens = 0: zeroed).  NORM_NONE has none.
+ *   dgate      of a gate of n entries: n fp32, summed over the tokens; of one with rows: tokens x n of the gate's type, rows lddg apart; NULL: not wanted
+ *   workspace  device memory of at least the bytes that dbspmspv_join_workspace names, on 16 bytes; only sums over tokens need it
+ */
+int dbspmspv_join_workspace(const dbspmspv_join_opts *opts, int32_t tokens, int64_t n, int64_t *bytes);
+int dbspmspv_join_backward(const dbspmspv_join_opts *opts, int32_t tokens, int64_t n, const void *out, int64_t ldo, const void *b, int64_t ldb, const float *stats, const void *w_block,
+                           const void *c_block, const void *gate, int64_t ldg, const void *w_next, const uint64_t *random, const void *dh, int64_t lddh, const void *dout, int64_t lddo,
+                           void *dr, int64_t lddr, void *db, int64_t lddb, float *dw_block, float *dc_block, void *dgate, int64_t lddg, float *dw_next, float *dc_next, void *workspace,
+                           int64_t workspace_bytes, dbspmspv_stream_t stream);
+
+/* y = drop(x), tokens x n in bf16 or (f32 = 1) fp32; in place where y is x.  Its gradient is the same call on dy with the same `random`.  A dropped entry is 0 whatever it was; with drop = 0 x is copied and
+ * `random` may be NULL.  Dropout of a block's output costs no call of its own: see dbspmspv_join.  n up to 2^31 - 1. */
+int dbspmspv_dropout(const void *x, int64_t ldx, int f32, int32_t tokens, int64_t n, float drop, const uint64_t *random, void *y, int64_t ldy, dbspmspv_stream_t stream);
+
+/*
+ * Log probabilities of the rows of `logits` (tokens x vocab, bf16 or fp32) with z = logits / temperature: one pass over the logits.
+ *   targets    a token id for every row, or NULL.  Negative: the row has none (its logprob is 0).  vocab or more: its logprob is NaN.
+ *   logprob    out: z[target] - log(sum exp(z)), or NULL;   entropy  out: -sum p log p, or NULL
+ *   stats      out, for the gradient: two fp32 a token, the largest logit M and log(sum exp((logits - M) / temperature)), or NULL
+ *   top        0 to 64, at most vocab: so many alternatives go to top_ids (tokens x top int32) and top_logprobs (or NULL), the largest logits first, equal ones by their index.
+ * -inf is a logit like others: probability 0, nothing to the entropy.  A row of them only: logprob and top_logprobs -inf, entropy 0, stats -inf.  A row with a NaN or +inf: logprob, entropy and top_logprobs
+ * are NaN (top_ids: NaN before everything else).
+ * The gradient: dlogits = (S - p sum(S) - dentropy p (log p + entropy)) / temperature, where S has dlogprob at the target and dtop (tokens x top) at top_ids (negative ones and those of vocab or more
+ * take part in nothing; a row whose target is vocab or more becomes NaN where dlogprob is given); zeros for a row with nothing left.  `entropy` and `stats` as the forward call left them.
+ * dlogprob, dentropy, dtop: fp32, NULL: none.  dlogits: tokens x vocab, bf16 or fp32 (dlogits_f32), in place where it is `logits`.
+ */
+int dbspmspv_logprobs(const void *logits, int64_t ldl, int logits_f32, int32_t tokens, int32_t vocab, float temperature, const int32_t *targets, float *logprob, float *entropy, float *stats,
+                      int32_t top, int32_t *top_ids, float *top_logprobs, dbspmspv_stream_t stream);
+int dbspmspv_logprobs_backward(const void *logits, int64_t ldl, int logits_f32, int32_t tokens, int32_t vocab, float temperature, const int32_t *targets, const float *stats, const float *entropy,
+                               int32_t top, const int32_t *top_ids, const float *dlogprob, const float *dentropy, const float *dtop, void *dlogits, int64_t ldd, int dlogits_f32,
+                               dbspmspv_stream_t stream);
+
 /* Waits for the stream the handle's last run / decode / db_bfs / linear call was enqueued on (not for the
  * whole device) and copies the statistics to the HOST struct `out`.  Returns the deferred
  * device status of the last call, which is then cleared.                                      */

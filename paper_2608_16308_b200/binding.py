@@ -23,6 +23,7 @@ LIB_PATH = os.environ.get("DBSPMSPV_LIBRARY") or os.path.join(HERE, "libdbspmspv
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALLOC, ERR_CUDA, ERR_CAPACITY, ERR_TIMEOUT, ERR_BOUNDS, ERR_TOO_LARGE, ERR_INTERNAL = range(10)
 F32, BF16, PATTERN = 0, 1, 2
 PLUS_TIMES, OR_AND, MIN_PLUS = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 PATH_AUTO, PATH_PUSH, PATH_PULL = 0, 1, 2
 FORMAT_AUTO, FORMAT_COO, FORMAT_CSR = 0, 1, 2
@@ -37,6 +38,7 @@ EXPORTED_SYMBOLS = (
     "dbspmspv_set_run_opts", "dbspmspv_destroy", "dbspmspv_strerror", "dbspmspv_compact_noalloc",
     "dbspmspv_test_bounded_wait", "dbspmspv_test_corrupt_entry", "dbspmspv_decode_batch", "dbspmspv_run_masked", "dbspmspv_count_call_bytes", "dbspmspv_probe_floor",
     "dbspmspv_linear_workspace", "dbspmspv_linear", "dbspmspv_gated", "dbspmspv_linear_backward", "dbspmspv_gated_backward",
+    "dbspmspv_default_join_opts", "dbspmspv_join_workspace", "dbspmspv_join", "dbspmspv_join_backward", "dbspmspv_dropout", "dbspmspv_logprobs", "dbspmspv_logprobs_backward",
 )
 
 
@@ -59,6 +61,12 @@ class RunOpts(ctypes.Structure):
                 ("decode_threshold", ctypes.c_float), ("decode_relu", ctypes.c_int32),
                 ("decode_x_f32", ctypes.c_int32), ("no_small_call", ctypes.c_int32),
                 ("reserved", ctypes.c_int32 * 2)]
+
+
+class JoinOpts(ctypes.Structure):
+    _fields_ = [("norm_block", ctypes.c_int32), ("norm_next", ctypes.c_int32), ("eps_block", ctypes.c_float), ("eps_next", ctypes.c_float),
+                ("scale", ctypes.c_float), ("drop", ctypes.c_float), ("stream_f32", ctypes.c_int32), ("block_f32", ctypes.c_int32),
+                ("params_f32", ctypes.c_int32), ("dblock_f32", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2)]
 
 
 class Stats(ctypes.Structure):
@@ -118,6 +126,16 @@ def lib() -> ctypes.CDLL:
         L.dbspmspv_gated.argtypes = [vp, vp, vp, i64, i32, ctypes.c_int, vp, i64, vp, vp, i64, vp, i64, vp]
         L.dbspmspv_linear_backward.argtypes = [vp, vp, i64, i32, ctypes.c_int, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp]
         L.dbspmspv_gated_backward.argtypes = [vp, vp, vp, i64, i32, ctypes.c_int, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp]
+        f32 = ctypes.c_float
+        L.dbspmspv_default_join_opts.argtypes = [ctypes.POINTER(JoinOpts)]
+        L.dbspmspv_default_join_opts.restype = None
+        L.dbspmspv_join_workspace.argtypes = [ctypes.POINTER(JoinOpts), i32, i64, ctypes.POINTER(i64)]
+        L.dbspmspv_join.argtypes = [ctypes.POINTER(JoinOpts), i32, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp]
+        L.dbspmspv_join_backward.argtypes = [ctypes.POINTER(JoinOpts), i32, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp,
+                                             vp, i64, vp]
+        L.dbspmspv_dropout.argtypes = [vp, i64, ctypes.c_int, i32, i64, f32, vp, vp, i64, vp]
+        L.dbspmspv_logprobs.argtypes = [vp, i64, ctypes.c_int, i32, i32, f32, vp, vp, vp, vp, i32, vp, vp, vp]
+        L.dbspmspv_logprobs_backward.argtypes = [vp, i64, ctypes.c_int, i32, i32, f32, vp, vp, vp, i32, vp, vp, vp, vp, vp, i64, ctypes.c_int, vp]
         L.dbspmspv_get_stats.argtypes = [vp, ctypes.POINTER(Stats)]
         L.dbspmspv_export_coo.argtypes = [vp, vp, vp, vp]
         L.dbspmspv_export_blocks.argtypes = [vp, vp, vp, vp, vp]
@@ -204,8 +222,19 @@ def _bind_streams() -> None:
 #                            workspace_bytes, stream=None)
 #   dbspmspv_gated_backward(gate, up, x, ldx, tokens, act, g, u, ldgu, dy, lddy, dx, lddx, dw_gate, dw_up,
 #                           workspace, workspace_bytes, stream=None)
+#   dbspmspv_join(opts, tokens, n, r, ldr, b, ldb, w_block, c_block, gate, ldg, w_next, c_next, random, out, ldo, h, ldh,
+#                 stats, stream=None)                                         opts: a JoinOpts (default_join_opts())
+#   dbspmspv_join_backward(opts, tokens, n, out, ldo, b, ldb, stats, w_block, c_block, gate, ldg, w_next, random, dh, lddh,
+#                          dout, lddo, dr, lddr, db, lddb, dw_block, dc_block, dgate, lddg, dw_next, dc_next, workspace,
+#                          workspace_bytes, stream=None)
+#   dbspmspv_dropout(x, ldx, f32, tokens, n, drop, random, y, ldy, stream=None)
+#   dbspmspv_logprobs(logits, ldl, logits_f32, tokens, vocab, temperature, targets, logprob, entropy, stats, top, top_ids,
+#                     top_logprobs, stream=None)
+#   dbspmspv_logprobs_backward(logits, ldl, logits_f32, tokens, vocab, temperature, targets, stats, entropy, top, top_ids,
+#                              dlogprob, dentropy, dtop, dlogits, ldd, dlogits_f32, stream=None)
 _FAST = ("dbspmspv_run", "dbspmspv_run_masked", "dbspmspv_decode", "dbspmspv_decode_batch", "db_bfs", "db_sssp",
-         "dbspmspv_linear", "dbspmspv_gated", "dbspmspv_linear_backward", "dbspmspv_gated_backward")
+         "dbspmspv_linear", "dbspmspv_gated", "dbspmspv_linear_backward", "dbspmspv_gated_backward",
+         "dbspmspv_join", "dbspmspv_join_backward", "dbspmspv_dropout", "dbspmspv_logprobs", "dbspmspv_logprobs_backward")
 
 
 def _not_built(*_args, **_kwargs):
@@ -216,7 +245,8 @@ def _not_built(*_args, **_kwargs):
 if _fastcall is not None:
     _fastcall.set_loader(_load_fast, _plain)
 (dbspmspv_run, dbspmspv_run_masked, dbspmspv_decode, dbspmspv_decode_batch, db_bfs, db_sssp,
- dbspmspv_linear, dbspmspv_gated, dbspmspv_linear_backward, dbspmspv_gated_backward) = (
+ dbspmspv_linear, dbspmspv_gated, dbspmspv_linear_backward, dbspmspv_gated_backward,
+ dbspmspv_join, dbspmspv_join_backward, dbspmspv_dropout, dbspmspv_logprobs, dbspmspv_logprobs_backward) = (
     getattr(_fastcall, name, _not_built) for name in _FAST)
 
 
@@ -229,6 +259,12 @@ def default_create_opts() -> CreateOpts:
 def default_run_opts() -> RunOpts:
     o = RunOpts()
     lib().dbspmspv_default_run_opts(ctypes.byref(o))
+    return o
+
+
+def default_join_opts() -> JoinOpts:
+    o = JoinOpts()
+    lib().dbspmspv_default_join_opts(ctypes.byref(o))
     return o
 
 
@@ -257,6 +293,13 @@ def dbspmspv_linear_workspace(h, up, tokens: int, backward: bool) -> int:
     """Bytes of workspace that a call on `tokens` tokens may need (dbspmspv_linear_workspace)."""
     out = ctypes.c_int64()
     _check(lib().dbspmspv_linear_workspace(h, up, tokens, int(backward), ctypes.byref(out)), "dbspmspv_linear_workspace")
+    return out.value
+
+
+def dbspmspv_join_workspace(opts: JoinOpts, tokens: int, n: int) -> int:
+    """Bytes of workspace that the gradient of a join needs for its sums over the tokens (dbspmspv_join_workspace)."""
+    out = ctypes.c_int64()
+    _check(lib().dbspmspv_join_workspace(ctypes.byref(opts), tokens, n, ctypes.byref(out)), "dbspmspv_join_workspace")
     return out.value
 
 

@@ -1,5 +1,6 @@
 /* Argument marshalling of the hot entry points (dbspmspv_run, dbspmspv_run_masked, dbspmspv_decode,
- * dbspmspv_decode_batch, db_bfs, db_sssp, dbspmspv_linear, dbspmspv_gated and their gradients) as a CPython extension: the same names, arguments,
+ * dbspmspv_decode_batch, db_bfs, db_sssp, dbspmspv_linear, dbspmspv_gated, dbspmspv_join, dbspmspv_logprobs and their gradients,
+ * dbspmspv_dropout) as a CPython extension: the same names, arguments,
  * defaults and errors as a ctypes wrapper, at a tenth of its cost.
  *
  * What bounds a short call is the host.  Through ctypes the marshalling alone took 6 us of a 10 us
@@ -13,7 +14,8 @@
 #include <Python.h>
 #include <stdint.h>
 
-enum { F_RUN, F_RUN_MASKED, F_DECODE, F_DECODE_BATCH, F_BFS, F_SSSP, F_LINEAR, F_GATED, F_LINEAR_BACKWARD, F_GATED_BACKWARD, N_FUNCS };
+enum { F_RUN, F_RUN_MASKED, F_DECODE, F_DECODE_BATCH, F_BFS, F_SSSP, F_LINEAR, F_GATED, F_LINEAR_BACKWARD, F_GATED_BACKWARD,
+       F_JOIN, F_JOIN_BACKWARD, F_DROPOUT, F_LOGPROBS, F_LOGPROBS_BACKWARD, N_FUNCS };
 
 static void *g_addr[N_FUNCS];
 static PyObject *g_load;          /* called once: loads the library and calls setup() */
@@ -85,6 +87,27 @@ static int as_i32(PyObject *o, int32_t *out) {
     if (!as_i64(o, &v)) return 0;
     *out = (int32_t)v;
     return 1;
+}
+
+static int as_f32(PyObject *o, float *out) {
+    PyObject *p = PyFloat_Check(o) ? Py_NewRef(o) : plain(o);
+    if (!p) return 0;
+    *out = (float)PyFloat_AsDouble(p);
+    Py_DECREF(p);
+    return !PyErr_Occurred();
+}
+
+/* a structure of options (a ctypes instance, whose memory it is), or None for NULL */
+static int as_struct(PyObject *o, Py_ssize_t size, void **out) {
+    Py_buffer b;
+    *out = NULL;
+    if (o == Py_None) return 1;
+    if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) return 0;
+    *out = b.buf;
+    const int ok = b.len == size;
+    PyBuffer_Release(&b);                 /* (the caller's reference keeps it) */
+    if (!ok) PyErr_SetString(PyExc_TypeError, "a structure of another size is wanted");
+    return ok;
 }
 
 /* the stream argument: None (or absent) is torch's current stream on the current device */
@@ -304,6 +327,101 @@ static PyObject *f_gated_backward(PyObject *self, PyObject *const *args, Py_ssiz
     return finish(s, "dbspmspv_gated_backward");
 }
 
+/* The calls without a handle: what their slots hold, a letter each (p address, l 64 bits, i 32 bits, f float, o a structure of join options, s the stream) */
+enum { MOST_SLOTS = 32, JOIN_OPTS_BYTES = 48 };
+typedef union {
+    void *p;
+    int64_t l;
+    int32_t i;
+    float f;
+} slot_t;
+static int take(const char *fn, const char *kinds, PyObject *const *args, Py_ssize_t nargs, PyObject *kw, const char *const *names, int n, slot_t *v) {
+    PyObject *a[MOST_SLOTS];
+    if (!ready() || !unpack(fn, args, nargs, kw, names, n, a)) return 0;
+    for (int k = 0; k < n; ++k) {
+        int ok = 0;
+        switch (kinds[k]) {
+            case 'p': ok = as_pointer(a[k], &v[k].p); break;
+            case 'l': ok = as_i64(a[k], &v[k].l); break;
+            case 'i': ok = as_i32(a[k], &v[k].i); break;
+            case 'f': ok = as_f32(a[k], &v[k].f); break;
+            case 'o': ok = as_struct(a[k], JOIN_OPTS_BYTES, &v[k].p); break;
+            case 's': ok = as_stream(a[k], &v[k].p); break;
+        }
+        if (!ok) return 0;
+    }
+    return 1;
+}
+
+typedef int (*join_fn)(const void *, int32_t, int64_t, const void *, int64_t, const void *, int64_t, const void *, const void *, const void *, int64_t, const void *, const void *,
+                       const void *, void *, int64_t, void *, int64_t, void *, void *);
+static PyObject *f_join(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kw) {
+    static const char *const names[] = {"opts", "tokens", "n", "r", "ldr", "b", "ldb", "w_block", "c_block", "gate", "ldg", "w_next", "c_next", "random", "out", "ldo", "h", "ldh", "stats", "stream"};
+    slot_t v[20];
+    if (!take("dbspmspv_join", "oilplplppplpppplplps", args, nargs, kw, names, 20, v)) return NULL;
+    int s;
+    Py_BEGIN_ALLOW_THREADS
+    s = ((join_fn)g_addr[F_JOIN])(v[0].p, v[1].i, v[2].l, v[3].p, v[4].l, v[5].p, v[6].l, v[7].p, v[8].p, v[9].p, v[10].l, v[11].p, v[12].p, v[13].p, v[14].p, v[15].l, v[16].p, v[17].l,
+                                  v[18].p, v[19].p);
+    Py_END_ALLOW_THREADS
+    return finish(s, "dbspmspv_join");
+}
+
+typedef int (*join_backward_fn)(const void *, int32_t, int64_t, const void *, int64_t, const void *, int64_t, const void *, const void *, const void *, const void *, int64_t, const void *,
+                                const void *, const void *, int64_t, const void *, int64_t, void *, int64_t, void *, int64_t, void *, void *, void *, int64_t, void *, void *, void *, int64_t,
+                                void *);
+static PyObject *f_join_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kw) {
+    static const char *const names[] = {"opts", "tokens", "n", "out", "ldo", "b", "ldb", "stats", "w_block", "c_block", "gate", "ldg", "w_next", "random", "dh", "lddh", "dout", "lddo", "dr",
+                                        "lddr", "db", "lddb", "dw_block", "dc_block", "dgate", "lddg", "dw_next", "dc_next", "workspace", "workspace_bytes", "stream"};
+    slot_t v[31];
+    if (!take("dbspmspv_join_backward", "oilplplpppplppplplplplppplpppls", args, nargs, kw, names, 31, v)) return NULL;
+    int s;
+    Py_BEGIN_ALLOW_THREADS
+    s = ((join_backward_fn)g_addr[F_JOIN_BACKWARD])(v[0].p, v[1].i, v[2].l, v[3].p, v[4].l, v[5].p, v[6].l, v[7].p, v[8].p, v[9].p, v[10].p, v[11].l, v[12].p, v[13].p, v[14].p, v[15].l,
+                                                    v[16].p, v[17].l, v[18].p, v[19].l, v[20].p, v[21].l, v[22].p, v[23].p, v[24].p, v[25].l, v[26].p, v[27].p, v[28].p, v[29].l, v[30].p);
+    Py_END_ALLOW_THREADS
+    return finish(s, "dbspmspv_join_backward");
+}
+
+typedef int (*dropout_fn)(const void *, int64_t, int, int32_t, int64_t, float, const void *, void *, int64_t, void *);
+static PyObject *f_dropout(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kw) {
+    static const char *const names[] = {"x", "ldx", "f32", "tokens", "n", "drop", "random", "y", "ldy", "stream"};
+    slot_t v[10];
+    if (!take("dbspmspv_dropout", "pliilfppls", args, nargs, kw, names, 10, v)) return NULL;
+    int s;
+    Py_BEGIN_ALLOW_THREADS
+    s = ((dropout_fn)g_addr[F_DROPOUT])(v[0].p, v[1].l, v[2].i, v[3].i, v[4].l, v[5].f, v[6].p, v[7].p, v[8].l, v[9].p);
+    Py_END_ALLOW_THREADS
+    return finish(s, "dbspmspv_dropout");
+}
+
+typedef int (*logprobs_fn)(const void *, int64_t, int, int32_t, int32_t, float, const void *, void *, void *, void *, int32_t, void *, void *, void *);
+static PyObject *f_logprobs(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kw) {
+    static const char *const names[] = {"logits", "ldl", "logits_f32", "tokens", "vocab", "temperature", "targets", "logprob", "entropy", "stats", "top", "top_ids", "top_logprobs", "stream"};
+    slot_t v[14];
+    if (!take("dbspmspv_logprobs", "pliiifppppipps", args, nargs, kw, names, 14, v)) return NULL;
+    int s;
+    Py_BEGIN_ALLOW_THREADS
+    s = ((logprobs_fn)g_addr[F_LOGPROBS])(v[0].p, v[1].l, v[2].i, v[3].i, v[4].i, v[5].f, v[6].p, v[7].p, v[8].p, v[9].p, v[10].i, v[11].p, v[12].p, v[13].p);
+    Py_END_ALLOW_THREADS
+    return finish(s, "dbspmspv_logprobs");
+}
+
+typedef int (*logprobs_backward_fn)(const void *, int64_t, int, int32_t, int32_t, float, const void *, const void *, const void *, int32_t, const void *, const void *, const void *, const void *,
+                                    void *, int64_t, int, void *);
+static PyObject *f_logprobs_backward(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kw) {
+    static const char *const names[] = {"logits", "ldl", "logits_f32", "tokens", "vocab", "temperature", "targets", "stats", "entropy", "top", "top_ids", "dlogprob", "dentropy", "dtop", "dlogits",
+                                        "ldd", "dlogits_f32", "stream"};
+    slot_t v[18];
+    if (!take("dbspmspv_logprobs_backward", "pliiifpppippppplis", args, nargs, kw, names, 18, v)) return NULL;
+    int s;
+    Py_BEGIN_ALLOW_THREADS
+    s = ((logprobs_backward_fn)g_addr[F_LOGPROBS_BACKWARD])(v[0].p, v[1].l, v[2].i, v[3].i, v[4].i, v[5].f, v[6].p, v[7].p, v[8].p, v[9].i, v[10].p, v[11].p, v[12].p, v[13].p, v[14].p, v[15].l,
+                                                            v[16].i, v[17].p);
+    Py_END_ALLOW_THREADS
+    return finish(s, "dbspmspv_logprobs_backward");
+}
+
 /* set_loader(load, plain) */
 static PyObject *f_set_loader(PyObject *self, PyObject *args) {
     PyObject *load, *pl;
@@ -341,6 +459,8 @@ static PyMethodDef methods[] = {
     FAST("dbspmspv_run", f_run), FAST("dbspmspv_run_masked", f_run_masked), FAST("dbspmspv_decode", f_decode),
     FAST("dbspmspv_decode_batch", f_decode_batch), FAST("db_bfs", f_bfs), FAST("db_sssp", f_sssp),
     FAST("dbspmspv_linear", f_linear), FAST("dbspmspv_gated", f_gated), FAST("dbspmspv_linear_backward", f_linear_backward), FAST("dbspmspv_gated_backward", f_gated_backward),
+    FAST("dbspmspv_join", f_join), FAST("dbspmspv_join_backward", f_join_backward), FAST("dbspmspv_dropout", f_dropout),
+    FAST("dbspmspv_logprobs", f_logprobs), FAST("dbspmspv_logprobs_backward", f_logprobs_backward),
     {"set_loader", f_set_loader, METH_VARARGS, NULL}, {"setup", f_setup, METH_VARARGS, NULL}, {"streams", f_streams, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL}};
 
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
