@@ -1,13 +1,15 @@
 // Log probabilities of the rows of logits, with entropy and top alternatives, and the gradient.
 //
 // One pass: every thread keeps the largest logit m that it has met, s = sum e and u = sum x e with e = 2^x, x = (l - m) log2(e) / T, and moves s and u over when m
-// grows (u to u + d s, both times 2^d); states of threads, warps and the blocks of a cluster are joined the same way.  Then log sum = log s, entropy = log s - log(2) u / s.  Relative to m nothing overflows, whatever
-// the logits.  What bounds it is HBM, with the exponential's pipe (16 a clock and SM) at two thirds of its rate for bf16.
+// grows (u to u + d s, both times 2^d); states of threads, warps and the blocks of a cluster are brought to their largest m and added.  Then log sum = log s, entropy = log s - log(2) u / s.  Relative to
+// m nothing overflows, whatever the logits.  What bounds it is HBM (fp32) or instructions (bf16: six an entry, and the exponential's pipe, 16 a clock and SM, at two thirds of its rate), so two entries are
+// multiplied and added at a time, and x is one product-and-sum with the rounded m log2(e) / T, whose rounding is made up for once per thread.  Thread blocks walk the rows, and the vectors to come, the next
+// row's too, are copied ahead into slots of shared memory that belong to the thread itself (cp.async, no barrier): the sums and the selection at the end of a row leave HBM busy.
 //
-// Alternatives.  A thread's own logits (its unit) are known by their largest and its place.  Where at least k groups of threads have a unit of at least tau, no logit below tau is among the k largest, so
-// tau is the least of the groups' largest; only units that reach it are read a second time (they come from L2), and of their logits those that reach tau are counted against each other: a candidate's place
-// is the number of those in front of it.  No order of the logits makes this long: units that share the largest value are told apart by their places, tau is searched exactly if too many are
-// left, and the last resort (NaN, or k units full of the largest) is k passes.
+// Alternatives.  A thread's own logits (its unit) are known by their largest and its place.  Where at least k groups of threads have a unit of at least tau, no logit below tau is among the k largest; the
+// k-th largest of the groups' largest (or a little less) is such a tau.  Only units that reach it are read a second time (they come from L2), and of their logits those that reach tau are counted against
+// each other: a candidate's place is the number of those in front of it.  No order of the logits makes this long: if too many reach tau (equal ones above all), tau is searched exactly among the units, told apart by their places; the last
+// resort (NaN, or k units full of the largest) is k passes.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -16,18 +18,26 @@
 
 namespace dbs {
 
-constexpr int LP_CTA = 512, LP_WARPS = LP_CTA / 32;
+constexpr int LP_CTA = 128, LP_WARPS = LP_CTA / 32;
 constexpr int LP_MAX_TOP = 64;
-constexpr int LP_CANDIDATES = LP_CTA;        // a thread ranks one
+constexpr int LP_CANDIDATES = 256;
 constexpr int LP_CLUSTER = 8;
-constexpr int LP_FLIGHT = 4;                 // loads of 16 bytes in flight per thread
+constexpr int LP_FLIGHT = 4;                 // vectors of 16 bytes that a thread takes in one round
+constexpr int LP_AHEAD = 3;                  // rounds in flight or in hand
+constexpr int LP_PER_SM = 7;                 // thread blocks
+constexpr int LP_SMEM = LP_AHEAD * LP_FLIGHT * LP_CTA * 16;
+constexpr int LP_GROUP = 2;                  // threads of a group: 64 groups
+constexpr int LP_GROUPS = LP_CTA / LP_GROUP;
+constexpr int LP_SLACK = 4;                  // groups more than k that may reach tau
 constexpr float LP_NONE = -1000.f;           // 2^LP_NONE is 0, and its product with 0 too
-static_assert(LP_WARPS <= 32 && LP_MAX_TOP <= LP_CTA / 8, "groups of eight lanes and more");
+constexpr float LP_LOW = -1e30f;             // what -inf is taken for in sums: its probability is 0 as well, and 0 times it is 0
+constexpr float LP_NEAR = 4096.f;            // |m log2(e) / T| up to which the short form of x is good
+static_assert(LP_WARPS <= 32 && LP_MAX_TOP <= LP_GROUPS && LP_GROUPS == 64, "a group for every alternative, two to a lane");
 
 struct LpArgs {
     const void *logits;
     int64_t ld;
-    int32_t tokens, vocab, cluster, top;
+    int32_t tokens, vocab, cluster, top, rounds;  // rounds: of a thread block's share of a row, at most
     float slope, inv_t;                       // log2(e) / T, 1 / T
     const int32_t *targets;
     float *logprob, *entropy, *stats;
@@ -57,14 +67,22 @@ __device__ __forceinline__ float of_order(uint32_t k) {
 __device__ __forceinline__ uint64_t candidate(float l, uint32_t index) { return (uint64_t)order_of(l) << 32 | (0xFFFFFFFEu - index); }   // never all ones, not even of a NaN
 __device__ __forceinline__ int32_t place_of(uint64_t c) { return (int32_t)(0xFFFFFFFEu - (uint32_t)c); }
 
+// States of the lanes brought to the largest m of a warp's first `lanes` lanes (a power of two) and added; the same in each of them
 struct LpState {
     float m, s, u;
-    __device__ __forceinline__ void join(float m2, float s2, float u2, float slope) {
-        const float top = fmaxf(m, m2);
-        const float d = m == top ? 0.f : fmaxf((m - top) * slope, LP_NONE), d2 = m2 == top ? 0.f : fmaxf((m2 - top) * slope, LP_NONE);
-        const float f = exp_2(d), f2 = exp_2(d2);
-        u = (u + d * s) * f + (u2 + d2 * s2) * f2;
-        s = s * f + s2 * f2;
+    template <int LANES>
+    __device__ __forceinline__ void join(float slope) {
+        float top = m;
+#pragma unroll
+        for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+        const float d = m == top ? 0.f : fmaxf((m - top) * slope, LP_NONE), f = exp_2(d);
+        u = (u + d * s) * f;
+        s *= f;
+#pragma unroll
+        for (int o = LANES / 2; o; o >>= 1) {
+            s += __shfl_xor_sync(FULL, s, o);
+            u += __shfl_xor_sync(FULL, u, o);
+        }
         m = top;
     }
 };
@@ -83,7 +101,7 @@ struct LpRow {
         if (head > vocab) head = vocab;
         vectors = (vocab - head) / V;
         tail = vocab - head - vectors * V;
-        const int per = (vectors + cluster - 1) / cluster;
+        const int per = cluster == 1 ? vectors : (vectors + cluster - 1) / cluster;
         from = rank * per < vectors ? rank * per : vectors;
         to = from + per < vectors ? from + per : vectors;
         if (rank != 0) head = -head;         // (its size is still needed for the places)
@@ -92,7 +110,8 @@ struct LpRow {
     __device__ __forceinline__ int heads() const { return head > 0 ? head : 0; }
     __device__ __forceinline__ int place(int vector) const { return (head < 0 ? -head : head) + vector * V; }
     __device__ __forceinline__ float one(int i) const { return F32 ? reinterpret_cast<const float *>(p)[i] : bf16_lo(reinterpret_cast<const uint16_t *>(p)[i]); }
-    __device__ __forceinline__ uint4 raw(int vector) const { return *reinterpret_cast<const uint4 *>(p + (int64_t)place(vector) * (F32 ? 4 : 2)); }
+    __device__ __forceinline__ const uint4 *at(int vector) const { return reinterpret_cast<const uint4 *>(p + (int64_t)place(vector) * (F32 ? 4 : 2)); }
+    __device__ __forceinline__ uint4 raw(int vector) const { return *at(vector); }
     __device__ __forceinline__ static void values(uint4 q, float v[V]) {
         if constexpr (F32) {
             v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
@@ -101,27 +120,71 @@ struct LpRow {
 };
 
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b ? a : b; }
+__device__ __forceinline__ uint32_t max_bf16(uint32_t a, uint32_t b) {       // two at a time, NaN left out
+    uint32_t d;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t max_nan_bf16(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// whether x may be l slope - ref: the rounding of ref is small, and LP_LOW slope is a number far below it
+__device__ __forceinline__ bool short_form(float ref, float slope) { return fabsf(ref) <= LP_NEAR && slope <= LP_NEAR && slope >= 1e-20f; }
+// largest of N vectors, NaN left out
+template <bool F32, int N = 1>
+__device__ __forceinline__ float largest(const uint4 (&q)[N]) {
+    if constexpr (F32) {
+        float l = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < N; ++i) l = fmaxf(l, fmaxf(fmaxf(__uint_as_float(q[i].x), __uint_as_float(q[i].y)), fmaxf(__uint_as_float(q[i].z), __uint_as_float(q[i].w))));
+        return l;
+    } else {
+        uint32_t w = max_bf16(max_bf16(q[0].x, q[0].y), max_bf16(q[0].z, q[0].w));
+#pragma unroll
+        for (int i = 1; i < N; ++i) w = max_bf16(w, max_bf16(max_bf16(q[i].x, q[i].y), max_bf16(q[i].z, q[i].w)));
+        return fmaxf(bf16_lo(w), bf16_hi(w));
+    }
+}
+template <bool F32>
+__device__ __forceinline__ float largest(uint4 q) {
+    const uint4 one[1] = {q};
+    return largest<F32, 1>(one);
+}
+// a vector's entries two at a time; CLAMP: -inf (and what lies near it) as LP_LOW
+template <bool F32, bool CLAMP>
+__device__ __forceinline__ void pairs_of(uint4 q, f32x2 v[F32 ? 2 : 4]) {
+    if constexpr (F32) {
+        auto one = [](uint32_t w) { return CLAMP ? max_nan(__uint_as_float(w), LP_LOW) : __uint_as_float(w); };
+        v[0] = pair(one(q.x), one(q.y));
+        v[1] = pair(one(q.z), one(q.w));
+    } else {
+        constexpr uint32_t LOW2 = 0xF14AF14Au;                               // -1.0e30 in bf16, twice
+        auto two = [](uint32_t w) { return bf16_pair(CLAMP ? max_nan_bf16(w, LOW2) : w); };
+        v[0] = two(q.x); v[1] = two(q.y); v[2] = two(q.z); v[3] = two(q.w);
+    }
+}
 
 struct LpShared {
-    float m[LP_WARPS], s[LP_WARPS], u[LP_WARPS];
-    uint64_t group[LP_WARPS];
+    float m[2][LP_WARPS], s[2][LP_WARPS], u[2][LP_WARPS];       // of rows in turn
+    uint32_t group[2][LP_GROUPS];
+    uint64_t largest[LP_WARPS];
     uint64_t found[LP_CANDIDATES];
-    uint64_t best[LP_CLUSTER][LP_MAX_TOP];   // of every block of the cluster, in the first one
+    uint64_t best[LP_CLUSTER * LP_MAX_TOP];  // of every block of the cluster, in the first one
     float cm[LP_CLUSTER], cs[LP_CLUSTER], cu[LP_CLUSTER];
     uint16_t units[LP_CTA];
     int n_units, n_found;
 };
 
-// logits of at least tau among the units of at least tau -> sh.found (their number in sh.n_found, which may be more than there is room for)
+// logits of at least tau among the units of at least tau -> sh.found (their number in sh.n_found, which may be more than there is room for).  The counts are 0 before it.
 template <bool F32>
 __device__ __forceinline__ void lp_collect(const LpRow<F32> &row, LpShared &sh, uint64_t unit, uint64_t tau, int vocab) {
     const int tid = threadIdx.x;
-    if (tid == 0) sh.n_units = sh.n_found = 0;
-    __syncthreads();
     if (unit >= tau && unit) sh.units[atomicAdd(&sh.n_units, 1)] = (uint16_t)tid;
+    const float least = of_order((uint32_t)(tau >> 32));
     auto meet = [&](float l, int place, int of) {
-        if (candidate(l, of) >= tau) {
+        if (!tau || (l >= least && candidate(l, of) >= tau)) {
             const int i = atomicAdd(&sh.n_found, 1);
             if (i < LP_CANDIDATES) sh.found[i] = candidate(l, place);
         }
@@ -129,48 +192,72 @@ __device__ __forceinline__ void lp_collect(const LpRow<F32> &row, LpShared &sh, 
     if (tid < row.heads()) meet(row.one(tid), tid, tid);
     if (tid < row.tail) meet(row.one(vocab - row.tail + tid), vocab - row.tail + tid, vocab - row.tail + tid);
     __syncthreads();
-    const int per = (row.to - row.from + LP_CTA - 1) / LP_CTA, all = sh.n_units * per;
+    const int n_units = sh.n_units, all = n_units * ((row.to - row.from + LP_CTA - 1) / LP_CTA);
     for (int i = tid; i < all; i += LP_CTA) {
-        const int v = row.from + i / sh.n_units * LP_CTA + sh.units[i % sh.n_units];
+        const unsigned round = (unsigned)i / (unsigned)n_units;
+        const int v = row.from + (int)round * LP_CTA + sh.units[i - (int)round * n_units];
         if (v >= row.to) continue;
+        const uint4 q = row.raw(v);
+        if (tau && largest<F32>(q) < least) continue;
         float l[LpRow<F32>::V];
-        LpRow<F32>::values(row.raw(v), l);
+        LpRow<F32>::values(q, l);
 #pragma unroll
         for (int j = 0; j < LpRow<F32>::V; ++j) meet(l[j], row.place(v) + j, row.place(v));
     }
     __syncthreads();
 }
 
-// the block's k largest into best[0 .. k), zeros behind them
+// a number that at least k of the 64 group maxima reach (two to a lane), and not many more: halves what lies between the least and the largest
+__device__ __forceinline__ uint32_t lp_least(uint32_t a, uint32_t b, int k) {
+    uint32_t lo = __reduce_min_sync(FULL, min(a, b)), hi = __reduce_max_sync(FULL, max(a, b));
+    while (lo < hi) {
+        const uint32_t mid = hi - (hi - lo) / 2;
+        const int n = __popc(__ballot_sync(FULL, a >= mid)) + __popc(__ballot_sync(FULL, b >= mid));
+        if (n >= k) lo = mid;
+        else hi = mid - 1;
+        if (n >= k && n <= k + LP_SLACK) break;
+    }
+    return lo;
+}
+
+// the block's k largest into best[0 .. k), zeros behind them.  `most`: the thread's largest, as order_of has it (0: it has none); `group`: what at least k groups' largest reach, as order_of has it.
 template <bool F32>
-__device__ __forceinline__ void lp_top(const LpRow<F32> &row, LpShared &sh, uint64_t unit, bool plain, int k, int vocab, uint64_t *best) {
+__device__ __forceinline__ void lp_top(const LpRow<F32> &row, LpShared &sh, uint32_t most, uint32_t group, bool plain, int k, int vocab, uint64_t *best) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid < k) best[tid] = 0;
+    uint64_t unit = most ? (uint64_t)most << 32 | 0xFFFFFFFFu : 0;         // (the place is needed where values do not decide)
     bool done = false;
     if (plain) {
-        uint64_t g = unit, least;
-        const int lanes = k <= LP_WARPS ? 32 : k <= 2 * LP_WARPS ? 16 : 8;
-        for (int o = 1; o < lanes; o <<= 1) g = max64(g, __shfl_xor_sync(FULL, g, o));
-        for (int o = lanes; o < 32; o <<= 1) g = min64(g, __shfl_xor_sync(FULL, g, o));
-        if (lane == 0) sh.group[warp] = g;
-        __syncthreads();
-        least = sh.group[0];
-        for (int w = 1; w < LP_WARPS; ++w) least = min64(least, sh.group[w]);
-        // (a group without logits: the search below finds tau)
-        if (least) lp_collect(row, sh, unit, least, vocab);
-        if (!least || sh.n_found > LP_CANDIDATES) {
-            least = 0;
-            for (int bit = 63; bit >= 0; --bit) {
-                const uint64_t trial = least | 1ull << bit;
-                if (__syncthreads_count(unit >= trial) >= k) least = trial;
+        // (a group without logits: the search finds tau)
+        if (group) lp_collect(row, sh, unit, (uint64_t)group << 32, vocab);
+        if (!group || sh.n_found > LP_CANDIDATES) {
+            // the unit's place: of the first vector (or entry) that has its largest
+            if (unit) {
+                const float most = of_order((uint32_t)(unit >> 32));
+                int place = tid < row.heads() && row.one(tid) == most ? tid : -1;
+                for (int v = row.from + tid; place < 0 && v < row.to; v += LP_CTA)
+                    if (largest<F32>(row.raw(v)) == most) place = row.place(v);
+                unit = candidate(most, place < 0 ? vocab - row.tail + tid : place);
             }
-            lp_collect(row, sh, unit, least, vocab);
+            uint64_t tau = 0;
+            for (int bit = 63; bit >= 0; --bit) {
+                const uint64_t trial = tau | 1ull << bit;
+                if (__syncthreads_count(unit >= trial) >= k) tau = trial;
+            }
+            if (tid == 0) sh.n_units = sh.n_found = 0;
+            __syncthreads();
+            lp_collect(row, sh, unit, tau, vocab);
         }
-        done = sh.n_found <= LP_CANDIDATES;
-        if (done && tid < sh.n_found) {
-            const uint64_t mine = sh.found[tid];
+        const int n = sh.n_found;
+        done = n <= LP_CANDIDATES;
+        for (int c = tid; done && c < max(n, k); c += LP_CTA) {
+            if (c >= n) {
+                best[c] = 0;
+                continue;
+            }
+            const uint64_t mine = sh.found[c];
             int before = 0;
-            for (int i = 0; i < sh.n_found; ++i) before += sh.found[i] > mine;
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) before += sh.found[i] > mine;
             if (before < k) best[before] = mine;
         }
     }
@@ -183,138 +270,208 @@ __device__ __forceinline__ void lp_top(const LpRow<F32> &row, LpShared &sh, uint
                 const uint64_t c = candidate(l, place);
                 if (c < last) b = max64(b, c);
             };
-            if (tid < row.heads()) meet(row.one(tid), tid);
-            if (tid < row.tail) meet(row.one(vocab - row.tail + tid), vocab - row.tail + tid);
-            for (int v = row.from + tid; v < row.to; v += LP_CTA) {
-                float l[LpRow<F32>::V];
-                LpRow<F32>::values(row.raw(v), l);
+            if (last) {                       // (0: there are no more here)
+                if (tid < row.heads()) meet(row.one(tid), tid);
+                if (tid < row.tail) meet(row.one(vocab - row.tail + tid), vocab - row.tail + tid);
+                for (int v = row.from + tid; v < row.to; v += LP_CTA) {
+                    float l[LpRow<F32>::V];
+                    LpRow<F32>::values(row.raw(v), l);
 #pragma unroll
-                for (int i = 0; i < LpRow<F32>::V; ++i) meet(l[i], row.place(v) + i);
+                    for (int i = 0; i < LpRow<F32>::V; ++i) meet(l[i], row.place(v) + i);
+                }
             }
             for (int o = 16; o; o >>= 1) b = max64(b, __shfl_xor_sync(FULL, b, o));
             __syncthreads();
-            if (lane == 0) sh.group[warp] = b;
+            if (lane == 0) sh.largest[warp] = b;
             __syncthreads();
-            last = sh.group[0];
-            for (int w = 1; w < LP_WARPS; ++w) last = max64(last, sh.group[w]);
+            last = sh.largest[0];
+            for (int w = 1; w < LP_WARPS; ++w) last = max64(last, sh.largest[w]);
             if (tid == 0) best[j] = last;
-            if (!last) break;                 // (no more logits here; the same in every thread)
         }
     }
-    __syncthreads();
 }
 
-template <bool F32>
-__global__ void __launch_bounds__(LP_CTA, 2) k_logprobs(const __grid_constant__ LpArgs a) {
+template <bool F32, bool ENTROPY>
+__global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_constant__ LpArgs a) {
+    extern __shared__ __align__(16) uint4 s_slots[];
     __shared__ LpShared sh;
     constexpr int V = LpRow<F32>::V;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rank = (int)(blockIdx.x % a.cluster);
-    const int64_t t = blockIdx.x / a.cluster;
-    if (a.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    const int rank = (int)(blockIdx.x % a.cluster), step = gridDim.x / a.cluster;
+    uint4 *slot = s_slots + tid;              // [round][vector][thread]
+    if (tid == 0) sh.n_units = sh.n_found = 0;
     pdl_wait();
     pdl_trigger();
-    const LpRow<F32> row(a.logits, a.ld, t, a.vocab, rank, a.cluster);
-    int target = -1;
-    float at_target = 0.f;
-    if (a.targets && rank == 0 && tid == 0) {
-        target = a.targets[t];
-        if (target >= 0 && target < a.vocab) at_target = row.one(target);
-    }
     const float slope = a.slope;
-    LpState st = {-INFINITY, 0.f, 0.f};
-    int unit_at = tid < row.heads() ? tid : row.from + tid < row.to ? row.place(row.from + tid) : tid < row.tail ? a.vocab - row.tail + tid : -1;
-    auto meet = [&](float most, int place) {
-        if (most > st.m) {
-            const float d = fmaxf((st.m - most) * slope, LP_NONE), f = exp_2(d);
-            st.u = (st.u + d * st.s) * f;
-            st.s *= f;
-            st.m = most;
-            unit_at = place;
+    // rounds to come: of row t_next, the n_next-th
+    int64_t t_next = blockIdx.x / a.cluster;
+    int n_next = 0;
+    LpRow<F32> next(a.logits, a.ld, t_next < a.tokens ? t_next : 0, a.vocab, rank, a.cluster);
+    auto ahead = [&](int at) {
+        if (t_next < a.tokens) {
+            const int v0 = next.from + n_next * LP_FLIGHT * LP_CTA + tid;
+#pragma unroll
+            for (int i = 0; i < LP_FLIGHT; ++i)
+                if (v0 + i * LP_CTA < next.to) copy_ahead(slot + (at * LP_FLIGHT + i) * LP_CTA, next.at(v0 + i * LP_CTA));
+            if (++n_next == a.rounds) {
+                n_next = 0;
+                t_next += step;
+                if (t_next < a.tokens) next = LpRow<F32>(a.logits, a.ld, t_next, a.vocab, rank, a.cluster);
+            }
         }
+        close_ahead();
     };
-    auto add = [&](float l) {
-        const float x = (l - (st.m == -INFINITY ? 0.f : st.m)) * slope, e = exp_2(x);
-        st.s += e;
-        st.u += max_nan(x, LP_NONE) * e;
-    };
-    if (tid < row.heads()) {
-        const float l = row.one(tid);
-        meet(l, tid);
-        add(l);
-    }
-    for (int v0 = row.from + tid; v0 < row.to; v0 += LP_FLIGHT * LP_CTA) {
-        uint4 q[LP_FLIGHT];
 #pragma unroll
-        for (int i = 0; i < LP_FLIGHT; ++i)
-            if (v0 + i * LP_CTA < row.to) q[i] = row.raw(v0 + i * LP_CTA);
-#pragma unroll
-        for (int i = 0; i < LP_FLIGHT; ++i) {
-            if (v0 + i * LP_CTA >= row.to) break;
-            float l[V];
-            LpRow<F32>::values(q[i], l);
-            float most = l[0];
-#pragma unroll
-            for (int j = 1; j < V; ++j) most = fmaxf(most, l[j]);
-            meet(most, row.place(v0 + i * LP_CTA));
-#pragma unroll
-            for (int j = 0; j < V; ++j) add(l[j]);
+    for (int i = 0; i < LP_AHEAD; ++i) ahead(i);
+    int at = 0, parity = 0;
+    for (int64_t t = blockIdx.x / a.cluster; t < a.tokens; t += step, parity ^= 1) {
+        // (a cluster: the first block has started, and is done with what the others gave it)
+        if (a.cluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        const LpRow<F32> row(a.logits, a.ld, t, a.vocab, rank, a.cluster);
+        int target = -1;
+        float at_target = 0.f;
+        if (a.targets && rank == 0 && tid == 0) {
+            target = a.targets[t];
+            if (target >= 0 && target < a.vocab) at_target = row.one(target);
         }
-    }
-    if (tid < row.tail) {
-        const float l = row.one(a.vocab - row.tail + tid);
-        meet(l, a.vocab - row.tail + tid);
-        add(l);
-    }
-    const uint64_t unit = unit_at < 0 ? 0 : candidate(st.m, unit_at);
+        float m = -INFINITY, ref = 0.f;       // ref = fl(m slope): x = l slope - ref is off by m slope - ref
+        f32x2 s = 0, u = 0;
+        bool near = false;
+        // the sums relative to m in place of ref, and back: 2^-r and 2^r, |r| <= 2^-13
+        auto settled = [&](float sign, float s0, float u0) {
+            const float r = near ? sign * fmaf(m, slope, -ref) : 0.f, y = r * 0.6931471805599453f, f = 1.f - y + 0.5f * y * y;
+            return make_float2(s0 * f, (u0 - r * s0) * f);
+        };
+        auto meet = [&](float most) {
+            if (most > m) {
+                float2 v = settled(1.f, sum2(s), sum2(u));
+                const float d = fmaxf((m - most) * slope, LP_NONE), f = exp_2(d);
+                m = most;
+                ref = most * slope;
+                near = short_form(ref, slope);
+                v = settled(-1.f, v.x * f, (v.y + d * v.x) * f);
+                s = pair(v.x, 0.f);
+                u = pair(v.y, 0.f);
+            }
+        };
+        auto add = [&](float l) {             // any m: one that is -inf has met -inf and NaN only
+            const float x = near ? fmaf(max_nan(l, LP_LOW), slope, -ref) : (l - (m == -INFINITY ? 0.f : m)) * slope, e = exp_2(x);
+            s = add2(s, pair(e, 0.f));
+            if (ENTROPY) u = add2(u, pair(max_nan(x, LP_NONE) * e, 0.f));
+        };
+        const bool any = tid < row.heads() || row.from + tid < row.to || tid < row.tail;
+        if (tid < row.heads()) {
+            const float l = row.one(tid);
+            meet(l);
+            add(l);
+        }
+        int left = (row.to - row.from - tid + LP_CTA - 1) / LP_CTA;         // vectors of this thread
+        for (int n = 0; n < a.rounds; ++n, left -= LP_FLIGHT) {
+            wait_ahead<LP_AHEAD - 1>();
+            uint4 q[LP_FLIGHT];
+            constexpr uint32_t NONE = F32 ? 0xFF800000u : 0xFF80FF80u;      // -inf
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const float m2 = __shfl_xor_sync(FULL, st.m, o), s2 = __shfl_xor_sync(FULL, st.s, o), u2 = __shfl_xor_sync(FULL, st.u, o);
-        st.join(m2, s2, u2, slope);
-    }
-    if (lane == 0) { sh.m[warp] = st.m; sh.s[warp] = st.s; sh.u[warp] = st.u; }
-    __syncthreads();
-    st = {sh.m[0], sh.s[0], sh.u[0]};
-    for (int w = 1; w < LP_WARPS; ++w) st.join(sh.m[w], sh.s[w], sh.u[w], slope);
-    uint64_t *best = sh.best[0];
-    if (a.top) {
-        // (behind the sums: NaN or +inf among the block's logits makes its sum NaN)
-        if (rank) best = sh.found;            // (the first block's room is for all)
-        lp_top(row, sh, unit, st.s == st.s, a.top, a.vocab, rank ? sh.best[1] : sh.best[0]);
-        if (rank) best = sh.best[1];
-    }
-    if (a.cluster > 1) {
-        namespace cg = cooperative_groups;
-        auto c = cg::this_cluster();
-        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-        if (rank) {
+            for (int i = 0; i < LP_FLIGHT; ++i) q[i] = i < left ? slot[(at * LP_FLIGHT + i) * LP_CTA] : make_uint4(NONE, NONE, NONE, NONE);
+            meet(largest<F32, LP_FLIGHT>(q));
+            if (near) {
+                f32x2 v = 0;
+                auto sums = [&](auto CLAMP) {
+#pragma unroll
+                    for (int i = 0; i < LP_FLIGHT; ++i) {
+                        if (i >= left) break;
+                        f32x2 l[V / 2];
+                        pairs_of<F32, decltype(CLAMP)::value>(q[i], l);
+#pragma unroll
+                        for (int j = 0; j < V / 2; ++j) {
+                            const f32x2 x = fma2(l[j], both(slope), both(-ref));
+                            const float2 xx = apart(x);
+                            const f32x2 e = pair(exp_2(xx.x), exp_2(xx.y));
+                            if (!decltype(CLAMP)::value) s = add2(s, e);
+                            if (ENTROPY) v = fma2(x, e, v);
+                        }
+                    }
+                };
+                sums(std::false_type{});
+                // -inf times its probability, 0: once more with -inf as LP_LOW (NaN stays)
+                if (ENTROPY && sum2(v) != sum2(v)) {
+                    v = 0;
+                    sums(std::true_type{});
+                }
+                u = add2(u, v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < LP_FLIGHT; ++i) {
+                    if (i >= left) break;
+                    float l[V];
+                    LpRow<F32>::values(q[i], l);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) add(l[j]);
+                }
+            }
+            ahead(at);
+            at = at + 1 == LP_AHEAD ? 0 : at + 1;
+        }
+        if (tid < row.tail) {
+            const float l = row.one(a.vocab - row.tail + tid);
+            meet(l);
+            add(l);
+        }
+        const float2 mine = settled(1.f, sum2(s), sum2(u));
+        LpState st = {m, mine.x, mine.y};
+        const uint32_t most = any ? order_of(m) : 0u;
+        if (a.top) {
+            uint32_t g = most;
+#pragma unroll
+            for (int o = 1; o < LP_GROUP; o <<= 1) g = max(g, __shfl_xor_sync(FULL, g, o));
+            if (lane % LP_GROUP == 0) sh.group[parity][tid / LP_GROUP] = g;
+        }
+        st.join<32>(slope);
+        if (lane == 0) { sh.m[parity][warp] = st.m; sh.s[parity][warp] = st.s; sh.u[parity][warp] = st.u; }
+        __syncthreads();
+        st = {sh.m[parity][lane % LP_WARPS], sh.s[parity][lane % LP_WARPS], sh.u[parity][lane % LP_WARPS]};
+        st.join<LP_WARPS>(slope);
+        if (a.top) {
+            // (NaN or +inf among the block's logits makes its sum NaN)
+            lp_top(row, sh, most, lp_least(sh.group[parity][lane], sh.group[parity][lane + 32], a.top), st.s == st.s, a.top, a.vocab, sh.best);
+            __syncthreads();
+            if (tid == 0) sh.n_units = sh.n_found = 0;
+        }
+        if (a.cluster > 1) {
+            namespace cg = cooperative_groups;
+            auto c = cg::this_cluster();
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
             LpShared *first = c.map_shared_rank(&sh, 0);
             if (tid == 0) { first->cm[rank] = st.m; first->cs[rank] = st.s; first->cu[rank] = st.u; }
-            if (tid < a.top) first->best[rank][tid] = best[tid];
+            if (rank && tid < a.top) first->best[rank * a.top + tid] = sh.best[tid];
+            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+            const int r = lane % LP_CLUSTER;
+            st = r < a.cluster ? LpState{sh.cm[r], sh.cs[r], sh.cu[r]} : LpState{-INFINITY, 0.f, 0.f};
+            st.join<LP_CLUSTER>(slope);
         }
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (rank) return;
-        for (int r = 1; r < a.cluster; ++r) st.join(sh.cm[r], sh.cs[r], sh.cu[r], slope);
-    }
-    const bool nothing = st.m == -INFINITY && st.s == 0.f;
-    const float total = nothing ? -INFINITY : logf(st.s);
-    if (tid == 0) {
-        if (a.stats) reinterpret_cast<float2 *>(a.stats)[t] = make_float2(st.m, total);
-        if (a.entropy) a.entropy[t] = nothing ? 0.f : total - 0.6931471805599453f * (st.u / st.s);
-        if (a.logprob) a.logprob[t] = target < 0 ? 0.f : target >= a.vocab ? __uint_as_float(0x7FC00000u) : nothing ? -INFINITY : (at_target - st.m) * a.inv_t - total;
-    }
-    // the blocks' alternatives among each other
-    const int all = a.top * a.cluster;
-    for (int i = tid; i < all; i += LP_CTA) {
-        const uint64_t mine = sh.best[i / a.top][i % a.top];
-        if (!mine) continue;
-        int before = i % a.top;
-        for (int r = 0; r < a.cluster; ++r)
-            if (r != i / a.top)
-                for (int j = 0; j < a.top && sh.best[r][j] > mine; ++j) ++before;
-        if (before >= a.top) continue;
-        if (a.top_ids) a.top_ids[t * a.top + before] = place_of(mine);
-        if (a.top_logprobs) a.top_logprobs[t * a.top + before] = nothing ? -INFINITY : (of_order((uint32_t)(mine >> 32)) - st.m) * a.inv_t - total;
+        if (rank == 0 && tid < max(a.top * a.cluster, 1)) {
+            const bool nothing = st.m == -INFINITY && st.s == 0.f;
+            const float total = nothing ? -INFINITY : logf(st.s);
+            if (tid == 0) {
+                if (a.stats) reinterpret_cast<float2 *>(a.stats)[t] = make_float2(st.m, total);
+                if (ENTROPY) a.entropy[t] = nothing ? 0.f : total - 0.6931471805599453f * (st.u / st.s);
+                if (a.logprob)
+                    a.logprob[t] = target < 0 ? 0.f : target >= a.vocab ? __uint_as_float(0x7FC00000u) : nothing ? -INFINITY : (at_target - st.m) * a.inv_t - total;
+            }
+            // the blocks' alternatives among each other
+            const int all = a.top * a.cluster;
+            for (int i = tid; i < all; i += LP_CTA) {
+                const uint64_t mine = sh.best[i];
+                int before = i;
+                if (a.cluster > 1) {
+                    before = 0;
+#pragma unroll 8
+                    for (int j = 0; j < all; ++j) before += sh.best[j] > mine;
+                }
+                if (!mine || before >= a.top) continue;
+                if (a.top_ids) a.top_ids[t * a.top + before] = place_of(mine);
+                if (a.top_logprobs) a.top_logprobs[t * a.top + before] = nothing ? -INFINITY : (of_order((uint32_t)(mine >> 32)) - st.m) * a.inv_t - total;
+            }
+        }
     }
 }
 
@@ -328,11 +485,10 @@ struct LpGrad {
     const int32_t *targets, *top_ids;
     const float *stats, *entropy, *dlogprob, *dentropy, *dtop;
 };
-constexpr int LG2_CTA = 256, LG2_ROUNDS = 2;                     // eights of a thread
-constexpr int LG2_EIGHTS = LG2_CTA * LG2_ROUNDS;                 // of a block
+constexpr int LG_ROWS_WAVES = 3, LG_ROWS_CTA = 256, LG_ROWS_FLIGHT = 2;            // threads, eights in flight of each
 
 template <bool F32, bool OUT32>
-__global__ void __launch_bounds__(LG2_CTA) k_logprobs_backward(const __grid_constant__ LpGrad a) {
+__global__ void __launch_bounds__(LG_ROWS_CTA) k_logprobs_backward(const __grid_constant__ LpGrad a) {
     __shared__ float s_given;
     __shared__ int s_id[LP_MAX_TOP + 1];
     __shared__ float s_weight[LP_MAX_TOP + 1];
@@ -354,18 +510,15 @@ __global__ void __launch_bounds__(LG2_CTA) k_logprobs_backward(const __grid_cons
     if (head > a.vocab) head = a.vocab;
     const int eights = (a.vocab - head) / 8, tail_at = head + eights * 8;
     const bool whole = (reinterpret_cast<uintptr_t>(in + (int64_t)head * IN) & 15u) == 0;
-    const int first = chunk * LG2_EIGHTS + tid;
-    float l[LG2_ROUNDS][8];
+    // this block's eights
+    const int per = (eights + a.chunks - 1) / a.chunks, from8 = min(chunk * per, eights), to8 = min(from8 + per, eights);
+    uint4 q_next[LG_ROWS_FLIGHT][F32 ? 2 : 1];
+    auto load = [&](int e0) {
 #pragma unroll
-    for (int r = 0; r < LG2_ROUNDS; ++r) {
-        const int e = first + r * LG2_CTA;
-        if (e < eights) {
-            uint4 x, y;
-            load_raw<F32>(in, head + e * 8, a.vocab, whole, x, y);
-            if (F32) eight_of(x, y, l[r]);
-            else eight_of(x, l[r]);
-        }
-    }
+        for (int r = 0; r < LG_ROWS_FLIGHT; ++r)
+            if (e0 + r * LG_ROWS_CTA < to8) load_raw<F32>(in, head + (e0 + r * LG_ROWS_CTA) * 8, a.vocab, whole, q_next[r][0], q_next[r][F32 ? 1 : 0]);
+    };
+    load(from8 + tid);
     // entries at the ends of the row, and those that have a gradient of their own: read before anything is written (dlogits may be the logits)
     const bool last = chunk == a.chunks - 1;
     const int edge = chunk == 0 && tid < head ? tid : last && tid >= 32 && tid - 32 < a.vocab - tail_at ? tail_at + tid - 32 : -1;
@@ -392,8 +545,8 @@ __global__ void __launch_bounds__(LG2_CTA) k_logprobs_backward(const __grid_cons
     int id = -1;
     if (tid <= a.top) {
         id = s_id[tid];
-        // (this block's own: the ends of the row are the first one's and the last one's)
-        const int at = head + chunk * LG2_EIGHTS * 8, from = chunk == 0 ? 0 : min(at, tail_at), to = last ? a.vocab : min(at + LG2_EIGHTS * 8, tail_at);
+        // (this block's own; the ends of the row are the first one's and the last one's)
+        const int from = chunk == 0 ? 0 : head + from8 * 8, to = last ? a.vocab : head + to8 * 8;
         if (id < from || id >= to) id = -1;
         if (id >= 0) {
             l_mine = one(id);
@@ -408,20 +561,47 @@ __global__ void __launch_bounds__(LG2_CTA) k_logprobs_backward(const __grid_cons
     }
     __syncthreads();
     const bool nothing = st.x == -INFINITY && !(st.y != st.y);
-    const float given = s_given;
     constexpr float LN2 = 0.6931471805599453f;
-    const float shift = st.y * 1.4426950408889634f;
+    const float given = s_given, shift = st.y * 1.4426950408889634f;
     auto slope = [&](float v, float own) {
         const float x = (v - st.x) * a.slope - shift, p = exp_2(x);
         return nothing ? 0.f : (own - p * (given + dh * (max_nan(x, LP_NONE) * LN2 + h))) * a.inv_t;
     };
+    // p (c0 + c1 x) with x = l slope - ref, two entries at a time; ref is rounded, and what that makes of p and x is in c0 and c1
+    const float most = st.x * a.slope, ref = most + shift;
+    const bool near = short_form(most, a.slope) && short_form(ref, a.slope);
+    const float part = ref - most, low = near ? fmaf(st.x, a.slope, -most) + ((most - (ref - part)) + (shift - part)) : 0.f, y = low * LN2;
+    const float k = nothing ? 0.f : -a.inv_t * (1.f - y + 0.5f * y * y);
+    const f32x2 c0 = both(nothing ? 0.f : k * (given + dh * (h - y))), c1 = both(nothing ? 0.f : k * dh * LN2);
+    for (int e0 = from8 + tid; e0 < to8; e0 += LG_ROWS_FLIGHT * LG_ROWS_CTA) {
+        uint4 q[LG_ROWS_FLIGHT][F32 ? 2 : 1];
 #pragma unroll
-    for (int r = 0; r < LG2_ROUNDS; ++r) {
-        const int e = first + r * LG2_CTA;
-        if (e < eights) {
+        for (int r = 0; r < LG_ROWS_FLIGHT; ++r)
+#pragma unroll
+            for (int i = 0; i < (F32 ? 2 : 1); ++i) q[r][i] = q_next[r][i];
+        load(e0 + LG_ROWS_FLIGHT * LG_ROWS_CTA);
+#pragma unroll
+        for (int r = 0; r < LG_ROWS_FLIGHT; ++r) {
+            const int e = e0 + r * LG_ROWS_CTA;
+            if (e >= to8) break;
             float d[8];
+            if (near) {
+                f32x2 l[4];
+                pairs_of<F32, true>(q[r][0], l);
+                if (F32) pairs_of<F32, true>(q[r][F32 ? 1 : 0], l + 2);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = slope(l[r][j], 0.f);
+                for (int j = 0; j < 4; ++j) {
+                    const f32x2 x = fma2(l[j], both(a.slope), both(-ref));
+                    const float2 xx = apart(x), v = apart(mul2(pair(exp_2(xx.x), exp_2(xx.y)), fma2(x, c1, c0)));
+                    d[2 * j] = v.x;
+                    d[2 * j + 1] = v.y;
+                }
+            } else {
+                if (F32) eight_of(q[r][0], q[r][F32 ? 1 : 0], d);
+                else eight_of(q[r][0], d);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[j] = slope(d[j], 0.f);
+            }
             store_eight<OUT32>(out, head + e * 8, a.vocab, true, d);
         }
     }

@@ -2,6 +2,8 @@
 // Entry points; kernels: join.cuh, logprobs.cuh.  No handle: the current device, and nothing that lasts longer than a call.
 #include <math.h>
 
+#include <type_traits>
+
 #include "internal.cuh"
 #include "join.cuh"
 #include "logprobs.cuh"
@@ -26,24 +28,26 @@ __global__ void __launch_bounds__(DR_CTA) k_dropout(const __grid_constant__ Drop
     if (eight * 8 >= a.n) return;
     const int col = (int)eight * 8;
     const bool whole = a.n - col >= 8;
-    const Numbers num = numbers_of(a.drop);
     uint4 p[DR_ROWS], q[DR_ROWS];
 #pragma unroll
     for (int r = 0; r < DR_ROWS; ++r)
         if (t0 + r * tall < a.tokens) load_raw<F32>(row_at<F32>(a.x, t0 + r * tall), col, a.n, whole && a.x.aligned, p[r], q[r]);
+    const Numbers num = numbers_of(a.drop);
+    const Columns cols = columns_of(num, (uint32_t)eight);
 #pragma unroll
     for (int r = 0; r < DR_ROWS; ++r) {
         const int64_t t = t0 + r * tall;
         if (t >= a.tokens) break;
+        void *to = const_cast<void *>(row_at<F32>(a.y, t));
         if (a.drop.random) {
-            float v[8];
-            if (F32) eight_of(p[r], q[r], v);
-            else eight_of(p[r], v);
-            drop_eight(a.drop, num, (uint32_t)eight, (uint32_t)t, v);
-            p[r] = F32 ? fp32_four(v) : bf16_eight(v);
-            q[r] = fp32_four(v + 4);
-        }
-        store_raw<F32>(const_cast<void *>(row_at<F32>(a.y, t)), col, a.n, whole && a.y.aligned, p[r], q[r]);
+            f32x2 v[4];
+            if (F32) pairs_of_eight(p[r], q[r], v);
+            else pairs_of_eight(p[r], v);
+            drop_eight(a.drop, num, cols, (uint32_t)t, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], both(a.drop.scale));
+            store_eight<F32>(to, col, a.n, whole && a.y.aligned, v);
+        } else store_raw<F32>(to, col, a.n, whole && a.y.aligned, p[r], q[r]);
     }
 }
 
@@ -51,43 +55,47 @@ static int64_t ceil64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 template <typename... P> static bool on_bytes(uintptr_t bytes, P... p) { return (((reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0) && ...); }
 static bool rows_ok(const void *p, int64_t ld, int64_t width) { return !p || ld >= width; }
 
+// Threads that an SM holds of the joins' kernels, by their registers
+constexpr int JOIN_FORWARD_THREADS = 768, JOIN_BACKWARD_THREADS = 512;
+
 // ---- joins -----------------------------------------------------------------------------------
-static JoinPlan join_plan(int sms, int64_t tokens, int64_t n, int pieces) {
+static JoinPlan join_plan(int sms, int64_t tokens, int64_t n, int eights, int pieces, int params, int threads_per_sm) {
     JoinPlan p;
-    const int warps = (int)ceil64(n, 256);
+    const int warps = (int)ceil64(n, (int64_t)256 * eights), most = JOIN_COLS / 256 / eights;
+    p.eights = eights;
     p.cluster = 1;
-    while (p.cluster * JOIN_WARPS < warps) p.cluster *= 2;
+    while (p.cluster * most < warps) p.cluster *= 2;
     p.warps = (int)ceil64(warps, p.cluster);
     p.teams = 1;
     // several short rows to a thread block, once there is a block for every SM
     while (p.cluster == 1 && 2 * p.teams * p.warps <= 8 && tokens >= (int64_t)2 * p.teams * sms) p.teams *= 2;
-    const int threads = p.warps * p.teams * 32, by_registers = 65536 / (64 * threads), by_memory = (int)((227 * 1024) / (join_smem(p, pieces) + 1024));
+    const int by_registers = threads_per_sm / (p.warps * p.teams * 32), by_memory = (int)((227 * 1024) / (join_smem(p, pieces, params) + 1024));
     int per_sm = by_registers < by_memory ? by_registers : by_memory;
-    if (per_sm < 1) per_sm = 1;
-    if (per_sm > 24) per_sm = 24;
+    per_sm = per_sm < 1 ? 1 : per_sm > 24 ? 24 : per_sm;
     const int64_t want = ceil64(tokens, p.teams), room = (int64_t)sms * per_sm / p.cluster;
     p.clusters = (int)(want < room ? want : room < 1 ? 1 : room);
     return p;
 }
+// Two eights a thread share what a sum over the row costs; rows of up to 1024 columns have too few for that
+static int join_eights(int64_t n, bool sums_of_biases) { return n > 1024 && !sums_of_biases ? 2 : 1; }
 static bool norm_ok(int norm) { return norm >= DBSPMSPV_NORM_NONE && norm <= DBSPMSPV_NORM_LAYER; }
 static bool opts_ok(const dbspmspv_join_opts *o) {
     return o && norm_ok(o->norm_block) && norm_ok(o->norm_next) && o->eps_block >= 0.f && o->eps_next >= 0.f && isfinite(o->eps_block) && isfinite(o->eps_next) && isfinite(o->scale) &&
            o->drop >= 0.f && o->drop <= 1.f;
 }
-static JoinArgs join_args(const dbspmspv_join_opts &o, int32_t tokens, int64_t n, const JoinPlan &p, int pieces) {
+static JoinArgs join_args(const dbspmspv_join_opts &o, int32_t tokens, int64_t n, const JoinPlan &p, int pieces, int params) {
     JoinArgs a = {};
     a.params_f32 = o.params_f32 != 0;
     a.scale = o.scale; a.eps_block = o.eps_block; a.eps_next = o.eps_next; a.inv_n = (float)(1.0 / (double)n);
     a.norm_block = o.norm_block; a.norm_next = o.norm_next;
-    a.tokens = tokens; a.n = (int32_t)n; a.warps = p.warps; a.teams = p.teams; a.pieces = pieces;
+    a.tokens = tokens; a.n = (int32_t)n; a.warps = p.warps; a.teams = p.teams; a.pieces = pieces; a.params = params;
     return a;
 }
-constexpr int JOIN_MAX_PIECES = 9;
+// Room for the sums of any gradient call of this size: a team per token at most, and never more than fit the GPU with the fewest pieces
 static int64_t join_room(int sms, int64_t tokens, int64_t n) {
-    // (the fewest pieces are the most teams)
     int64_t most = 0;
-    for (int pieces = 1; pieces <= JOIN_MAX_PIECES; ++pieces) {
-        const JoinPlan p = join_plan(sms, tokens, n, pieces);
+    for (int eights = 1; eights <= 2; ++eights) {
+        const JoinPlan p = join_plan(sms, tokens, n, eights, 1, 4, JOIN_BACKWARD_THREADS);
         const int64_t teams = (int64_t)p.clusters * p.teams;
         if (teams > most) most = teams;
     }
@@ -123,8 +131,10 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
     if ((s = current_device(&dev, &sms)) != DBSPMSPV_OK) return s;
     if (!on_current_device(r ? r : b, dev) || !on_current_device(out ? out : h, dev)) return DBSPMSPV_ERR_INVALID_ARG;
     const int gate_pieces = b && gate && ldg ? (o->params_f32 ? 2 : 1) : 0, pieces = (o->stream_f32 ? 2 : 1) + (o->block_f32 ? 2 : 1) + gate_pieces;
-    const JoinPlan p = join_plan(sms, tokens, n, pieces);
-    JoinArgs a = join_args(*o, tokens, n, p, pieces);
+    const bool bias = (b && c_block) || c_next;
+    const int params = bias ? 8 : 4, eights = join_eights(n, false);
+    const JoinPlan p = join_plan(sms, tokens, n, eights, pieces, params, JOIN_FORWARD_THREADS);
+    JoinArgs a = join_args(*o, tokens, n, p, pieces, params);
     a.r = rows_of(r, ldr, o->stream_f32); a.b = rows_of(b, ldb, o->block_f32); a.out = rows_of(out, ldo, o->stream_f32); a.h = rows_of(h, ldh, false);
     if (b) {
         if (gate_pieces) a.gate = rows_of(gate, ldg, o->params_f32);
@@ -133,10 +143,16 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
         a.drop = drop_of(o->drop, random);
     }
     a.w_next = w_next; a.c_next = c_next; a.stats = stats;
-    a.params_aligned = on_bytes(16, w_block, c_block, gate_pieces ? nullptr : gate, w_next, c_next);
     if (!b) a.norm_block = DBSPMSPV_NORM_NONE;
-    auto kernel = o->stream_f32 ? (o->block_f32 ? k_join<true, true> : k_join<true, false>) : (o->block_f32 ? k_join<false, true> : k_join<false, false>);
-    return launch_rows(kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, pieces), static_cast<cudaStream_t>(stream), a);
+    auto pick = [&](auto E, auto B) {
+        constexpr int E_ = decltype(E)::value;
+        constexpr bool B_ = decltype(B)::value;
+        return o->stream_f32 ? (o->block_f32 ? k_join<true, true, E_, B_> : k_join<true, false, E_, B_>) : (o->block_f32 ? k_join<false, true, E_, B_> : k_join<false, false, E_, B_>);
+    };
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    auto kernel = eights == 2 ? (bias ? pick(Two{}, std::true_type{}) : pick(Two{}, std::false_type{})) : (bias ? pick(One{}, std::true_type{}) : pick(One{}, std::false_type{}));
+    return launch_rows(kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, pieces, params), static_cast<cudaStream_t>(stream), a);
 }
 
 int dbspmspv_join_workspace(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, int64_t *bytes) {
@@ -181,8 +197,10 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
     if (!on_current_device(dh ? dh : dout, dev) || (dr && !on_current_device(dr, dev))) return DBSPMSPV_ERR_INVALID_ARG;
     if (sums && (!workspace || workspace_bytes < join_room(sms, tokens, n))) return DBSPMSPV_ERR_INVALID_ARG;
     const int gate_pieces = rows && block ? (o->params_f32 ? 2 : 1) : 0, pieces = 1 + 2 * (o->stream_f32 ? 2 : 1) + (o->block_f32 ? 2 : 1) + gate_pieces;
-    const JoinPlan p = join_plan(sms, tokens, n, pieces);
-    JoinArgs a = join_args(*o, tokens, n, p, pieces);
+    const bool bias = dc_block || dc_next || (dgate && !rows && c_block);
+    const int params = gate_pieces && dgate ? 6 : 4, eights = join_eights(n, bias);
+    const JoinPlan p = join_plan(sms, tokens, n, eights, pieces, params, JOIN_BACKWARD_THREADS);
+    JoinArgs a = join_args(*o, tokens, n, p, pieces, params);
     a.dh = rows_of(dh, lddh, false); a.dout = rows_of(dout, lddo, o->stream_f32); a.dr = rows_of(dr, lddr, o->stream_f32);
     if (nn && dh) a.out = rows_of(out, ldo, o->stream_f32);
     if (block) {
@@ -195,20 +213,22 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
         a.drop = drop_of(o->drop, random);
     }
     a.w_next = w_next; a.stats = const_cast<float *>(stats);
-    a.params_aligned = on_bytes(16, w_block, c_block, rows ? nullptr : gate, w_next);
     a.parts = sums ? static_cast<float *>(workspace) : nullptr;
     a.ldp = ceil64(n, 8) * 8;
-    const bool bias = dc_block || dc_next || (dgate && !rows && c_block);
-    auto pick = [&](auto B) {
-        constexpr bool BIAS = decltype(B)::value;
-        return o->stream_f32 ? (o->block_f32 ? k_join_backward<true, true, BIAS> : k_join_backward<true, false, BIAS>)
-                             : (o->block_f32 ? k_join_backward<false, true, BIAS> : k_join_backward<false, false, BIAS>);
+    auto pick = [&](auto E, auto B) {
+        constexpr int E_ = decltype(E)::value;
+        constexpr bool B_ = decltype(B)::value;
+        return o->stream_f32 ? (o->block_f32 ? k_join_backward<true, true, E_, B_> : k_join_backward<true, false, E_, B_>)
+                             : (o->block_f32 ? k_join_backward<false, true, E_, B_> : k_join_backward<false, false, E_, B_>);
     };
-    s = launch_rows(bias ? pick(std::true_type{}) : pick(std::false_type{}), p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, pieces), st, a);
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    auto kernel = bias ? pick(One{}, std::true_type{}) : eights == 2 ? pick(Two{}, std::false_type{}) : pick(One{}, std::false_type{});
+    s = launch_rows(kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, pieces, params), st, a);
     if (s != DBSPMSPV_OK || !sums) return s;
-    JoinSums j = {a.parts, a.ldp, p.clusters * p.teams, (int32_t)n, a.params_f32, w_block, c_block, rows ? nullptr : gate,
+    JoinSums j = {a.parts, a.ldp, p.clusters * p.teams, (int32_t)n, a.params_f32, a.drop.random ? o->scale * a.drop.scale : o->scale, w_block, c_block, rows ? nullptr : gate,
                   dw_block, dc_block, rows ? nullptr : static_cast<float *>(dgate), dw_next, dc_next};
-    return launch_rows(bias ? k_join_sums<true> : k_join_sums<false>, (int)ceil64(n, JOIN_SUMS_X), JOIN_SUMS_X * JOIN_SUMS_Y, 1, 0, st, j);
+    return launch_rows(bias ? k_join_sums<true> : k_join_sums<false>, (int)ceil64(n, JOIN_SUMS_COLS), JOIN_SUMS_CTA, 1, 0, st, j);
 }
 
 int dbspmspv_dropout(const void *x, int64_t ldx, int f32, int32_t tokens, int64_t n, float drop, const uint64_t *random, void *y, int64_t ldy, dbspmspv_stream_t stream) {
@@ -239,12 +259,14 @@ int dbspmspv_logprobs(const void *logits, int64_t ldl, int logits_f32, int32_t t
     int dev, sms, s;
     if ((s = current_device(&dev, &sms)) != DBSPMSPV_OK) return s;
     if (!on_current_device(logits, dev)) return DBSPMSPV_ERR_INVALID_ARG;
-    LpArgs a = {logits, ldl, tokens, vocab, 1, top, (float)(1.4426950408889634 / (double)temperature), (float)(1.0 / (double)temperature), logprob ? targets : nullptr, logprob, entropy, stats, top_ids, top_logprobs};
+    LpArgs a = {logits, ldl, tokens, vocab, 1, top, 0, (float)(1.4426950408889634 / (double)temperature), (float)(1.0 / (double)temperature), logprob ? targets : nullptr, logprob, entropy, stats, top_ids, top_logprobs};
     // a row is shared out while there are SMs without one and every block has a vector for each of its threads
     const int64_t vectors = vocab / (logits_f32 ? 4 : 8);
-    while (a.cluster < LP_CLUSTER && (int64_t)2 * a.cluster * tokens <= sms && vectors >= (int64_t)2 * a.cluster * LP_CTA) a.cluster *= 2;
-    if ((int64_t)tokens * a.cluster > INT32_MAX) return DBSPMSPV_ERR_UNSUPPORTED;
-    return launch_rows(logits_f32 ? k_logprobs<true> : k_logprobs<false>, tokens * a.cluster, LP_CTA, a.cluster, 0, static_cast<cudaStream_t>(stream), a);
+    while (a.cluster < LP_CLUSTER && (int64_t)2 * a.cluster * tokens <= (int64_t)sms * LP_PER_SM && vectors >= (int64_t)2 * a.cluster * LP_CTA) a.cluster *= 2;
+    a.rounds = (int32_t)ceil64(ceil64(vectors, a.cluster), LP_CTA * LP_FLIGHT);
+    const int64_t room = (int64_t)sms * LP_PER_SM, clusters = a.cluster > 1 || tokens < room ? tokens : room;
+    auto kernel = logits_f32 ? (entropy ? k_logprobs<true, true> : k_logprobs<true, false>) : (entropy ? k_logprobs<false, true> : k_logprobs<false, false>);
+    return launch_rows(kernel, (int)clusters * a.cluster, LP_CTA, a.cluster, LP_SMEM, static_cast<cudaStream_t>(stream), a);
 }
 
 int dbspmspv_logprobs_backward(const void *logits, int64_t ldl, int logits_f32, int32_t tokens, int32_t vocab, float temperature, const int32_t *targets, const float *stats, const float *entropy,
@@ -259,13 +281,14 @@ int dbspmspv_logprobs_backward(const void *logits, int64_t ldl, int logits_f32, 
     int dev, sms, s;
     if ((s = current_device(&dev, &sms)) != DBSPMSPV_OK) return s;
     if (!on_current_device(logits, dev) || !on_current_device(dlogits, dev)) return DBSPMSPV_ERR_INVALID_ARG;
-    const int64_t chunks = ceil64(ceil64(vocab, 8), LG2_EIGHTS);
+    // a row is shared out until there are LG_ROWS_WAVES rounds of thread blocks, or two loads left to a thread
+    const int64_t most = ceil64(vocab, (int64_t)8 * LG_ROWS_CTA * LG_ROWS_FLIGHT), want = ceil64((int64_t)sms * 5 * LG_ROWS_WAVES, tokens), chunks = want < most ? want : most;
     if (chunks * tokens > INT32_MAX) return DBSPMSPV_ERR_UNSUPPORTED;
     LpGrad a = {logits, dlogits, ldl, ldd, tokens, vocab, dtop ? top : 0, (int32_t)chunks, (float)(1.4426950408889634 / (double)temperature), (float)(1.0 / (double)temperature),
                 targets, top_ids, stats, entropy, dlogprob, dentropy, dtop};
     auto kernel = logits_f32 ? (dlogits_f32 ? k_logprobs_backward<true, true> : k_logprobs_backward<true, false>)
                              : (dlogits_f32 ? k_logprobs_backward<false, true> : k_logprobs_backward<false, false>);
-    return launch_rows(kernel, (int)(chunks * tokens), LG2_CTA, 1, 0, static_cast<cudaStream_t>(stream), a);
+    return launch_rows(kernel, (int)(chunks * tokens), LG_ROWS_CTA, 1, 0, static_cast<cudaStream_t>(stream), a);
 }
 
 }  // extern "C"

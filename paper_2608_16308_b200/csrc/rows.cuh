@@ -33,6 +33,45 @@ __device__ __forceinline__ void eight_of(uint4 a, uint4 b, float v[8]) {
     v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
     v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
 }
+// Two fp32 in a register pair: sm_100 multiplies and adds them with one instruction.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+    f32x2 p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ f32x2 both(float v) { return pair(v, v); }
+__device__ __forceinline__ float2 apart(f32x2 p) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float sum2(f32x2 p) {
+    const float2 v = apart(p);
+    return v.x + v.y;
+}
+__device__ __forceinline__ f32x2 as_pair(uint32_t lo, uint32_t hi) { return pair(__uint_as_float(lo), __uint_as_float(hi)); }
+__device__ __forceinline__ f32x2 bf16_pair(uint32_t w) { return pair(bf16_lo(w), bf16_hi(w)); }
+
+__device__ __forceinline__ void pairs_of_eight(uint4 q, f32x2 v[4]) { v[0] = bf16_pair(q.x); v[1] = bf16_pair(q.y); v[2] = bf16_pair(q.z); v[3] = bf16_pair(q.w); }
+__device__ __forceinline__ void pairs_of_eight(uint4 a, uint4 b, f32x2 v[4]) { v[0] = as_pair(a.x, a.y); v[1] = as_pair(a.z, a.w); v[2] = as_pair(b.x, b.y); v[3] = as_pair(b.z, b.w); }
+__device__ __forceinline__ uint32_t two_bf16(f32x2 p) { const float2 v = apart(p); return two_bf16(v.x, v.y); }
+__device__ __forceinline__ uint4 bf16_eight(const f32x2 v[4]) { return make_uint4(two_bf16(v[0]), two_bf16(v[1]), two_bf16(v[2]), two_bf16(v[3])); }
 __device__ __forceinline__ uint4 bf16_eight(const float v[8]) { return make_uint4(two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])); }
 
 // Columns col to col + 7 of a row of n (col < n), zeros behind its end.  `whole`: all eight are there and begin on 16 bytes.
@@ -85,6 +124,14 @@ __device__ __forceinline__ void store_raw(void *row, int col, int n, bool whole,
         }
     }
 }
+template <bool F32>
+__device__ __forceinline__ void store_eight(void *row, int col, int n, bool whole, const f32x2 v[4]) {
+    if (F32) {
+        const float2 a = apart(v[0]), b = apart(v[1]), c = apart(v[2]), d = apart(v[3]);
+        store_raw<true>(row, col, n, whole, make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)),
+                        make_uint4(__float_as_uint(c.x), __float_as_uint(c.y), __float_as_uint(d.x), __float_as_uint(d.y)));
+    } else store_raw<false>(row, col, n, whole, bf16_eight(v), uint4{});
+}
 __device__ __forceinline__ uint4 fp32_four(const float *v) { return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])); }
 template <bool F32>
 __device__ __forceinline__ void store_eight(void *row, int col, int n, bool whole, const float v[8]) {
@@ -96,44 +143,62 @@ __device__ __forceinline__ const void *row_at(const Rows &r, int64_t t) {
     return static_cast<const uint8_t *>(r.p) + t * r.ld * (F32 ? 4 : 2);
 }
 
+// Copies into shared memory that a thread makes for itself: group by group, and no barrier where it reads them itself
+__device__ __forceinline__ void copy_ahead(void *smem, const void *p) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
+}
+__device__ __forceinline__ void close_ahead() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void wait_ahead() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
 // ---- dropout ---------------------------------------------------------------------------------
 // Philox 4x32-10 (Salmon, Moraes, Dror, Shaw, 2011): ten rounds of two 32 x 32 -> 64 bit products and their exclusive ors.
 struct Drop {
     const uint64_t *random;   // seed, offset; null: nothing is dropped
-    uint32_t below;           // P << 16 (P < 65536)
-    int32_t all;              // P = 65536: everything is dropped
+    uint32_t above;           // a word is kept if it is above this: (P << 16) - 1, and all ones for P = 65536
     float scale;              // 65536 / (65536 - P)
 };
+// What rows and columns have in common: keys of the rounds, and the first one's products with the offset
 struct Numbers {
-    uint32_t k0, k1, c2, c3;
+    uint32_t k0, k1, c3, first, second;
 };
+constexpr uint32_t PHILOX_M0 = 0xD2511F53u, PHILOX_M1 = 0xCD9E8D57u, PHILOX_W0 = 0x9E3779B9u, PHILOX_W1 = 0xBB67AE85u;
 __device__ __forceinline__ Numbers numbers_of(const Drop &d) {
     if (!d.random) return Numbers{};
-    const uint64_t seed = d.random[0], offset = d.random[1];
-    return Numbers{(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)offset, (uint32_t)(offset >> 32)};
+    const uint64_t seed = d.random[0], offset = d.random[1], q = (uint64_t)(uint32_t)offset * PHILOX_M1;
+    return Numbers{(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)(offset >> 32), (uint32_t)(q >> 32) ^ (uint32_t)seed, (uint32_t)q};
 }
-__device__ __forceinline__ uint4 philox(uint32_t c0, uint32_t c1, const Numbers &s) {
-    uint32_t c2 = s.c2, c3 = s.c3, k0 = s.k0, k1 = s.k1;
+// The counter is (eight, token, offset): what depends on the columns alone is worked out once for all tokens, three of the six products in the first three rounds among it (a fourth is the token's alone)
+struct Columns {
+    uint32_t a, b, c, d;
+};
+__device__ __forceinline__ Columns columns_of(const Numbers &s, uint32_t eight) {
+    const uint64_t p1 = (uint64_t)eight * PHILOX_M0, q2 = (uint64_t)((uint32_t)(p1 >> 32) ^ s.c3 ^ s.k1) * PHILOX_M1;
+    const uint64_t p3 = (uint64_t)((uint32_t)(q2 >> 32) ^ s.second ^ (s.k0 + PHILOX_W0)) * PHILOX_M0;
+    return Columns{(uint32_t)p1 ^ (s.k1 + PHILOX_W1), (uint32_t)q2 ^ (s.k0 + 2 * PHILOX_W0), (uint32_t)(p3 >> 32) ^ (s.k1 + 2 * PHILOX_W1), (uint32_t)p3};
+}
+__device__ __forceinline__ uint4 philox(const Numbers &s, const Columns &w, uint32_t token) {
+    const uint64_t p2 = (uint64_t)(s.first ^ token) * PHILOX_M0, q3 = (uint64_t)((uint32_t)(p2 >> 32) ^ w.a) * PHILOX_M1;
+    uint32_t c0 = (uint32_t)(q3 >> 32) ^ w.b, c1 = (uint32_t)q3, c2 = w.c ^ (uint32_t)p2, c3 = w.d, k0 = s.k0 + 3 * PHILOX_W0, k1 = s.k1 + 3 * PHILOX_W1;
 #pragma unroll
-    for (int r = 0; r < 10; ++r) {
-        const uint64_t p = (uint64_t)c0 * 0xD2511F53u, q = (uint64_t)c2 * 0xCD9E8D57u;
+    for (int r = 3; r < 10; ++r) {
+        const uint64_t p = (uint64_t)c0 * PHILOX_M0, q = (uint64_t)c2 * PHILOX_M1;
         c0 = (uint32_t)(q >> 32) ^ c1 ^ k0;
         c1 = (uint32_t)q;
         c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
         c3 = (uint32_t)p;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
+        k0 += PHILOX_W0;
+        k1 += PHILOX_W1;
     }
     return make_uint4(c0, c1, c2, c3);
 }
-// v[j] scaled, or 0 where entry 8 * eight + j of the token is dropped: its 16 bits are below P exactly if the word that begins with them is below P << 16
-__device__ __forceinline__ void drop_eight(const Drop &d, const Numbers &s, uint32_t eight, uint32_t token, float v[8]) {
-    const uint4 q = philox(eight, token, s);
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+// v with zeros where entries of the token are dropped (what makes up for them is the caller's to multiply): 16 bits are below P exactly if the word that begins with them is below P << 16
+__device__ __forceinline__ void drop_eight(const Drop &d, const Numbers &s, const Columns &w, uint32_t token, f32x2 v[4]) {
+    const uint4 q = philox(s, w, token);
+    const uint32_t bits[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t bits = j % 2 ? w[j / 2] : w[j / 2] << 16;
-        v[j] = bits >= d.below && !d.all ? v[j] * d.scale : 0.f;
+    for (int j = 0; j < 4; ++j) {
+        const float2 x = apart(v[j]);
+        v[j] = pair(bits[j] << 16 > d.above ? x.x : 0.f, bits[j] > d.above ? x.y : 0.f);
     }
 }
 
@@ -141,7 +206,8 @@ __device__ __forceinline__ void drop_eight(const Drop &d, const Numbers &s, uint
 inline Drop drop_of(float p, const void *random) {
     const int32_t below = (int32_t)((double)p * 65536.0 + 0.5);
     if (below == 0) return Drop{};
-    return Drop{static_cast<const uint64_t *>(random), below >= 65536 ? 0u : (uint32_t)below << 16, below >= 65536, below >= 65536 ? 0.f : 65536.f / (65536 - below)};
+    if (below >= 65536) return Drop{static_cast<const uint64_t *>(random), 0xFFFFFFFFu, 0.f};
+    return Drop{static_cast<const uint64_t *>(random), ((uint32_t)below << 16) - 1u, 65536.f / (65536 - below)};
 }
 
 // Whether `p` is memory that kernels of the current device may use as theirs: not the host's own, not another device's.
@@ -171,7 +237,7 @@ inline int current_device(int *dev, int *sms) {
 // One launch in clusters of `cluster` thread blocks, set up while the kernel in front of it drains (every kernel launched so begins with pdl_wait).
 template <typename... P, typename... A>
 inline int launch_rows(void (*kernel)(P...), int blocks, int threads, int cluster, size_t smem, cudaStream_t st, const A &...args) {
-    if (smem > 48 * 1024) DBS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (smem > 16 * 1024) DBS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3(blocks);
     c.blockDim = dim3(threads);

@@ -332,6 +332,10 @@ class Logprobs:
         want = (own - p * (S + dH * (lp0 + H))) / T
         ax = torch.where(p > 0, x.abs() + k[:, 1:].abs(), 0.0)
         bound = (size * 80 * E + p * (2.0 ** -21 + 8 * E * ax) * (SA + dH.abs() * (lp0.abs() + H)) + p * (80 * E * SA + 8 * E * dH.abs() * (ax + H))) / T
+        # (the exponent is taken from a reference that is M log2(e) / T rounded, off by E |M| log2(e) / T at most; what makes up for that is itself rounded: E times as much again.  It shows where
+        # all else is 0: the only logit left)
+        ref = torch.where(nothing, 0.0, k[:, :1]).abs() * 1.45 / T + k[:, 1:].abs() * 1.45
+        bound = bound + torch.where(ref <= 4200, 8 * E * E * ref * p * (SA + dH.abs()) / T, 0.0)
         want, bound = torch.where(nothing, 0.0, want), torch.where(nothing, 0.0, bound)
         step = HALF if self.dl.buf.dtype == torch.bfloat16 else E
         near(self.dl.v, want, bound + step * (want.abs() + bound) + 1e-37)
