@@ -1,10 +1,12 @@
 // A block joins the residual stream: out = r + scale drop(gate * norm_block(b)), h = norm_next(out), and the gradient of that.
 //
-// A row is owned by a team of warps, one or two times eight columns a thread: the values stay on the chip between the sums over the row (one for each norm, two for a layer norm; backwards one
-// for each norm) and every array is read and written once.  A warp is a team for short rows, a thread block holds several teams then; rows of more than 4096 columns are shared out to a cluster
-// whose blocks add up through each other's shared memory.  Teams walk the tokens.  The rows to come are copied ahead into slots of shared memory that belong to the thread itself (cp.async, no
-// barrier): a sum over the row would else leave HBM idle.  Weights, gate, scales and biases of a thread's columns lie beside them in fp32, multiplied with one another once: what is left is HBM and, with
-// dropout, nearly as many instructions; so products and sums go two entries at a time.
+// A row is owned by a team of warps; a warp takes 256 or 512 columns of it, eight or twice eight a lane: the values stay on the chip between the sums over the row (one for each norm, two for a layer norm;
+// backwards one for each norm) and every array is read and written once.  A warp is a team for short rows, a thread block holds several teams then; rows of more than 4096 columns are shared out to a
+// cluster whose blocks send their sums into each other's shared memory.  Teams walk the tokens.  The rows to come are copied ahead into shared memory of the warp (cp.async): a sum over the row would else
+// leave HBM idle.  Weights, gate, scales and biases of the columns lie beside them in fp32, multiplied with one another once.  What is left is HBM and, with dropout, nearly as many
+// instructions; so products and sums go two entries at a time, and where all rows are whole eights on 16 bytes (WHOLE) a row's address is one product-and-sum and its copy one instruction.
+// Other rows: of one on 16 bytes the last eight goes entry by entry; one that is not is copied and written in words of 4 bytes, side by side across the warp, and in shared memory moved by half a word
+// where it begins between two.
 //
 // Sums over the tokens (gradients of weights, biases and a shared gate) are held by the threads of a column and written once per team; a second kernel adds the teams up in a
 // fixed order.  With a shared gate g and weight w both gradients follow from one sum: A = sum drop(G) xhat gives dw = scale g A and dg = scale (w A + c B), B = sum drop(G).
@@ -21,11 +23,12 @@ constexpr int JOIN_CLUSTER = 8;
 constexpr int64_t JOIN_MAX_N = JOIN_COLS * JOIN_CLUSTER;
 constexpr int JOIN_AHEAD = 2;                // rows in flight or in hand, per team
 constexpr int JOIN_SUMS_COLS = 32, JOIN_SUMS_CTA = 256;
-// threads at most: of kernels with two eights a thread, and with one
-template <int E> constexpr int join_cta() { return JOIN_COLS / 8 / E; }
+constexpr int JOIN_WAIT = 1 << 20;           // tries of a wait for a cluster's sums, before it gives up
+// threads at most: of kernels with two eights a lane, and with one
+template <int E> __host__ __device__ constexpr int join_cta() { return JOIN_COLS / 8 / E; }
 
 struct JoinPlan {
-    int eights;                              // of a thread: 1, 2
+    int eights;                              // of a lane: 1, 2
     int warps, teams, cluster;               // warps of a team in a thread block, teams in it, blocks to a row
     int clusters;                            // in the grid
 };
@@ -34,7 +37,7 @@ struct JoinArgs {
     Rows r, b, gate, out, h;                 // forward (gate: rows, else gate_vec)
     Rows dh, dout, dr, db, dgate;            // backward (out: what the forward call left)
     const void *w_block, *c_block, *gate_vec, *w_next, *c_next;
-    int32_t params_f32, pieces, params;      // pieces of 16 bytes of an eight, in a slot and for its columns
+    int32_t params_f32, room, params;        // bytes that a warp's eights of one row take in shared memory; pieces of 16 bytes of factors for an eight
     float *stats;
     Drop drop;
     float scale, eps_block, eps_next, inv_n;
@@ -43,35 +46,131 @@ struct JoinArgs {
     int64_t ldp;
 };
 
-// an eight of row t into its slot (pieces `step` apart)
+// ---- rows in a warp's shared memory --------------------------------------------------------------
+// A lane's eight lies at 16 * lane; fp32: the first four there and the others 512 bytes behind (WHOLE), or all at 32 * lane.  What is not WHOLE has 16 bytes more: rows that begin between two words.
+template <bool F32, bool WHOLE> __host__ __device__ constexpr int eight_room() { return (F32 ? 1024 : 512) + (WHOLE ? 0 : 16); }
+// whether row t of bf16 begins between two words
+__device__ __forceinline__ int between(const Rows &r, int64_t t) { return (int)((reinterpret_cast<uintptr_t>(r.p) >> 1) + t * r.ld) & 1; }
+
+struct WarpEight {
+    int lane, col, cnt;                      // the warp's first column; the lane's entries, 0 to 8
+    __device__ __forceinline__ int mine() const { return col + lane * 8; }
+};
+// the warp's eights of row t, columns from w.col on, towards shared memory at `to`
 template <bool F32>
-__device__ __forceinline__ void row_ahead(const Rows &r, int64_t t, int col, int n, uint4 *slot, int step) {
-    const void *row = row_at<F32>(r, t);
-    if (r.aligned && col + 8 <= n) {
-        const uint8_t *p = static_cast<const uint8_t *>(row) + (int64_t)col * (F32 ? 4 : 2);
-        copy_ahead(slot, p);
-        if (F32) copy_ahead(slot + step, p + 16);
-    } else {
-        uint4 a, b;
-        load_raw<F32>(row, col, n, false, a, b);
-        slot[0] = a;
-        if (F32) slot[step] = b;
+__device__ __forceinline__ void row_ahead(const Rows &r, int64_t t, const WarpEight &w, int n, uint8_t *to) {
+    const uint8_t *row = static_cast<const uint8_t *>(row_at<F32>(r, t));
+    if (r.aligned) {
+        const uint8_t *p = row + (int64_t)w.mine() * (F32 ? 4 : 2);
+        uint4 *at = reinterpret_cast<uint4 *>(to + w.lane * (F32 ? 32 : 16));
+        if (w.cnt == 8) {
+            copy_ahead(at, p);
+            if (F32) copy_ahead(at + 1, p + 16);
+        } else if (w.cnt) {
+            uint4 a, b;
+            load_raw<F32>(row, w.mine(), n, false, a, b);
+            at[0] = a;
+            if (F32) at[1] = b;
+        }
+        return;
+    }
+    const int here = min(256, n - w.col);    // entries of the warp
+    if (here <= 0) return;
+    if (F32) {
+        const uint8_t *p = row + (int64_t)w.col * 4;
+#pragma unroll
+        for (int i = w.lane; i < 256; i += 32)
+            if (i < here) copy_word_ahead(to + i * 4, p + i * 4);
+        return;
+    }
+    // entry e of the words is the row's w.col + e - odd
+    const int odd = between(r, t), first = w.col ? 0 : odd, end = n - w.col + odd;
+    const uint8_t *p = row + (int64_t)w.col * 2 - 2 * odd;
+    for (int i = w.lane; 2 * i < here + odd; i += 32) {
+        const int e = 2 * i;
+        if (e >= first && e + 1 < end) copy_word_ahead(to + i * 4, p + i * 4);
+        else if (e >= first) reinterpret_cast<uint16_t *>(to)[e] = reinterpret_cast<const uint16_t *>(p)[e];
+        else if (e + 1 < end) reinterpret_cast<uint16_t *>(to)[e + 1] = reinterpret_cast<const uint16_t *>(p)[e + 1];
     }
 }
+// the same where all rows are whole eights on 16 bytes: `mine` is the lane's place in row 0
 template <bool F32>
-__device__ __forceinline__ void row_here(const uint4 *slot, int step, f32x2 v[4]) {
-    if (F32) pairs_of_eight(slot[0], slot[step], v);
-    else pairs_of_eight(slot[0], v);
+__device__ __forceinline__ void row_ahead(const uint8_t *mine, uint32_t stride, uint32_t t, const WarpEight &w, uint8_t *to) {
+    const uint8_t *p = mine + (uint64_t)t * stride;
+    copy_ahead(to + w.lane * 16, p);
+    if (F32) copy_ahead(to + 512 + w.lane * 16, p + 16);
 }
-__device__ __forceinline__ void row_here(bool f32, const uint4 *slot, int step, f32x2 v[4]) {
-    if (f32) row_here<true>(slot, step, v);
-    else row_here<false>(slot, step, v);
+// the lane's eight, zeros behind the row's end
+template <bool F32, bool WHOLE>
+__device__ __forceinline__ void row_here(const Rows &r, int64_t t, const WarpEight &w, const uint8_t *at, f32x2 v[4]) {
+    if (F32) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(at + w.lane * (WHOLE ? 16 : 32));
+        pairs_of_eight(p[0], p[WHOLE ? 32 : 1], v);
+    } else {
+        uint4 q = *reinterpret_cast<const uint4 *>(at + w.lane * 16);
+        if (!WHOLE && !r.aligned && between(r, t)) {
+            const uint32_t next = *reinterpret_cast<const uint32_t *>(at + w.lane * 16 + 16);
+            q = make_uint4(__funnelshift_r(q.x, q.y, 16), __funnelshift_r(q.y, q.z, 16), __funnelshift_r(q.z, q.w, 16), __funnelshift_r(q.w, next, 16));
+        }
+        pairs_of_eight(q, v);
+    }
+    if (!WHOLE && w.cnt < 8) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 x = apart(v[j]);
+            v[j] = pair(2 * j < w.cnt ? x.x : 0.f, 2 * j + 1 < w.cnt ? x.y : 0.f);
+        }
+    }
 }
+// the warp's eights to row t; `room`: 1024 bytes of the warp's shared memory
+template <bool F32>
+__device__ __forceinline__ void row_out(const Rows &r, int64_t t, const WarpEight &w, int n, const f32x2 v[4], uint8_t *room) {
+    void *row = const_cast<void *>(row_at<F32>(r, t));
+    if (r.aligned) {
+        if (w.cnt) store_eight<F32>(row, w.mine(), n, w.cnt == 8, v);
+        return;
+    }
+    const int here = min(256, n - w.col);
+    if (F32) {
+        f32x2 *mine = reinterpret_cast<f32x2 *>(room + w.lane * 32);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mine[j] = v[j];
+        __syncwarp();
+        uint32_t *p = static_cast<uint32_t *>(row) + w.col;
+#pragma unroll
+        for (int i = w.lane; i < 256; i += 32)
+            if (i < here) p[i] = reinterpret_cast<const uint32_t *>(room)[i];
+    } else {
+        *reinterpret_cast<uint4 *>(room + w.lane * 16) = bf16_eight(v);
+        __syncwarp();
+        const int odd = between(r, t);
+        uint16_t *p = static_cast<uint16_t *>(row) + w.col;
+        const uint16_t *from = reinterpret_cast<const uint16_t *>(room);
+        for (int i = w.lane; i < 129; i += 32) {
+            const int e = 2 * i - odd;       // entries e and e + 1 of the warp's share a word of the row
+            if (e >= 0 && e + 1 < here) *reinterpret_cast<uint32_t *>(p + e) = (uint32_t)from[e] | (uint32_t)from[e + 1] << 16;
+            else if (e >= 0 && e < here) p[e] = from[e];
+            else if (e == -1 && here > 0) p[0] = from[0];
+        }
+    }
+    __syncwarp();
+}
+// and where all rows are whole eights on 16 bytes
+template <bool F32>
+__device__ __forceinline__ void row_out(uint8_t *mine, uint32_t stride, uint32_t t, const f32x2 v[4]) {
+    uint8_t *p = mine + (uint64_t)t * stride;
+    if (F32) {
+        ulonglong2 *q = reinterpret_cast<ulonglong2 *>(p);
+        q[0] = make_ulonglong2(v[0], v[1]);
+        q[1] = make_ulonglong2(v[2], v[3]);
+    } else *reinterpret_cast<uint4 *>(p) = bf16_eight(v);
+}
+
 __device__ __forceinline__ float vector_one(const void *p, bool f32, int i) {
     return f32 ? static_cast<const float *>(p)[i] : __uint_as_float((uint32_t) static_cast<const uint16_t *>(p)[i] << 16);
 }
 // factors of eight columns in fp32, the product of what is given (null: 1); zeros behind the row's end
-__device__ __forceinline__ void columns_here(uint4 *to, int step, int col, int n, bool f32, float scale, const void *v, const void *w) {
+__device__ __forceinline__ void columns_here(uint4 *to, int col, int n, bool f32, float scale, const void *v, const void *w) {
     float x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -80,12 +179,20 @@ __device__ __forceinline__ void columns_here(uint4 *to, int step, int col, int n
         if (col + j < n && w) x[j] *= vector_one(w, f32, col + j);
     }
     to[0] = fp32_four(x);
-    to[step] = fp32_four(x + 4);
+    to[32] = fp32_four(x + 4);
 }
 
+__device__ __forceinline__ void factors_here(const uint4 *at, f32x2 v[4]) {
+    const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(at), b = *reinterpret_cast<const ulonglong2 *>(at + 32);
+    v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+}
+
+// Sums over the row.  In a thread block they meet at a barrier of the team's; in a cluster every warp sends its own to each block's shared memory, where an mbarrier counts the bytes (no fence, which would wait
+// for the rows written meanwhile).  Two buffers in turn: who writes one again has passed a barrier that its readers reached behind their reading.
 struct JoinTeam {
-    int lane, warp, warps, team, teams, rank, cluster, parity, room;
-    float *sums;                             // [parity][team][2][room]: zeros behind the warps'
+    int lane, warp, warps, team, teams, rank, cluster, room;
+    uint32_t turn;                           // sums so far
+    float *sums;                             // [buffer][team][2][room]: zeros behind the warps'; then, of a cluster, its barriers
     __device__ __forceinline__ JoinTeam(const JoinArgs &a, float *s) {
         lane = threadIdx.x & 31;
         const int w = threadIdx.x >> 5;
@@ -95,18 +202,26 @@ struct JoinTeam {
         warp = w - team * warps;
         asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
         asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
-        parity = 0;
+        turn = 0;
         sums = s;
         room = (warps * cluster + 3) & ~3;
         for (int i = threadIdx.x; i < 4 * teams * room; i += blockDim.x) s[i] = 0.f;
-        // (a cluster: every block has started before its shared memory is written)
-        if (cluster > 1) meet();
-        else __syncthreads();
+        if (cluster > 1) {
+            if (threadIdx.x < 2) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(barrier(threadIdx.x)) : "memory");
+            // (every block's barriers are there before another one sends)
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            meet();
+        } else __syncthreads();
     }
     __device__ __forceinline__ int64_t first() const { return (int64_t)(blockIdx.x / cluster) * teams + team; }
     __device__ __forceinline__ int64_t step() const { return (int64_t)(gridDim.x / cluster) * teams; }
     __device__ __forceinline__ static void meet() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-    // Sums over the row, the same in every thread of it.  Two buffers in turn: who writes one again has passed a barrier that its readers reached behind their reading.
+    // (no block ends while another one may still send to it)
+    __device__ __forceinline__ void done() const {
+        if (cluster > 1) meet();
+    }
+    __device__ __forceinline__ uint32_t barrier(int i) const { return (uint32_t)__cvta_generic_to_shared(sums + 4 * teams * room) + 8 * i; }
+    // the same sums in every thread of the row
     template <int K>
     __device__ __forceinline__ void add(float (&v)[K]) {
 #pragma unroll
@@ -115,23 +230,33 @@ struct JoinTeam {
             for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(FULL, v[k], o);
         const int all = warps * cluster;
         if (all == 1) return;
-        float *s = sums + (parity * teams + team) * 2 * room;
-        parity ^= 1;
+        bool late = false;                   // a wait that ran out: the row becomes NaN
+        const int buffer = turn & 1;
+        float *s = sums + (buffer * teams + team) * 2 * room;
         if (cluster == 1) {
             if (lane == 0)
 #pragma unroll
                 for (int k = 0; k < K; ++k) s[k * room + warp] = v[k];
             asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(warps * 32) : "memory");
         } else {
-            namespace cg = cooperative_groups;
-            auto c = cg::this_cluster();
+            if (threadIdx.x == 0)
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(barrier(buffer)), "r"(all * K * 4) : "memory");
             if (lane < cluster) {
-                float *to = c.map_shared_rank(s, lane);
 #pragma unroll
-                for (int k = 0; k < K; ++k) to[k * room + rank * warps + warp] = v[k];
+                for (int k = 0; k < K; ++k) {
+                    uint32_t to, bar;
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(s + k * room + rank * warps + warp)), "r"(lane));
+                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(barrier(buffer)), "r"(lane));
+                    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to), "r"(__float_as_uint(v[k])), "r"(bar) : "memory");
+                }
             }
-            meet();
+            const uint32_t phase = (turn >> 1) & 1;
+            uint32_t ok = 0;
+            for (int i = 0; i < JOIN_WAIT && !ok; ++i)
+                asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(barrier(buffer)), "r"(phase) : "memory");
+            late = !ok;
         }
+        ++turn;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             float4 x = *reinterpret_cast<const float4 *>(s + k * room);
@@ -140,129 +265,145 @@ struct JoinTeam {
                 x = *reinterpret_cast<const float4 *>(s + k * room + i);
                 v[k] += (x.x + x.y) + (x.z + x.w);
             }
+            if (late) v[k] = __uint_as_float(0x7FC00000u);
         }
     }
 };
 
 // mean and 1 / deviation of the row whose entries the threads hold (zeros behind its end)
-template <int E>
-__device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4], const int (&cnt)[E], int norm, float eps, float inv_n) {
-    if (norm == DBSPMSPV_NORM_NONE) return make_float2(0.f, 1.f);
+template <int E, bool WHOLE>
+__device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4], const WarpEight (&w)[E], int norm, float eps, float inv_n) {
     float mean = 0.f, s[1];
-    f32x2 p = 0;
-    if (norm == DBSPMSPV_NORM_LAYER) {
+    f32x2 p[2] = {0, 0};
+    if (norm == DBSPMSPV_NORM_RMS) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) p = add2(p, v[e][j]);
-        s[0] = sum2(p);
+            for (int j = 0; j < 4; ++j) p[j % 2] = fma2(v[e][j], v[e][j], p[j % 2]);
+        s[0] = sum2(add2(p[0], p[1]));
+    } else if (norm == DBSPMSPV_NORM_LAYER) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[j % 2] = add2(p[j % 2], v[e][j]);
+        s[0] = sum2(add2(p[0], p[1]));
         tm.add(s);
         mean = s[0] * inv_n;
-        p = 0;
-    }
+        s[0] = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e)
+        for (int e = 0; e < E; ++e) {
+            if (WHOLE && w[e].cnt == 0) continue;                            // (zeros behind the end have no difference from the mean)
+            p[0] = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const f32x2 d = add2(v[e][j], both(-mean));
-            p = fma2(d, d, p);
-        }
-    s[0] = sum2(p);
-    if (norm == DBSPMSPV_NORM_LAYER)
-#pragma unroll
-        for (int e = 0; e < E; ++e)          // (the zeros behind the end have no difference: once more without them)
-            if (cnt[e] < 8) {
-                s[0] = 0.f;
-#pragma unroll
-                for (int i = 0; i < E; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float2 x = apart(v[i][j]);
-                        if (2 * j < cnt[i]) s[0] += (x.x - mean) * (x.x - mean);
-                        if (2 * j + 1 < cnt[i]) s[0] += (x.y - mean) * (x.y - mean);
-                    }
-                break;
+            for (int j = 0; j < 4; ++j) {
+                f32x2 d = add2(v[e][j], both(-mean));
+                if (!WHOLE && w[e].cnt < 8) {
+                    const float2 x = apart(d);
+                    d = pair(2 * j < w[e].cnt ? x.x : 0.f, 2 * j + 1 < w[e].cnt ? x.y : 0.f);
+                }
+                p[0] = fma2(d, d, p[0]);
             }
+            s[0] += sum2(p[0]);
+        }
+    } else return make_float2(0.f, 1.f);
     tm.add(s);
     return make_float2(mean, rsqrtf(s[0] * inv_n + eps));
 }
 
-// Shared memory: the slots [ahead][eight][piece][thread], the columns' factors [eight][piece][thread], the teams' sums
-inline size_t join_smem(const JoinPlan &p, int pieces, int params) {
-    return (size_t)(JOIN_AHEAD * pieces + params) * p.eights * p.warps * p.teams * 32 * 16 + (size_t)4 * p.teams * ((p.warps * p.cluster + 3) & ~3) * 4;
+// A warp's shared memory: the rows [ahead][eight][array], the columns' factors [eight][piece][lane], room for rows that are written in words.  Behind the warps': the teams' sums, barriers.
+__host__ __device__ inline int join_warp_bytes(int eights, int room, int params, bool whole) { return JOIN_AHEAD * room + eights * params * 512 + (whole ? 0 : 1024); }
+inline size_t join_smem(const JoinPlan &p, int room, int params, bool whole) {
+    return (size_t)join_warp_bytes(p.eights, room, params, whole) * p.warps * p.teams + (size_t)4 * p.teams * ((p.warps * p.cluster + 3) & ~3) * 4 + 16;
 }
 
-// What both kernels begin with: this thread's columns, slots and factors
-template <int E>
-struct JoinThread {
-    uint4 *slots, *factors;
-    int step, pieces, params, col[E], cnt[E];
-    __device__ __forceinline__ JoinThread(const JoinArgs &a, uint4 *s_dyn, const JoinTeam &tm) {
-        step = blockDim.x;
-        pieces = a.pieces;
-        params = a.params;
-        slots = s_dyn + threadIdx.x;
-        factors = slots + JOIN_AHEAD * E * a.pieces * step;
+// What both kernels begin with: the warp's columns and its shared memory
+template <int E, bool WHOLE>
+struct JoinWarp {
+    uint8_t *rows, *spare;
+    uint4 *factors;
+    int room;
+    WarpEight w[E];
+    __device__ __forceinline__ JoinWarp(const JoinArgs &a, uint8_t *s_dyn, const JoinTeam &tm) {
+        room = a.room;
+        rows = s_dyn + (threadIdx.x >> 5) * join_warp_bytes(E, a.room, a.params, WHOLE);
+        factors = reinterpret_cast<uint4 *>(rows + JOIN_AHEAD * room) + tm.lane;
+        spare = rows + JOIN_AHEAD * room + E * a.params * 512;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            col[e] = (((tm.rank * E + e) * tm.warps + tm.warp) * 32 + tm.lane) * 8;
-            cnt[e] = max(0, min(8, a.n - col[e]));
+            w[e].lane = tm.lane;
+            w[e].col = ((tm.rank * tm.warps + tm.warp) * E + e) * 256;
+            w[e].cnt = max(0, min(8, a.n - w[e].mine()));
         }
-        for (int i = 0; i < JOIN_AHEAD * E * a.pieces; ++i) slots[i * step] = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = tm.lane; i < JOIN_AHEAD * room / 16; i += 32) reinterpret_cast<uint4 *>(rows)[i] = make_uint4(0u, 0u, 0u, 0u);
+        __syncwarp();
     }
-    __device__ __forceinline__ uint4 *slot(int at, int e, int piece) const { return slots + ((at * E + e) * pieces + piece) * step; }
-    __device__ __forceinline__ uint4 *factor(int e, int piece) const { return factors + (e * params + piece) * step; }
+    __device__ __forceinline__ uint4 *factor(int e, int params, int piece) const { return factors + (e * params + piece) * 32; }
+    // the lane's place in row 0
+    template <bool F32>
+    __device__ __forceinline__ uint8_t *mine(const Rows &r) const { return static_cast<uint8_t *>(r.p) + (int64_t)w[0].mine() * (F32 ? 4 : 2); }
 };
 
 // factors: gate * w_block * scales (or without a gate that has rows), w_next, then (BIAS) c_block * gate * scales, c_next
-template <bool SF32, bool BF32, int E, bool BIAS>
+template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE>
 __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __grid_constant__ JoinArgs a) {
-    extern __shared__ __align__(16) uint4 s_dyn[];
-    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + (size_t)(JOIN_AHEAD * a.pieces + a.params) * E * blockDim.x));
-    const JoinThread<E> me(a, s_dyn, tm);
-    const int n = a.n, step = me.step;
-    constexpr int RP = SF32 ? 2 : 1, BP = BF32 ? 2 : 1;
+    extern __shared__ __align__(16) uint8_t s_dyn[];
+    constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, PARAMS = BIAS ? 8 : 4;
+    // where a lane's eights of r, b and the gate lie in a row's shared memory
+    constexpr int AT_R = 0, AT_B = E * eight_room<SF32, WHOLE>(), AT_G = AT_B + E * eight_room<BF32, WHOLE>();
+    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, PARAMS, WHOLE) * (blockDim.x >> 5)));
+    const JoinWarp<E, WHOLE> me(a, s_dyn, tm);
+    const int n = a.n;
     pdl_wait();
     pdl_trigger();
-    const int64_t first = tm.first(), walk = tm.step();
-    auto ahead = [&](int64_t t, int at) {
-        if (t < a.tokens)
+    const uint32_t tokens = a.tokens, walk = (uint32_t)tm.step(), first = (uint32_t)tm.first();
+    const uint8_t *my_r = me.template mine<SF32>(a.r), *my_b = me.template mine<BF32>(a.b);
+    uint8_t *my_out = me.template mine<SF32>(a.out), *my_h = me.template mine<false>(a.h);
+    const uint32_t r_step = (uint32_t)a.r.ld * SZ, b_step = (uint32_t)a.b.ld * BZ, out_step = (uint32_t)a.out.ld * SZ, h_step = (uint32_t)a.h.ld * 2;
+    auto ahead = [&](uint32_t t, uint8_t *to) {
+        if (t < tokens)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                if (me.cnt[e] == 0) continue;
-                if (a.r.p) row_ahead<SF32>(a.r, t, me.col[e], n, me.slot(at, e, 0), step);
-                if (a.b.p) row_ahead<BF32>(a.b, t, me.col[e], n, me.slot(at, e, RP), step);
+                if (WHOLE) {
+                    if (me.w[e].cnt == 0) continue;
+                    row_ahead<SF32>(my_r + e * 256 * SZ, r_step, t, me.w[e], to + AT_R + e * eight_room<SF32, WHOLE>());
+                    row_ahead<BF32>(my_b + e * 256 * BZ, b_step, t, me.w[e], to + AT_B + e * eight_room<BF32, WHOLE>());
+                } else {
+                    if (a.r.p) row_ahead<SF32>(a.r, t, me.w[e], n, to + AT_R + e * eight_room<SF32, WHOLE>());
+                    if (a.b.p) row_ahead<BF32>(a.b, t, me.w[e], n, to + AT_B + e * eight_room<BF32, WHOLE>());
+                }
                 if (a.gate.p) {
-                    if (a.params_f32) row_ahead<true>(a.gate, t, me.col[e], n, me.slot(at, e, RP + BP), step);
-                    else row_ahead<false>(a.gate, t, me.col[e], n, me.slot(at, e, RP + BP), step);
+                    if (a.params_f32) row_ahead<true>(a.gate, t, me.w[e], n, to + AT_G + e * eight_room<true, false>());
+                    else row_ahead<false>(a.gate, t, me.w[e], n, to + AT_G + e * eight_room<false, false>());
                 }
             }
         close_ahead();
     };
 #pragma unroll
-    for (int i = 0; i < JOIN_AHEAD; ++i) ahead(first + i * walk, i);
+    for (int i = 0; i < JOIN_AHEAD; ++i) ahead(first + i * walk, me.rows + i * me.room);
     const Numbers num = numbers_of(a.drop);
     const float scale = a.drop.random ? a.scale * a.drop.scale : a.scale;
     Columns cols[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        cols[e] = columns_of(num, (uint32_t)me.col[e] >> 3);
-        columns_here(me.factor(e, 0), step, me.col[e], n, a.params_f32, scale, a.w_block, a.gate_vec);
-        columns_here(me.factor(e, 2), step, me.col[e], n, a.params_f32, 1.f, a.w_next, nullptr);
+        const int col = me.w[e].mine();
+        cols[e] = columns_of(num, (uint32_t)col >> 3);
+        columns_here(me.factor(e, PARAMS, 0), col, n, a.params_f32, scale, a.w_block, a.gate_vec);
+        columns_here(me.factor(e, PARAMS, 2), col, n, a.params_f32, 1.f, a.w_next, nullptr);
         if (BIAS) {
-            columns_here(me.factor(e, 4), step, me.col[e], n, a.params_f32, a.c_block ? scale : 0.f, a.c_block, a.gate_vec);
-            columns_here(me.factor(e, 6), step, me.col[e], n, a.params_f32, a.c_next ? 1.f : 0.f, a.c_next, nullptr);
+            columns_here(me.factor(e, PARAMS, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, a.c_block, a.gate_vec);
+            columns_here(me.factor(e, PARAMS, 6), col, n, a.params_f32, a.c_next ? 1.f : 0.f, a.c_next, nullptr);
         }
     }
-    int at = 0;
-    for (int64_t t = first; t < a.tokens; t += walk) {
+    uint8_t *at = me.rows;
+    for (uint32_t t = first; t < tokens; t += walk) {
         wait_ahead<JOIN_AHEAD - 1>();
+        if (!WHOLE) __syncwarp();             // (words are other lanes')
         f32x2 v[E][4], x[E][4], w[4];
         float2 sb = make_float2(0.f, 1.f);
-        if (a.b.p) {
+        if (WHOLE || a.b.p) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) row_here<BF32>(me.slot(at, e, RP), step, v[e]);
-            sb = norm_stats<E>(tm, v, me.cnt, a.norm_block, a.eps_block, a.inv_n);
+            for (int e = 0; e < E; ++e) row_here<BF32, WHOLE>(a.b, t, me.w[e], at + AT_B + e * eight_room<BF32, WHOLE>(), v[e]);
+            sb = norm_stats<E, WHOLE>(tm, v, me.w, a.norm_block, a.eps_block, a.inv_n);
             const f32x2 inv = both(sb.y), shift = both(-sb.x * sb.y);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -270,114 +411,136 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
                 for (int j = 0; j < 4; ++j) v[e][j] = fma2(v[e][j], inv, shift);
                 if (BIAS) {
                     f32x2 c[4];
-                    row_here<true>(me.factor(e, 0), step, w);
-                    row_here<true>(me.factor(e, 4), step, c);
+                    factors_here(me.factor(e, PARAMS, 0), w);
+                    factors_here(me.factor(e, PARAMS, 4), c);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[e][j] = fma2(v[e][j], w[j], c[j]);
                 }
                 if (a.gate.p) {
-                    row_here(a.params_f32, me.slot(at, e, RP + BP), step, w);
+                    if (a.params_f32) row_here<true, false>(a.gate, t, me.w[e], at + AT_G + e * eight_room<true, false>(), w);
+                    else row_here<false, false>(a.gate, t, me.w[e], at + AT_G + e * eight_room<false, false>(), w);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[e][j] = mul2(v[e][j], w[j]);
                 }
-                if (a.drop.random) drop_eight(a.drop, num, cols[e], (uint32_t)t, v[e]);
-                row_here<SF32>(me.slot(at, e, 0), step, x[e]);
-                if (!BIAS) row_here<true>(me.factor(e, 0), step, w);
+                if (a.drop.random) drop_eight(a.drop, num, cols[e], t, v[e]);
+                row_here<SF32, WHOLE>(a.r, t, me.w[e], at + AT_R + e * eight_room<SF32, WHOLE>(), x[e]);
+                if (!BIAS) factors_here(me.factor(e, PARAMS, 0), w);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[e][j] = BIAS ? add2(v[e][j], x[e][j]) : fma2(v[e][j], w[j], x[e][j]);
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) row_here<SF32>(me.slot(at, e, 0), step, x[e]);
+            for (int e = 0; e < E; ++e) row_here<SF32, WHOLE>(a.r, t, me.w[e], at + AT_R + e * eight_room<SF32, WHOLE>(), x[e]);
         }
+        if (!WHOLE) __syncwarp();
         ahead(t + JOIN_AHEAD * walk, at);
-        at = at + 1 == JOIN_AHEAD ? 0 : at + 1;
-        if (a.out.p)
+        at = at == me.rows ? me.rows + me.room : me.rows;
+        static_assert(JOIN_AHEAD == 2, "two rows in turn");
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (me.cnt[e]) store_eight<SF32>(const_cast<void *>(row_at<SF32>(a.out, t)), me.col[e], n, me.cnt[e] == 8 && a.out.aligned, x[e]);
-        if (!a.h.p && !a.stats) continue;
-        const float2 sn = norm_stats<E>(tm, x, me.cnt, a.norm_next, a.eps_next, a.inv_n);
+        for (int e = 0; e < E; ++e) {
+            if (WHOLE) {
+                if (me.w[e].cnt) row_out<SF32>(my_out + e * 256 * SZ, out_step, t, x[e]);
+            } else if (a.out.p) row_out<SF32>(a.out, t, me.w[e], n, x[e], me.spare);
+        }
+        if (!WHOLE && !a.h.p && !a.stats) continue;
+        const float2 sn = norm_stats<E, WHOLE>(tm, x, me.w, a.norm_next, a.eps_next, a.inv_n);
         if (a.stats && tm.rank == 0 && tm.warp == 0 && tm.lane == 0) reinterpret_cast<float4 *>(a.stats)[t] = make_float4(sb.x, sb.y, sn.x, sn.y);
-        if (a.h.p) {
-            const f32x2 inv = both(sn.y), shift = both(-sn.x * sn.y);
+        if (!WHOLE && !a.h.p) continue;
+        const f32x2 inv = both(sn.y), shift = both(-sn.x * sn.y);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (me.cnt[e] == 0) continue;
-                f32x2 c[4];
-                row_here<true>(me.factor(e, 2), step, w);
-                if (BIAS) row_here<true>(me.factor(e, 6), step, c);
+        for (int e = 0; e < E; ++e) {
+            f32x2 c[4];
+            factors_here(me.factor(e, PARAMS, 2), w);
+            if (BIAS) factors_here(me.factor(e, PARAMS, 6), c);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f32x2 y = fma2(x[e][j], inv, shift);
-                    x[e][j] = BIAS ? fma2(y, w[j], c[j]) : mul2(y, w[j]);
-                }
-                store_eight<false>(const_cast<void *>(row_at<false>(a.h, t)), me.col[e], n, me.cnt[e] == 8 && a.h.aligned, x[e]);
+            for (int j = 0; j < 4; ++j) {
+                const f32x2 y = fma2(x[e][j], inv, shift);
+                x[e][j] = BIAS ? fma2(y, w[j], c[j]) : mul2(y, w[j]);
             }
+            if (WHOLE) {
+                if (me.w[e].cnt) row_out<false>(my_h + e * 512, h_step, t, x[e]);
+            } else row_out<false>(a.h, t, me.w[e], n, x[e], me.spare);
         }
     }
+    tm.done();
 }
 
-// factors: w_next, gate * w_block * scales (or without a gate that has rows), then c_block * scales for the gradient of such a gate.  Sums over a team's tokens: dw_next, A, then (BIAS) dc_next, B.
-template <bool SF32, bool BF32, int E, bool BIAS>
+// factors: w_next, gate * w_block * scales (or without a gate that has rows), c_block * scales for the gradient of such a gate.  Sums over a team's tokens: dw_next, A, then (BIAS) dc_next, B.
+template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE>
 __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward(const __grid_constant__ JoinArgs a) {
-    extern __shared__ __align__(16) uint4 s_dyn[];
-    constexpr int SP = SF32 ? 2 : 1, BP = BF32 ? 2 : 1, SUMS = BIAS ? 4 : 2;
-    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + (size_t)(JOIN_AHEAD * a.pieces + a.params) * E * blockDim.x));
-    const JoinThread<E> me(a, s_dyn, tm);
-    const int n = a.n, step = me.step;
+    extern __shared__ __align__(16) uint8_t s_dyn[];
+    constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, SUMS = BIAS ? 4 : 2;
+    constexpr int S8 = eight_room<SF32, WHOLE>(), B8 = eight_room<BF32, WHOLE>(), H8 = eight_room<false, WHOLE>();
+    constexpr int AT_DOUT = E * H8, AT_OUT = AT_DOUT + E * S8, AT_B = AT_OUT + E * S8, AT_G = AT_B + E * B8;
+    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, a.params, WHOLE) * (blockDim.x >> 5)));
+    const JoinWarp<E, WHOLE> me(a, s_dyn, tm);
+    const int n = a.n;
     pdl_wait();
     pdl_trigger();
-    const int64_t first = tm.first(), walk = tm.step();
-    const bool block = a.parts || a.db.p || a.dgate.p;
-    // pieces: dh, dout, out, b, gate
-    constexpr int DOUT = 1, OUT = DOUT + SP, B = OUT + SP, GATE = B + BP;
-    auto ahead = [&](int64_t t, int at) {
-        if (t < a.tokens)
+    const uint32_t tokens = a.tokens, walk = (uint32_t)tm.step(), first = (uint32_t)tm.first();
+    const bool block = WHOLE || a.parts || a.db.p || a.dgate.p;
+    const uint8_t *my_dh = me.template mine<false>(a.dh), *my_dout = me.template mine<SF32>(a.dout), *my_out = me.template mine<SF32>(a.out), *my_b = me.template mine<BF32>(a.b);
+    uint8_t *my_dr = me.template mine<SF32>(a.dr), *my_db = a.db.f32 ? me.template mine<true>(a.db) : me.template mine<false>(a.db);
+    const uint32_t dh_step = (uint32_t)a.dh.ld * 2, dout_step = (uint32_t)a.dout.ld * SZ, out_step = (uint32_t)a.out.ld * SZ, b_step = (uint32_t)a.b.ld * BZ, dr_step = (uint32_t)a.dr.ld * SZ,
+                   db_step = (uint32_t)a.db.ld * (a.db.f32 ? 4 : 2);
+    auto ahead = [&](uint32_t t, uint8_t *to) {
+        if (t < tokens)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                if (me.cnt[e] == 0) continue;
-                if (a.dh.p) row_ahead<false>(a.dh, t, me.col[e], n, me.slot(at, e, 0), step);
-                if (a.dout.p) row_ahead<SF32>(a.dout, t, me.col[e], n, me.slot(at, e, DOUT), step);
-                if (a.out.p) row_ahead<SF32>(a.out, t, me.col[e], n, me.slot(at, e, OUT), step);
-                if (a.b.p) row_ahead<BF32>(a.b, t, me.col[e], n, me.slot(at, e, B), step);
+                if (WHOLE) {
+                    if (me.w[e].cnt == 0) continue;
+                    row_ahead<false>(my_dh + e * 512, dh_step, t, me.w[e], to + e * H8);
+                    row_ahead<SF32>(my_dout + e * 256 * SZ, dout_step, t, me.w[e], to + AT_DOUT + e * S8);
+                    row_ahead<SF32>(my_out + e * 256 * SZ, out_step, t, me.w[e], to + AT_OUT + e * S8);
+                    row_ahead<BF32>(my_b + e * 256 * BZ, b_step, t, me.w[e], to + AT_B + e * B8);
+                } else {
+                    if (a.dh.p) row_ahead<false>(a.dh, t, me.w[e], n, to + e * H8);
+                    if (a.dout.p) row_ahead<SF32>(a.dout, t, me.w[e], n, to + AT_DOUT + e * S8);
+                    if (a.out.p) row_ahead<SF32>(a.out, t, me.w[e], n, to + AT_OUT + e * S8);
+                    if (a.b.p) row_ahead<BF32>(a.b, t, me.w[e], n, to + AT_B + e * B8);
+                }
                 if (a.gate.p) {
-                    if (a.params_f32) row_ahead<true>(a.gate, t, me.col[e], n, me.slot(at, e, GATE), step);
-                    else row_ahead<false>(a.gate, t, me.col[e], n, me.slot(at, e, GATE), step);
+                    if (a.params_f32) row_ahead<true>(a.gate, t, me.w[e], n, to + AT_G + e * eight_room<true, false>());
+                    else row_ahead<false>(a.gate, t, me.w[e], n, to + AT_G + e * eight_room<false, false>());
                 }
             }
         close_ahead();
     };
 #pragma unroll
-    for (int i = 0; i < JOIN_AHEAD; ++i) ahead(first + i * walk, i);
+    for (int i = 0; i < JOIN_AHEAD; ++i) ahead(first + i * walk, me.rows + i * me.room);
     const Numbers num = numbers_of(a.drop);
     const float scale = a.drop.random ? a.scale * a.drop.scale : a.scale;
     Columns cols[E];
     f32x2 sum[SUMS][E][4];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        cols[e] = columns_of(num, (uint32_t)me.col[e] >> 3);
-        columns_here(me.factor(e, 0), step, me.col[e], n, a.params_f32, 1.f, a.w_next, nullptr);
-        columns_here(me.factor(e, 2), step, me.col[e], n, a.params_f32, scale, a.w_block, a.gate_vec);
-        if (a.dgate.p) columns_here(me.factor(e, 4), step, me.col[e], n, a.params_f32, a.c_block ? scale : 0.f, a.c_block, nullptr);
+        const int col = me.w[e].mine();
+        cols[e] = columns_of(num, (uint32_t)col >> 3);
+        columns_here(me.factor(e, a.params, 0), col, n, a.params_f32, 1.f, a.w_next, nullptr);
+        columns_here(me.factor(e, a.params, 2), col, n, a.params_f32, scale, a.w_block, a.gate_vec);
+        if (a.dgate.p) columns_here(me.factor(e, a.params, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, a.c_block, nullptr);
 #pragma unroll
         for (int k = 0; k < SUMS; ++k)
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum[k][e][j] = 0;
     }
-    int at = 0;
-    for (int64_t t = first; t < a.tokens; t += walk) {
-        const float4 st = a.stats ? reinterpret_cast<const float4 *>(a.stats)[t] : make_float4(0.f, 1.f, 0.f, 1.f);
+    const float4 *stats = reinterpret_cast<const float4 *>(a.stats);
+    float4 st_next = stats && first < tokens ? stats[first] : make_float4(0.f, 1.f, 0.f, 1.f);
+    uint8_t *at = me.rows;
+    for (uint32_t t = first; t < tokens; t += walk) {
+        const float4 st = st_next;
+        if (stats && t + walk < tokens) st_next = stats[t + walk];
         wait_ahead<JOIN_AHEAD - 1>();
+        if (!WHOLE) __syncwarp();
         f32x2 g[E][4], u[E][4], w[4];
         // g: normalised out, u: dh * w_next
         const f32x2 inv_out = both(st.w), shift_out = both(-st.z * st.w);
         f32x2 p0 = 0, p1 = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            row_here<false>(me.slot(at, e, 0), step, u[e]);
-            row_here<SF32>(me.slot(at, e, OUT), step, g[e]);
-            row_here<true>(me.factor(e, 0), step, w);
+            row_here<false, WHOLE>(a.dh, t, me.w[e], at + e * H8, u[e]);
+            row_here<SF32, WHOLE>(a.out, t, me.w[e], at + AT_OUT + e * S8, g[e]);
+            factors_here(me.factor(e, a.params, 0), w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 g[e][j] = fma2(g[e][j], inv_out, shift_out);
@@ -389,7 +552,7 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
             }
         }
         f32x2 slope = both(1.f), along = 0, mean = 0;
-        if (a.norm_next != DBSPMSPV_NORM_NONE && a.dh.p) {
+        if (a.norm_next != DBSPMSPV_NORM_NONE && (WHOLE || a.dh.p)) {
             float s[2] = {sum2(p0), sum2(p1)};
             tm.add(s);
             slope = inv_out;
@@ -401,30 +564,33 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
         p0 = p1 = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            row_here<SF32>(me.slot(at, e, DOUT), step, w);
+            row_here<SF32, WHOLE>(a.dout, t, me.w[e], at + AT_DOUT + e * S8, w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) g[e][j] = add2(w[j], fma2(u[e][j], slope, fma2(g[e][j], along, mean)));
-            if (me.cnt[e] && a.dr.p) store_eight<SF32>(const_cast<void *>(row_at<SF32>(a.dr, t)), me.col[e], n, me.cnt[e] == 8 && a.dr.aligned, g[e]);
+            if (WHOLE) {
+                if (me.w[e].cnt) row_out<SF32>(my_dr + e * 256 * SZ, dr_step, t, g[e]);
+            } else if (a.dr.p) row_out<SF32>(a.dr, t, me.w[e], n, g[e], me.spare);
             if (!block) continue;
-            if (a.drop.random) drop_eight(a.drop, num, cols[e], (uint32_t)t, g[e]);
-            row_here<BF32>(me.slot(at, e, B), step, u[e]);
+            if (a.drop.random) drop_eight(a.drop, num, cols[e], t, g[e]);
+            row_here<BF32, WHOLE>(a.b, t, me.w[e], at + AT_B + e * B8, u[e]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) u[e][j] = fma2(u[e][j], inv_b, shift_b);
             if (a.gate.p) {
-                if (a.dgate.p && me.cnt[e]) {
+                if (a.dgate.p) {
                     f32x2 d[4];
-                    row_here<true>(me.factor(e, 2), step, w);
-                    row_here<true>(me.factor(e, 4), step, d);
+                    factors_here(me.factor(e, a.params, 2), w);
+                    factors_here(me.factor(e, a.params, 4), d);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) d[j] = mul2(g[e][j], fma2(u[e][j], w[j], d[j]));
-                    if (a.params_f32) store_eight<true>(const_cast<void *>(row_at<true>(a.dgate, t)), me.col[e], n, me.cnt[e] == 8 && a.dgate.aligned, d);
-                    else store_eight<false>(const_cast<void *>(row_at<false>(a.dgate, t)), me.col[e], n, me.cnt[e] == 8 && a.dgate.aligned, d);
+                    if (a.params_f32) row_out<true>(a.dgate, t, me.w[e], n, d, me.spare);
+                    else row_out<false>(a.dgate, t, me.w[e], n, d, me.spare);
                 }
-                row_here(a.params_f32, me.slot(at, e, GATE), step, w);
+                if (a.params_f32) row_here<true, false>(a.gate, t, me.w[e], at + AT_G + e * eight_room<true, false>(), w);
+                else row_here<false, false>(a.gate, t, me.w[e], at + AT_G + e * eight_room<false, false>(), w);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) g[e][j] = mul2(g[e][j], w[j]);
             }
-            row_here<true>(me.factor(e, 2), step, w);
+            factors_here(me.factor(e, a.params, 2), w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 sum[1][e][j] = fma2(g[e][j], u[e][j], sum[1][e][j]);
@@ -434,9 +600,10 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
                 p1 = add2(g[e][j], p1);
             }
         }
+        if (!WHOLE) __syncwarp();
         ahead(t + JOIN_AHEAD * walk, at);
-        at = at + 1 == JOIN_AHEAD ? 0 : at + 1;
-        if (!a.db.p) continue;
+        at = at == me.rows ? me.rows + me.room : me.rows;
+        if (!WHOLE && !a.db.p) continue;
         slope = both(1.f);
         along = mean = 0;
         if (a.norm_block != DBSPMSPV_NORM_NONE) {
@@ -448,19 +615,23 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            if (me.cnt[e] == 0) continue;
 #pragma unroll
             for (int j = 0; j < 4; ++j) g[e][j] = fma2(g[e][j], slope, fma2(u[e][j], along, mean));
-            if (a.db.f32) store_eight<true>(const_cast<void *>(row_at<true>(a.db, t)), me.col[e], n, me.cnt[e] == 8 && a.db.aligned, g[e]);
-            else store_eight<false>(const_cast<void *>(row_at<false>(a.db, t)), me.col[e], n, me.cnt[e] == 8 && a.db.aligned, g[e]);
+            if (WHOLE) {
+                if (me.w[e].cnt == 0) continue;
+                if (a.db.f32) row_out<true>(my_db + e * 1024, db_step, t, g[e]);
+                else row_out<false>(my_db + e * 512, db_step, t, g[e]);
+            } else if (a.db.f32) row_out<true>(a.db, t, me.w[e], n, g[e], me.spare);
+            else row_out<false>(a.db, t, me.w[e], n, g[e], me.spare);
         }
     }
-    if (!a.parts) return;
+    if (a.parts)
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        if (me.cnt[e])
+        for (int e = 0; e < E; ++e)
+            if (me.w[e].cnt)
 #pragma unroll
-            for (int k = 0; k < SUMS; ++k) store_eight<true>(a.parts + (first * SUMS + k) * a.ldp, me.col[e], (int)a.ldp, true, sum[k][e]);
+                for (int k = 0; k < SUMS; ++k) store_eight<true>(a.parts + (first * (int64_t)SUMS + k) * a.ldp, me.w[e].mine(), (int)a.ldp, true, sum[k][e]);
+    tm.done();
 }
 
 // The teams' sums added up, and what follows from them

@@ -147,6 +147,9 @@ __device__ __forceinline__ const void *row_at(const Rows &r, int64_t t) {
 __device__ __forceinline__ void copy_ahead(void *smem, const void *p) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
 }
+__device__ __forceinline__ void copy_word_ahead(void *smem, const void *p) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
+}
 __device__ __forceinline__ void close_ahead() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void wait_ahead() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
@@ -203,6 +206,10 @@ __device__ __forceinline__ void drop_eight(const Drop &d, const Numbers &s, cons
 }
 
 // ---- the host's side ----------------------------------------------------------------------------
+inline int64_t ceil64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+template <typename... P> inline bool on_bytes(uintptr_t bytes, P... p) { return (((reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0) && ...); }
+inline bool rows_ok(const void *p, int64_t ld, int64_t width) { return !p || ld >= width; }
+
 inline Drop drop_of(float p, const void *random) {
     const int32_t below = (int32_t)((double)p * 65536.0 + 0.5);
     if (below == 0) return Drop{};
