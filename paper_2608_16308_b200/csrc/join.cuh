@@ -22,7 +22,7 @@ constexpr int JOIN_COLS = 4096;              // of a row in one thread block; mo
 constexpr int JOIN_CLUSTER = 8;
 constexpr int64_t JOIN_MAX_N = JOIN_COLS * JOIN_CLUSTER;
 constexpr int JOIN_AHEAD = 2;                // rows in flight or in hand, per team
-constexpr int JOIN_SUMS_COLS = 32, JOIN_SUMS_CTA = 256;
+constexpr int JOIN_SUMS_COLS = 32, JOIN_SUMS_CTA = 512;
 constexpr int JOIN_WAIT = 1 << 20;           // tries of a wait for a cluster's sums, before it gives up
 // threads at most: of kernels with two eights a lane, and with one
 template <int E> __host__ __device__ constexpr int join_cta() { return JOIN_COLS / 8 / E; }
@@ -93,12 +93,12 @@ __device__ __forceinline__ void row_ahead(const Rows &r, int64_t t, const WarpEi
         else if (e + 1 < end) reinterpret_cast<uint16_t *>(to)[e + 1] = reinterpret_cast<const uint16_t *>(p)[e + 1];
     }
 }
-// the same where all rows are whole eights on 16 bytes: `mine` is the lane's place in row 0
+// the same where all rows are whole eights on 16 bytes: `mine` is the lane's place in row 0.  (An eight behind the row's end is 0 bytes long: no branch.)
 template <bool F32>
 __device__ __forceinline__ void row_ahead(const uint8_t *mine, uint32_t stride, uint32_t t, const WarpEight &w, uint8_t *to) {
     const uint8_t *p = mine + (uint64_t)t * stride;
-    copy_ahead(to + w.lane * 16, p);
-    if (F32) copy_ahead(to + 512 + w.lane * 16, p + 16);
+    copy_ahead(to + w.lane * 16, p, w.cnt * 2);
+    if (F32) copy_ahead(to + 512 + w.lane * 16, p + 16, w.cnt * 2);
 }
 // the lane's eight, zeros behind the row's end
 template <bool F32, bool WHOLE>
@@ -189,8 +189,10 @@ __device__ __forceinline__ void factors_here(const uint4 *at, f32x2 v[4]) {
 
 // Sums over the row.  In a thread block they meet at a barrier of the team's; in a cluster every warp sends its own to each block's shared memory, where an mbarrier counts the bytes (no fence, which would wait
 // for the rows written meanwhile).  Two buffers in turn: who writes one again has passed a barrier that its readers reached behind their reading.
+__host__ __device__ inline int join_sums_room(int warps, int cluster) { return warps * cluster < 8 ? 8 : (warps * cluster + 3) & ~3; }
 struct JoinTeam {
     int lane, warp, warps, team, teams, rank, cluster, room;
+    bool alone;                              // a warp has the whole row
     uint32_t turn;                           // sums so far
     float *sums;                             // [buffer][team][2][room]: zeros behind the warps'; then, of a cluster, its barriers
     __device__ __forceinline__ JoinTeam(const JoinArgs &a, float *s) {
@@ -204,7 +206,8 @@ struct JoinTeam {
         asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
         turn = 0;
         sums = s;
-        room = (warps * cluster + 3) & ~3;
+        room = join_sums_room(warps, cluster);
+        alone = warps * cluster == 1;
         for (int i = threadIdx.x; i < 4 * teams * room; i += blockDim.x) s[i] = 0.f;
         if (cluster > 1) {
             if (threadIdx.x < 2) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(barrier(threadIdx.x)) : "memory");
@@ -228,44 +231,49 @@ struct JoinTeam {
         for (int o = 16; o; o >>= 1)
 #pragma unroll
             for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(FULL, v[k], o);
-        const int all = warps * cluster;
-        if (all == 1) return;
-        bool late = false;                   // a wait that ran out: the row becomes NaN
+        if (alone) return;
         const int buffer = turn & 1;
         float *s = sums + (buffer * teams + team) * 2 * room;
+        ++turn;
         if (cluster == 1) {
             if (lane == 0)
 #pragma unroll
                 for (int k = 0; k < K; ++k) s[k * room + warp] = v[k];
             asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(warps * 32) : "memory");
-        } else {
-            if (threadIdx.x == 0)
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(barrier(buffer)), "r"(all * K * 4) : "memory");
-            if (lane < cluster) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    uint32_t to, bar;
-                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(s + k * room + rank * warps + warp)), "r"(lane));
-                    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(barrier(buffer)), "r"(lane));
-                    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to), "r"(__float_as_uint(v[k])), "r"(bar) : "memory");
+            for (int k = 0; k < K; ++k) {
+                const float4 x = *reinterpret_cast<const float4 *>(s + k * room), y = *reinterpret_cast<const float4 *>(s + k * room + 4);
+                v[k] = ((x.x + x.y) + (x.z + x.w)) + ((y.x + y.y) + (y.z + y.w));
+                for (int i = 8; i < warps; i += 4) {
+                    const float4 z = *reinterpret_cast<const float4 *>(s + k * room + i);
+                    v[k] += (z.x + z.y) + (z.z + z.w);
                 }
             }
-            const uint32_t phase = (turn >> 1) & 1;
-            uint32_t ok = 0;
-            for (int i = 0; i < JOIN_WAIT && !ok; ++i)
-                asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(barrier(buffer)), "r"(phase) : "memory");
-            late = !ok;
+            return;
         }
-        ++turn;
+        const int all = warps * cluster;
+        if (threadIdx.x == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(barrier(buffer)), "r"(all * K * 4) : "memory");
+        if (lane < cluster) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                uint32_t to, bar;
+                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(s + k * room + rank * warps + warp)), "r"(lane));
+                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(barrier(buffer)), "r"(lane));
+                asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to), "r"(__float_as_uint(v[k])), "r"(bar) : "memory");
+            }
+        }
+        const uint32_t phase = ((turn - 1) >> 1) & 1;
+        uint32_t ok = 0;
+        for (int i = 0; i < JOIN_WAIT && !ok; ++i)
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(barrier(buffer)), "r"(phase) : "memory");
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            float4 x = *reinterpret_cast<const float4 *>(s + k * room);
-            v[k] = (x.x + x.y) + (x.z + x.w);
-            for (int i = 4; i < all; i += 4) {
-                x = *reinterpret_cast<const float4 *>(s + k * room + i);
+            v[k] = 0.f;
+            for (int i = 0; i < all; i += 4) {
+                const float4 x = *reinterpret_cast<const float4 *>(s + k * room + i);
                 v[k] += (x.x + x.y) + (x.z + x.w);
             }
-            if (late) v[k] = __uint_as_float(0x7FC00000u);
+            if (!ok) v[k] = __uint_as_float(0x7FC00000u);                    // a wait that ran out: the row becomes NaN
         }
     }
 };
@@ -310,10 +318,22 @@ __device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4
     return make_float2(mean, rsqrtf(s[0] * inv_n + eps));
 }
 
+// the row's sums of u * xhat and, behind a layer norm, of u
+__device__ __forceinline__ float2 slope_sums(JoinTeam &tm, int norm, f32x2 along, f32x2 mean) {
+    if (norm == DBSPMSPV_NORM_LAYER) {
+        float s[2] = {sum2(along), sum2(mean)};
+        tm.add(s);
+        return make_float2(s[0], s[1]);
+    }
+    float s[1] = {sum2(along)};
+    tm.add(s);
+    return make_float2(s[0], 0.f);
+}
+
 // A warp's shared memory: the rows [ahead][eight][array], the columns' factors [eight][piece][lane], room for rows that are written in words.  Behind the warps': the teams' sums, barriers.
 __host__ __device__ inline int join_warp_bytes(int eights, int room, int params, bool whole) { return JOIN_AHEAD * room + eights * params * 512 + (whole ? 0 : 1024); }
 inline size_t join_smem(const JoinPlan &p, int room, int params, bool whole) {
-    return (size_t)join_warp_bytes(p.eights, room, params, whole) * p.warps * p.teams + (size_t)4 * p.teams * ((p.warps * p.cluster + 3) & ~3) * 4 + 16;
+    return (size_t)join_warp_bytes(p.eights, room, params, whole) * p.warps * p.teams + (size_t)4 * p.teams * join_sums_room(p.warps, p.cluster) * 4 + 16;
 }
 
 // What both kernels begin with: the warp's columns and its shared memory
@@ -344,7 +364,7 @@ struct JoinWarp {
 };
 
 // factors: gate * w_block * scales (or without a gate that has rows), w_next, then (BIAS) c_block * gate * scales, c_next
-template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE>
+template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE, bool GATES>
 __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __grid_constant__ JoinArgs a) {
     extern __shared__ __align__(16) uint8_t s_dyn[];
     constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, PARAMS = BIAS ? 8 : 4;
@@ -358,20 +378,18 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
     const uint32_t tokens = a.tokens, walk = (uint32_t)tm.step(), first = (uint32_t)tm.first();
     const uint8_t *my_r = me.template mine<SF32>(a.r), *my_b = me.template mine<BF32>(a.b);
     uint8_t *my_out = me.template mine<SF32>(a.out), *my_h = me.template mine<false>(a.h);
-    const uint32_t r_step = (uint32_t)a.r.ld * SZ, b_step = (uint32_t)a.b.ld * BZ, out_step = (uint32_t)a.out.ld * SZ, h_step = (uint32_t)a.h.ld * 2;
     auto ahead = [&](uint32_t t, uint8_t *to) {
         if (t < tokens)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 if (WHOLE) {
-                    if (me.w[e].cnt == 0) continue;
-                    row_ahead<SF32>(my_r + e * 256 * SZ, r_step, t, me.w[e], to + AT_R + e * eight_room<SF32, WHOLE>());
-                    row_ahead<BF32>(my_b + e * 256 * BZ, b_step, t, me.w[e], to + AT_B + e * eight_room<BF32, WHOLE>());
+                    row_ahead<SF32>(my_r + e * 256 * SZ, a.r.step, t, me.w[e], to + AT_R + e * eight_room<SF32, WHOLE>());
+                    row_ahead<BF32>(my_b + e * 256 * BZ, a.b.step, t, me.w[e], to + AT_B + e * eight_room<BF32, WHOLE>());
                 } else {
                     if (a.r.p) row_ahead<SF32>(a.r, t, me.w[e], n, to + AT_R + e * eight_room<SF32, WHOLE>());
                     if (a.b.p) row_ahead<BF32>(a.b, t, me.w[e], n, to + AT_B + e * eight_room<BF32, WHOLE>());
                 }
-                if (a.gate.p) {
+                if (GATES) {
                     if (a.params_f32) row_ahead<true>(a.gate, t, me.w[e], n, to + AT_G + e * eight_room<true, false>());
                     else row_ahead<false>(a.gate, t, me.w[e], n, to + AT_G + e * eight_room<false, false>());
                 }
@@ -416,13 +434,16 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[e][j] = fma2(v[e][j], w[j], c[j]);
                 }
-                if (a.gate.p) {
+                if (GATES) {
                     if (a.params_f32) row_here<true, false>(a.gate, t, me.w[e], at + AT_G + e * eight_room<true, false>(), w);
                     else row_here<false, false>(a.gate, t, me.w[e], at + AT_G + e * eight_room<false, false>(), w);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[e][j] = mul2(v[e][j], w[j]);
                 }
-                if (a.drop.random) drop_eight(a.drop, num, cols[e], t, v[e]);
+            }
+            if (a.drop.random) drop_eights<E, true>(a.drop, num, cols, t, v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
                 row_here<SF32, WHOLE>(a.r, t, me.w[e], at + AT_R + e * eight_room<SF32, WHOLE>(), x[e]);
                 if (!BIAS) factors_here(me.factor(e, PARAMS, 0), w);
 #pragma unroll
@@ -439,7 +460,7 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             if (WHOLE) {
-                if (me.w[e].cnt) row_out<SF32>(my_out + e * 256 * SZ, out_step, t, x[e]);
+                if (me.w[e].cnt) row_out<SF32>(my_out + e * 256 * SZ, a.out.step, t, x[e]);
             } else if (a.out.p) row_out<SF32>(a.out, t, me.w[e], n, x[e], me.spare);
         }
         if (!WHOLE && !a.h.p && !a.stats) continue;
@@ -458,7 +479,7 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
                 x[e][j] = BIAS ? fma2(y, w[j], c[j]) : mul2(y, w[j]);
             }
             if (WHOLE) {
-                if (me.w[e].cnt) row_out<false>(my_h + e * 512, h_step, t, x[e]);
+                if (me.w[e].cnt) row_out<false>(my_h + e * 512, a.h.step, t, x[e]);
             } else row_out<false>(a.h, t, me.w[e], n, x[e], me.spare);
         }
     }
@@ -466,7 +487,7 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
 }
 
 // factors: w_next, gate * w_block * scales (or without a gate that has rows), c_block * scales for the gradient of such a gate.  Sums over a team's tokens: dw_next, A, then (BIAS) dc_next, B.
-template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE>
+template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE, bool GATES>
 __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward(const __grid_constant__ JoinArgs a) {
     extern __shared__ __align__(16) uint8_t s_dyn[];
     constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, SUMS = BIAS ? 4 : 2;
@@ -481,25 +502,22 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
     const bool block = WHOLE || a.parts || a.db.p || a.dgate.p;
     const uint8_t *my_dh = me.template mine<false>(a.dh), *my_dout = me.template mine<SF32>(a.dout), *my_out = me.template mine<SF32>(a.out), *my_b = me.template mine<BF32>(a.b);
     uint8_t *my_dr = me.template mine<SF32>(a.dr), *my_db = a.db.f32 ? me.template mine<true>(a.db) : me.template mine<false>(a.db);
-    const uint32_t dh_step = (uint32_t)a.dh.ld * 2, dout_step = (uint32_t)a.dout.ld * SZ, out_step = (uint32_t)a.out.ld * SZ, b_step = (uint32_t)a.b.ld * BZ, dr_step = (uint32_t)a.dr.ld * SZ,
-                   db_step = (uint32_t)a.db.ld * (a.db.f32 ? 4 : 2);
     auto ahead = [&](uint32_t t, uint8_t *to) {
         if (t < tokens)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 if (WHOLE) {
-                    if (me.w[e].cnt == 0) continue;
-                    row_ahead<false>(my_dh + e * 512, dh_step, t, me.w[e], to + e * H8);
-                    row_ahead<SF32>(my_dout + e * 256 * SZ, dout_step, t, me.w[e], to + AT_DOUT + e * S8);
-                    row_ahead<SF32>(my_out + e * 256 * SZ, out_step, t, me.w[e], to + AT_OUT + e * S8);
-                    row_ahead<BF32>(my_b + e * 256 * BZ, b_step, t, me.w[e], to + AT_B + e * B8);
+                    row_ahead<false>(my_dh + e * 512, a.dh.step, t, me.w[e], to + e * H8);
+                    row_ahead<SF32>(my_dout + e * 256 * SZ, a.dout.step, t, me.w[e], to + AT_DOUT + e * S8);
+                    row_ahead<SF32>(my_out + e * 256 * SZ, a.out.step, t, me.w[e], to + AT_OUT + e * S8);
+                    if (a.b.p) row_ahead<BF32>(my_b + e * 256 * BZ, a.b.step, t, me.w[e], to + AT_B + e * B8);
                 } else {
                     if (a.dh.p) row_ahead<false>(a.dh, t, me.w[e], n, to + e * H8);
                     if (a.dout.p) row_ahead<SF32>(a.dout, t, me.w[e], n, to + AT_DOUT + e * S8);
                     if (a.out.p) row_ahead<SF32>(a.out, t, me.w[e], n, to + AT_OUT + e * S8);
                     if (a.b.p) row_ahead<BF32>(a.b, t, me.w[e], n, to + AT_B + e * B8);
                 }
-                if (a.gate.p) {
+                if (GATES) {
                     if (a.params_f32) row_ahead<true>(a.gate, t, me.w[e], n, to + AT_G + e * eight_room<true, false>());
                     else row_ahead<false>(a.gate, t, me.w[e], n, to + AT_G + e * eight_room<false, false>());
                 }
@@ -518,7 +536,7 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
         cols[e] = columns_of(num, (uint32_t)col >> 3);
         columns_here(me.factor(e, a.params, 0), col, n, a.params_f32, 1.f, a.w_next, nullptr);
         columns_here(me.factor(e, a.params, 2), col, n, a.params_f32, scale, a.w_block, a.gate_vec);
-        if (a.dgate.p) columns_here(me.factor(e, a.params, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, a.c_block, nullptr);
+        if (GATES && a.dgate.p) columns_here(me.factor(e, a.params, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, a.c_block, nullptr);
 #pragma unroll
         for (int k = 0; k < SUMS; ++k)
 #pragma unroll
@@ -543,21 +561,22 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
             factors_here(me.factor(e, a.params, 0), w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                g[e][j] = fma2(g[e][j], inv_out, shift_out);
-                sum[0][e][j] = fma2(u[e][j], g[e][j], sum[0][e][j]);
-                if (BIAS) sum[2][e][j] = add2(u[e][j], sum[2][e][j]);
-                u[e][j] = mul2(u[e][j], w[j]);
-                p0 = fma2(u[e][j], g[e][j], p0);
-                p1 = add2(u[e][j], p1);
+                g[e][j] = fma1(g[e][j], inv_out, shift_out);
+                sum[0][e][j] = fma1(u[e][j], g[e][j], sum[0][e][j]);
+                if (BIAS) sum[2][e][j] = add1(u[e][j], sum[2][e][j]);
+                u[e][j] = mul1(u[e][j], w[j]);
+                p0 = fma1(u[e][j], g[e][j], p0);
             }
+            if (a.norm_next == DBSPMSPV_NORM_LAYER)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p1 = add1(u[e][j], p1);
         }
         f32x2 slope = both(1.f), along = 0, mean = 0;
         if (a.norm_next != DBSPMSPV_NORM_NONE && (WHOLE || a.dh.p)) {
-            float s[2] = {sum2(p0), sum2(p1)};
-            tm.add(s);
+            const float2 s = slope_sums(tm, a.norm_next, p0, p1);
             slope = inv_out;
-            along = both(-st.w * (s[0] * a.inv_n));
-            if (a.norm_next == DBSPMSPV_NORM_LAYER) mean = both(-st.w * (s[1] * a.inv_n));
+            along = both(-st.w * (s.x * a.inv_n));
+            mean = both(-st.w * (s.y * a.inv_n));
         }
         // g: G, then drop(G), then that times gate, w and scales;  u: the normalised b
         const f32x2 inv_b = both(st.y), shift_b = both(-st.x * st.y);
@@ -566,39 +585,44 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
         for (int e = 0; e < E; ++e) {
             row_here<SF32, WHOLE>(a.dout, t, me.w[e], at + AT_DOUT + e * S8, w);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) g[e][j] = add2(w[j], fma2(u[e][j], slope, fma2(g[e][j], along, mean)));
+            for (int j = 0; j < 4; ++j) g[e][j] = add1(w[j], fma1(u[e][j], slope, fma1(g[e][j], along, mean)));
             if (WHOLE) {
-                if (me.w[e].cnt) row_out<SF32>(my_dr + e * 256 * SZ, dr_step, t, g[e]);
+                if (me.w[e].cnt) row_out<SF32>(my_dr + e * 256 * SZ, a.dr.step, t, g[e]);
             } else if (a.dr.p) row_out<SF32>(a.dr, t, me.w[e], n, g[e], me.spare);
+        }
+        if (block && a.drop.random) drop_eights<E, true>(a.drop, num, cols, t, g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
             if (!block) continue;
-            if (a.drop.random) drop_eight(a.drop, num, cols[e], t, g[e]);
             row_here<BF32, WHOLE>(a.b, t, me.w[e], at + AT_B + e * B8, u[e]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) u[e][j] = fma2(u[e][j], inv_b, shift_b);
-            if (a.gate.p) {
-                if (a.dgate.p) {
+            for (int j = 0; j < 4; ++j) u[e][j] = fma1(u[e][j], inv_b, shift_b);
+            if (GATES) {
+                if (GATES && a.dgate.p) {
                     f32x2 d[4];
                     factors_here(me.factor(e, a.params, 2), w);
                     factors_here(me.factor(e, a.params, 4), d);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) d[j] = mul2(g[e][j], fma2(u[e][j], w[j], d[j]));
+                    for (int j = 0; j < 4; ++j) d[j] = mul1(g[e][j], fma1(u[e][j], w[j], d[j]));
                     if (a.params_f32) row_out<true>(a.dgate, t, me.w[e], n, d, me.spare);
                     else row_out<false>(a.dgate, t, me.w[e], n, d, me.spare);
                 }
                 if (a.params_f32) row_here<true, false>(a.gate, t, me.w[e], at + AT_G + e * eight_room<true, false>(), w);
                 else row_here<false, false>(a.gate, t, me.w[e], at + AT_G + e * eight_room<false, false>(), w);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) g[e][j] = mul2(g[e][j], w[j]);
+                for (int j = 0; j < 4; ++j) g[e][j] = mul1(g[e][j], w[j]);
             }
             factors_here(me.factor(e, a.params, 2), w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                sum[1][e][j] = fma2(g[e][j], u[e][j], sum[1][e][j]);
-                if (BIAS) sum[3][e][j] = add2(g[e][j], sum[3][e][j]);
-                g[e][j] = mul2(g[e][j], w[j]);
-                p0 = fma2(g[e][j], u[e][j], p0);
-                p1 = add2(g[e][j], p1);
+                sum[1][e][j] = fma1(g[e][j], u[e][j], sum[1][e][j]);
+                if (BIAS) sum[3][e][j] = add1(g[e][j], sum[3][e][j]);
+                g[e][j] = mul1(g[e][j], w[j]);
+                p0 = fma1(g[e][j], u[e][j], p0);
             }
+            if (a.norm_block == DBSPMSPV_NORM_LAYER)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p1 = add1(g[e][j], p1);
         }
         if (!WHOLE) __syncwarp();
         ahead(t + JOIN_AHEAD * walk, at);
@@ -607,20 +631,19 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
         slope = both(1.f);
         along = mean = 0;
         if (a.norm_block != DBSPMSPV_NORM_NONE) {
-            float s[2] = {sum2(p0), sum2(p1)};
-            tm.add(s);
+            const float2 s = slope_sums(tm, a.norm_block, p0, p1);
             slope = inv_b;
-            along = both(-st.y * (s[0] * a.inv_n));
-            if (a.norm_block == DBSPMSPV_NORM_LAYER) mean = both(-st.y * (s[1] * a.inv_n));
+            along = both(-st.y * (s.x * a.inv_n));
+            mean = both(-st.y * (s.y * a.inv_n));
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) g[e][j] = fma2(g[e][j], slope, fma2(u[e][j], along, mean));
+            for (int j = 0; j < 4; ++j) g[e][j] = fma1(g[e][j], slope, fma1(u[e][j], along, mean));
             if (WHOLE) {
                 if (me.w[e].cnt == 0) continue;
-                if (a.db.f32) row_out<true>(my_db + e * 1024, db_step, t, g[e]);
-                else row_out<false>(my_db + e * 512, db_step, t, g[e]);
+                if (a.db.f32) row_out<true>(my_db + e * 1024, a.db.step, t, g[e]);
+                else row_out<false>(my_db + e * 512, a.db.step, t, g[e]);
             } else if (a.db.f32) row_out<true>(a.db, t, me.w[e], n, g[e], me.spare);
             else row_out<false>(a.db, t, me.w[e], n, g[e], me.spare);
         }
@@ -655,7 +678,7 @@ __global__ void __launch_bounds__(JOIN_SUMS_CTA) k_join_sums(const __grid_consta
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (at < a.ldp)                           // (rows of the parts are whole eights)
-#pragma unroll 4
+#pragma unroll 5
         for (int i = y; i < a.teams; i += Y)
 #pragma unroll
             for (int k = 0; k < SUMS; ++k) {

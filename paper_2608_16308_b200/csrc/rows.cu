@@ -29,20 +29,20 @@ __global__ void __launch_bounds__(DR_CTA) k_dropout(const __grid_constant__ Drop
     for (int r = 0; r < DR_ROWS; ++r)
         if (t0 + r * tall < a.tokens) load_raw<F32>(row_at<F32>(a.x, t0 + r * tall), col, a.n, whole && a.x.aligned, p[r], q[r]);
     const Numbers num = numbers_of(a.drop);
-    const Columns cols = columns_of(num, (uint32_t)eight);
+    const Columns cols[1] = {columns_of(num, (uint32_t)eight)};
 #pragma unroll
     for (int r = 0; r < DR_ROWS; ++r) {
         const int64_t t = t0 + r * tall;
         if (t >= a.tokens) break;
         void *to = const_cast<void *>(row_at<F32>(a.y, t));
         if (a.drop.random) {
-            f32x2 v[4];
-            if (F32) pairs_of_eight(p[r], q[r], v);
-            else pairs_of_eight(p[r], v);
-            drop_eight(a.drop, num, cols, (uint32_t)t, v);
+            f32x2 v[1][4];
+            if (F32) pairs_of_eight(p[r], q[r], v[0]);
+            else pairs_of_eight(p[r], v[0]);
+            drop_eights<1, false>(a.drop, num, cols, (uint32_t)t, v);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], both(a.drop.scale));
-            store_eight<F32>(to, col, a.n, whole && a.y.aligned, v);
+            for (int j = 0; j < 4; ++j) v[0][j] = mul2(v[0][j], both(a.drop.scale));
+            store_eight<F32>(to, col, a.n, whole && a.y.aligned, v[0]);
         } else store_raw<F32>(to, col, a.n, whole && a.y.aligned, p[r], q[r]);
     }
 }

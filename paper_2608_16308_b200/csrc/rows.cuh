@@ -13,9 +13,10 @@ struct Rows {
     void *p;
     int64_t ld;
     int32_t f32, aligned;
+    uint32_t step;            // ... in bytes (its low 32 bits)
 };
 inline Rows rows_of(const void *p, int64_t ld, bool f32) {
-    return Rows{const_cast<void *>(p), ld, f32, (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * (f32 ? 4 : 2)) % 16 == 0};
+    return Rows{const_cast<void *>(p), ld, f32, (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (ld * (f32 ? 4 : 2)) % 16 == 0, (uint32_t)(ld * (f32 ? 4 : 2))};
 }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -60,6 +61,19 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
     f32x2 d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
+}
+// The same one after the other.  Where registers are short the pairs cost more moves than they save (gradient of a join, 4096 x 4096: 61.1 us in pairs, 58.1 one by one; forwards 33.0 and 33.6).
+__device__ __forceinline__ f32x2 fma1(f32x2 a, f32x2 b, f32x2 c) {
+    const float2 x = apart(a), y = apart(b), z = apart(c);
+    return pair(fmaf(x.x, y.x, z.x), fmaf(x.y, y.y, z.y));
+}
+__device__ __forceinline__ f32x2 mul1(f32x2 a, f32x2 b) {
+    const float2 x = apart(a), y = apart(b);
+    return pair(x.x * y.x, x.y * y.y);
+}
+__device__ __forceinline__ f32x2 add1(f32x2 a, f32x2 b) {
+    const float2 x = apart(a), y = apart(b);
+    return pair(x.x + y.x, x.y + y.y);
 }
 __device__ __forceinline__ float sum2(f32x2 p) {
     const float2 v = apart(p);
@@ -147,6 +161,10 @@ __device__ __forceinline__ const void *row_at(const Rows &r, int64_t t) {
 __device__ __forceinline__ void copy_ahead(void *smem, const void *p) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
 }
+// ... of which `bytes` are read and the rest is zeros
+__device__ __forceinline__ void copy_ahead(void *smem, const void *p, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void copy_word_ahead(void *smem, const void *p) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
 }
@@ -179,29 +197,50 @@ __device__ __forceinline__ Columns columns_of(const Numbers &s, uint32_t eight) 
     const uint64_t p3 = (uint64_t)((uint32_t)(q2 >> 32) ^ s.second ^ (s.k0 + PHILOX_W0)) * PHILOX_M0;
     return Columns{(uint32_t)p1 ^ (s.k1 + PHILOX_W1), (uint32_t)q2 ^ (s.k0 + 2 * PHILOX_W0), (uint32_t)(p3 >> 32) ^ (s.k1 + 2 * PHILOX_W1), (uint32_t)p3};
 }
-__device__ __forceinline__ uint4 philox(const Numbers &s, const Columns &w, uint32_t token) {
-    const uint64_t p2 = (uint64_t)(s.first ^ token) * PHILOX_M0, q3 = (uint64_t)((uint32_t)(p2 >> 32) ^ w.a) * PHILOX_M1;
-    uint32_t c0 = (uint32_t)(q3 >> 32) ^ w.b, c1 = (uint32_t)q3, c2 = w.c ^ (uint32_t)p2, c3 = w.d, k0 = s.k0 + 3 * PHILOX_W0, k1 = s.k1 + 3 * PHILOX_W1;
+// the numbers of E eights of a token
+template <int E, bool KEYS_ANEW>
+__device__ __forceinline__ void philox(const Numbers &s, const Columns (&w)[E], uint32_t token, uint4 (&out)[E]) {
+    const uint64_t p2 = (uint64_t)(s.first ^ token) * PHILOX_M0;
+    uint32_t c0[E], c1[E], c2[E], c3[E], k0 = s.k0 + 3 * PHILOX_W0, k1 = s.k1 + 3 * PHILOX_W1;
+    // (the keys of the rounds are added up again for every token: kept, they would take fourteen registers that the joins' kernels do not have; gradient of 4096 x 4096 68 -> 62 us)
+    if (KEYS_ANEW) asm volatile("" : "+r"(k0), "+r"(k1));
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const uint64_t q3 = (uint64_t)((uint32_t)(p2 >> 32) ^ w[e].a) * PHILOX_M1;
+        c0[e] = (uint32_t)(q3 >> 32) ^ w[e].b;
+        c1[e] = (uint32_t)q3;
+        c2[e] = w[e].c ^ (uint32_t)p2;
+        c3[e] = w[e].d;
+    }
 #pragma unroll
     for (int r = 3; r < 10; ++r) {
-        const uint64_t p = (uint64_t)c0 * PHILOX_M0, q = (uint64_t)c2 * PHILOX_M1;
-        c0 = (uint32_t)(q >> 32) ^ c1 ^ k0;
-        c1 = (uint32_t)q;
-        c2 = (uint32_t)(p >> 32) ^ c3 ^ k1;
-        c3 = (uint32_t)p;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint64_t p = (uint64_t)c0[e] * PHILOX_M0, q = (uint64_t)c2[e] * PHILOX_M1;
+            c0[e] = (uint32_t)(q >> 32) ^ c1[e] ^ k0;
+            c1[e] = (uint32_t)q;
+            c2[e] = (uint32_t)(p >> 32) ^ c3[e] ^ k1;
+            c3[e] = (uint32_t)p;
+        }
         k0 += PHILOX_W0;
         k1 += PHILOX_W1;
     }
-    return make_uint4(c0, c1, c2, c3);
+#pragma unroll
+    for (int e = 0; e < E; ++e) out[e] = make_uint4(c0[e], c1[e], c2[e], c3[e]);
 }
 // v with zeros where entries of the token are dropped (what makes up for them is the caller's to multiply): 16 bits are below P exactly if the word that begins with them is below P << 16
-__device__ __forceinline__ void drop_eight(const Drop &d, const Numbers &s, const Columns &w, uint32_t token, f32x2 v[4]) {
-    const uint4 q = philox(s, w, token);
-    const uint32_t bits[4] = {q.x, q.y, q.z, q.w};
+template <int E, bool KEYS_ANEW>
+__device__ __forceinline__ void drop_eights(const Drop &d, const Numbers &s, const Columns (&w)[E], uint32_t token, f32x2 (&v)[E][4]) {
+    uint4 q[E];
+    philox<E, KEYS_ANEW>(s, w, token, q);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float2 x = apart(v[j]);
-        v[j] = pair(bits[j] << 16 > d.above ? x.x : 0.f, bits[j] > d.above ? x.y : 0.f);
+    for (int e = 0; e < E; ++e) {
+        const uint32_t bits[4] = {q[e].x, q[e].y, q[e].z, q[e].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 x = apart(v[e][j]);
+            v[e][j] = pair(bits[j] << 16 > d.above ? x.x : 0.f, bits[j] > d.above ? x.y : 0.f);
+        }
     }
 }
 
