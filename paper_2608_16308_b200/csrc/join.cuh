@@ -169,19 +169,33 @@ __device__ __forceinline__ void row_out(uint8_t *mine, uint32_t stride, uint32_t
 __device__ __forceinline__ float vector_one(const void *p, bool f32, int i) {
     return f32 ? static_cast<const float *>(p)[i] : __uint_as_float((uint32_t) static_cast<const uint16_t *>(p)[i] << 16);
 }
-// factors of eight columns in fp32, the product of what is given (null: 1); zeros behind the row's end
-__device__ __forceinline__ void columns_here(uint4 *to, int col, int n, bool f32, float scale, const void *v, const void *w) {
-    float x[8];
+// Eight entries of a vector of parameters as they lie.  (Those of all vectors are loaded before the first is used: a short call waits for them once.)
+struct Eight {
+    uint4 a, b;
+};
+__device__ __forceinline__ Eight vector_eight(const void *p, bool f32, int col, int n) {
+    Eight q = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+    const bool whole = col + 8 <= n && (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
+    if (p && f32) load_raw<true>(p, col, n, whole, q.a, q.b);
+    else if (p) load_raw<false>(p, col, n, whole, q.a, q.b);
+    return q;
+}
+__device__ __forceinline__ void vector_values(const Eight &q, const void *p, bool f32, float v[8]) {
+    if (f32) eight_of(q.a, q.b, v);
+    else eight_of(q.a, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        x[j] = col + j < n ? scale : 0.f;
-        if (col + j < n && v) x[j] *= vector_one(v, f32, col + j);
-        if (col + j < n && w) x[j] *= vector_one(w, f32, col + j);
-    }
+    for (int j = 0; j < 8; ++j) v[j] = p ? v[j] : 1.f;
+}
+// factors of eight columns in fp32: scale and two vectors (null: ones) multiplied; zeros behind the row's end
+__device__ __forceinline__ void columns_here(uint4 *to, int col, int n, bool f32, float scale, const Eight &v, const void *has_v, const Eight &w, const void *has_w) {
+    float x[8], y[8];
+    vector_values(v, has_v, f32, x);
+    vector_values(w, has_w, f32, y);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = col + j < n ? scale * x[j] * y[j] : 0.f;
     to[0] = fp32_four(x);
     to[32] = fp32_four(x + 4);
 }
-
 __device__ __forceinline__ void factors_here(const uint4 *at, f32x2 v[4]) {
     const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(at), b = *reinterpret_cast<const ulonglong2 *>(at + 32);
     v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
@@ -401,15 +415,30 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
     const Numbers num = numbers_of(a.drop);
     const float scale = a.drop.random ? a.scale * a.drop.scale : a.scale;
     Columns cols[E];
+    // (both eights' vectors side by side, but for biases, which would not fit the registers)
+    constexpr int SIDE = BIAS ? 1 : E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int col = me.w[e].mine();
-        cols[e] = columns_of(num, (uint32_t)col >> 3);
-        columns_here(me.factor(e, PARAMS, 0), col, n, a.params_f32, scale, a.w_block, a.gate_vec);
-        columns_here(me.factor(e, PARAMS, 2), col, n, a.params_f32, 1.f, a.w_next, nullptr);
-        if (BIAS) {
-            columns_here(me.factor(e, PARAMS, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, a.c_block, a.gate_vec);
-            columns_here(me.factor(e, PARAMS, 6), col, n, a.params_f32, a.c_next ? 1.f : 0.f, a.c_next, nullptr);
+    for (int e0 = 0; e0 < E; e0 += SIDE) {
+        Eight wb[SIDE], wn[SIDE], gv[SIDE], cb[SIDE], cn[SIDE];
+#pragma unroll
+        for (int i = 0; i < SIDE; ++i) {
+            const int col = me.w[e0 + i].mine();
+            wb[i] = vector_eight(a.w_block, a.params_f32, col, n);
+            wn[i] = vector_eight(a.w_next, a.params_f32, col, n);
+            gv[i] = vector_eight(a.gate_vec, a.params_f32, col, n);
+            if (BIAS) cb[i] = vector_eight(a.c_block, a.params_f32, col, n);
+            if (BIAS) cn[i] = vector_eight(a.c_next, a.params_f32, col, n);
+        }
+#pragma unroll
+        for (int i = 0; i < SIDE; ++i) {
+            const int e = e0 + i, col = me.w[e].mine();
+            cols[e] = columns_of(num, (uint32_t)col >> 3);
+            columns_here(me.factor(e, PARAMS, 0), col, n, a.params_f32, scale, wb[i], a.w_block, gv[i], a.gate_vec);
+            columns_here(me.factor(e, PARAMS, 2), col, n, a.params_f32, 1.f, wn[i], a.w_next, wn[i], nullptr);
+            if (BIAS) {
+                columns_here(me.factor(e, PARAMS, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, cb[i], a.c_block, gv[i], a.gate_vec);
+                columns_here(me.factor(e, PARAMS, 6), col, n, a.params_f32, a.c_next ? 1.f : 0.f, cn[i], a.c_next, cn[i], nullptr);
+            }
         }
     }
     uint8_t *at = me.rows;
@@ -530,13 +559,22 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
     const float scale = a.drop.random ? a.scale * a.drop.scale : a.scale;
     Columns cols[E];
     f32x2 sum[SUMS][E][4];
+    Eight wb[E], wn[E], gv[E], cb[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int col = me.w[e].mine();
+        wb[e] = vector_eight(a.w_block, a.params_f32, col, n);
+        wn[e] = vector_eight(a.w_next, a.params_f32, col, n);
+        gv[e] = vector_eight(a.gate_vec, a.params_f32, col, n);
+        if (GATES) cb[e] = vector_eight(a.c_block, a.params_f32, col, n);
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int col = me.w[e].mine();
         cols[e] = columns_of(num, (uint32_t)col >> 3);
-        columns_here(me.factor(e, a.params, 0), col, n, a.params_f32, 1.f, a.w_next, nullptr);
-        columns_here(me.factor(e, a.params, 2), col, n, a.params_f32, scale, a.w_block, a.gate_vec);
-        if (GATES && a.dgate.p) columns_here(me.factor(e, a.params, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, a.c_block, nullptr);
+        columns_here(me.factor(e, a.params, 0), col, n, a.params_f32, 1.f, wn[e], a.w_next, wn[e], nullptr);
+        columns_here(me.factor(e, a.params, 2), col, n, a.params_f32, scale, wb[e], a.w_block, gv[e], a.gate_vec);
+        if (GATES && a.dgate.p) columns_here(me.factor(e, a.params, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, cb[e], a.c_block, cb[e], nullptr);
 #pragma unroll
         for (int k = 0; k < SUMS; ++k)
 #pragma unroll

@@ -16,7 +16,8 @@ inline int join_threads(int eights, bool backward) { return backward ? 512 : eig
 inline int eight_bytes(bool f32, bool whole) { return f32 ? (whole ? eight_room<true, true>() : eight_room<true, false>()) : (whole ? eight_room<false, true>() : eight_room<false, false>()); }
 inline JoinPlan join_plan(int sms, int64_t tokens, int64_t n, int eights, int room, int params, bool whole, bool backward) {
     JoinPlan p;
-    const int warps = (int)ceil64(n, (int64_t)256 * eights), most = JOIN_COLS / 256 / eights;
+    // eight warps of a row in a thread block: two blocks to an SM, of which one works while the other waits for its sums (one eight a lane: up to the columns that eight blocks take)
+    const int warps = (int)ceil64(n, (int64_t)256 * eights), most = warps <= 8 * JOIN_CLUSTER ? 8 : JOIN_COLS / 256 / eights;
     p.eights = eights;
     p.cluster = (int)ceil64(warps, most);
     p.warps = (int)ceil64(warps, p.cluster);

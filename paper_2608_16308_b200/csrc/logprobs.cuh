@@ -28,6 +28,7 @@ constexpr int LP_PER_SM = 7;                 // thread blocks
 constexpr int LP_SMEM = LP_AHEAD * LP_FLIGHT * LP_CTA * 16;
 constexpr int LP_GROUP = 2;                  // threads of a group: 64 groups
 constexpr int LP_GROUPS = LP_CTA / LP_GROUP;
+constexpr int LP_CLUSTER_GROUPS = 128;       // of a cluster's row
 constexpr int LP_SLACK = 4;                  // groups more than k that may reach tau
 constexpr float LP_NONE = -1000.f;           // 2^LP_NONE is 0, and its product with 0 too
 constexpr float LP_LOW = -1e30f;             // what -inf is taken for in sums: its probability is 0 as well, and 0 times it is 0
@@ -171,10 +172,17 @@ struct LpShared {
     uint32_t group[2][LP_GROUPS];
     uint64_t largest[LP_WARPS];
     uint64_t found[LP_CANDIDATES];
-    uint64_t best[LP_CLUSTER * LP_MAX_TOP];  // of every block of the cluster, in the first one
-    float cm[LP_CLUSTER], cs[LP_CLUSTER], cu[LP_CLUSTER];
+    uint64_t best[LP_MAX_TOP];
     uint16_t units[LP_CTA];
     int n_units, n_found;
+};
+
+// What the blocks of a cluster tell each other: their sums, their groups' largest, how many candidates they have; and, in the first block, these
+struct LpCluster {
+    float m[LP_CLUSTER], s[LP_CLUSTER], u[LP_CLUSTER];
+    uint32_t groups[LP_CLUSTER_GROUPS];
+    int found[LP_CLUSTER];
+    uint64_t best[LP_CLUSTER * LP_MAX_TOP], flat[LP_CLUSTER * LP_MAX_TOP];
 };
 
 // logits of at least tau among the units of at least tau -> sh.found (their number in sh.n_found, which may be more than there is room for).  The counts are 0 before it.
@@ -207,12 +215,22 @@ __device__ __forceinline__ void lp_collect(const LpRow<F32> &row, LpShared &sh, 
     __syncthreads();
 }
 
-// a number that at least k of the 64 group maxima reach (two to a lane), and not many more: halves what lies between the least and the largest
-__device__ __forceinline__ uint32_t lp_least(uint32_t a, uint32_t b, int k) {
-    uint32_t lo = __reduce_min_sync(FULL, min(a, b)), hi = __reduce_max_sync(FULL, max(a, b));
+// a number that at least k of the groups' largest reach (N to a lane), and not many more: halves what lies between the least and the largest
+template <int N>
+__device__ __forceinline__ uint32_t lp_least(const uint32_t (&g)[N], int k) {
+    uint32_t lo = g[0], hi = g[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) {
+        lo = min(lo, g[i]);
+        hi = max(hi, g[i]);
+    }
+    lo = __reduce_min_sync(FULL, lo);
+    hi = __reduce_max_sync(FULL, hi);
     while (lo < hi) {
         const uint32_t mid = hi - (hi - lo) / 2;
-        const int n = __popc(__ballot_sync(FULL, a >= mid)) + __popc(__ballot_sync(FULL, b >= mid));
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __popc(__ballot_sync(FULL, g[i] >= mid));
         if (n >= k) lo = mid;
         else hi = mid - 1;
         if (n >= k && n <= k + LP_SLACK) break;
@@ -291,6 +309,7 @@ __device__ __forceinline__ void lp_top(const LpRow<F32> &row, LpShared &sh, uint
     }
 }
 
+static_assert(LP_MAX_TOP <= LP_CTA && LP_MAX_TOP <= LP_CLUSTER_GROUPS && LP_CLUSTER_GROUPS / 2 <= LP_CTA, "a thread for every candidate of a block");
 template <bool F32, bool ENTROPY>
 __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_constant__ LpArgs a) {
     extern __shared__ __align__(16) uint4 s_slots[];
@@ -299,6 +318,7 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)(blockIdx.x % a.cluster), step = gridDim.x / a.cluster;
     uint4 *slot = s_slots + tid;              // [round][vector][thread]
+    LpCluster *all = reinterpret_cast<LpCluster *>(s_slots + LP_SMEM / 16);  // (of a cluster)
     if (tid == 0) sh.n_units = sh.n_found = 0;
     pdl_wait();
     pdl_trigger();
@@ -430,25 +450,90 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
         __syncthreads();
         st = {sh.m[parity][lane % LP_WARPS], sh.s[parity][lane % LP_WARPS], sh.u[parity][lane % LP_WARPS]};
         st.join<LP_WARPS>(slope);
-        if (a.top) {
-            // (NaN or +inf among the block's logits makes its sum NaN)
-            lp_top(row, sh, most, lp_least(sh.group[parity][lane], sh.group[parity][lane + 32], a.top), st.s == st.s, a.top, a.vocab, sh.best);
-            __syncthreads();
-            if (tid == 0) sh.n_units = sh.n_found = 0;
-        }
-        if (a.cluster > 1) {
+        // (NaN or +inf among a block's logits makes its sum NaN)
+        bool ranked = false;
+        if (a.cluster == 1) {
+            if (a.top) {
+                const uint32_t g[2] = {sh.group[parity][lane], sh.group[parity][lane + 32]};
+                lp_top(row, sh, most, lp_least<2>(g, a.top), st.s == st.s, a.top, a.vocab, sh.best);
+                __syncthreads();
+                if (tid == 0) sh.n_units = sh.n_found = 0;
+            }
+        } else {
             namespace cg = cooperative_groups;
             auto c = cg::this_cluster();
+            const bool plain = st.s == st.s;
             asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-            LpShared *first = c.map_shared_rank(&sh, 0);
-            if (tid == 0) { first->cm[rank] = st.m; first->cs[rank] = st.s; first->cu[rank] = st.u; }
-            if (rank && tid < a.top) first->best[rank * a.top + tid] = sh.best[tid];
+            if (tid < a.cluster) {
+                LpCluster *to = c.map_shared_rank(all, tid);
+                to->m[rank] = st.m; to->s[rank] = st.s; to->u[rank] = st.u;
+            }
+            if (a.top) {
+                // fewer and larger groups: as many for the row, whatever the cluster
+                const int mine_of = LP_CLUSTER_GROUPS / a.cluster, lanes = LP_CTA / mine_of;
+                uint32_t g = most;
+                for (int o = 1; o < lanes; o <<= 1) g = max(g, __shfl_xor_sync(FULL, g, o));
+                if (lane % lanes < a.cluster)
+                    for (int r = lane % lanes; r < a.cluster; r += lanes) c.map_shared_rank(all, r)->groups[rank * mine_of + tid / lanes] = g;
+            }
             asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
             const int r = lane % LP_CLUSTER;
-            st = r < a.cluster ? LpState{sh.cm[r], sh.cs[r], sh.cu[r]} : LpState{-INFINITY, 0.f, 0.f};
+            st = r < a.cluster ? LpState{all->m[r], all->s[r], all->u[r]} : LpState{-INFINITY, 0.f, 0.f};
             st.join<LP_CLUSTER>(slope);
+            LpCluster *first = c.map_shared_rank(all, 0);
+            uint32_t least = 0;
+            if (a.top && st.s == st.s) {
+                // one tau for the whole row: few candidates in any block
+                uint32_t g[LP_CLUSTER_GROUPS / 32];
+#pragma unroll
+                for (int i = 0; i < LP_CLUSTER_GROUPS / 32; ++i) g[i] = all->groups[i * 32 + lane];
+                least = lp_least(g, a.top);
+            }
+            if (least) {
+                // (few tokens: every thread looks through its own logits, which lie in shared memory if the rounds in flight held them all)
+                const float l_least = of_order(least);
+                auto meet_one = [&](float l, int place) {
+                    if (l >= l_least) {
+                        const int i = atomicAdd(&sh.n_found, 1);
+                        if (i < LP_CANDIDATES) sh.found[i] = candidate(l, place);
+                    }
+                };
+                if (tid < row.heads()) meet_one(row.one(tid), tid);
+                if (tid < row.tail) meet_one(row.one(a.vocab - row.tail + tid), a.vocab - row.tail + tid);
+                if (most >= least) {
+                    const bool here = a.rounds <= LP_AHEAD;
+#pragma unroll 4
+                    for (int i = 0; row.from + tid + i * LP_CTA < row.to; ++i) {
+                        const int v = row.from + tid + i * LP_CTA;
+                        const uint4 q = here ? slot[i * LP_CTA] : row.raw(v);
+                        if (!(largest<F32>(q) >= l_least)) continue;
+                        float l[V];
+                        LpRow<F32>::values(q, l);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) meet_one(l[j], row.place(v) + j);
+                    }
+                }
+                __syncthreads();
+                const int n = sh.n_found;
+                if (tid < n && n <= LP_MAX_TOP) first->best[rank * LP_MAX_TOP + tid] = sh.found[tid];
+                if (tid < a.cluster) c.map_shared_rank(all, tid)->found[rank] = n;
+                asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+                ranked = true;
+                for (int i = 0; i < a.cluster; ++i) ranked = ranked && all->found[i] <= LP_MAX_TOP;
+                if (!ranked && tid == 0) sh.n_units = sh.n_found = 0;
+                __syncthreads();
+            }
+            if (a.top && !ranked) {
+                // every block's own, then the blocks' among each other
+                const uint32_t g[2] = {sh.group[parity][lane], sh.group[parity][lane + 32]};
+                lp_top(row, sh, most, lp_least<2>(g, a.top), plain, a.top, a.vocab, sh.best);
+                __syncthreads();
+                if (tid < LP_MAX_TOP) first->best[rank * LP_MAX_TOP + tid] = tid < a.top ? sh.best[tid] : 0;
+                if (tid < a.cluster) c.map_shared_rank(all, tid)->found[rank] = a.top;
+                asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+            }
         }
-        if (rank == 0 && tid < max(a.top * a.cluster, 1)) {
+        if (rank == 0 && tid < max(a.cluster > 1 && a.top ? LP_CTA : a.top, 1)) {
             const bool nothing = st.m == -INFINITY && st.s == 0.f;
             const float total = nothing ? -INFINITY : logf(st.s);
             if (tid == 0) {
@@ -457,19 +542,27 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
                 if (a.logprob)
                     a.logprob[t] = target < 0 ? 0.f : target >= a.vocab ? __uint_as_float(0x7FC00000u) : nothing ? -INFINITY : (at_target - st.m) * a.inv_t - total;
             }
-            // the blocks' alternatives among each other
-            const int all = a.top * a.cluster;
-            for (int i = tid; i < all; i += LP_CTA) {
-                const uint64_t mine = sh.best[i];
-                int before = i;
-                if (a.cluster > 1) {
-                    before = 0;
-#pragma unroll 8
-                    for (int j = 0; j < all; ++j) before += sh.best[j] > mine;
+            auto give = [&](uint64_t mine, int place) {
+                if (a.top_ids) a.top_ids[t * a.top + place] = place_of(mine);
+                if (a.top_logprobs) a.top_logprobs[t * a.top + place] = nothing ? -INFINITY : (of_order((uint32_t)(mine >> 32)) - st.m) * a.inv_t - total;
+            };
+            if (a.cluster == 1) {
+                if (tid < a.top && sh.best[tid]) give(sh.best[tid], tid);
+            } else if (a.top) {
+                int n = 0;
+                for (int r = 0; r < a.cluster; ++r) {
+                    const int here = all->found[r];
+                    if (tid < here) all->flat[n + tid] = all->best[r * LP_MAX_TOP + tid];
+                    n += here;
                 }
-                if (!mine || before >= a.top) continue;
-                if (a.top_ids) a.top_ids[t * a.top + before] = place_of(mine);
-                if (a.top_logprobs) a.top_logprobs[t * a.top + before] = nothing ? -INFINITY : (of_order((uint32_t)(mine >> 32)) - st.m) * a.inv_t - total;
+                __syncthreads();
+                for (int i = tid; i < n; i += LP_CTA) {
+                    const uint64_t mine = all->flat[i];
+                    int before = 0;
+#pragma unroll 8
+                    for (int j = 0; j < n; ++j) before += all->flat[j] > mine;
+                    if (mine && before < a.top) give(mine, before);
+                }
             }
         }
     }

@@ -86,7 +86,7 @@ int dbspmspv_logprobs(const void *logits, int64_t ldl, int logits_f32, int32_t t
     a.rounds = (int32_t)ceil64(ceil64(vectors, a.cluster), LP_CTA * LP_FLIGHT);
     const int64_t room = (int64_t)sms * LP_PER_SM, clusters = a.cluster > 1 || tokens < room ? tokens : room;
     auto kernel = logits_f32 ? (entropy ? k_logprobs<true, true> : k_logprobs<true, false>) : (entropy ? k_logprobs<false, true> : k_logprobs<false, false>);
-    return launch_rows(kernel, (int)clusters * a.cluster, LP_CTA, a.cluster, LP_SMEM, static_cast<cudaStream_t>(stream), a);
+    return launch_rows(kernel, (int)clusters * a.cluster, LP_CTA, a.cluster, LP_SMEM + (a.cluster > 1 ? sizeof(LpCluster) : 0), static_cast<cudaStream_t>(stream), a);
 }
 
 int dbspmspv_logprobs_backward(const void *logits, int64_t ldl, int logits_f32, int32_t tokens, int32_t vocab, float temperature, const int32_t *targets, const float *stats, const float *entropy,
