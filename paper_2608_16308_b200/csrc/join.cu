@@ -30,7 +30,7 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
     const bool bias = (b && c_block) || c_next, rows = b && gate && ldg;
     const Rows R = rows_of(r, ldr, o->stream_f32), BR = rows_of(b, ldb, o->block_f32), OUT = rows_of(out, ldo, o->stream_f32), H = rows_of(h, ldh, false), G = rows_of(rows ? gate : nullptr, ldg, o->params_f32);
     const bool whole = all_whole(n, R, BR, OUT, H) && (!rows || G.aligned);
-    const int params = bias ? 8 : 4, eights = join_eights(n, false);
+    const int params = bias ? 8 : 4, eights = join_eights(sms, tokens, n, false);
     const int room = eights * (eight_bytes(o->stream_f32, whole) + eight_bytes(o->block_f32, whole) + (rows ? eight_bytes(o->params_f32, false) : 0));
     const JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, false);
     JoinArgs a = join_args(*o, tokens, n, p, room, params);
@@ -47,7 +47,7 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
         constexpr bool s = decltype(S)::value, l = decltype(BL)::value, w = decltype(W)::value, g = decltype(GA)::value;
         return eights == 2 ? (bias ? k_join<s, l, 2, true, w, g> : k_join<s, l, 2, false, w, g>) : (bias ? k_join<s, l, 1, true, w, g> : k_join<s, l, 1, false, w, g>);
     });
-    return launch_rows(kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, room, params, whole), static_cast<cudaStream_t>(stream), a);
+    return launch_rows(dev, kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, room, params, whole), static_cast<cudaStream_t>(stream), a);
 }
 
 }  // extern "C"

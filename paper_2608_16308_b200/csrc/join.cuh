@@ -233,69 +233,85 @@ struct JoinTeam {
     __device__ __forceinline__ int64_t first() const { return (int64_t)(blockIdx.x / cluster) * teams + team; }
     __device__ __forceinline__ int64_t step() const { return (int64_t)(gridDim.x / cluster) * teams; }
     __device__ __forceinline__ static void meet() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-    // (no block ends while another one may still send to it)
-    __device__ __forceinline__ void done() const {
-        if (cluster > 1) meet();
-    }
     __device__ __forceinline__ uint32_t barrier(int i) const { return (uint32_t)__cvta_generic_to_shared(sums + 4 * teams * room) + 8 * i; }
-    // the same sums in every thread of the row
     template <int K>
-    __device__ __forceinline__ void add(float (&v)[K]) {
+    __device__ __forceinline__ static void add_warp(float (&v)[K]) {
 #pragma unroll
         for (int o = 16; o; o >>= 1)
 #pragma unroll
             for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(FULL, v[k], o);
-        if (alone) return;
-        const int buffer = turn & 1;
-        float *s = sums + (buffer * teams + team) * 2 * room;
+    }
+    // every warp's K numbers to every warp of the row: [number][room], warps in the order of their columns.  False: a wait ran out.
+    template <int K>
+    __device__ __forceinline__ bool exchange(const float (&v)[K], const float *&s) {
+        const int buffer = turn & 1, phase = (turn >> 1) & 1;
+        float *to = sums + (buffer * teams + team) * 2 * room;
+        s = to;
         ++turn;
         if (cluster == 1) {
             if (lane == 0)
 #pragma unroll
-                for (int k = 0; k < K; ++k) s[k * room + warp] = v[k];
+                for (int k = 0; k < K; ++k) to[k * room + warp] = v[k];
             asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(warps * 32) : "memory");
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const float4 x = *reinterpret_cast<const float4 *>(s + k * room), y = *reinterpret_cast<const float4 *>(s + k * room + 4);
-                v[k] = ((x.x + x.y) + (x.z + x.w)) + ((y.x + y.y) + (y.z + y.w));
-                for (int i = 8; i < warps; i += 4) {
-                    const float4 z = *reinterpret_cast<const float4 *>(s + k * room + i);
-                    v[k] += (z.x + z.y) + (z.z + z.w);
-                }
-            }
-            return;
+            return true;
         }
-        const int all = warps * cluster;
-        if (threadIdx.x == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(barrier(buffer)), "r"(all * K * 4) : "memory");
+        if (threadIdx.x == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(barrier(buffer)), "r"(warps * cluster * K * 4) : "memory");
         if (lane < cluster) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                uint32_t to, bar;
-                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(s + k * room + rank * warps + warp)), "r"(lane));
+                uint32_t there, bar;
+                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(to + k * room + rank * warps + warp)), "r"(lane));
                 asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(barrier(buffer)), "r"(lane));
-                asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to), "r"(__float_as_uint(v[k])), "r"(bar) : "memory");
+                asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(there), "r"(__float_as_uint(v[k])), "r"(bar) : "memory");
             }
         }
-        const uint32_t phase = ((turn - 1) >> 1) & 1;
         uint32_t ok = 0;
         for (int i = 0; i < JOIN_WAIT && !ok; ++i)
             asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(barrier(buffer)), "r"(phase) : "memory");
+        return ok;
+    }
+    // the same sums in every thread of the row; NaN where a wait ran out
+    template <int K>
+    __device__ __forceinline__ void add(float (&v)[K]) {
+        add_warp(v);
+        if (alone) return;
+        const float *s;
+        const bool ok = exchange(v, s);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            v[k] = 0.f;
-            for (int i = 0; i < all; i += 4) {
-                const float4 x = *reinterpret_cast<const float4 *>(s + k * room + i);
-                v[k] += (x.x + x.y) + (x.z + x.w);
+            const float4 x = *reinterpret_cast<const float4 *>(s + k * room), y = *reinterpret_cast<const float4 *>(s + k * room + 4);
+            v[k] = ((x.x + x.y) + (x.z + x.w)) + ((y.x + y.y) + (y.z + y.w));
+            for (int i = 8; i < warps * cluster; i += 4) {
+                const float4 z = *reinterpret_cast<const float4 *>(s + k * room + i);
+                v[k] += (z.x + z.y) + (z.z + z.w);
             }
-            if (!ok) v[k] = __uint_as_float(0x7FC00000u);                    // a wait that ran out: the row becomes NaN
+            if (!ok) v[k] = __uint_as_float(0x7FC00000u);
         }
+    }
+    // Mean of the row and the sum of the squared differences from it, from each warp's own: those of its entries from its own mean, and of that mean from the row's (Chan, Golub and LeVeque, 1979).
+    // cols: of a warp; n: of the row
+    __device__ __forceinline__ float2 spread(float sum, float squares, int cols, int n) {
+        const float inv_n = 1.f / n;
+        if (alone) return make_float2(sum * inv_n, squares);
+        const float *s, v[2] = {sum, squares};
+        const bool ok = exchange(v, s);
+        float mean = 0.f, all = 0.f;
+        for (int i = 0; i < warps * cluster; ++i) mean += s[i];
+        mean *= inv_n;
+        for (int i = 0; i < warps * cluster; ++i) {
+            const int has = min(cols, n - i * cols);
+            if (has <= 0) break;
+            const float d = s[i] / has - mean;
+            all += s[room + i] + has * d * d;
+        }
+        return ok ? make_float2(mean, all) : make_float2(__uint_as_float(0x7FC00000u), 0.f);
     }
 };
 
 // mean and 1 / deviation of the row whose entries the threads hold (zeros behind its end)
 template <int E, bool WHOLE>
-__device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4], const WarpEight (&w)[E], int norm, float eps, float inv_n) {
-    float mean = 0.f, s[1];
+__device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4], const WarpEight (&w)[E], int n, int norm, float eps, float inv_n) {
+    float s[1];
     f32x2 p[2] = {0, 0};
     if (norm == DBSPMSPV_NORM_RMS) {
 #pragma unroll
@@ -303,33 +319,38 @@ __device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4
 #pragma unroll
             for (int j = 0; j < 4; ++j) p[j % 2] = fma2(v[e][j], v[e][j], p[j % 2]);
         s[0] = sum2(add2(p[0], p[1]));
-    } else if (norm == DBSPMSPV_NORM_LAYER) {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) p[j % 2] = add2(p[j % 2], v[e][j]);
-        s[0] = sum2(add2(p[0], p[1]));
         tm.add(s);
-        mean = s[0] * inv_n;
-        s[0] = 0.f;
+        return make_float2(0.f, rsqrtf(s[0] * inv_n + eps));
+    }
+    if (norm != DBSPMSPV_NORM_LAYER) return make_float2(0.f, 1.f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            if (WHOLE && w[e].cnt == 0) continue;                            // (zeros behind the end have no difference from the mean)
-            p[0] = 0;
+    for (int e = 0; e < E; ++e)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                f32x2 d = add2(v[e][j], both(-mean));
-                if (!WHOLE && w[e].cnt < 8) {
-                    const float2 x = apart(d);
-                    d = pair(2 * j < w[e].cnt ? x.x : 0.f, 2 * j + 1 < w[e].cnt ? x.y : 0.f);
-                }
-                p[0] = fma2(d, d, p[0]);
+        for (int j = 0; j < 4; ++j) p[j % 2] = add2(p[j % 2], v[e][j]);
+    s[0] = sum2(add2(p[0], p[1]));
+    JoinTeam::add_warp(s);
+    const float sum = s[0];
+    const int has = min(256 * E, n - w[0].col);
+    const f32x2 minus = both(has > 0 ? -sum / has : 0.f);
+    s[0] = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        f32x2 q = 0;
+        const int cnt = w[e].cnt;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f32x2 d = add2(v[e][j], minus);
+            if (!WHOLE && cnt < 8) {
+                const float2 x = apart(d);
+                d = pair(2 * j < cnt ? x.x : 0.f, 2 * j + 1 < cnt ? x.y : 0.f);
             }
-            s[0] += sum2(p[0]);
+            q = fma2(d, d, q);
         }
-    } else return make_float2(0.f, 1.f);
-    tm.add(s);
-    return make_float2(mean, rsqrtf(s[0] * inv_n + eps));
+        s[0] += WHOLE && cnt == 0 ? 0.f : sum2(q);                           // (zeros behind the row's end have no difference from the mean)
+    }
+    JoinTeam::add_warp(s);
+    const float2 all = tm.spread(sum, s[0], 256 * E, n);
+    return make_float2(all.x, rsqrtf(all.y * inv_n + eps));
 }
 
 // the row's sums of u * xhat and, behind a layer norm, of u
@@ -450,7 +471,7 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
         if (WHOLE || a.b.p) {
 #pragma unroll
             for (int e = 0; e < E; ++e) row_here<BF32, WHOLE>(a.b, t, me.w[e], at + AT_B + e * eight_room<BF32, WHOLE>(), v[e]);
-            sb = norm_stats<E, WHOLE>(tm, v, me.w, a.norm_block, a.eps_block, a.inv_n);
+            sb = norm_stats<E, WHOLE>(tm, v, me.w, n, a.norm_block, a.eps_block, a.inv_n);
             const f32x2 inv = both(sb.y), shift = both(-sb.x * sb.y);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -493,7 +514,7 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
             } else if (a.out.p) row_out<SF32>(a.out, t, me.w[e], n, x[e], me.spare);
         }
         if (!WHOLE && !a.h.p && !a.stats) continue;
-        const float2 sn = norm_stats<E, WHOLE>(tm, x, me.w, a.norm_next, a.eps_next, a.inv_n);
+        const float2 sn = norm_stats<E, WHOLE>(tm, x, me.w, n, a.norm_next, a.eps_next, a.inv_n);
         if (a.stats && tm.rank == 0 && tm.warp == 0 && tm.lane == 0) reinterpret_cast<float4 *>(a.stats)[t] = make_float4(sb.x, sb.y, sn.x, sn.y);
         if (!WHOLE && !a.h.p) continue;
         const f32x2 inv = both(sn.y), shift = both(-sn.x * sn.y);
@@ -512,7 +533,6 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
             } else row_out<false>(a.h, t, me.w[e], n, x[e], me.spare);
         }
     }
-    tm.done();
 }
 
 // factors: w_next, gate * w_block * scales (or without a gate that has rows), c_block * scales for the gradient of such a gate.  Sums over a team's tokens: dw_next, A, then (BIAS) dc_next, B.
@@ -692,10 +712,9 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
             if (me.w[e].cnt)
 #pragma unroll
                 for (int k = 0; k < SUMS; ++k) store_eight<true>(a.parts + (first * (int64_t)SUMS + k) * a.ldp, me.w[e].mine(), (int)a.ldp, true, sum[k][e]);
-    tm.done();
 }
 
-// The teams' sums added up, and what follows from them
+// The teams' sums added up, and what follows from them: 32 columns a thread block, four a lane, teams side by side
 struct JoinSums {
     const float *parts;
     int64_t ldp;
@@ -706,9 +725,10 @@ struct JoinSums {
 };
 template <bool BIAS>
 __global__ void __launch_bounds__(JOIN_SUMS_CTA) k_join_sums(const __grid_constant__ JoinSums a) {
-    constexpr int SUMS = BIAS ? 4 : 2, X = JOIN_SUMS_COLS / 4, Y = JOIN_SUMS_CTA / X;
-    __shared__ float4 s_sum[Y][SUMS][X];
-    const int x = threadIdx.x % X, y = threadIdx.x / X;
+    constexpr int SUMS = BIAS ? 4 : 2, X = JOIN_SUMS_COLS / 4, Y = JOIN_SUMS_CTA / X, WARPS = JOIN_SUMS_CTA / 32;
+    __shared__ float4 s_warp[WARPS][SUMS][X];
+    __shared__ float s_sum[SUMS][JOIN_SUMS_COLS];
+    const int tid = threadIdx.x, x = tid % X, y = tid / X;
     const int64_t at = (int64_t)blockIdx.x * JOIN_SUMS_COLS + 4 * x;
     pdl_wait();
     pdl_trigger();
@@ -724,16 +744,29 @@ __global__ void __launch_bounds__(JOIN_SUMS_CTA) k_join_sums(const __grid_consta
                 v[k].x += p.x; v[k].y += p.y; v[k].z += p.z; v[k].w += p.w;
             }
 #pragma unroll
-    for (int k = 0; k < SUMS; ++k) s_sum[y][k][x] = v[k];
+    for (int k = 0; k < SUMS; ++k) {
+#pragma unroll
+        for (int o = X; o < 32; o <<= 1) {
+            v[k].x += __shfl_xor_sync(FULL, v[k].x, o);
+            v[k].y += __shfl_xor_sync(FULL, v[k].y, o);
+            v[k].z += __shfl_xor_sync(FULL, v[k].z, o);
+            v[k].w += __shfl_xor_sync(FULL, v[k].w, o);
+        }
+        if (tid % 32 < X) s_warp[tid / 32][k][x] = v[k];
+    }
     __syncthreads();
-    const int col = blockIdx.x * JOIN_SUMS_COLS + threadIdx.x;
-    if (threadIdx.x >= JOIN_SUMS_COLS || col >= a.n) return;
+    if (tid < SUMS * JOIN_SUMS_COLS) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) t += reinterpret_cast<const float *>(s_warp[i])[tid];
+        (&s_sum[0][0])[tid] = t;
+    }
+    __syncthreads();
+    const int col = blockIdx.x * JOIN_SUMS_COLS + tid;
+    if (tid >= JOIN_SUMS_COLS || col >= a.n) return;
     float s[SUMS];
 #pragma unroll
-    for (int k = 0; k < SUMS; ++k) {
-        s[k] = 0.f;
-        for (int i = 0; i < Y; ++i) s[k] += reinterpret_cast<const float *>(&s_sum[i][k][0])[threadIdx.x];
-    }
+    for (int k = 0; k < SUMS; ++k) s[k] = s_sum[k][tid];
     s[1] *= a.scale;
     const float g = a.gate_vec ? vector_one(a.gate_vec, a.params_f32, col) : 1.f;
     if (a.dw_next) a.dw_next[col] = s[0];

@@ -49,7 +49,7 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
     const Rows BR = rows_of(block && (nb || dgate) ? b : nullptr, ldb, o->block_f32), DB = rows_of(db, lddb, o->dblock_f32);
     const Rows G = rows_of(gates ? gate : nullptr, ldg, o->params_f32), DG = rows_of(gates ? dgate : nullptr, lddg, o->params_f32);
     const bool whole = all_whole(n, DH, DOUT, DR, OUT, DB) && (!BR.p || all_whole(n, BR)) && (!gates || (G.aligned && DG.aligned));
-    const int params = gates && dgate ? 6 : 4, eights = join_eights(n, bias);
+    const int params = gates && dgate ? 6 : 4, eights = join_eights(sms, tokens, n, bias);
     const int room = eights * (eight_bytes(false, whole) + 2 * eight_bytes(o->stream_f32, whole) + eight_bytes(o->block_f32, whole) + (gates ? eight_bytes(o->params_f32, false) : 0));
     const JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, true);
     JoinArgs a = join_args(*o, tokens, n, p, room, params);
@@ -66,11 +66,11 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
         constexpr bool s = decltype(S)::value, l = decltype(BL)::value, w = decltype(W)::value, g = decltype(GA)::value;
         return bias ? k_join_backward<s, l, 1, true, w, g> : eights == 2 ? k_join_backward<s, l, 2, false, w, g> : k_join_backward<s, l, 1, false, w, g>;
     });
-    s = launch_rows(kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, room, params, whole), st, a);
+    s = launch_rows(dev, kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, room, params, whole), st, a);
     if (s != DBSPMSPV_OK || !sums) return s;
     JoinSums j = {a.parts, a.ldp, p.clusters * p.teams, (int32_t)n, a.params_f32, a.drop.random ? o->scale * a.drop.scale : o->scale, w_block, c_block, rows ? nullptr : gate,
                   dw_block, dc_block, rows ? nullptr : static_cast<float *>(dgate), dw_next, dc_next};
-    return launch_rows(bias ? k_join_sums<true> : k_join_sums<false>, (int)ceil64(n, JOIN_SUMS_COLS), JOIN_SUMS_CTA, 1, 0, st, j);
+    return launch_rows(dev, bias ? k_join_sums<true> : k_join_sums<false>, (int)ceil64(n, JOIN_SUMS_COLS), JOIN_SUMS_CTA, 1, 0, st, j);
 }
 
 }  // extern "C"

@@ -16,8 +16,7 @@ inline int join_threads(int eights, bool backward) { return backward ? 512 : eig
 inline int eight_bytes(bool f32, bool whole) { return f32 ? (whole ? eight_room<true, true>() : eight_room<true, false>()) : (whole ? eight_room<false, true>() : eight_room<false, false>()); }
 inline JoinPlan join_plan(int sms, int64_t tokens, int64_t n, int eights, int room, int params, bool whole, bool backward) {
     JoinPlan p;
-    // eight warps of a row in a thread block: two blocks to an SM, of which one works while the other waits for its sums (one eight a lane: up to the columns that eight blocks take)
-    const int warps = (int)ceil64(n, (int64_t)256 * eights), most = warps <= 8 * JOIN_CLUSTER ? 8 : JOIN_COLS / 256 / eights;
+    const int warps = (int)ceil64(n, (int64_t)256 * eights), most = JOIN_COLS / 256 / eights;
     p.eights = eights;
     p.cluster = (int)ceil64(warps, most);
     p.warps = (int)ceil64(warps, p.cluster);
@@ -31,8 +30,12 @@ inline JoinPlan join_plan(int sms, int64_t tokens, int64_t n, int eights, int ro
     p.clusters = (int)(want < blocks ? want : blocks < 1 ? 1 : blocks);
     return p;
 }
-// Two eights a lane share what a sum over the row costs; rows of up to 1024 columns have too few for that
-inline int join_eights(int64_t n, bool sums_of_biases) { return n > 1024 && !sums_of_biases ? 2 : 1; }
+// Two eights a lane share what a sum over the row costs.  One of rows of up to 1024 columns, of those that would leave more than a quarter of the lanes without columns, and where there are no more rows than
+// SMs hold at once: then the way through a row is what a call takes (333 rows of 1037: 8.3 us with two, 6.9 with one).
+inline int join_eights(int sms, int64_t tokens, int64_t n, bool sums_of_biases) {
+    const int64_t wide = ceil64(n, 512) * 512;
+    return n > 1024 && !sums_of_biases && 4 * n >= 3 * wide && (tokens > 2 * sms || n > 2048 * JOIN_CLUSTER) ? 2 : 1;
+}
 // whether every row is whole eights on 16 bytes (and its place one product of 32 bits)
 template <typename... R> inline bool all_whole(int64_t n, const R &...r) { return n % 8 == 0 && ((r.p && r.aligned && r.ld * (r.f32 ? 4 : 2) <= (int64_t)UINT32_MAX) && ...); }
 inline bool norm_ok(int norm) { return norm >= DBSPMSPV_NORM_NONE && norm <= DBSPMSPV_NORM_LAYER; }

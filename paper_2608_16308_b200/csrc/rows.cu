@@ -66,7 +66,7 @@ int dbspmspv_dropout(const void *x, int64_t ldx, int f32, int32_t tokens, int64_
     a.chunks = (int32_t)ceil64(eights, a.wide);
     const int64_t blocks = a.chunks * ceil64(tokens, (int64_t)(DR_CTA / a.wide) * DR_ROWS);
     if (blocks > INT32_MAX) return DBSPMSPV_ERR_UNSUPPORTED;
-    return launch_rows(f32 ? k_dropout<true> : k_dropout<false>, (int)blocks, DR_CTA, 1, 0, static_cast<cudaStream_t>(stream), a);
+    return launch_rows(dev, f32 ? k_dropout<true> : k_dropout<false>, (int)blocks, DR_CTA, 1, 0, static_cast<cudaStream_t>(stream), a);
 }
 
 int dbspmspv_logprobs(const void *logits, int64_t ldl, int logits_f32, int32_t tokens, int32_t vocab, float temperature, const int32_t *targets, float *logprob, float *entropy, float *stats,
@@ -86,7 +86,7 @@ int dbspmspv_logprobs(const void *logits, int64_t ldl, int logits_f32, int32_t t
     a.rounds = (int32_t)ceil64(ceil64(vectors, a.cluster), LP_CTA * LP_FLIGHT);
     const int64_t room = (int64_t)sms * LP_PER_SM, clusters = a.cluster > 1 || tokens < room ? tokens : room;
     auto kernel = logits_f32 ? (entropy ? k_logprobs<true, true> : k_logprobs<true, false>) : (entropy ? k_logprobs<false, true> : k_logprobs<false, false>);
-    return launch_rows(kernel, (int)clusters * a.cluster, LP_CTA, a.cluster, LP_SMEM + (a.cluster > 1 ? sizeof(LpCluster) : 0), static_cast<cudaStream_t>(stream), a);
+    return launch_rows(dev, kernel, (int)clusters * a.cluster, LP_CTA, a.cluster, LP_SMEM + (a.cluster > 1 ? sizeof(LpCluster) : 0), static_cast<cudaStream_t>(stream), a);
 }
 
 int dbspmspv_logprobs_backward(const void *logits, int64_t ldl, int logits_f32, int32_t tokens, int32_t vocab, float temperature, const int32_t *targets, const float *stats, const float *entropy,
@@ -108,7 +108,7 @@ int dbspmspv_logprobs_backward(const void *logits, int64_t ldl, int logits_f32, 
                 targets, top_ids, stats, entropy, dlogprob, dentropy, dtop};
     auto kernel = logits_f32 ? (dlogits_f32 ? k_logprobs_backward<true, true> : k_logprobs_backward<true, false>)
                              : (dlogits_f32 ? k_logprobs_backward<false, true> : k_logprobs_backward<false, false>);
-    return launch_rows(kernel, (int)(chunks * tokens), LG_ROWS_CTA, 1, 0, static_cast<cudaStream_t>(stream), a);
+    return launch_rows(dev, kernel, (int)(chunks * tokens), LG_ROWS_CTA, 1, 0, static_cast<cudaStream_t>(stream), a);
 }
 
 }  // extern "C"

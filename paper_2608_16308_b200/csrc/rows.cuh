@@ -280,10 +280,33 @@ inline int current_device(int *dev, int *sms) {
     return DBSPMSPV_OK;
 }
 
+// Lets a kernel have all of an SM's shared memory, once per kernel and device (the call takes the thread half a microsecond, a launch two).  The kernels that were told are kept in a small table; one that
+// finds no place there is told again.
+inline int allow_smem(const void *kernel, int dev) {
+    constexpr int PLACES = 256, TRIES = 8;
+    static const void *told[64][PLACES];
+    const size_t first = (reinterpret_cast<uintptr_t>(kernel) >> 4) * 2654435761u >> 8;
+    const void **free = nullptr;
+    for (int i = 0; i < TRIES && !free; ++i) {
+        const void **at = &told[dev][(first + i) % PLACES], *known = __atomic_load_n(at, __ATOMIC_ACQUIRE);
+        if (known == kernel) return DBSPMSPV_OK;
+        if (!known) free = at;
+    }
+    cudaFuncAttributes f;
+    DBS_CUDA(cudaFuncGetAttributes(&f, kernel));
+    DBS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - (int)f.sharedSizeBytes));
+    const void *none = nullptr;
+    if (free) __atomic_compare_exchange_n(free, &none, kernel, false, __ATOMIC_RELEASE, __ATOMIC_RELAXED);
+    return DBSPMSPV_OK;
+}
+
 // One launch in clusters of `cluster` thread blocks, set up while the kernel in front of it drains (every kernel launched so begins with pdl_wait).
 template <typename... P, typename... A>
-inline int launch_rows(void (*kernel)(P...), int blocks, int threads, int cluster, size_t smem, cudaStream_t st, const A &...args) {
-    if (smem > 16 * 1024) DBS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+inline int launch_rows(int dev, void (*kernel)(P...), int blocks, int threads, int cluster, size_t smem, cudaStream_t st, const A &...args) {
+    if (smem > 16 * 1024) {
+        const int s = allow_smem(reinterpret_cast<const void *>(kernel), dev);
+        if (s != DBSPMSPV_OK) return s;
+    }
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3(blocks);
     c.blockDim = dim3(threads);
