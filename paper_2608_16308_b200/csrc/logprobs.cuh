@@ -174,7 +174,7 @@ struct LpShared {
     uint64_t found[LP_CANDIDATES];
     uint64_t best[LP_MAX_TOP];
     uint16_t units[LP_CTA];
-    int n_units, n_found;
+    int n_units[2], n_found[2];              // of rows in turn
 };
 
 // What the blocks of a cluster tell each other: their sums, their groups' largest, how many candidates they have; and, in the first block, these
@@ -185,22 +185,23 @@ struct LpCluster {
     uint64_t best[LP_CLUSTER * LP_MAX_TOP], flat[LP_CLUSTER * LP_MAX_TOP];
 };
 
-// logits of at least tau among the units of at least tau -> sh.found (their number in sh.n_found, which may be more than there is room for).  The counts are 0 before it.
+// logits of at least tau among the units of at least tau -> sh.found (their number in sh.n_found, which may be more than there is room for).  The counts are 0 before it; all threads are behind a barrier
+// that they reached behind their last reading.
 template <bool F32>
-__device__ __forceinline__ void lp_collect(const LpRow<F32> &row, LpShared &sh, uint64_t unit, uint64_t tau, int vocab) {
+__device__ __forceinline__ void lp_collect(const LpRow<F32> &row, LpShared &sh, int parity, uint64_t unit, uint64_t tau, int vocab) {
     const int tid = threadIdx.x;
-    if (unit >= tau && unit) sh.units[atomicAdd(&sh.n_units, 1)] = (uint16_t)tid;
+    if (unit >= tau && unit) sh.units[atomicAdd(&sh.n_units[parity], 1)] = (uint16_t)tid;
     const float least = of_order((uint32_t)(tau >> 32));
     auto meet = [&](float l, int place, int of) {
         if (!tau || (l >= least && candidate(l, of) >= tau)) {
-            const int i = atomicAdd(&sh.n_found, 1);
+            const int i = atomicAdd(&sh.n_found[parity], 1);
             if (i < LP_CANDIDATES) sh.found[i] = candidate(l, place);
         }
     };
     if (tid < row.heads()) meet(row.one(tid), tid, tid);
     if (tid < row.tail) meet(row.one(vocab - row.tail + tid), vocab - row.tail + tid, vocab - row.tail + tid);
     __syncthreads();
-    const int n_units = sh.n_units, all = n_units * ((row.to - row.from + LP_CTA - 1) / LP_CTA);
+    const int n_units = sh.n_units[parity], all = n_units * ((row.to - row.from + LP_CTA - 1) / LP_CTA);
     for (int i = tid; i < all; i += LP_CTA) {
         const unsigned round = (unsigned)i / (unsigned)n_units;
         const int v = row.from + (int)round * LP_CTA + sh.units[i - (int)round * n_units];
@@ -238,16 +239,16 @@ __device__ __forceinline__ uint32_t lp_least(const uint32_t (&g)[N], int k) {
     return lo;
 }
 
-// the block's k largest into best[0 .. k), zeros behind them.  `most`: the thread's largest, as order_of has it (0: it has none); `group`: what at least k groups' largest reach, as order_of has it.
-template <bool F32>
-__device__ __forceinline__ void lp_top(const LpRow<F32> &row, LpShared &sh, uint32_t most, uint32_t group, bool plain, int k, int vocab, uint64_t *best) {
+// the block's k largest to out(candidate, place), zeros behind them, every place from one thread.  `most`: the thread's largest, as order_of has it (0: it has none); `group`: what at least k groups' largest reach, as order_of has it.
+template <bool F32, typename Out>
+__device__ __forceinline__ void lp_top(const LpRow<F32> &row, LpShared &sh, int parity, uint32_t most, uint32_t group, bool plain, int k, int vocab, Out out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint64_t unit = most ? (uint64_t)most << 32 | 0xFFFFFFFFu : 0;         // (the place is needed where values do not decide)
     bool done = false;
     if (plain) {
         // (a group without logits: the search finds tau)
-        if (group) lp_collect(row, sh, unit, (uint64_t)group << 32, vocab);
-        if (!group || sh.n_found > LP_CANDIDATES) {
+        if (group) lp_collect(row, sh, parity, unit, (uint64_t)group << 32, vocab);
+        if (!group || sh.n_found[parity] > LP_CANDIDATES) {
             // the unit's place: of the first vector (or entry) that has its largest
             if (unit) {
                 const float most = of_order((uint32_t)(unit >> 32));
@@ -261,22 +262,22 @@ __device__ __forceinline__ void lp_top(const LpRow<F32> &row, LpShared &sh, uint
                 const uint64_t trial = tau | 1ull << bit;
                 if (__syncthreads_count(unit >= trial) >= k) tau = trial;
             }
-            if (tid == 0) sh.n_units = sh.n_found = 0;
+            if (tid == 0) sh.n_units[parity] = sh.n_found[parity] = 0;
             __syncthreads();
-            lp_collect(row, sh, unit, tau, vocab);
+            lp_collect(row, sh, parity, unit, tau, vocab);
         }
-        const int n = sh.n_found;
+        const int n = sh.n_found[parity];
         done = n <= LP_CANDIDATES;
         for (int c = tid; done && c < max(n, k); c += LP_CTA) {
             if (c >= n) {
-                best[c] = 0;
+                out(0ull, c);
                 continue;
             }
             const uint64_t mine = sh.found[c];
             int before = 0;
 #pragma unroll 4
             for (int i = 0; i < n; ++i) before += sh.found[i] > mine;
-            if (before < k) best[before] = mine;
+            if (before < k) out(mine, before);
         }
     }
     if (!done) {
@@ -304,7 +305,7 @@ __device__ __forceinline__ void lp_top(const LpRow<F32> &row, LpShared &sh, uint
             __syncthreads();
             last = sh.largest[0];
             for (int w = 1; w < LP_WARPS; ++w) last = max64(last, sh.largest[w]);
-            if (tid == 0) best[j] = last;
+            if (tid == 0) out(last, j);
         }
     }
 }
@@ -319,7 +320,7 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
     const int rank = (int)(blockIdx.x % a.cluster), step = gridDim.x / a.cluster;
     uint4 *slot = s_slots + tid;              // [round][vector][thread]
     LpCluster *all = reinterpret_cast<LpCluster *>(s_slots + LP_SMEM / 16);  // (of a cluster)
-    if (tid == 0) sh.n_units = sh.n_found = 0;
+    if (tid < 2) sh.n_units[tid] = sh.n_found[tid] = 0;
     pdl_wait();
     pdl_trigger();
     const float slope = a.slope;
@@ -448,16 +449,31 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
         st.join<32>(slope);
         if (lane == 0) { sh.m[parity][warp] = st.m; sh.s[parity][warp] = st.s; sh.u[parity][warp] = st.u; }
         __syncthreads();
+        if (tid == 0) sh.n_units[parity ^ 1] = sh.n_found[parity ^ 1] = 0;
         st = {sh.m[parity][lane % LP_WARPS], sh.s[parity][lane % LP_WARPS], sh.u[parity][lane % LP_WARPS]};
         st.join<LP_WARPS>(slope);
+        // what the row gives, once st is the whole row's
+        auto nothing = [&] { return st.m == -INFINITY && st.s == 0.f; };
+        auto total = [&] { return nothing() ? -INFINITY : logf(st.s); };
+        auto give_sums = [&] {
+            const bool none = nothing();
+            const float log_sum = total();
+            if (a.stats) reinterpret_cast<float2 *>(a.stats)[t] = make_float2(st.m, log_sum);
+            if (ENTROPY) a.entropy[t] = none ? 0.f : log_sum - 0.6931471805599453f * (st.u / st.s);
+            if (a.logprob) a.logprob[t] = target < 0 ? 0.f : target >= a.vocab ? __uint_as_float(0x7FC00000u) : none ? -INFINITY : (at_target - st.m) * a.inv_t - log_sum;
+        };
+        auto give = [&](uint64_t mine, int place) {
+            if (!mine) return;
+            if (a.top_ids) a.top_ids[t * a.top + place] = place_of(mine);
+            if (a.top_logprobs) a.top_logprobs[t * a.top + place] = nothing() ? -INFINITY : (of_order((uint32_t)(mine >> 32)) - st.m) * a.inv_t - total();
+        };
         // (NaN or +inf among a block's logits makes its sum NaN)
         bool ranked = false;
         if (a.cluster == 1) {
+            if (tid == 0) give_sums();
             if (a.top) {
                 const uint32_t g[2] = {sh.group[parity][lane], sh.group[parity][lane + 32]};
-                lp_top(row, sh, most, lp_least<2>(g, a.top), st.s == st.s, a.top, a.vocab, sh.best);
-                __syncthreads();
-                if (tid == 0) sh.n_units = sh.n_found = 0;
+                lp_top(row, sh, parity, most, lp_least<2>(g, a.top), st.s == st.s, a.top, a.vocab, give);
             }
         } else {
             namespace cg = cooperative_groups;
@@ -490,65 +506,51 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
                 least = lp_least(g, a.top);
             }
             if (least) {
-                // (few tokens: every thread looks through its own logits, which lie in shared memory if the rounds in flight held them all)
-                const float l_least = of_order(least);
-                auto meet_one = [&](float l, int place) {
-                    if (l >= l_least) {
-                        const int i = atomicAdd(&sh.n_found, 1);
-                        if (i < LP_CANDIDATES) sh.found[i] = candidate(l, place);
-                    }
-                };
-                if (tid < row.heads()) meet_one(row.one(tid), tid);
-                if (tid < row.tail) meet_one(row.one(a.vocab - row.tail + tid), a.vocab - row.tail + tid);
-                if (most >= least) {
-                    const bool here = a.rounds <= LP_AHEAD;
-#pragma unroll 4
-                    for (int i = 0; row.from + tid + i * LP_CTA < row.to; ++i) {
-                        const int v = row.from + tid + i * LP_CTA;
-                        const uint4 q = here ? slot[i * LP_CTA] : row.raw(v);
-                        if (!(largest<F32>(q) >= l_least)) continue;
-                        float l[V];
-                        LpRow<F32>::values(q, l);
+                if (a.rounds > LP_AHEAD) lp_collect(row, sh, parity, most ? (uint64_t)most << 32 | 0xFFFFFFFFu : 0, (uint64_t)least << 32, a.vocab);
+                else {
+                    // (every round is still in shared memory: each thread looks through its own logits)
+                    const float l_least = of_order(least);
+                    auto meet_one = [&](float l, int place) {
+                        if (l >= l_least) {
+                            const int i = atomicAdd(&sh.n_found[parity], 1);
+                            if (i < LP_CANDIDATES) sh.found[i] = candidate(l, place);
+                        }
+                    };
+                    if (tid < row.heads()) meet_one(row.one(tid), tid);
+                    if (tid < row.tail) meet_one(row.one(a.vocab - row.tail + tid), a.vocab - row.tail + tid);
+                    if (most >= least)
+                        for (int i = 0; row.from + tid + i * LP_CTA < row.to; ++i) {
+                            const uint4 q = slot[i * LP_CTA];
+                            if (!(largest<F32>(q) >= l_least)) continue;
+                            float l[V];
+                            LpRow<F32>::values(q, l);
 #pragma unroll
-                        for (int j = 0; j < V; ++j) meet_one(l[j], row.place(v) + j);
-                    }
+                            for (int j = 0; j < V; ++j) meet_one(l[j], row.place(row.from + tid + i * LP_CTA) + j);
+                        }
+                    __syncthreads();
                 }
-                __syncthreads();
-                const int n = sh.n_found;
+                const int n = sh.n_found[parity];
                 if (tid < n && n <= LP_MAX_TOP) first->best[rank * LP_MAX_TOP + tid] = sh.found[tid];
                 if (tid < a.cluster) c.map_shared_rank(all, tid)->found[rank] = n;
                 asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
                 ranked = true;
                 for (int i = 0; i < a.cluster; ++i) ranked = ranked && all->found[i] <= LP_MAX_TOP;
-                if (!ranked && tid == 0) sh.n_units = sh.n_found = 0;
+                if (!ranked && tid == 0) sh.n_units[parity] = sh.n_found[parity] = 0;
                 __syncthreads();
             }
             if (a.top && !ranked) {
                 // every block's own, then the blocks' among each other
                 const uint32_t g[2] = {sh.group[parity][lane], sh.group[parity][lane + 32]};
-                lp_top(row, sh, most, lp_least<2>(g, a.top), plain, a.top, a.vocab, sh.best);
+                lp_top(row, sh, parity, most, lp_least<2>(g, a.top), plain, a.top, a.vocab, [&](uint64_t c, int place) { sh.best[place] = c; });
                 __syncthreads();
                 if (tid < LP_MAX_TOP) first->best[rank * LP_MAX_TOP + tid] = tid < a.top ? sh.best[tid] : 0;
                 if (tid < a.cluster) c.map_shared_rank(all, tid)->found[rank] = a.top;
                 asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
             }
         }
-        if (rank == 0 && tid < max(a.cluster > 1 && a.top ? LP_CTA : a.top, 1)) {
-            const bool nothing = st.m == -INFINITY && st.s == 0.f;
-            const float total = nothing ? -INFINITY : logf(st.s);
-            if (tid == 0) {
-                if (a.stats) reinterpret_cast<float2 *>(a.stats)[t] = make_float2(st.m, total);
-                if (ENTROPY) a.entropy[t] = nothing ? 0.f : total - 0.6931471805599453f * (st.u / st.s);
-                if (a.logprob)
-                    a.logprob[t] = target < 0 ? 0.f : target >= a.vocab ? __uint_as_float(0x7FC00000u) : nothing ? -INFINITY : (at_target - st.m) * a.inv_t - total;
-            }
-            auto give = [&](uint64_t mine, int place) {
-                if (a.top_ids) a.top_ids[t * a.top + place] = place_of(mine);
-                if (a.top_logprobs) a.top_logprobs[t * a.top + place] = nothing ? -INFINITY : (of_order((uint32_t)(mine >> 32)) - st.m) * a.inv_t - total;
-            };
-            if (a.cluster == 1) {
-                if (tid < a.top && sh.best[tid]) give(sh.best[tid], tid);
-            } else if (a.top) {
+        if (a.cluster > 1 && rank == 0) {
+            if (tid == 0) give_sums();
+            if (a.top) {
                 int n = 0;
                 for (int r = 0; r < a.cluster; ++r) {
                     const int here = all->found[r];
@@ -561,7 +563,7 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
                     int before = 0;
 #pragma unroll 8
                     for (int j = 0; j < n; ++j) before += all->flat[j] > mine;
-                    if (mine && before < a.top) give(mine, before);
+                    if (before < a.top) give(mine, before);
                 }
             }
         }
@@ -578,13 +580,10 @@ struct LpGrad {
     const int32_t *targets, *top_ids;
     const float *stats, *entropy, *dlogprob, *dentropy, *dtop;
 };
-constexpr int LG_ROWS_WAVES = 3, LG_ROWS_CTA = 256, LG_ROWS_FLIGHT = 2;            // threads, eights in flight of each
+constexpr int LG_ROWS_WAVES = 3, LG_ROWS_PER_SM = 8, LG_ROWS_CTA = 128, LG_ROWS_FLIGHT = 2;            // threads, eights in flight of each
 
 template <bool F32, bool OUT32>
 __global__ void __launch_bounds__(LG_ROWS_CTA) k_logprobs_backward(const __grid_constant__ LpGrad a) {
-    __shared__ float s_given;
-    __shared__ int s_id[LP_MAX_TOP + 1];
-    __shared__ float s_weight[LP_MAX_TOP + 1];
     constexpr int IN = F32 ? 4 : 2, OUT = OUT32 ? 4 : 2;
     const int tid = threadIdx.x;
     const int64_t t = blockIdx.x / a.chunks;
@@ -616,46 +615,48 @@ __global__ void __launch_bounds__(LG_ROWS_CTA) k_logprobs_backward(const __grid_
     const bool last = chunk == a.chunks - 1;
     const int edge = chunk == 0 && tid < head ? tid : last && tid >= 32 && tid - 32 < a.vocab - tail_at ? tail_at + tid - 32 : -1;
     const float l_edge = edge >= 0 ? one(edge) : 0.f;
-    if (tid <= a.top) {
-        int id = -1;
-        float w = 0.f;
-        if (tid == a.top) {
-            if (a.dlogprob) {
-                id = a.targets[t];
-                w = id < 0 ? 0.f : id >= a.vocab ? __uint_as_float(0x7FC00000u) : a.dlogprob[t];
-            }
-        } else if (a.dtop) {
-            id = a.top_ids[t * a.top + tid];
-            if (id >= 0 && id < a.vocab) w = a.dtop[t * a.top + tid];
+    // the entries that are given a gradient: every warp adds it up for itself, and thread j keeps the j-th's place and logit
+    float given = 0.f, mine = 0.f, l_mine = 0.f;
+    int id = -1;
+    auto weight = [&](int j, int &at) {       // the target's behind the alternatives'
+        at = -1;
+        if (j == a.top && a.dlogprob) {
+            at = a.targets[t];
+            return at < 0 ? 0.f : at >= a.vocab ? __uint_as_float(0x7FC00000u) : a.dlogprob[t];
         }
-        s_id[tid] = id >= 0 && id < a.vocab ? id : -1;
-        s_weight[tid] = w;
+        if (j < a.top) {
+            at = a.top_ids[t * a.top + j];
+            return at >= 0 && at < a.vocab ? a.dtop[t * a.top + j] : 0.f;
+        }
+        return 0.f;
+    };
+#pragma unroll
+    for (int j0 = 0; j0 <= LP_MAX_TOP; j0 += 32) {
+        int at;
+        if (j0 <= a.top) given += weight(j0 + tid % 32, at);
     }
     const float2 st = reinterpret_cast<const float2 *>(a.stats)[t];
     const float dh = a.dentropy ? a.dentropy[t] : 0.f, h = a.dentropy ? a.entropy[t] : 0.f;
-    __syncthreads();
-    float mine = 0.f, l_mine = 0.f;
-    int id = -1;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) given += __shfl_xor_sync(FULL, given, o);
     if (tid <= a.top) {
-        id = s_id[tid];
+        mine = weight(tid, id);
         // (this block's own; the ends of the row are the first one's and the last one's)
         const int from = chunk == 0 ? 0 : head + from8 * 8, to = last ? a.vocab : head + to8 * 8;
         if (id < from || id >= to) id = -1;
         if (id >= 0) {
             l_mine = one(id);
-            for (int j = 0; j <= a.top; ++j)
-                if (s_id[j] == id) mine += s_weight[j];
+            for (int j = 0; j <= a.top; ++j) {
+                int at;
+                const float w = weight(j, at);
+                if (j != tid && at == id) mine += w;
+            }
         }
-    }
-    if (tid == 0) {
-        float g = 0.f;
-        for (int j = 0; j <= a.top; ++j) g += s_weight[j];
-        s_given = g;
     }
     __syncthreads();
     const bool nothing = st.x == -INFINITY && !(st.y != st.y);
     constexpr float LN2 = 0.6931471805599453f;
-    const float given = s_given, shift = st.y * 1.4426950408889634f;
+    const float shift = st.y * 1.4426950408889634f;
     auto slope = [&](float v, float own) {
         const float x = (v - st.x) * a.slope - shift, p = exp_2(x);
         return nothing ? 0.f : (own - p * (given + dh * (max_nan(x, LP_NONE) * LN2 + h))) * a.inv_t;
@@ -684,8 +685,8 @@ __global__ void __launch_bounds__(LG_ROWS_CTA) k_logprobs_backward(const __grid_
                 if (F32) pairs_of<F32, true>(q[r][F32 ? 1 : 0], l + 2);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const f32x2 x = fma2(l[j], both(a.slope), both(-ref));
-                    const float2 xx = apart(x), v = apart(mul2(pair(exp_2(xx.x), exp_2(xx.y)), fma2(x, c1, c0)));
+                    const f32x2 x = fma1(l[j], both(a.slope), both(-ref));
+                    const float2 xx = apart(x), v = apart(mul1(pair(exp_2(xx.x), exp_2(xx.y)), fma1(x, c1, c0)));
                     d[2 * j] = v.x;
                     d[2 * j + 1] = v.y;
                 }

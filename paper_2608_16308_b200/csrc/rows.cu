@@ -101,8 +101,9 @@ int dbspmspv_logprobs_backward(const void *logits, int64_t ldl, int logits_f32, 
     int dev, sms, s;
     if ((s = current_device(&dev, &sms)) != DBSPMSPV_OK) return s;
     if (!on_current_device(logits, dev) || !on_current_device(dlogits, dev)) return DBSPMSPV_ERR_INVALID_ARG;
-    // a row is shared out until there are LG_ROWS_WAVES rounds of thread blocks, or two loads left to a thread
-    const int64_t most = ceil64(vocab, (int64_t)8 * LG_ROWS_CTA * LG_ROWS_FLIGHT), want = ceil64((int64_t)sms * 5 * LG_ROWS_WAVES, tokens), chunks = want < most ? want : most;
+    // a row is shared out until there are LG_ROWS_WAVES rounds of thread blocks, but few rows to one round; and until two loads are left to a thread
+    const int64_t most = ceil64(vocab, (int64_t)8 * LG_ROWS_CTA * LG_ROWS_FLIGHT), at_once = (int64_t)sms * LG_ROWS_PER_SM;
+    const int64_t want = tokens < at_once / 2 ? at_once / tokens : ceil64(at_once * LG_ROWS_WAVES, tokens), chunks = want < most ? want : most;
     if (chunks * tokens > INT32_MAX) return DBSPMSPV_ERR_UNSUPPORTED;
     LpGrad a = {logits, dlogits, ldl, ldd, tokens, vocab, dtop ? top : 0, (int32_t)chunks, (float)(1.4426950408889634 / (double)temperature), (float)(1.0 / (double)temperature),
                 targets, top_ids, stats, entropy, dlogprob, dentropy, dtop};
