@@ -22,10 +22,10 @@ constexpr int JOIN_COLS = 4096;              // of a row in one thread block; mo
 constexpr int JOIN_CLUSTER = 8;
 constexpr int64_t JOIN_MAX_N = JOIN_COLS * JOIN_CLUSTER;
 constexpr int JOIN_AHEAD = 2;                // rows in flight or in hand, per team
-constexpr int JOIN_SUMS_COLS = 32, JOIN_SUMS_CTA = 512;
+constexpr int JOIN_SUMS_CTA = 512;
 constexpr int JOIN_WAIT = 1 << 20;           // tries of a wait for a cluster's sums, before it gives up
-// threads at most: of kernels with two eights a lane, and with one
-template <int E> __host__ __device__ constexpr int join_cta() { return JOIN_COLS / 8 / E; }
+// threads at most (two eights a lane, or rows of up to 2048 columns); of gradients with sums of biases (one eight a lane)
+__host__ __device__ constexpr int join_cta(bool sums_of_biases) { return sums_of_biases ? JOIN_COLS / 8 : JOIN_COLS / 16; }
 
 struct JoinPlan {
     int eights;                              // of a lane: 1, 2
@@ -46,114 +46,12 @@ struct JoinArgs {
     int64_t ldp;
 };
 
-// ---- rows in a warp's shared memory --------------------------------------------------------------
-// A lane's eight lies at 16 * lane; fp32: the first four there and the others 512 bytes behind (WHOLE), or all at 32 * lane.  What is not WHOLE has 16 bytes more: rows that begin between two words.
-template <bool F32, bool WHOLE> __host__ __device__ constexpr int eight_room() { return (F32 ? 1024 : 512) + (WHOLE ? 0 : 16); }
-// whether row t of bf16 begins between two words
-__device__ __forceinline__ int between(const Rows &r, int64_t t) { return (int)((reinterpret_cast<uintptr_t>(r.p) >> 1) + t * r.ld) & 1; }
-
-struct WarpEight {
-    int lane, col, cnt;                      // the warp's first column; the lane's entries, 0 to 8
-    __device__ __forceinline__ int mine() const { return col + lane * 8; }
-};
-// the warp's eights of row t, columns from w.col on, towards shared memory at `to`
-template <bool F32>
-__device__ __forceinline__ void row_ahead(const Rows &r, int64_t t, const WarpEight &w, int n, uint8_t *to) {
-    const uint8_t *row = static_cast<const uint8_t *>(row_at<F32>(r, t));
-    if (r.aligned) {
-        const uint8_t *p = row + (int64_t)w.mine() * (F32 ? 4 : 2);
-        uint4 *at = reinterpret_cast<uint4 *>(to + w.lane * (F32 ? 32 : 16));
-        if (w.cnt == 8) {
-            copy_ahead(at, p);
-            if (F32) copy_ahead(at + 1, p + 16);
-        } else if (w.cnt) {
-            uint4 a, b;
-            load_raw<F32>(row, w.mine(), n, false, a, b);
-            at[0] = a;
-            if (F32) at[1] = b;
-        }
-        return;
-    }
-    const int here = min(256, n - w.col);    // entries of the warp
-    if (here <= 0) return;
-    if (F32) {
-        const uint8_t *p = row + (int64_t)w.col * 4;
-#pragma unroll
-        for (int i = w.lane; i < 256; i += 32)
-            if (i < here) copy_word_ahead(to + i * 4, p + i * 4);
-        return;
-    }
-    // entry e of the words is the row's w.col + e - odd
-    const int odd = between(r, t), first = w.col ? 0 : odd, end = n - w.col + odd;
-    const uint8_t *p = row + (int64_t)w.col * 2 - 2 * odd;
-    for (int i = w.lane; 2 * i < here + odd; i += 32) {
-        const int e = 2 * i;
-        if (e >= first && e + 1 < end) copy_word_ahead(to + i * 4, p + i * 4);
-        else if (e >= first) reinterpret_cast<uint16_t *>(to)[e] = reinterpret_cast<const uint16_t *>(p)[e];
-        else if (e + 1 < end) reinterpret_cast<uint16_t *>(to)[e + 1] = reinterpret_cast<const uint16_t *>(p)[e + 1];
-    }
-}
 // the same where all rows are whole eights on 16 bytes: `mine` is the lane's place in row 0.  (An eight behind the row's end is 0 bytes long: no branch.)
 template <bool F32>
 __device__ __forceinline__ void row_ahead(const uint8_t *mine, uint32_t stride, uint32_t t, const WarpEight &w, uint8_t *to) {
     const uint8_t *p = mine + (uint64_t)t * stride;
     copy_ahead(to + w.lane * 16, p, w.cnt * 2);
     if (F32) copy_ahead(to + 512 + w.lane * 16, p + 16, w.cnt * 2);
-}
-// the lane's eight, zeros behind the row's end
-template <bool F32, bool WHOLE>
-__device__ __forceinline__ void row_here(const Rows &r, int64_t t, const WarpEight &w, const uint8_t *at, f32x2 v[4]) {
-    if (F32) {
-        const uint4 *p = reinterpret_cast<const uint4 *>(at + w.lane * (WHOLE ? 16 : 32));
-        pairs_of_eight(p[0], p[WHOLE ? 32 : 1], v);
-    } else {
-        uint4 q = *reinterpret_cast<const uint4 *>(at + w.lane * 16);
-        if (!WHOLE && !r.aligned && between(r, t)) {
-            const uint32_t next = *reinterpret_cast<const uint32_t *>(at + w.lane * 16 + 16);
-            q = make_uint4(__funnelshift_r(q.x, q.y, 16), __funnelshift_r(q.y, q.z, 16), __funnelshift_r(q.z, q.w, 16), __funnelshift_r(q.w, next, 16));
-        }
-        pairs_of_eight(q, v);
-    }
-    if (!WHOLE && w.cnt < 8) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 x = apart(v[j]);
-            v[j] = pair(2 * j < w.cnt ? x.x : 0.f, 2 * j + 1 < w.cnt ? x.y : 0.f);
-        }
-    }
-}
-// the warp's eights to row t; `room`: 1024 bytes of the warp's shared memory
-template <bool F32>
-__device__ __forceinline__ void row_out(const Rows &r, int64_t t, const WarpEight &w, int n, const f32x2 v[4], uint8_t *room) {
-    void *row = const_cast<void *>(row_at<F32>(r, t));
-    if (r.aligned) {
-        if (w.cnt) store_eight<F32>(row, w.mine(), n, w.cnt == 8, v);
-        return;
-    }
-    const int here = min(256, n - w.col);
-    if (F32) {
-        f32x2 *mine = reinterpret_cast<f32x2 *>(room + w.lane * 32);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mine[j] = v[j];
-        __syncwarp();
-        uint32_t *p = static_cast<uint32_t *>(row) + w.col;
-#pragma unroll
-        for (int i = w.lane; i < 256; i += 32)
-            if (i < here) p[i] = reinterpret_cast<const uint32_t *>(room)[i];
-    } else {
-        *reinterpret_cast<uint4 *>(room + w.lane * 16) = bf16_eight(v);
-        __syncwarp();
-        const int odd = between(r, t);
-        uint16_t *p = static_cast<uint16_t *>(row) + w.col;
-        const uint16_t *from = reinterpret_cast<const uint16_t *>(room);
-        for (int i = w.lane; i < 129; i += 32) {
-            const int e = 2 * i - odd;       // entries e and e + 1 of the warp's share a word of the row
-            if (e >= 0 && e + 1 < here) *reinterpret_cast<uint32_t *>(p + e) = (uint32_t)from[e] | (uint32_t)from[e + 1] << 16;
-            else if (e >= 0 && e < here) p[e] = from[e];
-            else if (e == -1 && here > 0) p[0] = from[0];
-        }
-    }
-    __syncwarp();
 }
 // and where all rows are whole eights on 16 bytes
 template <bool F32>
@@ -400,7 +298,7 @@ struct JoinWarp {
 
 // factors: gate * w_block * scales (or without a gate that has rows), w_next, then (BIAS) c_block * gate * scales, c_next
 template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE, bool GATES>
-__global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __grid_constant__ JoinArgs a) {
+__global__ void __launch_bounds__(join_cta(false), E == 1 ? 4 : 3) k_join(const __grid_constant__ JoinArgs a) {
     extern __shared__ __align__(16) uint8_t s_dyn[];
     constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, PARAMS = BIAS ? 8 : 4;
     // where a lane's eights of r, b and the gate lie in a row's shared memory
@@ -537,7 +435,7 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 2 : 3) k_join(const __
 
 // factors: w_next, gate * w_block * scales (or without a gate that has rows), c_block * scales for the gradient of such a gate.  Sums over a team's tokens: dw_next, A, then (BIAS) dc_next, B.
 template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE, bool GATES>
-__global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward(const __grid_constant__ JoinArgs a) {
+__global__ void __launch_bounds__(join_cta(BIAS), BIAS ? 1 : 2) k_join_backward(const __grid_constant__ JoinArgs a) {
     extern __shared__ __align__(16) uint8_t s_dyn[];
     constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, SUMS = BIAS ? 4 : 2;
     constexpr int S8 = eight_room<SF32, WHOLE>(), B8 = eight_room<BF32, WHOLE>(), H8 = eight_room<false, WHOLE>();
@@ -714,7 +612,8 @@ __global__ void __launch_bounds__(join_cta<E>(), E == 1 ? 1 : 2) k_join_backward
                 for (int k = 0; k < SUMS; ++k) store_eight<true>(a.parts + (first * (int64_t)SUMS + k) * a.ldp, me.w[e].mine(), (int)a.ldp, true, sum[k][e]);
 }
 
-// The teams' sums added up, and what follows from them: 32 columns a thread block, four a lane, teams side by side
+// The teams' sums added up, and what follows from them: COLS columns a thread block, four a lane, teams side by side.  32 columns are whole lines of the parts, 8 are sectors; these for rows of
+// fewer than 2048 columns, which make few thread blocks (with the gradient in front of it, 4000 rows of 1000: 21.7 -> 20.8 us, but 4096 of 4096: 46.9 -> 50.2).
 struct JoinSums {
     const float *parts;
     int64_t ldp;
@@ -723,13 +622,13 @@ struct JoinSums {
     const void *w_block, *c_block, *gate_vec;
     float *dw_block, *dc_block, *dgate, *dw_next, *dc_next;
 };
-template <bool BIAS>
+template <bool BIAS, int COLS>
 __global__ void __launch_bounds__(JOIN_SUMS_CTA) k_join_sums(const __grid_constant__ JoinSums a) {
-    constexpr int SUMS = BIAS ? 4 : 2, X = JOIN_SUMS_COLS / 4, Y = JOIN_SUMS_CTA / X, WARPS = JOIN_SUMS_CTA / 32;
+    constexpr int SUMS = BIAS ? 4 : 2, X = COLS / 4, Y = JOIN_SUMS_CTA / X, WARPS = JOIN_SUMS_CTA / 32;
     __shared__ float4 s_warp[WARPS][SUMS][X];
-    __shared__ float s_sum[SUMS][JOIN_SUMS_COLS];
+    __shared__ float s_sum[SUMS][COLS];
     const int tid = threadIdx.x, x = tid % X, y = tid / X;
-    const int64_t at = (int64_t)blockIdx.x * JOIN_SUMS_COLS + 4 * x;
+    const int64_t at = (int64_t)blockIdx.x * COLS + 4 * x;
     pdl_wait();
     pdl_trigger();
     float4 v[SUMS];
@@ -755,15 +654,15 @@ __global__ void __launch_bounds__(JOIN_SUMS_CTA) k_join_sums(const __grid_consta
         if (tid % 32 < X) s_warp[tid / 32][k][x] = v[k];
     }
     __syncthreads();
-    if (tid < SUMS * JOIN_SUMS_COLS) {
+    if (tid < SUMS * COLS) {
         float t = 0.f;
 #pragma unroll
         for (int i = 0; i < WARPS; ++i) t += reinterpret_cast<const float *>(s_warp[i])[tid];
         (&s_sum[0][0])[tid] = t;
     }
     __syncthreads();
-    const int col = blockIdx.x * JOIN_SUMS_COLS + tid;
-    if (tid >= JOIN_SUMS_COLS || col >= a.n) return;
+    const int col = blockIdx.x * COLS + tid;
+    if (tid >= COLS || col >= a.n) return;
     float s[SUMS];
 #pragma unroll
     for (int k = 0; k < SUMS; ++k) s[k] = s_sum[k][tid];

@@ -51,7 +51,7 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
     const bool whole = all_whole(n, DH, DOUT, DR, OUT, DB) && (!BR.p || all_whole(n, BR)) && (!gates || (G.aligned && DG.aligned));
     const int params = gates && dgate ? 6 : 4, eights = join_eights(sms, tokens, n, bias);
     const int room = eights * (eight_bytes(false, whole) + 2 * eight_bytes(o->stream_f32, whole) + eight_bytes(o->block_f32, whole) + (gates ? eight_bytes(o->params_f32, false) : 0));
-    const JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, true);
+    const JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, true, bias);
     JoinArgs a = join_args(*o, tokens, n, p, room, params);
     a.dh = DH; a.dout = DOUT; a.dr = DR; a.out = OUT; a.b = BR; a.db = DB; a.gate = G; a.dgate = DG;
     if (block) {
@@ -70,7 +70,9 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
     if (s != DBSPMSPV_OK || !sums) return s;
     JoinSums j = {a.parts, a.ldp, p.clusters * p.teams, (int32_t)n, a.params_f32, a.drop.random ? o->scale * a.drop.scale : o->scale, w_block, c_block, rows ? nullptr : gate,
                   dw_block, dc_block, rows ? nullptr : static_cast<float *>(dgate), dw_next, dc_next};
-    return launch_rows(dev, bias ? k_join_sums<true> : k_join_sums<false>, (int)ceil64(n, JOIN_SUMS_COLS), JOIN_SUMS_CTA, 1, 0, st, j);
+    const int cols = n < 2048 ? 8 : 32;
+    auto add_up = cols == 32 ? (bias ? k_join_sums<true, 32> : k_join_sums<false, 32>) : (bias ? k_join_sums<true, 8> : k_join_sums<false, 8>);
+    return launch_rows(dev, add_up, (int)ceil64(n, cols), JOIN_SUMS_CTA, 1, 0, st, j);
 }
 
 }  // extern "C"

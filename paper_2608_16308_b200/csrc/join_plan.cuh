@@ -11,12 +11,12 @@
 
 namespace dbs {
 
-// Threads that an SM holds of the joins' kernels, by their registers (forwards; backwards)
-inline int join_threads(int eights, bool backward) { return backward ? 512 : eights == 2 ? 768 : 1024; }
+// Threads that an SM holds of the joins' kernels, by their registers
+inline int join_threads(int eights, bool backward) { return !backward ? (eights == 2 ? 768 : 1024) : 512; }
 inline int eight_bytes(bool f32, bool whole) { return f32 ? (whole ? eight_room<true, true>() : eight_room<true, false>()) : (whole ? eight_room<false, true>() : eight_room<false, false>()); }
-inline JoinPlan join_plan(int sms, int64_t tokens, int64_t n, int eights, int room, int params, bool whole, bool backward) {
+inline JoinPlan join_plan(int sms, int64_t tokens, int64_t n, int eights, int room, int params, bool whole, bool backward, bool biases) {
     JoinPlan p;
-    const int warps = (int)ceil64(n, (int64_t)256 * eights), most = JOIN_COLS / 256 / eights;
+    const int warps = (int)ceil64(n, (int64_t)256 * eights), most = join_cta(backward && biases) / 32;
     p.eights = eights;
     p.cluster = (int)ceil64(warps, most);
     p.warps = (int)ceil64(warps, p.cluster);
@@ -30,11 +30,11 @@ inline JoinPlan join_plan(int sms, int64_t tokens, int64_t n, int eights, int ro
     p.clusters = (int)(want < blocks ? want : blocks < 1 ? 1 : blocks);
     return p;
 }
-// Two eights a lane share what a sum over the row costs.  One of rows of up to 1024 columns, of those that would leave more than a quarter of the lanes without columns, and where there are no more rows than
-// SMs hold at once: then the way through a row is what a call takes (333 rows of 1037: 8.3 us with two, 6.9 with one).
+// Two eights a lane share what a sum over the row costs: from 1024 columns on where no more than a quarter of the lanes has none and there are more rows than SMs hold at once (333 rows of 1037: 8.3 us with two,
+// 7.5 with one; 4000 rows of 1000, gradient: 24.5 and 21.7), and from 2048 on in any case.  Gradients with sums of biases have no registers for two.
 inline int join_eights(int sms, int64_t tokens, int64_t n, bool sums_of_biases) {
-    const int64_t wide = ceil64(n, 512) * 512;
-    return n > 1024 && !sums_of_biases && 4 * n >= 3 * wide && (tokens > 2 * sms || n > 2048 * JOIN_CLUSTER) ? 2 : 1;
+    if (sums_of_biases || n <= 1024) return 1;
+    return n > 2048 || (4 * n >= 3 * (ceil64(n, 512) * 512) && tokens > 2 * sms) ? 2 : 1;
 }
 // whether every row is whole eights on 16 bytes (and its place one product of 32 bits)
 template <typename... R> inline bool all_whole(int64_t n, const R &...r) { return n % 8 == 0 && ((r.p && r.aligned && r.ld * (r.f32 ? 4 : 2) <= (int64_t)UINT32_MAX) && ...); }
@@ -54,8 +54,11 @@ inline JoinArgs join_args(const dbspmspv_join_opts &o, int32_t tokens, int64_t n
 // Room for the sums of any gradient call of this size: the most teams that any of them has (those with the least shared memory, bf16 throughout)
 inline int64_t join_room(int sms, int64_t tokens, int64_t n) {
     int64_t most = 0;
-    for (int eights = 1; eights <= 2; ++eights) {
-        const JoinPlan p = join_plan(sms, tokens, n, eights, eights * 4 * eight_bytes(false, true), 4, true, true);
+    for (int form = 0; form < 3; ++form) {
+        const bool biases = form == 2;
+        const int eights = form == 1 ? 2 : 1;
+        if (form == 0 && n > 2048) continue;
+        const JoinPlan p = join_plan(sms, tokens, n, eights, eights * 4 * eight_bytes(false, true), 4, true, true, biases);
         const int64_t teams = (int64_t)p.clusters * p.teams;
         if (teams > most) most = teams;
     }

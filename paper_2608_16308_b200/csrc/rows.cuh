@@ -171,6 +171,108 @@ __device__ __forceinline__ void copy_word_ahead(void *smem, const void *p) {
 __device__ __forceinline__ void close_ahead() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void wait_ahead() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
+// ---- rows in a warp's shared memory --------------------------------------------------------------
+// A lane's eight lies at 16 * lane; fp32: the first four there and the others 512 bytes behind (WHOLE), or all at 32 * lane.  What is not WHOLE has 16 bytes more: rows that begin between two words.
+template <bool F32, bool WHOLE> __host__ __device__ constexpr int eight_room() { return (F32 ? 1024 : 512) + (WHOLE ? 0 : 16); }
+// whether row t of bf16 begins between two words
+__device__ __forceinline__ int between(const Rows &r, int64_t t) { return (int)((reinterpret_cast<uintptr_t>(r.p) >> 1) + t * r.ld) & 1; }
+
+struct WarpEight {
+    int lane, col, cnt;                      // the warp's first column; the lane's entries, 0 to 8
+    __device__ __forceinline__ int mine() const { return col + lane * 8; }
+};
+// the warp's eights of row t, columns from w.col on, towards shared memory at `to`
+template <bool F32>
+__device__ __forceinline__ void row_ahead(const Rows &r, int64_t t, const WarpEight &w, int n, uint8_t *to) {
+    const uint8_t *row = static_cast<const uint8_t *>(row_at<F32>(r, t));
+    if (r.aligned) {
+        const uint8_t *p = row + (int64_t)w.mine() * (F32 ? 4 : 2);
+        uint4 *at = reinterpret_cast<uint4 *>(to + w.lane * (F32 ? 32 : 16));
+        if (w.cnt == 8) {
+            copy_ahead(at, p);
+            if (F32) copy_ahead(at + 1, p + 16);
+        } else if (w.cnt) {
+            uint4 a, b;
+            load_raw<F32>(row, w.mine(), n, false, a, b);
+            at[0] = a;
+            if (F32) at[1] = b;
+        }
+        return;
+    }
+    const int here = min(256, n - w.col);    // entries of the warp
+    if (here <= 0) return;
+    if (F32) {
+        const uint8_t *p = row + (int64_t)w.col * 4;
+#pragma unroll
+        for (int i = w.lane; i < 256; i += 32)
+            if (i < here) copy_word_ahead(to + i * 4, p + i * 4);
+        return;
+    }
+    // entry e of the words is the row's w.col + e - odd
+    const int odd = between(r, t), first = w.col ? 0 : odd, end = n - w.col + odd;
+    const uint8_t *p = row + (int64_t)w.col * 2 - 2 * odd;
+    for (int i = w.lane; 2 * i < here + odd; i += 32) {
+        const int e = 2 * i;
+        if (e >= first && e + 1 < end) copy_word_ahead(to + i * 4, p + i * 4);
+        else if (e >= first) reinterpret_cast<uint16_t *>(to)[e] = reinterpret_cast<const uint16_t *>(p)[e];
+        else if (e + 1 < end) reinterpret_cast<uint16_t *>(to)[e + 1] = reinterpret_cast<const uint16_t *>(p)[e + 1];
+    }
+}
+// the lane's eight, zeros behind the row's end
+template <bool F32, bool WHOLE>
+__device__ __forceinline__ void row_here(const Rows &r, int64_t t, const WarpEight &w, const uint8_t *at, f32x2 v[4]) {
+    if (F32) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(at + w.lane * (WHOLE ? 16 : 32));
+        pairs_of_eight(p[0], p[WHOLE ? 32 : 1], v);
+    } else {
+        uint4 q = *reinterpret_cast<const uint4 *>(at + w.lane * 16);
+        if (!WHOLE && !r.aligned && between(r, t)) {
+            const uint32_t next = *reinterpret_cast<const uint32_t *>(at + w.lane * 16 + 16);
+            q = make_uint4(__funnelshift_r(q.x, q.y, 16), __funnelshift_r(q.y, q.z, 16), __funnelshift_r(q.z, q.w, 16), __funnelshift_r(q.w, next, 16));
+        }
+        pairs_of_eight(q, v);
+    }
+    if (!WHOLE && w.cnt < 8) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 x = apart(v[j]);
+            v[j] = pair(2 * j < w.cnt ? x.x : 0.f, 2 * j + 1 < w.cnt ? x.y : 0.f);
+        }
+    }
+}
+// the warp's eights to row t; `room`: 1024 bytes of the warp's shared memory
+template <bool F32>
+__device__ __forceinline__ void row_out(const Rows &r, int64_t t, const WarpEight &w, int n, const f32x2 v[4], uint8_t *room) {
+    void *row = const_cast<void *>(row_at<F32>(r, t));
+    if (r.aligned) {
+        if (w.cnt) store_eight<F32>(row, w.mine(), n, w.cnt == 8, v);
+        return;
+    }
+    const int here = min(256, n - w.col);
+    if (F32) {
+        f32x2 *mine = reinterpret_cast<f32x2 *>(room + w.lane * 32);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mine[j] = v[j];
+        __syncwarp();
+        uint32_t *p = static_cast<uint32_t *>(row) + w.col;
+#pragma unroll
+        for (int i = w.lane; i < 256; i += 32)
+            if (i < here) p[i] = reinterpret_cast<const uint32_t *>(room)[i];
+    } else {
+        *reinterpret_cast<uint4 *>(room + w.lane * 16) = bf16_eight(v);
+        __syncwarp();
+        const int odd = between(r, t);
+        uint16_t *p = static_cast<uint16_t *>(row) + w.col;
+        const uint16_t *from = reinterpret_cast<const uint16_t *>(room);
+        for (int i = w.lane; i < 129; i += 32) {
+            const int e = 2 * i - odd;       // entries e and e + 1 of the warp's share a word of the row
+            if (e >= 0 && e + 1 < here) *reinterpret_cast<uint32_t *>(p + e) = (uint32_t)from[e] | (uint32_t)from[e + 1] << 16;
+            else if (e >= 0 && e < here) p[e] = from[e];
+            else if (e == -1 && here > 0) p[0] = from[0];
+        }
+    }
+    __syncwarp();
+}
 // ---- dropout ---------------------------------------------------------------------------------
 // Philox 4x32-10 (Salmon, Moraes, Dror, Shaw, 2011): ten rounds of two 32 x 32 -> 64 bit products and their exclusive ors.
 struct Drop {
