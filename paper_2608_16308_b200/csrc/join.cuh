@@ -12,7 +12,7 @@
 // fixed order.  With a shared gate g and weight w both gradients follow from one sum: A = sum drop(G) xhat gives dw = scale g A and dg = scale (w A + c B), B = sum drop(G).
 #pragma once
 
-#include <cooperative_groups.h>
+#include <type_traits>
 
 #include "rows.cuh"
 
@@ -67,16 +67,35 @@ __device__ __forceinline__ void row_out(uint8_t *mine, uint32_t stride, uint32_t
 __device__ __forceinline__ float vector_one(const void *p, bool f32, int i) {
     return f32 ? static_cast<const float *>(p)[i] : __uint_as_float((uint32_t) static_cast<const uint16_t *>(p)[i] << 16);
 }
-// Eight entries of a vector of parameters as they lie.  (Those of all vectors are loaded before the first is used: a short call waits for them once.)
+// Eight entries each of K vectors of parameters as they lie, of SIDE eights.  All loads stand side by side, without a branch between them: a short call waits for memory once.
 struct Eight {
     uint4 a, b;
 };
-__device__ __forceinline__ Eight vector_eight(const void *p, bool f32, int col, int n) {
-    Eight q = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
-    const bool whole = col + 8 <= n && (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
-    if (p && f32) load_raw<true>(p, col, n, whole, q.a, q.b);
-    else if (p) load_raw<false>(p, col, n, whole, q.a, q.b);
-    return q;
+template <int SIDE, int K>
+__device__ __forceinline__ void vectors_here(const void *(&p)[K], bool f32, const WarpEight *w, int n, Eight (&q)[SIDE][K]) {
+    const void *some = nullptr;              // (in the place of one that is not there)
+    uintptr_t low = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        some = some ? some : p[k];
+        low |= reinterpret_cast<uintptr_t>(p[k]);
+    }
+    if (!some) {
+#pragma unroll
+        for (int i = 0; i < SIDE * K; ++i) q[i / K][i % K] = Eight{make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+        return;
+    }
+    bool whole = (low & 15u) == 0;
+#pragma unroll
+    for (int i = 0; i < SIDE; ++i) whole = whole && w[i].cnt == 8;
+    auto load = [&](auto F32, auto WHOLE) {
+#pragma unroll
+        for (int i = 0; i < SIDE; ++i)
+#pragma unroll
+            for (int k = 0; k < K; ++k) load_raw<decltype(F32)::value>(p[k] ? p[k] : some, w[i].mine(), n, decltype(WHOLE)::value, q[i][k].a, q[i][k].b);
+    };
+    if (f32) whole ? load(std::true_type{}, std::true_type{}) : load(std::true_type{}, std::false_type{});
+    else whole ? load(std::false_type{}, std::true_type{}) : load(std::false_type{}, std::false_type{});
 }
 __device__ __forceinline__ void vector_values(const Eight &q, const void *p, bool f32, float v[8]) {
     if (f32) eight_of(q.a, q.b, v);
@@ -105,9 +124,11 @@ __host__ __device__ inline int join_sums_room(int warps, int cluster) { return w
 struct JoinTeam {
     int lane, warp, warps, team, teams, rank, cluster, room;
     bool alone;                              // a warp has the whole row
+    int last;                                // the last warp of the row with columns; their number, and that of the others
+    float cols_last, inv_last, cols;
     uint32_t turn;                           // sums so far
     float *sums;                             // [buffer][team][2][room]: zeros behind the warps'; then, of a cluster, its barriers
-    __device__ __forceinline__ JoinTeam(const JoinArgs &a, float *s) {
+    __device__ __forceinline__ JoinTeam(const JoinArgs &a, float *s, int columns) {
         lane = threadIdx.x & 31;
         const int w = threadIdx.x >> 5;
         warps = a.warps;
@@ -120,6 +141,10 @@ struct JoinTeam {
         sums = s;
         room = join_sums_room(warps, cluster);
         alone = warps * cluster == 1;
+        last = (a.n - 1) / columns;
+        cols = columns;
+        cols_last = a.n - last * columns;
+        inv_last = 1.f / cols_last;
         for (int i = threadIdx.x; i < 4 * teams * room; i += blockDim.x) s[i] = 0.f;
         if (cluster > 1) {
             if (threadIdx.x < 2) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(barrier(threadIdx.x)) : "memory");
@@ -187,20 +212,16 @@ struct JoinTeam {
         }
     }
     // Mean of the row and the sum of the squared differences from it, from each warp's own: those of its entries from its own mean, and of that mean from the row's (Chan, Golub and LeVeque, 1979).
-    // cols: of a warp; n: of the row
-    __device__ __forceinline__ float2 spread(float sum, float squares, int cols, int n) {
-        const float inv_n = 1.f / n;
+    __device__ __forceinline__ float2 spread(float sum, float squares, float inv_n) {
         if (alone) return make_float2(sum * inv_n, squares);
         const float *s, v[2] = {sum, squares};
         const bool ok = exchange(v, s);
         float mean = 0.f, all = 0.f;
-        for (int i = 0; i < warps * cluster; ++i) mean += s[i];
+        for (int i = 0; i <= last; ++i) mean += s[i];
         mean *= inv_n;
-        for (int i = 0; i < warps * cluster; ++i) {
-            const int has = min(cols, n - i * cols);
-            if (has <= 0) break;
-            const float d = s[i] / has - mean;
-            all += s[room + i] + has * d * d;
+        for (int i = 0; i <= last; ++i) {
+            const float d = s[i] * (i < last ? 1.f / cols : inv_last) - mean;
+            all += s[room + i] + (i < last ? cols : cols_last) * d * d;
         }
         return ok ? make_float2(mean, all) : make_float2(__uint_as_float(0x7FC00000u), 0.f);
     }
@@ -208,7 +229,7 @@ struct JoinTeam {
 
 // mean and 1 / deviation of the row whose entries the threads hold (zeros behind its end)
 template <int E, bool WHOLE>
-__device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4], const WarpEight (&w)[E], int n, int norm, float eps, float inv_n) {
+__device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4], const WarpEight (&w)[E], int norm, float eps, float inv_n) {
     float s[1];
     f32x2 p[2] = {0, 0};
     if (norm == DBSPMSPV_NORM_RMS) {
@@ -228,8 +249,8 @@ __device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4
     s[0] = sum2(add2(p[0], p[1]));
     JoinTeam::add_warp(s);
     const float sum = s[0];
-    const int has = min(256 * E, n - w[0].col);
-    const f32x2 minus = both(has > 0 ? -sum / has : 0.f);
+    const int place = w[0].col / (256 * E);
+    const f32x2 minus = both(-sum * (place < tm.last ? 1.f / (256 * E) : place == tm.last ? tm.inv_last : 0.f));
     s[0] = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -247,7 +268,7 @@ __device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4
         s[0] += WHOLE && cnt == 0 ? 0.f : sum2(q);                           // (zeros behind the row's end have no difference from the mean)
     }
     JoinTeam::add_warp(s);
-    const float2 all = tm.spread(sum, s[0], 256 * E, n);
+    const float2 all = tm.spread(sum, s[0], inv_n);
     return make_float2(all.x, rsqrtf(all.y * inv_n + eps));
 }
 
@@ -303,7 +324,7 @@ __global__ void __launch_bounds__(join_cta(false), E == 1 ? 4 : 3) k_join(const 
     constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, PARAMS = BIAS ? 8 : 4;
     // where a lane's eights of r, b and the gate lie in a row's shared memory
     constexpr int AT_R = 0, AT_B = E * eight_room<SF32, WHOLE>(), AT_G = AT_B + E * eight_room<BF32, WHOLE>();
-    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, PARAMS, WHOLE) * (blockDim.x >> 5)));
+    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, PARAMS, WHOLE) * (blockDim.x >> 5)), 256 * E);
     const JoinWarp<E, WHOLE> me(a, s_dyn, tm);
     const int n = a.n;
     pdl_wait();
@@ -338,25 +359,22 @@ __global__ void __launch_bounds__(join_cta(false), E == 1 ? 4 : 3) k_join(const 
     constexpr int SIDE = BIAS ? 1 : E;
 #pragma unroll
     for (int e0 = 0; e0 < E; e0 += SIDE) {
-        Eight wb[SIDE], wn[SIDE], gv[SIDE], cb[SIDE], cn[SIDE];
-#pragma unroll
-        for (int i = 0; i < SIDE; ++i) {
-            const int col = me.w[e0 + i].mine();
-            wb[i] = vector_eight(a.w_block, a.params_f32, col, n);
-            wn[i] = vector_eight(a.w_next, a.params_f32, col, n);
-            gv[i] = vector_eight(a.gate_vec, a.params_f32, col, n);
-            if (BIAS) cb[i] = vector_eight(a.c_block, a.params_f32, col, n);
-            if (BIAS) cn[i] = vector_eight(a.c_next, a.params_f32, col, n);
+        const void *given[BIAS ? 5 : 3] = {a.w_block, a.w_next, a.gate_vec};
+        if constexpr (BIAS) {
+            given[3] = a.c_block;
+            given[4] = a.c_next;
         }
+        Eight q[SIDE][BIAS ? 5 : 3];
+        vectors_here(given, a.params_f32, me.w + e0, n, q);
 #pragma unroll
         for (int i = 0; i < SIDE; ++i) {
             const int e = e0 + i, col = me.w[e].mine();
             cols[e] = columns_of(num, (uint32_t)col >> 3);
-            columns_here(me.factor(e, PARAMS, 0), col, n, a.params_f32, scale, wb[i], a.w_block, gv[i], a.gate_vec);
-            columns_here(me.factor(e, PARAMS, 2), col, n, a.params_f32, 1.f, wn[i], a.w_next, wn[i], nullptr);
-            if (BIAS) {
-                columns_here(me.factor(e, PARAMS, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, cb[i], a.c_block, gv[i], a.gate_vec);
-                columns_here(me.factor(e, PARAMS, 6), col, n, a.params_f32, a.c_next ? 1.f : 0.f, cn[i], a.c_next, cn[i], nullptr);
+            columns_here(me.factor(e, PARAMS, 0), col, n, a.params_f32, scale, q[i][0], a.w_block, q[i][2], a.gate_vec);
+            columns_here(me.factor(e, PARAMS, 2), col, n, a.params_f32, 1.f, q[i][1], a.w_next, q[i][1], nullptr);
+            if constexpr (BIAS) {
+                columns_here(me.factor(e, PARAMS, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, q[i][3], a.c_block, q[i][2], a.gate_vec);
+                columns_here(me.factor(e, PARAMS, 6), col, n, a.params_f32, a.c_next ? 1.f : 0.f, q[i][4], a.c_next, q[i][4], nullptr);
             }
         }
     }
@@ -369,7 +387,7 @@ __global__ void __launch_bounds__(join_cta(false), E == 1 ? 4 : 3) k_join(const 
         if (WHOLE || a.b.p) {
 #pragma unroll
             for (int e = 0; e < E; ++e) row_here<BF32, WHOLE>(a.b, t, me.w[e], at + AT_B + e * eight_room<BF32, WHOLE>(), v[e]);
-            sb = norm_stats<E, WHOLE>(tm, v, me.w, n, a.norm_block, a.eps_block, a.inv_n);
+            sb = norm_stats<E, WHOLE>(tm, v, me.w, a.norm_block, a.eps_block, a.inv_n);
             const f32x2 inv = both(sb.y), shift = both(-sb.x * sb.y);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -412,7 +430,7 @@ __global__ void __launch_bounds__(join_cta(false), E == 1 ? 4 : 3) k_join(const 
             } else if (a.out.p) row_out<SF32>(a.out, t, me.w[e], n, x[e], me.spare);
         }
         if (!WHOLE && !a.h.p && !a.stats) continue;
-        const float2 sn = norm_stats<E, WHOLE>(tm, x, me.w, n, a.norm_next, a.eps_next, a.inv_n);
+        const float2 sn = norm_stats<E, WHOLE>(tm, x, me.w, a.norm_next, a.eps_next, a.inv_n);
         if (a.stats && tm.rank == 0 && tm.warp == 0 && tm.lane == 0) reinterpret_cast<float4 *>(a.stats)[t] = make_float4(sb.x, sb.y, sn.x, sn.y);
         if (!WHOLE && !a.h.p) continue;
         const f32x2 inv = both(sn.y), shift = both(-sn.x * sn.y);
@@ -440,7 +458,7 @@ __global__ void __launch_bounds__(join_cta(BIAS), BIAS ? 1 : 2) k_join_backward(
     constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, SUMS = BIAS ? 4 : 2;
     constexpr int S8 = eight_room<SF32, WHOLE>(), B8 = eight_room<BF32, WHOLE>(), H8 = eight_room<false, WHOLE>();
     constexpr int AT_DOUT = E * H8, AT_OUT = AT_DOUT + E * S8, AT_B = AT_OUT + E * S8, AT_G = AT_B + E * B8;
-    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, a.params, WHOLE) * (blockDim.x >> 5)));
+    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, a.params, WHOLE) * (blockDim.x >> 5)), 256 * E);
     const JoinWarp<E, WHOLE> me(a, s_dyn, tm);
     const int n = a.n;
     pdl_wait();
@@ -477,22 +495,18 @@ __global__ void __launch_bounds__(join_cta(BIAS), BIAS ? 1 : 2) k_join_backward(
     const float scale = a.drop.random ? a.scale * a.drop.scale : a.scale;
     Columns cols[E];
     f32x2 sum[SUMS][E][4];
-    Eight wb[E], wn[E], gv[E], cb[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int col = me.w[e].mine();
-        wb[e] = vector_eight(a.w_block, a.params_f32, col, n);
-        wn[e] = vector_eight(a.w_next, a.params_f32, col, n);
-        gv[e] = vector_eight(a.gate_vec, a.params_f32, col, n);
-        if (GATES) cb[e] = vector_eight(a.c_block, a.params_f32, col, n);
-    }
+    const void *given[GATES ? 4 : 3] = {a.w_block, a.w_next, a.gate_vec};
+    if constexpr (GATES) given[3] = a.c_block;
+    Eight q[E][GATES ? 4 : 3];
+    vectors_here(given, a.params_f32, me.w, n, q);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int col = me.w[e].mine();
         cols[e] = columns_of(num, (uint32_t)col >> 3);
-        columns_here(me.factor(e, a.params, 0), col, n, a.params_f32, 1.f, wn[e], a.w_next, wn[e], nullptr);
-        columns_here(me.factor(e, a.params, 2), col, n, a.params_f32, scale, wb[e], a.w_block, gv[e], a.gate_vec);
-        if (GATES && a.dgate.p) columns_here(me.factor(e, a.params, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, cb[e], a.c_block, cb[e], nullptr);
+        columns_here(me.factor(e, a.params, 0), col, n, a.params_f32, 1.f, q[e][1], a.w_next, q[e][1], nullptr);
+        columns_here(me.factor(e, a.params, 2), col, n, a.params_f32, scale, q[e][0], a.w_block, q[e][2], a.gate_vec);
+        if constexpr (GATES)
+            if (a.dgate.p) columns_here(me.factor(e, a.params, 4), col, n, a.params_f32, a.c_block ? scale : 0.f, q[e][3], a.c_block, q[e][3], nullptr);
 #pragma unroll
         for (int k = 0; k < SUMS; ++k)
 #pragma unroll
