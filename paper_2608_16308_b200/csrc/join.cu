@@ -29,7 +29,7 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
     if (!on_current_device(r ? r : b, dev) || !on_current_device(out ? out : h, dev)) return DBSPMSPV_ERR_INVALID_ARG;
     const bool bias = (b && c_block) || c_next, rows = b && gate && ldg;
     const Rows R = rows_of(r, ldr, o->stream_f32), BR = rows_of(b, ldb, o->block_f32), OUT = rows_of(out, ldo, o->stream_f32), H = rows_of(h, ldh, false), G = rows_of(rows ? gate : nullptr, ldg, o->params_f32);
-    const bool whole = all_whole(n, R, BR, OUT, H) && (!rows || G.aligned);
+    const bool all = r && b && out && h, whole = all_whole(n, R, BR, OUT, H) && (!rows || (all && G.aligned));
     const int params = bias ? 8 : 4, eights = join_eights(sms, tokens, n, false);
     const int room = eights * (eight_bytes(o->stream_f32, whole) + eight_bytes(o->block_f32, whole) + (rows ? eight_bytes(o->params_f32, false) : 0));
     const JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, false, bias);
@@ -43,9 +43,19 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
     }
     a.w_next = w_next; a.c_next = c_next; a.stats = stats;
     if (!b) a.norm_block = DBSPMSPV_NORM_NONE;
-    auto kernel = by_types(o, whole, rows, [&](auto S, auto BL, auto W, auto GA) {
-        constexpr bool s = decltype(S)::value, l = decltype(BL)::value, w = decltype(W)::value, g = decltype(GA)::value;
-        return eights == 2 ? (bias ? k_join<s, l, 2, true, w, g> : k_join<s, l, 2, false, w, g>) : (bias ? k_join<s, l, 1, true, w, g> : k_join<s, l, 1, false, w, g>);
+    auto kernel = by_types(o, [&](auto S, auto BL) {
+        constexpr bool s = decltype(S)::value, l = decltype(BL)::value;
+        auto form = [&](auto F, auto GA) {
+            constexpr int f = decltype(F)::value;
+            constexpr bool g = decltype(GA)::value;
+            return eights == 2 ? (bias ? k_join<s, l, 2, true, f, g> : k_join<s, l, 2, false, f, g>) : (bias ? k_join<s, l, 1, true, f, g> : k_join<s, l, 1, false, f, g>);
+        };
+        using Any = std::integral_constant<int, JOIN_ANY>;
+        using Whole = std::integral_constant<int, JOIN_WHOLE>;
+        using All = std::integral_constant<int, JOIN_ALL>;
+        if (!whole) return rows ? form(Any{}, std::true_type{}) : form(Any{}, std::false_type{});
+        if (!all) return form(Whole{}, std::false_type{});
+        return rows ? form(All{}, std::true_type{}) : form(All{}, std::false_type{});
     });
     return launch_rows(dev, kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, room, params, whole), static_cast<cudaStream_t>(stream), a);
 }

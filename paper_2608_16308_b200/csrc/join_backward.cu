@@ -48,7 +48,7 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
     const Rows DH = rows_of(dh, lddh, false), DOUT = rows_of(dout, lddo, o->stream_f32), DR = rows_of(dr, lddr, o->stream_f32), OUT = rows_of(nn && dh ? out : nullptr, ldo, o->stream_f32);
     const Rows BR = rows_of(block && (nb || dgate) ? b : nullptr, ldb, o->block_f32), DB = rows_of(db, lddb, o->dblock_f32);
     const Rows G = rows_of(gates ? gate : nullptr, ldg, o->params_f32), DG = rows_of(gates ? dgate : nullptr, lddg, o->params_f32);
-    const bool whole = all_whole(n, DH, DOUT, DR, OUT, DB) && (!BR.p || all_whole(n, BR)) && (!gates || (G.aligned && DG.aligned));
+    const bool whole = dh && dout && dr && db && nn && all_whole(n, DH, DOUT, DR, OUT, BR, DB) && (!gates || (G.aligned && DG.aligned));
     const int params = gates && dgate ? 6 : 4, eights = join_eights(sms, tokens, n, bias);
     const int room = eights * (eight_bytes(false, whole) + 2 * eight_bytes(o->stream_f32, whole) + eight_bytes(o->block_f32, whole) + (gates ? eight_bytes(o->params_f32, false) : 0));
     const JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, true, bias);
@@ -62,9 +62,15 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
     a.w_next = w_next; a.stats = const_cast<float *>(stats);
     a.parts = sums ? static_cast<float *>(workspace) : nullptr;
     a.ldp = ceil64(n, 8) * 8;
-    auto kernel = by_types(o, whole, gates, [&](auto S, auto BL, auto W, auto GA) {
-        constexpr bool s = decltype(S)::value, l = decltype(BL)::value, w = decltype(W)::value, g = decltype(GA)::value;
-        return bias ? k_join_backward<s, l, 1, true, w, g> : eights == 2 ? k_join_backward<s, l, 2, false, w, g> : k_join_backward<s, l, 1, false, w, g>;
+    auto kernel = by_types(o, [&](auto S, auto BL) {
+        constexpr bool s = decltype(S)::value, l = decltype(BL)::value;
+        auto form = [&](auto W, auto GA) {
+            constexpr bool w = decltype(W)::value, g = decltype(GA)::value;
+            return bias ? k_join_backward<s, l, 1, true, w, g> : eights == 2 ? k_join_backward<s, l, 2, false, w, g> : k_join_backward<s, l, 1, false, w, g>;
+        };
+        using T = std::true_type;
+        using N = std::false_type;
+        return whole ? (gates ? form(T{}, T{}) : form(T{}, N{})) : (gates ? form(N{}, T{}) : form(N{}, N{}));
     });
     s = launch_rows(dev, kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, room, params, whole), st, a);
     if (s != DBSPMSPV_OK || !sums) return s;

@@ -36,8 +36,8 @@ inline int join_eights(int sms, int64_t tokens, int64_t n, bool sums_of_biases) 
     if (sums_of_biases || n <= 1024) return 1;
     return n > 2048 || (4 * n >= 3 * (ceil64(n, 512) * 512) && tokens > 2 * sms) ? 2 : 1;
 }
-// whether every row is whole eights on 16 bytes (and its place one product of 32 bits)
-template <typename... R> inline bool all_whole(int64_t n, const R &...r) { return n % 8 == 0 && ((r.p && r.aligned && r.ld * (r.f32 ? 4 : 2) <= (int64_t)UINT32_MAX) && ...); }
+// whether every row of what is there is whole eights on 16 bytes (and its place one product of 32 bits)
+template <typename... R> inline bool all_whole(int64_t n, const R &...r) { return n % 8 == 0 && ((!r.p || (r.aligned && r.ld * (r.f32 ? 4 : 2) <= (int64_t)UINT32_MAX)) && ...); }
 inline bool norm_ok(int norm) { return norm >= DBSPMSPV_NORM_NONE && norm <= DBSPMSPV_NORM_LAYER; }
 inline bool opts_ok(const dbspmspv_join_opts *o) {
     return o && norm_ok(o->norm_block) && norm_ok(o->norm_next) && o->eps_block >= 0.f && o->eps_next >= 0.f && isfinite(o->eps_block) && isfinite(o->eps_next) && isfinite(o->scale) &&
@@ -64,12 +64,11 @@ inline int64_t join_room(int sms, int64_t tokens, int64_t n) {
     }
     return most * 4 * ceil64(n, 8) * 8 * 4;
 }
-// A kernel for the options that are known when it is compiled: f(stream in fp32, block in fp32, whole eights, gate rows)
-template <typename F> inline auto by_types(const dbspmspv_join_opts *o, bool whole, bool gates, F f) {
+// A kernel for the types that are known when it is compiled: f(stream in fp32, block in fp32)
+template <typename F> inline auto by_types(const dbspmspv_join_opts *o, F f) {
     using T = std::true_type;
     using N = std::false_type;
-    auto types = [&](auto W, auto G) { return o->stream_f32 ? (o->block_f32 ? f(T{}, T{}, W, G) : f(T{}, N{}, W, G)) : (o->block_f32 ? f(N{}, T{}, W, G) : f(N{}, N{}, W, G)); };
-    return whole ? (gates ? types(T{}, T{}) : types(T{}, N{})) : (gates ? types(N{}, T{}) : types(N{}, N{}));
+    return o->stream_f32 ? (o->block_f32 ? f(T{}, T{}) : f(T{}, N{})) : (o->block_f32 ? f(N{}, T{}) : f(N{}, N{}));
 }
 
 }  // namespace dbs
