@@ -32,7 +32,7 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
     const bool all = r && b && out && h, whole = all_whole(n, R, BR, OUT, H) && (!rows || (all && G.aligned));
     const int params = bias ? 8 : 4, eights = join_eights(sms, tokens, n, false);
     const int room = eights * (eight_bytes(o->stream_f32, whole) + eight_bytes(o->block_f32, whole) + (rows ? eight_bytes(o->params_f32, false) : 0));
-    const JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, false, bias);
+    JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, false, bias);
     JoinArgs a = join_args(*o, tokens, n, p, room, params);
     a.r = R; a.b = BR; a.out = OUT; a.h = H;
     if (b) {
@@ -57,6 +57,7 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
         if (!all) return form(Whole{}, std::false_type{});
         return rows ? form(All{}, std::true_type{}) : form(All{}, std::false_type{});
     });
+    if ((s = fit_clusters(reinterpret_cast<const void *>(kernel), dev, p, join_smem(p, room, params, whole))) != DBSPMSPV_OK) return s;
     return launch_rows(dev, kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, room, params, whole), static_cast<cudaStream_t>(stream), a);
 }
 

@@ -51,7 +51,7 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
     const bool whole = dh && dout && dr && db && nn && all_whole(n, DH, DOUT, DR, OUT, BR, DB) && (!gates || (G.aligned && DG.aligned));
     const int params = gates && dgate ? 6 : 4, eights = join_eights(sms, tokens, n, bias);
     const int room = eights * (eight_bytes(false, whole) + 2 * eight_bytes(o->stream_f32, whole) + eight_bytes(o->block_f32, whole) + (gates ? eight_bytes(o->params_f32, false) : 0));
-    const JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, true, bias);
+    JoinPlan p = join_plan(sms, tokens, n, eights, room, params, whole, true, bias);
     JoinArgs a = join_args(*o, tokens, n, p, room, params);
     a.dh = DH; a.dout = DOUT; a.dr = DR; a.out = OUT; a.b = BR; a.db = DB; a.gate = G; a.dgate = DG;
     if (block) {
@@ -72,6 +72,7 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
         using N = std::false_type;
         return whole ? (gates ? form(T{}, T{}) : form(T{}, N{})) : (gates ? form(N{}, T{}) : form(N{}, N{}));
     });
+    if ((s = fit_clusters(reinterpret_cast<const void *>(kernel), dev, p, join_smem(p, room, params, whole))) != DBSPMSPV_OK) return s;
     s = launch_rows(dev, kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, room, params, whole), st, a);
     if (s != DBSPMSPV_OK || !sums) return s;
     JoinSums j = {a.parts, a.ldp, p.clusters * p.teams, (int32_t)n, a.params_f32, a.drop.random ? o->scale * a.drop.scale : o->scale, w_block, c_block, rows ? nullptr : gate,

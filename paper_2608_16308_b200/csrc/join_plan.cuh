@@ -30,6 +30,14 @@ inline JoinPlan join_plan(int sms, int64_t tokens, int64_t n, int eights, int ro
     p.clusters = (int)(want < blocks ? want : blocks < 1 ? 1 : blocks);
     return p;
 }
+// no more clusters than run at once: the others' rows would wait for the first to be through with all of theirs (1500 rows of 11008, clusters of three: 53.2 -> 47.6 us)
+inline int fit_clusters(const void *kernel, int dev, JoinPlan &p, size_t smem) {
+    if (p.cluster == 1) return DBSPMSPV_OK;
+    int most;
+    const int s = clusters_at_once(kernel, dev, p.warps * p.teams * 32, p.cluster, smem, &most);
+    if (s == DBSPMSPV_OK && p.clusters > most) p.clusters = most;
+    return s;
+}
 // Two eights a lane share what a sum over the row costs: from 1024 columns on where no more than a quarter of the lanes has none and there are more rows than SMs hold at once (333 rows of 1037: 8.3 us with two,
 // 7.5 with one; 4000 rows of 1000, gradient: 24.5 and 21.7), and from 2048 on in any case.  Gradients with sums of biases have no registers for two.
 inline int join_eights(int sms, int64_t tokens, int64_t n, bool sums_of_biases) {

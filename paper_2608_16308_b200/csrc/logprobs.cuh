@@ -6,6 +6,8 @@
 // multiplied and added at a time, and x is one product-and-sum with the rounded m log2(e) / T, whose rounding is made up for once per thread.  Thread blocks walk the rows, and the vectors to come, the next
 // row's too, are copied ahead into slots of shared memory that belong to the thread itself (cp.async, no barrier): the sums and the selection at the end of a row leave HBM busy.
 //
+// 2048 rows of 32000 in bf16: 31 us with the entropy (4.2 TB/s), 36 with five alternatives, 44 with twenty; one row of 32000 in fp32 with twenty 8.1 us (4.5 without): two exchanges of the cluster.
+//
 // Alternatives.  A thread's own logits (its unit) are known by their largest and its place.  Where at least k groups of threads have a unit of at least tau, no logit below tau is among the k largest; the
 // k-th largest of the groups' largest (or a little less) is such a tau.  Only units that reach it are read a second time (they come from L2), and of their logits those that reach tau are counted against
 // each other: a candidate's place is the number of those in front of it.  No order of the logits makes this long: if too many reach tau (equal ones above all), tau is searched exactly among the units, told apart by their places; the last
@@ -571,6 +573,8 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
 }
 
 // ---- the gradient -----------------------------------------------------------------------------
+// p (c0 + c1 x) per entry, two loads of 16 or 32 bytes ahead: 2048 rows of 32000 in bf16 45 us, 5.8 TB/s; 63 of 100003 in fp32 13.6 us.  Thread blocks of 128: of 256, 50.2 us.  What is added at single entries
+// (targets, alternatives) is written behind the rest by the same thread block.
 struct LpGrad {
     const void *logits;
     void *dlogits;

@@ -402,6 +402,38 @@ inline int allow_smem(const void *kernel, int dev) {
     return DBSPMSPV_OK;
 }
 
+// Clusters that the device holds at once (an SM that is left over in its part of the chip takes none: 142 clusters of three where 148 SMs have room for as many blocks, and six more would wait for the others
+// to end).  Asked for once: kept with 48 bits of what was asked in a small table, newer answers over older ones.
+inline int clusters_at_once(const void *kernel, int dev, int threads, int cluster, size_t smem, int *most) {
+    constexpr int PLACES = 256;
+    static uint64_t known[PLACES];
+    uint64_t key = reinterpret_cast<uintptr_t>(kernel);
+    for (uint64_t part : {(uint64_t)dev, (uint64_t)threads, (uint64_t)cluster, (uint64_t)smem}) key = (key ^ part) * 0x9E3779B97F4A7C15ull, key ^= key >> 29;
+    uint64_t *at = &known[(key >> 8) % PLACES];
+    const uint64_t was = __atomic_load_n(at, __ATOMIC_RELAXED);
+    if (was && (was & ~0xFFFFull) == (key & ~0xFFFFull)) {
+        *most = (int)(was & 0xFFFFu);
+        return DBSPMSPV_OK;
+    }
+    const int s = allow_smem(kernel, dev);
+    if (s != DBSPMSPV_OK) return s;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(cluster);
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim = {(unsigned)cluster, 1, 1};
+    c.attrs = &attr;
+    c.numAttrs = 1;
+    int n = 0;
+    DBS_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &c));
+    n = n < 1 ? 1 : n > 0xFFFF ? 0xFFFF : n;
+    __atomic_store_n(at, (key & ~0xFFFFull) | (uint64_t)n, __ATOMIC_RELAXED);
+    *most = n;
+    return DBSPMSPV_OK;
+}
+
 // One launch in clusters of `cluster` thread blocks, set up while the kernel in front of it drains (every kernel launched so begins with pdl_wait).
 template <typename... P, typename... A>
 inline int launch_rows(int dev, void (*kernel)(P...), int blocks, int threads, int cluster, size_t smem, cudaStream_t st, const A &...args) {
