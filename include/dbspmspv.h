@@ -437,6 +437,7 @@ int dbspmspv_dropout(const void *x, int64_t ldx, int f32, int32_t tokens, int64_
 
 /*
  * Log probabilities of the rows of `logits` (tokens x vocab, bf16 or fp32) with z = logits / temperature: one pass over the logits.
+ *   temperature  above 0, and not so small that 1.45 / temperature is past fp32's largest number
  *   targets    a token id for every row, or NULL.  Negative: the row has none (its logprob is 0).  vocab or more: its logprob is NaN.
  *   logprob    out: z[target] - log(sum exp(z)), or NULL;   entropy  out: -sum p log p, or NULL
  *   stats      out, for the gradient: two fp32 a token, the largest logit M and log(sum exp((logits - M) / temperature)), or NULL

@@ -7,6 +7,9 @@
 
 namespace dbs {
 
+// temperatures whose inverse, times log2(e), fp32 holds
+static bool temperature_ok(float t) { return t > 0.f && isfinite(t) && isfinite((float)(1.4426950408889634 / (double)t)); }
+
 // ---- dropout ---------------------------------------------------------------------------------
 // Bounded by HBM and, in bf16, by the generator's instructions as well: 2048 x 11008 18.8 us, 4.8 TB/s (15.0 where nothing is dropped; fp32 29.0 us, 6.2 TB/s).
 // A thread takes the same eight columns of DR_ROWS rows, whose loads do not wait for one another; thread blocks are as wide as the rows, if these are narrow.
@@ -115,7 +118,7 @@ int dbspmspv_dropout(const void *x, int64_t ldx, int f32, int32_t tokens, int64_
 int dbspmspv_logprobs(const void *logits, int64_t ldl, int logits_f32, int32_t tokens, int32_t vocab, float temperature, const int32_t *targets, float *logprob, float *entropy, float *stats,
                       int32_t top, int32_t *top_ids, float *top_logprobs, dbspmspv_stream_t stream) {
     using namespace dbs;
-    if (tokens < 0 || vocab < 1 || !(temperature > 0.f) || !isfinite(temperature) || top < 0 || top > LP_MAX_TOP || top > vocab || ldl < vocab) return DBSPMSPV_ERR_INVALID_ARG;
+    if (tokens < 0 || vocab < 1 || !temperature_ok(temperature) || top < 0 || top > LP_MAX_TOP || top > vocab || ldl < vocab) return DBSPMSPV_ERR_INVALID_ARG;
     if (tokens > 0 && (!logits || (logprob && !targets) || (top && !top_ids && !top_logprobs))) return DBSPMSPV_ERR_INVALID_ARG;
     if (!on_bytes(logits_f32 ? 4 : 2, logits) || !on_bytes(4, targets, logprob, entropy, top_ids, top_logprobs) || !on_bytes(8, stats)) return DBSPMSPV_ERR_INVALID_ARG;
     if (tokens == 0) return DBSPMSPV_OK;
@@ -136,7 +139,7 @@ int dbspmspv_logprobs_backward(const void *logits, int64_t ldl, int logits_f32, 
                                int32_t top, const int32_t *top_ids, const float *dlogprob, const float *dentropy, const float *dtop, void *dlogits, int64_t ldd, int dlogits_f32,
                                dbspmspv_stream_t stream) {
     using namespace dbs;
-    if (tokens < 0 || vocab < 1 || !(temperature > 0.f) || !isfinite(temperature) || top < 0 || top > LP_MAX_TOP || top > vocab || ldl < vocab || ldd < vocab) return DBSPMSPV_ERR_INVALID_ARG;
+    if (tokens < 0 || vocab < 1 || !temperature_ok(temperature) || top < 0 || top > LP_MAX_TOP || top > vocab || ldl < vocab || ldd < vocab) return DBSPMSPV_ERR_INVALID_ARG;
     if (tokens > 0 && (!logits || !dlogits || !stats || (dlogprob && !targets) || (dentropy && !entropy) || (dtop && (!top || !top_ids)))) return DBSPMSPV_ERR_INVALID_ARG;
     if (!on_bytes(logits_f32 ? 4 : 2, logits) || !on_bytes(dlogits_f32 ? 4 : 2, dlogits) || !on_bytes(4, targets, entropy, top_ids, dlogprob, dentropy, dtop) || !on_bytes(8, stats))
         return DBSPMSPV_ERR_INVALID_ARG;

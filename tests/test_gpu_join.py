@@ -65,19 +65,32 @@ def test_parts_of_a_join(kw):
         j.check()
 
 
-def test_in_place():
-    j = Join(20, 1000, gate="shared", drop=0.1, seed=2)
-    out, e, h, eh, st = j.want()
-    want_r = j.r
+@pytest.mark.parametrize("norms", ["none", "rms"])
+@pytest.mark.parametrize("t,n,pad,lead", [(20, 1000, 0, 0), (700, 1037, 0, 0), (700, 1037, 4, 1), (90, 5001, 0, 3)])
+@pytest.mark.parametrize("stream", [False, True])
+def test_in_place(norms, t, n, pad, lead, stream):
+    """r becomes out, dout becomes dr: rows in words too, whose neighbours' halves a warp writes while another one reads"""
+    kw = dict(block=norms, next=norms, gate="shared", drop=0.1, seed=2, pad=pad, lead=lead, stream=stream)
+    j = Join(t, n, **kw)
+    want = j.want()
     j.forward(out=j.r)
     torch.cuda.synchronize()
-    keep, j.want = j.want, lambda: (out, e, h, eh, st)
+    j.want = lambda: want
     j.check()
-    assert want_r is j.out
-    j = Join(20, 1000, gate="shared", drop=0.1, seed=2)
+    j = Join(t, n, **kw)
     j.backward(in_place=True)
     torch.cuda.synchronize()
     j.check_back()
+
+
+@pytest.mark.parametrize("has_b,has_r,out,h", [(False, True, False, True), (False, True, True, True), (True, False, True, True), (True, True, False, True), (True, True, True, False)])
+@pytest.mark.parametrize("n,pad", [(4096, 0), (520, 0), (521, 0), (11008, 8)])
+def test_what_is_missing(has_b, has_r, out, h, n, pad):
+    for t in (3, 400):
+        j = Join(t, n, gate="shared", drop=0.1, seed=3, pad=pad, has_b=has_b, has_r=has_r)
+        j.forward(want_out=out, h=h)
+        torch.cuda.synchronize()
+        j.check()
 
 
 ALL = ("dr", "db", "dgate", "dw_block", "dc_block", "dw_next", "dc_next")

@@ -48,11 +48,11 @@ REFUSED += [(B.dbspmspv_dropout, DROP, c) for c in (
     dict(tokens=-1), dict(n=0), dict(n=1 << 31, ldx=1 << 32, ldy=1 << 32), dict(drop=-0.5), dict(drop=1.01), dict(drop=float("nan")), dict(ldx=7), dict(ldy=7), dict(x=None), dict(y=None), dict(random=None),
     dict(x=ODD[1:]), dict(y=ODD), dict(random=A[1:]), dict(f32=0, x=ODD))]
 REFUSED += [(B.dbspmspv_logprobs, LOGP, c) for c in (
-    dict(tokens=-1), dict(vocab=0), dict(vocab=-3), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")), dict(top=-1), dict(top=9), dict(vocab=100, ldl=100, top=65, top_ids=A),
+    dict(tokens=-1), dict(vocab=0), dict(vocab=-3), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")), dict(temperature=1e-39), dict(top=-1), dict(top=9), dict(vocab=100, ldl=100, top=65, top_ids=A),
     dict(ldl=7), dict(logits=None), dict(targets=None), dict(top=2), dict(logits=ODD[1:]), dict(logits_f32=0, logits=ODD), dict(targets=ODD), dict(logprob=ODD), dict(entropy=ODD), dict(stats=A[1:]),
     dict(top=1, top_ids=ODD), dict(top=1, top_ids=A, top_logprobs=ODD))]
 REFUSED += [(B.dbspmspv_logprobs_backward, LBACK, c) for c in (
-    dict(tokens=-1), dict(vocab=0), dict(temperature=0.0), dict(top=65, vocab=100, ldl=100, ldd=100), dict(top=9), dict(top=-1), dict(ldl=7), dict(ldd=7), dict(logits=None), dict(dlogits=None), dict(stats=None),
+    dict(tokens=-1), dict(vocab=0), dict(temperature=0.0), dict(temperature=1e-39), dict(top=65, vocab=100, ldl=100, ldd=100), dict(top=9), dict(top=-1), dict(ldl=7), dict(ldd=7), dict(logits=None), dict(dlogits=None), dict(stats=None),
     dict(targets=None), dict(dentropy=A), dict(dtop=A), dict(dtop=A, top=2), dict(logits=ODD), dict(dlogits=ODD[1:]), dict(dlogits_f32=0, dlogits=ODD), dict(stats=A[1:]), dict(dlogprob=ODD))]
 
 
