@@ -175,7 +175,7 @@ template <int LEFT> __device__ __forceinline__ void wait_ahead() { asm volatile(
 // A lane's eight lies at 16 * lane; fp32: the first four there and the others 512 bytes behind (WHOLE), or all at 32 * lane.  What is not WHOLE has 16 bytes more: rows that begin between two words.
 template <bool F32, bool WHOLE> __host__ __device__ constexpr int eight_room() { return (F32 ? 1024 : 512) + (WHOLE ? 0 : 16); }
 // whether row t of bf16 begins between two words
-__device__ __forceinline__ int between(const Rows &r, int64_t t) { return (int)((reinterpret_cast<uintptr_t>(r.p) >> 1) + t * r.ld) & 1; }
+__device__ __forceinline__ int between(const Rows &r, int64_t t) { return ((int)(reinterpret_cast<uintptr_t>(r.p) >> 1) ^ ((int)t & (int)r.ld)) & 1; }
 
 struct WarpEight {
     int lane, col, cnt;                      // the warp's first column; the lane's entries, 0 to 8
@@ -211,6 +211,12 @@ __device__ __forceinline__ void row_ahead(const Rows &r, int64_t t, const WarpEi
     // entry e of the words is the row's w.col + e - odd
     const int odd = between(r, t), first = w.col ? 0 : odd, end = n - w.col + odd;
     const uint8_t *p = row + (int64_t)w.col * 2 - 2 * odd;
+    if (here == 256 && (!odd || (w.col && end > 257))) {                     // (every word is the row's own)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) copy_word_ahead(to + (w.lane + 32 * k) * 4, p + (w.lane + 32 * k) * 4);
+        if (odd && w.lane == 0) copy_word_ahead(to + 512, p + 512);
+        return;
+    }
     for (int i = w.lane; 2 * i < here + odd; i += 32) {
         const int e = 2 * i;
         if (e >= first && e + 1 < end) copy_word_ahead(to + i * 4, p + i * 4);
@@ -264,12 +270,26 @@ __device__ __forceinline__ void row_out(const Rows &r, int64_t t, const WarpEigh
         const int odd = between(r, t);
         uint16_t *p = static_cast<uint16_t *>(row) + w.col;
         const uint16_t *from = reinterpret_cast<const uint16_t *>(room);
-        for (int i = w.lane; i < 129; i += 32) {
-            const int e = 2 * i - odd;       // entries e and e + 1 of the warp's share a word of the row
-            if (e >= 0 && e + 1 < here) *reinterpret_cast<uint32_t *>(p + e) = (uint32_t)from[e] | (uint32_t)from[e + 1] << 16;
-            else if (e >= 0 && e < here) p[e] = from[e];
-            else if (e == -1 && here > 0) p[0] = from[0];
-        }
+        if (here == 256) {
+            const uint32_t *words = reinterpret_cast<const uint32_t *>(room);
+            uint32_t *to = reinterpret_cast<uint32_t *>(p - odd);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = w.lane + 32 * k;
+                if (!odd) to[i] = words[i];
+                else if (i) to[i] = __funnelshift_r(words[i - 1], words[i], 16);
+            }
+            if (odd && w.lane == 0) {
+                p[0] = from[0];
+                p[255] = from[255];
+            }
+        } else
+            for (int i = w.lane; i < 129; i += 32) {
+                const int e = 2 * i - odd;   // entries e and e + 1 of the warp's share a word of the row
+                if (e >= 0 && e + 1 < here) *reinterpret_cast<uint32_t *>(p + e) = (uint32_t)from[e] | (uint32_t)from[e + 1] << 16;
+                else if (e >= 0 && e < here) p[e] = from[e];
+                else if (e == -1 && here > 0) p[0] = from[0];
+            }
     }
     __syncwarp();
 }
