@@ -165,8 +165,8 @@ __device__ __forceinline__ void copy_ahead(void *smem, const void *p) {
 __device__ __forceinline__ void copy_ahead(void *smem, const void *p, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copy_word_ahead(void *smem, const void *p) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
+__device__ __forceinline__ void copy_word_ahead(void *smem, const void *p, uint32_t bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void close_ahead() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void wait_ahead() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
@@ -181,48 +181,42 @@ struct WarpEight {
     int lane, col, cnt;                      // the warp's first column; the lane's entries, 0 to 8
     __device__ __forceinline__ int mine() const { return col + lane * 8; }
 };
-// the warp's eights of row t, columns from w.col on, towards shared memory at `to`
+// The warp's eights of row t, columns from w.col on, towards shared memory at `to`.  Copies say how many bytes they read, so the row's end needs no loads of its own, for which the warp, and then its team, would wait
+// (rows of 4001 bf16, gradient: 163 us with them).  A row that begins between two words is copied from the word's begin: two bytes of what lies in front of it come along, but not in front of row 0.
 template <bool F32>
 __device__ __forceinline__ void row_ahead(const Rows &r, int64_t t, const WarpEight &w, int n, uint8_t *to) {
     const uint8_t *row = static_cast<const uint8_t *>(row_at<F32>(r, t));
+    const int here = min(256, n - w.col);    // entries of the warp
+    if (here <= 0) return;
     if (r.aligned) {
         const uint8_t *p = row + (int64_t)w.mine() * (F32 ? 4 : 2);
-        uint4 *at = reinterpret_cast<uint4 *>(to + w.lane * (F32 ? 32 : 16));
+        uint8_t *at = to + w.lane * (F32 ? 32 : 16);
         if (w.cnt == 8) {
             copy_ahead(at, p);
-            if (F32) copy_ahead(at + 1, p + 16);
+            if (F32) copy_ahead(at + 16, p + 16);
         } else if (w.cnt) {
-            uint4 a, b;
-            load_raw<F32>(row, w.mine(), n, false, a, b);
-            at[0] = a;
-            if (F32) at[1] = b;
+#pragma unroll
+            for (int k = 0; k < (F32 ? 8 : 4); ++k) copy_word_ahead(at + 4 * k, p + 4 * k, max(0, min(4, w.cnt * (F32 ? 4 : 2) - 4 * k)));
         }
         return;
     }
-    const int here = min(256, n - w.col);    // entries of the warp
-    if (here <= 0) return;
     if (F32) {
         const uint8_t *p = row + (int64_t)w.col * 4;
 #pragma unroll
-        for (int i = w.lane; i < 256; i += 32)
-            if (i < here) copy_word_ahead(to + i * 4, p + i * 4);
+        for (int i = w.lane; i < 256; i += 32) copy_word_ahead(to + i * 4, p + i * 4, i < here ? 4 : 0);
         return;
     }
     // entry e of the words is the row's w.col + e - odd
-    const int odd = between(r, t), first = w.col ? 0 : odd, end = n - w.col + odd;
+    const int odd = between(r, t), end = n - w.col + odd;
     const uint8_t *p = row + (int64_t)w.col * 2 - 2 * odd;
-    if (here == 256 && (!odd || (w.col && end > 257))) {                     // (every word is the row's own)
+    const bool front = odd && w.col == 0 && t == 0 && w.lane == 0;
+    if (front) reinterpret_cast<uint16_t *>(to)[1] = *reinterpret_cast<const uint16_t *>(row);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) copy_word_ahead(to + (w.lane + 32 * k) * 4, p + (w.lane + 32 * k) * 4);
-        if (odd && w.lane == 0) copy_word_ahead(to + 512, p + 512);
-        return;
+    for (int k = 0; k < 4; ++k) {
+        const int i = w.lane + 32 * k;
+        if (k || !front) copy_word_ahead(to + i * 4, p + i * 4, max(0, min(4, 2 * (end - 2 * i))));
     }
-    for (int i = w.lane; 2 * i < here + odd; i += 32) {
-        const int e = 2 * i;
-        if (e >= first && e + 1 < end) copy_word_ahead(to + i * 4, p + i * 4);
-        else if (e >= first) reinterpret_cast<uint16_t *>(to)[e] = reinterpret_cast<const uint16_t *>(p)[e];
-        else if (e + 1 < end) reinterpret_cast<uint16_t *>(to)[e + 1] = reinterpret_cast<const uint16_t *>(p)[e + 1];
-    }
+    if (odd && w.lane == 0) copy_word_ahead(to + 512, p + 512, max(0, min(4, 2 * (end - 256))));
 }
 // the lane's eight, zeros behind the row's end
 template <bool F32, bool WHOLE>
