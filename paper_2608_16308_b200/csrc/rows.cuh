@@ -263,27 +263,17 @@ __device__ __forceinline__ void row_out(const Rows &r, int64_t t, const WarpEigh
         __syncwarp();
         const int odd = between(r, t);
         uint16_t *p = static_cast<uint16_t *>(row) + w.col;
+        // word i of the row holds entries 2 i - odd and the next of the warp's share; an entry without a neighbour goes by itself
         const uint16_t *from = reinterpret_cast<const uint16_t *>(room);
-        if (here == 256) {
-            const uint32_t *words = reinterpret_cast<const uint32_t *>(room);
-            uint32_t *to = reinterpret_cast<uint32_t *>(p - odd);
+        const uint32_t *words = reinterpret_cast<const uint32_t *>(room);
+        uint32_t *to = reinterpret_cast<uint32_t *>(p - odd);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int i = w.lane + 32 * k;
-                if (!odd) to[i] = words[i];
-                else if (i) to[i] = __funnelshift_r(words[i - 1], words[i], 16);
-            }
-            if (odd && w.lane == 0) {
-                p[0] = from[0];
-                p[255] = from[255];
-            }
-        } else
-            for (int i = w.lane; i < 129; i += 32) {
-                const int e = 2 * i - odd;   // entries e and e + 1 of the warp's share a word of the row
-                if (e >= 0 && e + 1 < here) *reinterpret_cast<uint32_t *>(p + e) = (uint32_t)from[e] | (uint32_t)from[e + 1] << 16;
-                else if (e >= 0 && e < here) p[e] = from[e];
-                else if (e == -1 && here > 0) p[0] = from[0];
-            }
+        for (int k = 0; k < 4; ++k) {
+            const int i = w.lane + 32 * k, e = 2 * i - odd;
+            if (e >= 0 && e + 1 < here) to[i] = odd ? __funnelshift_r(words[i - 1], words[i], 16) : words[i];
+        }
+        if (here > 0 && odd && w.lane == 0) p[0] = from[0];
+        if (here > 0 && w.lane == 1 && ((here + odd) & 1)) p[here - 1] = from[here - 1];
     }
     __syncwarp();
 }
