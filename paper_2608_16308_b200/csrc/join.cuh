@@ -317,7 +317,8 @@ struct JoinWarp {
     __device__ __forceinline__ uint8_t *mine(const Rows &r) const { return static_cast<uint8_t *>(r.p) + (int64_t)w[0].mine() * (F32 ? 4 : 2); }
 };
 
-// 4096 rows of 4096 in bf16, root mean squares on both sides, a gate, dropout: 29.4 us, 4.57 TB/s (HBM copies 6.46; a third of 444 warp instructions a warp and 256 columns is dropout: 24 us without it and the gate).
+// 4096 rows of 4096 in bf16, root mean squares on both sides, a gate, dropout: 29.4 us, 4.57 TB/s (HBM copies 6.46): 297 warp instructions a warp and 256 columns at 2.1 a clock and SM, a quarter of them the generator's (24 us
+// without dropout and gate).
 // 1, 8 rows: 5.5 us, the calling thread.
 // factors: gate * w_block * scales (or without a gate that has rows), w_next, then (BIAS) c_block * gate * scales, c_next
 // FORM: rows of any kind; whole eights on 16 bytes; those, and r, b, out and h are all there (4096 x 4096 with their tests in the loop 32.8 us, 29.4 without).
@@ -457,7 +458,8 @@ __global__ void __launch_bounds__(join_cta(false), E == 1 ? 4 : 3) k_join(const 
     }
 }
 
-// 4096 rows of 4096 as above: 46.8 us with the sums behind it, 4.3 TB/s; 404 warp instructions a warp and 256 columns at 2.9 a clock and SM from 16 warps, whose registers (128) the sums over tokens take.
+// 4096 rows of 4096 as above: 46.8 us with the sums behind it, 4.3 TB/s; 412 warp instructions a warp and 256 columns at 2.05 a clock and SM from 16 warps, whose registers (128) the
+// sums over tokens take.
 // factors: w_next, gate * w_block * scales (or without a gate that has rows), c_block * scales for the gradient of such a gate.  Sums over a team's tokens: dw_next, A, then (BIAS) dc_next, B.
 template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE, bool GATES>
 __global__ void __launch_bounds__(join_cta(BIAS), BIAS ? 1 : 2) k_join_backward(const __grid_constant__ JoinArgs a) {

