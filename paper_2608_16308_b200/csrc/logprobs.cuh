@@ -179,7 +179,7 @@ struct LpShared {
     int n_units[2], n_found[2];              // of rows in turn
 };
 
-// What the blocks of a cluster tell each other: their sums, their groups' largest, how many candidates they have; and, in the first block, these
+// What the blocks of a cluster tell each other: their sums, their groups' largest, how many candidates they have (written once a row); and, in the first block, these
 struct LpCluster {
     float m[LP_CLUSTER], s[LP_CLUSTER], u[LP_CLUSTER];
     uint32_t groups[LP_CLUSTER_GROUPS];
@@ -545,8 +545,8 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
                 const uint32_t g[2] = {sh.group[parity][lane], sh.group[parity][lane + 32]};
                 lp_top(row, sh, parity, most, lp_least<2>(g, a.top), plain, a.top, a.vocab, [&](uint64_t c, int place) { sh.best[place] = c; });
                 __syncthreads();
+                // (`found` stays as it is: another block may still be reading there that not all candidates fitted)
                 if (tid < LP_MAX_TOP) first->best[rank * LP_MAX_TOP + tid] = tid < a.top ? sh.best[tid] : 0;
-                if (tid < a.cluster) c.map_shared_rank(all, tid)->found[rank] = a.top;
                 asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
             }
         }
@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
             if (a.top) {
                 int n = 0;
                 for (int r = 0; r < a.cluster; ++r) {
-                    const int here = all->found[r];
+                    const int here = ranked ? all->found[r] : a.top;
                     if (tid < here) all->flat[n + tid] = all->best[r * LP_MAX_TOP + tid];
                     n += here;
                 }
