@@ -155,16 +155,16 @@ __device__ __forceinline__ float largest(uint4 q) {
     const uint4 one[1] = {q};
     return largest<F32, 1>(one);
 }
-// a vector's entries two at a time; CLAMP: -inf (and what lies near it) as LP_LOW
+// a vector's entries two at a time; CLAMP: -inf (and what lies below `low`, in bf16 twice `low2`) as `low`
+constexpr uint32_t LP_LOW2 = 0xF14AF14Au;    // LP_LOW in bf16, twice
 template <bool F32, bool CLAMP>
-__device__ __forceinline__ void pairs_of(uint4 q, f32x2 v[F32 ? 2 : 4]) {
+__device__ __forceinline__ void pairs_of(uint4 q, f32x2 v[F32 ? 2 : 4], float low = LP_LOW, uint32_t low2 = LP_LOW2) {
     if constexpr (F32) {
-        auto one = [](uint32_t w) { return CLAMP ? max_nan(__uint_as_float(w), LP_LOW) : __uint_as_float(w); };
+        auto one = [&](uint32_t w) { return CLAMP ? max_nan(__uint_as_float(w), low) : __uint_as_float(w); };
         v[0] = pair(one(q.x), one(q.y));
         v[1] = pair(one(q.z), one(q.w));
     } else {
-        constexpr uint32_t LOW2 = 0xF14AF14Au;                               // -1.0e30 in bf16, twice
-        auto two = [](uint32_t w) { return bf16_pair(CLAMP ? max_nan_bf16(w, LOW2) : w); };
+        auto two = [&](uint32_t w) { return bf16_pair(CLAMP ? max_nan_bf16(w, low2) : w); };
         v[0] = two(q.x); v[1] = two(q.y); v[2] = two(q.z); v[3] = two(q.w);
     }
 }
@@ -670,6 +670,9 @@ __global__ void __launch_bounds__(LG_ROWS_CTA) k_logprobs_backward(const __grid_
     const bool near = short_form(most, a.slope) && short_form(ref, a.slope);
     const float part = ref - most, low = near ? fmaf(st.x, a.slope, -most) + ((most - (ref - part)) + (shift - part)) : 0.f, y = low * LN2;
     const float k = nothing ? 0.f : -a.inv_t * (1.f - y + 0.5f * y * y);
+    // -inf, and whatever else lies 1000 or so below the row's sum in units of log 2, is taken for a logit there: its p is 0, and c1 x of its size is a number that 0 can be multiplied with
+    const float low_logit = near ? (ref + LP_NONE) / a.slope : 0.f;
+    const uint32_t low_two = two_bf16(low_logit, low_logit);
     const f32x2 c0 = both(nothing ? 0.f : k * (given + dh * (h - y))), c1 = both(nothing ? 0.f : k * dh * LN2);
     for (int e0 = from8 + tid; e0 < to8; e0 += LG_ROWS_FLIGHT * LG_ROWS_CTA) {
         uint4 q[LG_ROWS_FLIGHT][F32 ? 2 : 1];
@@ -685,8 +688,8 @@ __global__ void __launch_bounds__(LG_ROWS_CTA) k_logprobs_backward(const __grid_
             float d[8];
             if (near) {
                 f32x2 l[4];
-                pairs_of<F32, true>(q[r][0], l);
-                if (F32) pairs_of<F32, true>(q[r][F32 ? 1 : 0], l + 2);
+                pairs_of<F32, true>(q[r][0], l, low_logit, low_two);
+                if (F32) pairs_of<F32, true>(q[r][F32 ? 1 : 0], l + 2, low_logit, low_two);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const f32x2 x = fma1(l[j], both(a.slope), both(-ref));
