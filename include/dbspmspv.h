@@ -445,7 +445,8 @@ int dbspmspv_dropout(const void *x, int64_t ldx, int f32, int32_t tokens, int64_
  * -inf is a logit like others: probability 0, nothing to the entropy.  A row of them only: logprob and top_logprobs -inf, entropy 0, stats -inf.  A row with a NaN or +inf: logprob, entropy and top_logprobs
  * are NaN (top_ids: NaN before everything else).
  * The gradient: dlogits = (S - p sum(S) - dentropy p (log p + entropy)) / temperature, where S has dlogprob at the target and dtop (tokens x top) at top_ids (negative ones and those of vocab or more
- * take part in nothing; a row whose target is vocab or more becomes NaN where dlogprob is given); zeros for a row with nothing left.  `entropy` and `stats` as the forward call left them.
+ * take part in nothing; an id that is given several times takes all its weights, added in the order of top_ids and the target's last; a row whose target is vocab or more becomes NaN where dlogprob is
+ * given); zeros for a row with nothing left.  `entropy` and `stats` as the forward call left them.
  * dlogprob, dentropy, dtop: fp32, NULL: none.  dlogits: tokens x vocab, bf16 or fp32 (dlogits_f32), in place where it is `logits`.
  */
 int dbspmspv_logprobs(const void *logits, int64_t ldl, int logits_f32, int32_t tokens, int32_t vocab, float temperature, const int32_t *targets, float *logprob, float *entropy, float *stats,

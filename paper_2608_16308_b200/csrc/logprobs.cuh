@@ -648,13 +648,19 @@ __global__ void __launch_bounds__(LG_ROWS_CTA) k_logprobs_backward(const __grid_
         // (this block's own; the ends of the row are the first one's and the last one's)
         const int from = chunk == 0 ? 0 : head + from8 * 8, to = last ? a.vocab : head + to8 * 8;
         if (id < from || id >= to) id = -1;
+        // an id that is given several times belongs to the first thread that has it, which adds the weights up in the order in which they are given (the others' stores would race with its own)
         if (id >= 0) {
             l_mine = one(id);
-            for (int j = 0; j <= a.top; ++j) {
-                int at;
-                const float w = weight(j, at);
-                if (j != tid && at == id) mine += w;
-            }
+            mine = 0.f;
+            bool first = true;
+#pragma unroll 8
+            for (int j = 0; j < a.top; ++j)
+                if (a.top_ids[t * a.top + j] == id) {
+                    first = first && j >= tid;
+                    mine += a.dtop[t * a.top + j];
+                }
+            if (a.dlogprob && a.targets[t] == id) mine += a.dlogprob[t];
+            if (!first) id = -1;
         }
     }
     __syncthreads();
