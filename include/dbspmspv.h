@@ -371,7 +371,9 @@ int dbspmspv_gated_backward(dbspmspv_handle_t gate, dbspmspv_handle_t up, const 
 
 /*
  * What stands between the layers of a network and behind the last one.  (Outside the paper's scope, like the layers above.)  These calls need no handle: they
- * run on the calling thread's current device, whose memory every array has to be (an array of the host or of another device: INVALID_ARG where it is the first input or output of the call).  Rows are
+ * run on the calling thread's current device, whose memory every array has to be, managed memory, or the host's if it is pinned.  An array of the host's other memory or of another device is found out and refused
+ * (INVALID_ARG) where it is the call's first input or the first output that is wanted (the join's gradient: the first that is read of out, b and stats, dh or else dout, and the first output); the others are
+ * the caller's word.  Rows are
  * tokens, ld... entries apart (at least their width; what lies between them is not used and not written); bf16 arrays begin on 2 bytes, fp32 and int32 arrays on 4, `random` on 8.
  * Arithmetic, sums and statistics are fp32; every output is rounded to its type once.  Results do not depend on the order in which thread blocks run.  (A sum's order, and so an output's last bits, may depend on how many tokens a call has.)  A token with an infinity or a NaN spoils its own
  * rows and the sums over tokens, no other row.  No output may overlap an input or another output, except where it says "in place": the same address, stride and type.

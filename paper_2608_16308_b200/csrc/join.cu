@@ -26,7 +26,7 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
     if (tokens == 0) return DBSPMSPV_OK;
     int dev, sms, s;
     if ((s = current_device(&dev, &sms)) != DBSPMSPV_OK) return s;
-    if (!on_current_device(r ? r : b, dev) || !on_current_device(out ? out : h, dev)) return DBSPMSPV_ERR_INVALID_ARG;
+    if (!on_current_device(first_of(r, b), dev) || !on_current_device(first_of(out, h), dev)) return DBSPMSPV_ERR_INVALID_ARG;
     const bool bias = (b && c_block) || c_next, rows = b && gate && ldg;
     const Rows R = rows_of(r, ldr, o->stream_f32), BR = rows_of(b, ldb, o->block_f32), OUT = rows_of(out, ldo, o->stream_f32), H = rows_of(h, ldh, false), G = rows_of(rows ? gate : nullptr, ldg, o->params_f32);
     const bool all = r && b && out && h, whole = all_whole(n, R, BR, OUT, H) && (!rows || (all && G.aligned));

@@ -42,12 +42,14 @@ int dbspmspv_join_backward(const dbspmspv_join_opts *o, int32_t tokens, int64_t 
     }
     int dev, sms, s;
     if ((s = current_device(&dev, &sms)) != DBSPMSPV_OK) return s;
-    if (!on_current_device(dh ? dh : dout, dev) || (dr && !on_current_device(dr, dev))) return DBSPMSPV_ERR_INVALID_ARG;
     if (sums && (!workspace || workspace_bytes < join_room(sms, tokens, n))) return DBSPMSPV_ERR_INVALID_ARG;
     const bool bias = dc_block || dc_next || (dgate && !rows && c_block), gates = rows && block;
     const Rows DH = rows_of(dh, lddh, false), DOUT = rows_of(dout, lddo, o->stream_f32), DR = rows_of(dr, lddr, o->stream_f32), OUT = rows_of(nn && dh ? out : nullptr, ldo, o->stream_f32);
     const Rows BR = rows_of(block && (nb || dgate) ? b : nullptr, ldb, o->block_f32), DB = rows_of(db, lddb, o->dblock_f32);
     const Rows G = rows_of(gates ? gate : nullptr, ldg, o->params_f32), DG = rows_of(gates ? dgate : nullptr, lddg, o->params_f32);
+    const void *kept = first_of(OUT.p, BR.p, stats);
+    if ((kept && !on_current_device(kept, dev)) || !on_current_device(first_of(dh, dout), dev) || !on_current_device(first_of(dr, db, dw_block, dc_block, dgate, dw_next, dc_next), dev))
+        return DBSPMSPV_ERR_INVALID_ARG;
     const bool whole = dh && dout && dr && db && nn && all_whole(n, DH, DOUT, DR, OUT, BR, DB) && (!gates || (G.aligned && DG.aligned));
     const int params = gates && dgate ? 6 : 4, eights = join_eights(sms, tokens, n, bias);
     const int room = eights * (eight_bytes(false, whole) + 2 * eight_bytes(o->stream_f32, whole) + eight_bytes(o->block_f32, whole) + (gates ? eight_bytes(o->params_f32, false) : 0));

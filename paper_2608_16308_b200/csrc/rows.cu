@@ -124,7 +124,8 @@ int dbspmspv_logprobs(const void *logits, int64_t ldl, int logits_f32, int32_t t
     if (tokens == 0) return DBSPMSPV_OK;
     int dev, sms, s;
     if ((s = current_device(&dev, &sms)) != DBSPMSPV_OK) return s;
-    if (!on_current_device(logits, dev)) return DBSPMSPV_ERR_INVALID_ARG;
+    const void *first = first_of(logprob, entropy, stats, top_ids, top_logprobs);
+    if (!on_current_device(logits, dev) || (first && !on_current_device(first, dev))) return DBSPMSPV_ERR_INVALID_ARG;
     LpArgs a = {logits, ldl, tokens, vocab, 1, top, 0, (float)(1.4426950408889634 / (double)temperature), (float)(1.0 / (double)temperature), logprob ? targets : nullptr, logprob, entropy, stats, top_ids, top_logprobs};
     // a row is shared out while there are SMs without one and every block has a vector for each of its threads
     const int64_t vectors = vocab / (logits_f32 ? 4 : 8);

@@ -362,7 +362,13 @@ inline Drop drop_of(float p, const void *random) {
     return Drop{static_cast<const uint64_t *>(random), ((uint32_t)below << 16) - 1u, 65536.f / (65536 - below)};
 }
 
-// Whether `p` is memory that kernels of the current device may use as theirs: not the host's own, not another device's.
+template <typename... P> inline const void *first_of(P... p) {                     // of those that are there
+    const void *all[] = {static_cast<const void *>(p)...};
+    for (const void *q : all)
+        if (q) return q;
+    return nullptr;
+}
+// Whether `p` is memory that kernels of the current device can reach: its own, managed, or the host's if that is pinned; not the host's other memory, not another device's.
 inline bool on_current_device(const void *p, int dev) {
     cudaPointerAttributes a;
     if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
