@@ -377,6 +377,8 @@ int dbspmspv_gated_backward(dbspmspv_handle_t gate, dbspmspv_handle_t up, const 
  * tokens, ld... entries apart (at least their width; what lies between them is not used and not written); bf16 arrays begin on 2 bytes, fp32 and int32 arrays on 4, `random` on 8.
  * Arithmetic, sums and statistics are fp32; every output is rounded to its type once.  Results do not depend on the order in which thread blocks run.  (A sum's order, and so an output's last bits, may depend on how many tokens a call has.)  A token with an infinity or a NaN spoils its own
  * rows and the sums over tokens, no other row.  No output may overlap an input or another output, except where it says "in place": the same address, stride and type.
+ * Rows of a join of more than 4096 columns are shared out to thread blocks that wait for each other's sums.  Should a wait run out (after about two seconds, which only a fault of the machine brings about), there
+ * is no handle to keep a status: the call ends, and that row and the rows behind it in the same thread blocks are NaN in everything that follows from the sums (h, stats, dr, db, the sums over tokens).
  * Asynchronous on `stream`, no memory is allocated, nothing is kept between calls: calls on several streams and captured calls overlap freely, each with its own workspace.
  *
  * Random numbers.  `random` is the address of two 64-bit numbers in DEVICE memory, seed and offset; a program writes a new offset for every call that is to draw new numbers (before the call on its
@@ -552,6 +554,10 @@ int dbspmspv_probe_floor(int kind, const int32_t *chain, int32_t start, int32_t 
  * `max_tries` tries (1 .. 4096, about 2 us each) and the kernel records DBSPMSPV_ERR_TIMEOUT,
  * which the next dbspmspv_get_stats returns.  The context stays usable.                       */
 int dbspmspv_test_bounded_wait(dbspmspv_handle_t h, int32_t max_tries, dbspmspv_stream_t stream);
+
+/* Test hook for the waits of joins of more than 4096 columns: two thread blocks exchange sums four times, and block `silent` (0 or 1; -1: none) sends nothing, so that the other one's wait runs out after
+ * `max_tries` tries (1 .. 4096, about 2 us each).  gave_up (device, two int32): how many of its exchanges each block went without. */
+int dbspmspv_test_cluster_wait(int32_t max_tries, int32_t silent, int32_t *gave_up, dbspmspv_stream_t stream);
 
 /* y<mask> = A x: dbspmspv_run with an output mask (the GraphBLAS form of the primitive; the
  * "strip the visited vertices" step of DB-BFS, Section 4.2, as an option of the call).

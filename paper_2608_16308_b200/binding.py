@@ -38,7 +38,7 @@ EXPORTED_SYMBOLS = (
     "dbspmspv_set_run_opts", "dbspmspv_destroy", "dbspmspv_strerror", "dbspmspv_compact_noalloc",
     "dbspmspv_test_bounded_wait", "dbspmspv_test_corrupt_entry", "dbspmspv_decode_batch", "dbspmspv_run_masked", "dbspmspv_count_call_bytes", "dbspmspv_probe_floor",
     "dbspmspv_linear_workspace", "dbspmspv_linear", "dbspmspv_gated", "dbspmspv_linear_backward", "dbspmspv_gated_backward",
-    "dbspmspv_default_join_opts", "dbspmspv_join_workspace", "dbspmspv_join", "dbspmspv_join_backward", "dbspmspv_dropout", "dbspmspv_logprobs", "dbspmspv_logprobs_backward",
+    "dbspmspv_test_cluster_wait", "dbspmspv_default_join_opts", "dbspmspv_join_workspace", "dbspmspv_join", "dbspmspv_join_backward", "dbspmspv_dropout", "dbspmspv_logprobs", "dbspmspv_logprobs_backward",
 )
 
 
@@ -142,6 +142,7 @@ def lib() -> ctypes.CDLL:
         L.dbspmspv_export_views.argtypes = [vp, vp, vp, vp, vp]
         L.dbspmspv_compact_noalloc.argtypes = [vp, vp, i64, vp, vp, i64, vp, vp]
         L.dbspmspv_test_bounded_wait.argtypes = [vp, i32, vp]
+        L.dbspmspv_test_cluster_wait.argtypes = [i32, i32, vp, vp]
         L.dbspmspv_test_corrupt_entry.argtypes = [vp, i32, ctypes.c_uint32]
         L.dbspmspv_count_call_bytes.argtypes = [vp, vp, i32, ctypes.c_int, ctypes.POINTER(CallBytes)]
         L.dbspmspv_probe_floor.argtypes = [ctypes.c_int, vp, i32, i32, vp, vp]
@@ -338,6 +339,10 @@ def dbspmspv_compact_noalloc(acc, hit_bitmap, m, y_idx, y_val, y_capacity, y_nnz
 def dbspmspv_test_bounded_wait(h, max_tries: int, stream: Optional[int] = None) -> None:
     _check(lib().dbspmspv_test_bounded_wait(h, max_tries, _stream() if stream is None else stream),
            "dbspmspv_test_bounded_wait")
+
+
+def dbspmspv_test_cluster_wait(max_tries: int, silent: int, gave_up, stream: Optional[int] = None) -> None:
+    _check(lib().dbspmspv_test_cluster_wait(max_tries, silent, _ptr(gave_up), _stream() if stream is None else stream), "dbspmspv_test_cluster_wait")
 
 
 def dbspmspv_test_corrupt_entry(h, position: int, block_index: int) -> None:

@@ -1,6 +1,26 @@
 // The join of a block with the residual stream: entry points (kernels: join.cuh; how rows are shared out: join_plan.cuh).  No handle: the current device, and nothing that lasts longer than a call.
 #include "join_plan.cuh"
 
+namespace dbs {
+
+// Two blocks of a cluster exchange numbers a few times; one of them may keep silent.  Counts the exchanges that gave up, and 100 for one that went wrong.
+static __global__ void __launch_bounds__(32) k_join_wait(const __grid_constant__ JoinArgs a, int tries, int silent, int32_t *gave_up) {
+    extern __shared__ __align__(16) uint8_t s_dyn[];
+    pdl_wait();
+    JoinTeam<true> tm(a, reinterpret_cast<float *>(s_dyn), 256);
+    if (tm.rank == silent) tm.give_up();
+    int n = 0;
+    for (int i = 0; i < 4; ++i) {
+        const float *s, v[2] = {(float)(tm.rank + 1), (float)i};
+        if (!tm.exchange(v, s, tries)) ++n;
+        else if (s[0] != 1.f || s[1] != 2.f || s[tm.room] != i || s[tm.room + 1] != i) n += 100;
+        __syncwarp();
+    }
+    if (tm.lane == 0) gave_up[tm.rank] = n;
+}
+
+}  // namespace dbs
+
 extern "C" {
 
 void dbspmspv_default_join_opts(dbspmspv_join_opts *o) {
@@ -59,6 +79,17 @@ int dbspmspv_join(const dbspmspv_join_opts *o, int32_t tokens, int64_t n, const 
     });
     if ((s = fit_clusters(reinterpret_cast<const void *>(kernel), dev, p, join_smem(p, room, params, whole))) != DBSPMSPV_OK) return s;
     return launch_rows(dev, kernel, p.clusters * p.cluster, p.warps * p.teams * 32, p.cluster, join_smem(p, room, params, whole), static_cast<cudaStream_t>(stream), a);
+}
+
+int dbspmspv_test_cluster_wait(int32_t max_tries, int32_t silent, int32_t *gave_up, dbspmspv_stream_t stream) {
+    using namespace dbs;
+    if (max_tries < 1 || max_tries > 4096 || silent < -1 || silent > 1 || !gave_up || !on_bytes(4, gave_up)) return DBSPMSPV_ERR_INVALID_ARG;
+    int dev, sms, s;
+    if ((s = current_device(&dev, &sms)) != DBSPMSPV_OK) return s;
+    if (!on_current_device(gave_up, dev)) return DBSPMSPV_ERR_INVALID_ARG;
+    JoinArgs a = {};
+    a.n = 512; a.warps = a.teams = 1;
+    return launch_rows(dev, k_join_wait, 2, 32, 2, 4 * join_sums_room(1, 2) * 4 + 16, static_cast<cudaStream_t>(stream), a, max_tries, silent, gave_up);
 }
 
 }  // extern "C"

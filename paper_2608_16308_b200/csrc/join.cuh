@@ -23,7 +23,7 @@ constexpr int JOIN_CLUSTER = 8;
 constexpr int64_t JOIN_MAX_N = JOIN_COLS * JOIN_CLUSTER;
 constexpr int JOIN_AHEAD = 2;                // rows in flight or in hand, per team
 constexpr int JOIN_SUMS_CTA = 512;
-constexpr int JOIN_WAIT = 1 << 20;           // tries of a wait for a cluster's sums, before it gives up
+constexpr int JOIN_WAIT = 1 << 20;           // tries of a wait for a cluster's sums, before it gives up: about two seconds
 // threads at most (two eights a lane, or rows of up to 2048 columns); of gradients with sums of biases (one eight a lane)
 __host__ __device__ constexpr int join_cta(bool sums_of_biases) { return sums_of_biases ? JOIN_COLS / 8 : JOIN_COLS / 16; }
 
@@ -121,12 +121,15 @@ __device__ __forceinline__ void factors_here(const uint4 *at, f32x2 v[4]) {
 // Sums over the row.  In a thread block they meet at a barrier of the team's; in a cluster every warp sends its own to each block's shared memory, where an mbarrier counts the bytes (no fence, which would wait
 // for the rows written meanwhile).  Two buffers in turn: who writes one again has passed a barrier that its readers reached behind their reading.
 __host__ __device__ inline int join_sums_room(int warps, int cluster) { return warps * cluster < 8 ? 8 : (warps * cluster + 3) & ~3; }
+// CLUSTERS: whether there can be any (one eight a lane and no sums of biases: rows of up to 2048 columns, of which a thread block has a team or more)
+template <bool CLUSTERS>
 struct JoinTeam {
     int lane, warp, warps, team, teams, rank, cluster, room;
     bool alone;                              // a warp has the whole row
     int last;                                // the last warp of the row with columns; their number, and that of the others
     float cols_last, inv_last, cols;
-    uint32_t turn;                           // sums so far
+    uint32_t turn;                           // sums so far; from LOST on a wait of this warp's for its cluster has run out: it neither sends nor waits any more, and what it would have summed is NaN
+    static constexpr uint32_t LOST = 1u << 31;
     float *sums;                             // [buffer][team][2][room]: zeros behind the warps'; then, of a cluster, its barriers
     __device__ __forceinline__ JoinTeam(const JoinArgs &a, float *s, int columns) {
         lane = threadIdx.x & 31;
@@ -135,8 +138,12 @@ struct JoinTeam {
         teams = a.teams;
         team = w / warps;
         warp = w - team * warps;
-        asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
+        rank = 0;
+        cluster = 1;
+        if (CLUSTERS) {
+            asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+            asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(cluster));
+        }
         turn = 0;
         sums = s;
         room = join_sums_room(warps, cluster);
@@ -146,7 +153,7 @@ struct JoinTeam {
         cols_last = a.n - last * columns;
         inv_last = 1.f / cols_last;
         for (int i = threadIdx.x; i < 4 * teams * room; i += blockDim.x) s[i] = 0.f;
-        if (cluster > 1) {
+        if (CLUSTERS && cluster > 1) {
             if (threadIdx.x < 2) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(barrier(threadIdx.x)) : "memory");
             // (every block's barriers are there before another one sends)
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -164,22 +171,28 @@ struct JoinTeam {
 #pragma unroll
             for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(FULL, v[k], o);
     }
+    // (One that exits before the others are done would be sent to behind its end: the cluster's barrier waits until all its threads have come here or exited.)
+    __device__ __forceinline__ void give_up() {
+        turn |= LOST;
+        asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
+    }
     // every warp's K numbers to every warp of the row: [number][room], warps in the order of their columns.  False: a wait ran out.
     template <int K>
-    __device__ __forceinline__ bool exchange(const float (&v)[K], const float *&s) {
+    __device__ __forceinline__ bool exchange(const float (&v)[K], const float *&s, int tries = JOIN_WAIT) {
         const int buffer = turn & 1, phase = (turn >> 1) & 1;
         float *to = sums + (buffer * teams + team) * 2 * room;
         s = to;
         ++turn;
-        if (cluster == 1) {
+        if (!CLUSTERS || cluster == 1) {
             if (lane == 0)
 #pragma unroll
                 for (int k = 0; k < K; ++k) to[k * room + warp] = v[k];
             asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(warps * 32) : "memory");
             return true;
         }
-        if (threadIdx.x == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(barrier(buffer)), "r"(warps * cluster * K * 4) : "memory");
-        if (lane < cluster) {
+        const bool on = turn < LOST;          // (a barrier whose phase was given up takes no second arrival)
+        if (threadIdx.x == 0 && on) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(barrier(buffer)), "r"(warps * cluster * K * 4) : "memory");
+        if (lane < cluster && on) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 uint32_t there, bar;
@@ -189,9 +202,11 @@ struct JoinTeam {
             }
         }
         uint32_t ok = 0;
-        for (int i = 0; i < JOIN_WAIT && !ok; ++i)
+        for (int i = on ? 0 : tries; i < tries && !ok; ++i)
             asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(barrier(buffer)), "r"(phase) : "memory");
-        return ok;
+        if (__all_sync(FULL, ok)) return true;
+        if (on) give_up();
+        return false;
     }
     // the same sums in every thread of the row; NaN where a wait ran out
     template <int K>
@@ -228,8 +243,8 @@ struct JoinTeam {
 };
 
 // mean and 1 / deviation of the row whose entries the threads hold (zeros behind its end)
-template <int E, bool WHOLE>
-__device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4], const WarpEight (&w)[E], int norm, float eps, float inv_n) {
+template <int E, bool WHOLE, typename Team>
+__device__ __forceinline__ float2 norm_stats(Team &tm, const f32x2 (&v)[E][4], const WarpEight (&w)[E], int norm, float eps, float inv_n) {
     float s[1];
     f32x2 p[2] = {0, 0};
     if (norm == DBSPMSPV_NORM_RMS) {
@@ -247,7 +262,7 @@ __device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4
 #pragma unroll
         for (int j = 0; j < 4; ++j) p[j % 2] = add2(p[j % 2], v[e][j]);
     s[0] = sum2(add2(p[0], p[1]));
-    JoinTeam::add_warp(s);
+    Team::add_warp(s);
     const float sum = s[0];
     const int place = w[0].col / (256 * E);
     const f32x2 minus = both(-sum * (place < tm.last ? 1.f / (256 * E) : place == tm.last ? tm.inv_last : 0.f));
@@ -267,13 +282,14 @@ __device__ __forceinline__ float2 norm_stats(JoinTeam &tm, const f32x2 (&v)[E][4
         }
         s[0] += WHOLE && cnt == 0 ? 0.f : sum2(q);                           // (zeros behind the row's end have no difference from the mean)
     }
-    JoinTeam::add_warp(s);
+    Team::add_warp(s);
     const float2 all = tm.spread(sum, s[0], inv_n);
     return make_float2(all.x, rsqrtf(all.y * inv_n + eps));
 }
 
 // the row's sums of u * xhat and, behind a layer norm, of u
-__device__ __forceinline__ float2 slope_sums(JoinTeam &tm, int norm, f32x2 along, f32x2 mean) {
+template <typename Team>
+__device__ __forceinline__ float2 slope_sums(Team &tm, int norm, f32x2 along, f32x2 mean) {
     if (norm == DBSPMSPV_NORM_LAYER) {
         float s[2] = {sum2(along), sum2(mean)};
         tm.add(s);
@@ -297,7 +313,8 @@ struct JoinWarp {
     uint4 *factors;
     int room;
     WarpEight w[E];
-    __device__ __forceinline__ JoinWarp(const JoinArgs &a, uint8_t *s_dyn, const JoinTeam &tm) {
+    template <typename Team>
+    __device__ __forceinline__ JoinWarp(const JoinArgs &a, uint8_t *s_dyn, const Team &tm) {
         room = a.room;
         rows = s_dyn + (threadIdx.x >> 5) * join_warp_bytes(E, a.room, a.params, WHOLE);
         factors = reinterpret_cast<uint4 *>(rows + JOIN_AHEAD * room) + tm.lane;
@@ -330,7 +347,7 @@ __global__ void __launch_bounds__(join_cta(false), E == 1 ? 4 : 3) k_join(const 
     constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, PARAMS = BIAS ? 8 : 4;
     // where a lane's eights of r, b and the gate lie in a row's shared memory
     constexpr int AT_R = 0, AT_B = E * eight_room<SF32, WHOLE>(), AT_G = AT_B + E * eight_room<BF32, WHOLE>();
-    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, PARAMS, WHOLE) * (blockDim.x >> 5)), 256 * E);
+    JoinTeam<(E == 2)> tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, PARAMS, WHOLE) * (blockDim.x >> 5)), 256 * E);
     const JoinWarp<E, WHOLE> me(a, s_dyn, tm);
     const int n = a.n;
     pdl_wait();
@@ -467,7 +484,7 @@ __global__ void __launch_bounds__(join_cta(BIAS), BIAS ? 1 : 2) k_join_backward(
     constexpr int SZ = SF32 ? 4 : 2, BZ = BF32 ? 4 : 2, SUMS = BIAS ? 4 : 2;
     constexpr int S8 = eight_room<SF32, WHOLE>(), B8 = eight_room<BF32, WHOLE>(), H8 = eight_room<false, WHOLE>();
     constexpr int AT_DOUT = E * H8, AT_OUT = AT_DOUT + E * S8, AT_B = AT_OUT + E * S8, AT_G = AT_B + E * B8;
-    JoinTeam tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, a.params, WHOLE) * (blockDim.x >> 5)), 256 * E);
+    JoinTeam<(E == 2 || BIAS)> tm(a, reinterpret_cast<float *>(s_dyn + join_warp_bytes(E, a.room, a.params, WHOLE) * (blockDim.x >> 5)), 256 * E);
     const JoinWarp<E, WHOLE> me(a, s_dyn, tm);
     const int n = a.n;
     pdl_wait();

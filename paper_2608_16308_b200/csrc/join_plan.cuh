@@ -39,7 +39,8 @@ inline int fit_clusters(const void *kernel, int dev, JoinPlan &p, size_t smem) {
     return s;
 }
 // Two eights a lane share what a sum over the row costs: from 1024 columns on where no more than a quarter of the lanes has none and there are more rows than SMs hold at once (333 rows of 1037: 8.3 us with two,
-// 7.5 with one; 4000 rows of 1000, gradient: 24.5 and 21.7), and from 2048 on in any case.  Gradients with sums of biases have no registers for two.
+// 7.5 with one; 4000 rows of 1000, gradient: 24.5 and 21.7), and from 2048 on in any case.  Gradients with sums of biases have no registers for two.  (One without such sums: 2048 columns at most, which
+// are a thread block's; its kernels know no clusters.)
 inline int join_eights(int sms, int64_t tokens, int64_t n, bool sums_of_biases) {
     if (sums_of_biases || n <= 1024) return 1;
     return n > 2048 || (4 * n >= 3 * (ceil64(n, 512) * 512) && tokens > 2 * sms) ? 2 : 1;
