@@ -3,9 +3,9 @@
 // A row is owned by a team of warps; a warp takes 256 or 512 columns of it, eight or twice eight a lane: the values stay on the chip between the sums over the row (one for each norm, two for a layer norm;
 // backwards one for each norm) and every array is read and written once.  A warp is a team for short rows, a thread block holds several teams then; rows of more than 4096 columns are shared out to a
 // cluster whose blocks send their sums into each other's shared memory.  Teams walk the tokens.  The rows to come are copied ahead into shared memory of the warp (cp.async): a sum over the row would else
-// leave HBM idle.  Weights, gate, scales and biases of the columns lie beside them in fp32, multiplied with one another once.  What is left is HBM and, with dropout, nearly as many
-// instructions; so products and sums go two entries at a time, and where all rows are whole eights on 16 bytes (WHOLE) a row's address is one product-and-sum and its copy one instruction.
-// Other rows: of one on 16 bytes the last eight goes entry by entry; one that is not is copied and written in words of 4 bytes, side by side across the warp, and in shared memory moved by half a word
+// leave HBM idle.  Weights, gate, scales and biases of the columns lie beside them in fp32, multiplied with one another once.  What is left is the way through a row, whose sums a team
+// waits for with one row in hand (half of an SM's issue rate and of HBM's); products and sums go two entries at a time, and where all rows are whole eights on 16 bytes (WHOLE) a row's address is one product-and-sum and its copy one instruction.
+// Other rows: of one on 16 bytes the last eight is copied in words and stored entry by entry; one that is not is copied and written in words of 4 bytes, side by side across the warp, and in shared memory moved by half a word
 // where it begins between two.
 //
 // Sums over the tokens (gradients of weights, biases and a shared gate) are held by the threads of a column and written once per team; a second kernel adds the teams up in a
@@ -334,7 +334,7 @@ struct JoinWarp {
     __device__ __forceinline__ uint8_t *mine(const Rows &r) const { return static_cast<uint8_t *>(r.p) + (int64_t)w[0].mine() * (F32 ? 4 : 2); }
 };
 
-// 4096 rows of 4096 in bf16, root mean squares on both sides, a gate, dropout: 29.4 us, 4.57 TB/s (HBM copies 6.46): 297 warp instructions a warp and 256 columns at 2.1 a clock and SM, a quarter of them the generator's (24 us
+// 4096 rows of 4096 in bf16, root mean squares on both sides, a gate, dropout: 29.3 us, 4.58 TB/s (HBM copies 6.46): 294 warp instructions a warp and 256 columns at 2.0 of 4 a clock and SM, a quarter of them the generator's (24 us
 // without dropout and gate).
 // 1, 8 rows: 5.5 us, the calling thread.
 // factors: gate * w_block * scales (or without a gate that has rows), w_next, then (BIAS) c_block * gate * scales, c_next
@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(join_cta(false), E == 1 ? 4 : 3) k_join(const 
     }
 }
 
-// 4096 rows of 4096 as above: 46.8 us with the sums behind it, 4.3 TB/s; 412 warp instructions a warp and 256 columns at 2.05 a clock and SM from 16 warps, whose registers (128) the
+// 4096 rows of 4096 as above: 46.8 us with the sums behind it, 4.3 TB/s; 413 warp instructions a warp and 256 columns at 2.06 a clock and SM from 16 warps, whose registers (128) the
 // sums over tokens take.
 // factors: w_next, gate * w_block * scales (or without a gate that has rows), c_block * scales for the gradient of such a gate.  Sums over a team's tokens: dw_next, A, then (BIAS) dc_next, B.
 template <bool SF32, bool BF32, int E, bool BIAS, bool WHOLE, bool GATES>

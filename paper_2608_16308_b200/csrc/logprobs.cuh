@@ -2,11 +2,12 @@
 //
 // One pass: every thread keeps the largest logit m that it has met, s = sum e and u = sum x e with e = 2^x, x = (l - m) log2(e) / T, and moves s and u over when m
 // grows (u to u + d s, both times 2^d); states of threads, warps and the blocks of a cluster are brought to their largest m and added.  Then log sum = log s, entropy = log s - log(2) u / s.  Relative to
-// m nothing overflows, whatever the logits.  What bounds it is HBM (fp32) or instructions (bf16: six an entry, and the exponential's pipe, 16 a clock and SM, at two thirds of its rate), so two entries are
+// m nothing overflows, whatever the logits.  Neither HBM nor the issue of instructions (half its rate) nor a pipe (exponentials 45 %) is full in bf16; what is left is the way through a round and the end of a row.  Two entries are
 // multiplied and added at a time, and x is one product-and-sum with the rounded m log2(e) / T, whose rounding is made up for once per thread.  Thread blocks walk the rows, and the vectors to come, the next
 // row's too, are copied ahead into slots of shared memory that belong to the thread itself (cp.async, no barrier): the sums and the selection at the end of a row leave HBM busy.
 //
-// 2048 rows of 32000 in bf16: 31 us with the entropy (4.2 TB/s), 36 with five alternatives, 44 with twenty; one row of 32000 in fp32 with twenty 8.1 us (4.5 without): two exchanges of the cluster.
+// 2048 rows of 32000 with the entropy, in bf16 32 us (4.1 TB/s), 37 with five alternatives, 45 with twenty, 47 without any where a third is masked (those sums are made twice); in fp32 62 with five; one row of 32000 in fp32
+// with twenty 7.9 us (4.5 without): two exchanges of the cluster.
 //
 // Alternatives.  A thread's own logits (its unit) are known by their largest and its place.  Where at least k groups of threads have a unit of at least tau, no logit below tau is among the k largest; the
 // k-th largest of the groups' largest (or a little less) is such a tau.  Only units that reach it are read a second time (they come from L2), and of their logits those that reach tau are counted against
@@ -573,7 +574,7 @@ __global__ void __launch_bounds__(LP_CTA, LP_PER_SM) k_logprobs(const __grid_con
 }
 
 // ---- the gradient -----------------------------------------------------------------------------
-// p (c0 + c1 x) per entry, two loads of 16 or 32 bytes ahead: 2048 rows of 32000 in bf16 45 us, 5.8 TB/s; 63 of 100003 in fp32 13.6 us.  Thread blocks of 128: of 256, 50.2 us.  What is added at single entries
+// p (c0 + c1 x) per entry, two loads of 16 or 32 bytes ahead: 2048 rows of 32000 in bf16 45 us, 5.8 TB/s; 63 of 100003 in fp32 13.4 us.  Thread blocks of 128: of 256, 50.2 us.  What is added at single entries
 // (targets, alternatives) is written behind the rest by the same thread block.
 struct LpGrad {
     const void *logits;
