@@ -65,6 +65,7 @@ __device__ __forceinline__ uint32_t order_of(float l) {
     const uint32_t b = __float_as_uint(l == 0.f ? 0.f : l);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+constexpr uint32_t LP_ORDER_LEAST = 0x007FFFFFu;                    // order_of(-inf)
 __device__ __forceinline__ float of_order(uint32_t k) {
     return k == 0xFFFFFFFFu ? __uint_as_float(0x7FC00000u) : __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
@@ -239,7 +240,8 @@ __device__ __forceinline__ uint32_t lp_least(const uint32_t (&g)[N], int k) {
         else hi = mid - 1;
         if (n >= k && n <= k + LP_SLACK) break;
     }
-    return lo;
+    // (between no logit, 0, and -inf there is none: a number from there stands for -inf, and of_order would make a NaN of it)
+    return lo ? max(lo, LP_ORDER_LEAST) : 0u;
 }
 
 // the block's k largest to out(candidate, place), zeros behind them, every place from one thread.  `most`: the thread's largest, as order_of has it (0: it has none); `group`: what at least k groups' largest reach, as order_of has it.
